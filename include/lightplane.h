@@ -16,7 +16,8 @@
  *     and keeps no pointer after a call returns.
  *   - Every function returns an lp_status and never throws or aborts; a message
  *     for the last failure on the calling thread is available from lp_last_error().
- *   - All floating point is IEEE binary32, tensors are dense and C-contiguous.
+ *   - All floating point is IEEE binary32 and tensors are dense and C-contiguous unless a call says
+ *     otherwise.
  */
 #ifndef LIGHTPLANE_H
 #define LIGHTPLANE_H
@@ -305,6 +306,118 @@ lp_status lp_splat_bwd(const lp_grid* target, const lp_rays* rays, const lp_spla
 
 lp_status lp_splat_bwd_workspace_bytes(const lp_grid* target, const lp_rays* rays, const lp_splat* splat,
                                        size_t* bytes);
+
+/* ---- Group norm with an activation over channel-last grids --------------------------------------
+ *
+ * What networks that work on the library's structures (between a Splatter and a Renderer) put between
+ * their layers.  x holds N samples (scenes, planes) of P positions with C channels each, channel last:
+ * element (n, p, c) sits at ((n P + p) stride + c), so voxel grids are P = NX NY NZ positions and a
+ * plane of a triplane P = NX NY, and a slice of the channels of a wider tensor has a stride beyond C.
+ * The C / G channels of a group and the positions of a sample are normalised together,
+ *     mean, var = of the sample's group (var without Bessel's correction), rstd = (var + eps)^(-1/2),
+ *     xh = (x - mean) rstd,   y = act(gamma xh + beta).
+ * occupancy [N][P] (the weight sums theta_w a Splatter writes are one): positions whose value is not
+ * above zero do not take part: x and d_y are not used there (they may hold anything, NaN included),
+ * y and d_x are 0.  A sample without any position that takes part has mean = rstd = 0.
+ * Statistics, sums and gamma, beta and their gradients are fp32 or wider whatever the tensors hold.
+ */
+typedef enum { LP_ACT_NONE = 0, LP_ACT_RELU = 1, LP_ACT_SILU = 2, LP_ACT_GELU = 3 /* with the error function */ } lp_act;
+
+typedef struct {
+    int64_t N, P;
+    int32_t C, G;             /* channels, groups; G divides C */
+    int32_t act;              /* lp_act */
+    float eps;                /* >= 0, finite */
+    int32_t x_dtype;          /* lp_dtype of x and d_x */
+    int32_t y_dtype;          /* lp_dtype of y and d_y: x_dtype, or a 16-bit type where x is fp32 */
+    int64_t x_stride;         /* elements from position to position of x and d_x, >= C; 0: C */
+    int64_t y_stride;         /* the same of y and d_y */
+    const float* gamma;       /* device [C], NULL: 1 */
+    const float* beta;        /* device [C], NULL: 0 */
+    const float* occupancy;   /* device [N][P], NULL: every position takes part */
+} lp_group_norm;
+
+/* Bytes of device workspace of the two calls below (either pointer may be NULL); they depend on
+   N, P, C, G and the device's compute-unit count. */
+lp_status lp_group_norm_workspace_bytes(const lp_group_norm* norm, size_t* fwd_bytes, size_t* bwd_bytes);
+
+/* Forward.  y is WRITTEN; stats [N][G][2] (device, fp32: mean, rstd; may be NULL) is written for the
+   backward.  workspace: device, 256-byte aligned, contents ignored on entry, undefined on exit.
+   y may be x itself where types and strides are alike.  N == 0 or P == 0 is a no-op. */
+lp_status lp_group_norm_fwd(const lp_group_norm* norm, const void* x, void* y, float* stats, void* workspace,
+                            size_t workspace_bytes, void* stream);
+
+/* Backward for the upstream gradient d_y, with x as the forward had it and the stats it wrote.  d_x is
+   WRITTEN (NULL: not wanted); d_gamma [C], d_beta [C] are ACCUMULATED into (either may be NULL), in an
+   order that does not change from call to call.  d_x may be d_y itself where types and strides are alike.
+   Of a ReLU the gradient at 0 is 0. */
+lp_status lp_group_norm_bwd(const lp_group_norm* norm, const void* x, const float* stats, const void* d_y, void* d_x,
+                            float* d_gamma, float* d_beta, void* workspace, size_t workspace_bytes, void* stream);
+
+/* ---- Orthogonalised updates of weight matrices --------------------------------------------------
+ *
+ * The step of the Muon optimiser (Jordan et al. 2024) for the weight matrices whose gradients the
+ * backward calls above accumulate, and for those of networks around them.  A matrix G (rows x cols) is
+ * replaced by what a few Newton-Schulz products make of it, which moves all its singular values towards 1:
+ *     X_0 = G / (||G||_F + eps),   A = X X^T,   X <- a X + (b A + c A A) X,   `steps` times
+ * (of a matrix with more rows than columns: on the transpose).  A matrix of zeros gives zeros.
+ * Products are computed on the matrix cores with operands as fp16 hi + lo parts at a power-of-two scale (22
+ * bits, three products, fp32 accumulation), whose error is that of fp32 products.
+ */
+#define LP_ORTH_MAX_STEPS 16
+
+typedef struct {
+    int32_t steps;       /* 1 .. LP_ORTH_MAX_STEPS */
+    const float* coeffs; /* HOST [steps][3]: a, b, c of every step; NULL: 3.4445, -4.775, 2.0315 in every step.
+                            Coefficients under which a singular value in [0, 1] could leave [0, 1024] are refused. */
+    float eps;           /* >= 0, finite */
+} lp_orth;
+
+/* `count` matrices of one shape, one behind the other: element (i, r, c) at (i rows + r) cols + c. */
+typedef struct {
+    int64_t count;
+    int32_t rows, cols;
+    const void* in; /* device, elements of type `dtype` */
+    void* out;      /* device, elements of type `dtype`; may be `in` */
+    int32_t dtype;  /* lp_dtype */
+} lp_matrices;
+
+/* Orthogonalises n lists of matrices.  `lists` is a HOST array; outputs are WRITTEN.  workspace: device,
+   256-byte aligned, contents ignored on entry, undefined on exit.  n == 0 is a no-op, and so is a list with
+   count, rows or cols 0. */
+lp_status lp_orthogonalize(int32_t n, const lp_matrices* lists, const lp_orth* orth, void* workspace,
+                           size_t workspace_bytes, void* stream);
+lp_status lp_orthogonalize_workspace_bytes(int32_t n, const lp_matrices* lists, size_t* bytes);
+
+/* How the step of a matrix is scaled. */
+typedef enum {
+    LP_MUON_SCALE_NONE = 0,
+    LP_MUON_SCALE_ASPECT = 1, /* sqrt(max(1, rows / cols)) */
+    LP_MUON_SCALE_RMS = 2     /* 0.2 sqrt(max(rows, cols)): steps as large as Adam's */
+} lp_muon_scale;
+
+typedef struct {
+    float lr, momentum, weight_decay; /* finite */
+    int32_t nesterov;                 /* 0 or 1 */
+    int32_t scale;                    /* lp_muon_scale */
+    lp_orth orth;
+} lp_muon;
+
+/* fp32 weights with their gradient and momentum, laid out as in lp_matrices. */
+typedef struct {
+    int64_t count;
+    int32_t rows, cols;
+    float* weight;     /* device, updated */
+    const float* grad; /* device */
+    float* momentum;   /* device, updated; zeros before the first step */
+} lp_muon_weights;
+
+/* One step over n lists of weights:
+     M <- momentum M + G,   U = G + momentum M (nesterov) or M,
+     W <- (1 - lr weight_decay) W - lr s orthogonalised(U). */
+lp_status lp_muon_step(int32_t n, const lp_muon_weights* lists, const lp_muon* muon, void* workspace,
+                       size_t workspace_bytes, void* stream);
+lp_status lp_muon_workspace_bytes(int32_t n, const lp_muon_weights* lists, size_t* bytes);
 
 /* Diagnostics, not part of the method: how one SIMD of this GPU overlaps matrix instructions
    (32x32x16 bf16 products, 32 cycles each) with vector instructions (4 cycles each); the split of

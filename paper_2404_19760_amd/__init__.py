@@ -26,6 +26,9 @@ LP_GRID_VOXEL, LP_GRID_TRIPLANE, LP_GRID_HASH, LP_GRID_HEXPLANE = 0, 1, 2, 3
 LP_MATH_DEFAULT, LP_MATH_GENERIC, LP_MATH_BF16X3 = 0, 1, 2
 LP_FEAT_SIGMOID, LP_FEAT_IDENTITY = 0, 1
 LP_F32, LP_BF16, LP_F16 = 0, 1, 2
+LP_ACT_NONE, LP_ACT_RELU, LP_ACT_SILU, LP_ACT_GELU = 0, 1, 2, 3
+LP_ORTH_MAX_STEPS = 16
+LP_MUON_SCALE_NONE, LP_MUON_SCALE_ASPECT, LP_MUON_SCALE_RMS = 0, 1, 2
 
 
 class LightplaneError(RuntimeError):
@@ -62,6 +65,31 @@ class _Rays(C.Structure):
     _fields_ = [("M", C.c_int64), ("S", C.c_int32),
                 ("origins", C.c_void_p), ("dirs", C.c_void_p),
                 ("near", C.c_void_p), ("far", C.c_void_p), ("scene", C.c_void_p), ("time", C.c_void_p)]
+
+
+class _GroupNorm(C.Structure):
+    _fields_ = [("N", C.c_int64), ("P", C.c_int64), ("C", C.c_int32), ("G", C.c_int32), ("act", C.c_int32), ("eps", C.c_float),
+                ("x_dtype", C.c_int32), ("y_dtype", C.c_int32), ("x_stride", C.c_int64), ("y_stride", C.c_int64),
+                ("gamma", C.c_void_p), ("beta", C.c_void_p), ("occupancy", C.c_void_p)]
+
+
+class _Orth(C.Structure):
+    _fields_ = [("steps", C.c_int32), ("coeffs", C.POINTER(C.c_float)), ("eps", C.c_float)]
+
+
+class _Matrices(C.Structure):
+    _fields_ = [("count", C.c_int64), ("rows", C.c_int32), ("cols", C.c_int32), ("input", C.c_void_p), ("out", C.c_void_p),
+                ("dtype", C.c_int32)]
+
+
+class _Muon(C.Structure):
+    _fields_ = [("lr", C.c_float), ("momentum", C.c_float), ("weight_decay", C.c_float), ("nesterov", C.c_int32),
+                ("scale", C.c_int32), ("orth", _Orth)]
+
+
+class _MuonWeights(C.Structure):
+    _fields_ = [("count", C.c_int64), ("rows", C.c_int32), ("cols", C.c_int32), ("weight", C.c_void_p), ("grad", C.c_void_p),
+                ("momentum", C.c_void_p)]
 
 
 def _load() -> C.CDLL:
@@ -124,6 +152,21 @@ def _load() -> C.CDLL:
     lib.lp_splat_bwd.argtypes = [C.POINTER(_Grid), C.POINTER(_Rays), C.POINTER(_Splat), C.POINTER(C.c_void_p),
                                  C.POINTER(C.c_void_p), C.c_void_p, C.POINTER(C.c_void_p), C.POINTER(C.c_void_p),
                                  C.POINTER(C.c_void_p), C.c_void_p, C.c_size_t, C.c_void_p]
+    lib.lp_group_norm_workspace_bytes.restype = C.c_int
+    lib.lp_group_norm_workspace_bytes.argtypes = [C.POINTER(_GroupNorm), C.POINTER(C.c_size_t), C.POINTER(C.c_size_t)]
+    lib.lp_group_norm_fwd.restype = C.c_int
+    lib.lp_group_norm_fwd.argtypes = [C.POINTER(_GroupNorm), C.c_void_p, C.c_void_p, C.c_void_p, C.c_void_p, C.c_size_t, C.c_void_p]
+    lib.lp_group_norm_bwd.restype = C.c_int
+    lib.lp_group_norm_bwd.argtypes = [C.POINTER(_GroupNorm), C.c_void_p, C.c_void_p, C.c_void_p, C.c_void_p, C.c_void_p, C.c_void_p,
+                                      C.c_void_p, C.c_size_t, C.c_void_p]
+    lib.lp_orthogonalize_workspace_bytes.restype = C.c_int
+    lib.lp_orthogonalize_workspace_bytes.argtypes = [C.c_int32, C.POINTER(_Matrices), C.POINTER(C.c_size_t)]
+    lib.lp_orthogonalize.restype = C.c_int
+    lib.lp_orthogonalize.argtypes = [C.c_int32, C.POINTER(_Matrices), C.POINTER(_Orth), C.c_void_p, C.c_size_t, C.c_void_p]
+    lib.lp_muon_workspace_bytes.restype = C.c_int
+    lib.lp_muon_workspace_bytes.argtypes = [C.c_int32, C.POINTER(_MuonWeights), C.POINTER(C.c_size_t)]
+    lib.lp_muon_step.restype = C.c_int
+    lib.lp_muon_step.argtypes = [C.c_int32, C.POINTER(_MuonWeights), C.POINTER(_Muon), C.c_void_p, C.c_size_t, C.c_void_p]
     return lib
 
 
@@ -576,6 +619,187 @@ def lp_splat_bwd(target: _Grid, rays: Rays, splat: Splat, theta_w: List[torch.Te
     del keep
 
 
+@dataclasses.dataclass
+class GroupNorm:
+    """Group norm with an activation over channel-last tensors [N][...][C] (a voxel grid [B][NX][NY][NZ][C], a plane
+    [B][NX][NY][C], ...): everything between the first and the last axis is normalised together with the channels of a
+    group.  gamma, beta: float32 [C] or None; occupancy: float32 [N][...] or None, positions whose value is not above zero
+    do not take part (the weight sums `theta_w` of a Splatter)."""
+    groups: int
+    gamma: Optional[torch.Tensor] = None
+    beta: Optional[torch.Tensor] = None
+    act: int = LP_ACT_NONE
+    eps: float = 1e-5
+    occupancy: Optional[torch.Tensor] = None
+
+    def c_struct(self, x: torch.Tensor, y_dtype=None, y_stride: int = 0) -> _GroupNorm:
+        y_dtype = x.dtype if y_dtype is None else y_dtype
+        if x.dtype not in _GRID_DTYPES or y_dtype not in _GRID_DTYPES:
+            raise ValueError("x and y must be float32, bfloat16 or float16")
+        if x.dim() < 2:
+            raise ValueError("x must have a first axis of samples and a last axis of channels")
+        shape = x.shape
+        c = shape[-1]
+        return _GroupNorm(shape[0], x.numel() // max(1, shape[0] * c) if c else 0, c, int(self.groups), int(self.act),
+                          float(self.eps), _GRID_DTYPES[x.dtype], _GRID_DTYPES[y_dtype], _position_stride(x, "x"), y_stride,
+                          _dev_f32(self.gamma, "gamma", (c,)), _dev_f32(self.beta, "beta", (c,)),
+                          _dev_f32(self.occupancy, "occupancy", shape[:-1]))
+
+
+def _position_stride(t: torch.Tensor, name: str) -> int:
+    """Elements from position to position of a channel-last tensor: dense, or a slice of the channels of a dense one."""
+    if not t.is_cuda:
+        raise ValueError(f"{name} must be on the GPU")
+    c = t.shape[-1]
+    if t.is_contiguous() or t.numel() == 0:
+        return c
+    strides, shape = t.stride(), t.shape
+    step, want = None, None
+    for k in range(t.dim() - 2, -1, -1):
+        if shape[k] == 1:
+            continue
+        if step is None:
+            step, want = strides[k], strides[k]
+        if strides[k] != want:
+            step = 0
+            break
+        want *= shape[k]
+    if not step or step < c or (c > 1 and strides[-1] != 1):
+        raise ValueError(f"{name} must be channel-last: dense, or a slice of the channels of a dense tensor")
+    return step
+
+
+def _channel_last(t: torch.Tensor, name: str, shape, dtype):
+    if t.shape != shape or t.dtype != dtype:
+        raise ValueError(f"{name} must have shape {tuple(shape)} and type {dtype}")
+    return _position_stride(t, name)
+
+
+def _no_overlap(written: torch.Tensor, read: torch.Tensor, written_name: str, read_name: str) -> None:
+    """A tensor that is written is the one that is read or lies apart from it."""
+    if written.numel() == 0 or read.numel() == 0 or (written.data_ptr() == read.data_ptr() and written.dtype == read.dtype
+                                                    and written.stride() == read.stride()):
+        return
+    end = lambda t: t.data_ptr() + t.element_size() * (1 + sum((n - 1) * s for n, s in zip(t.shape, t.stride())))
+    if written.untyped_storage().data_ptr() == read.untyped_storage().data_ptr() and \
+            written.data_ptr() < end(read) and read.data_ptr() < end(written) and \
+            (written.is_contiguous() or read.is_contiguous()):
+        raise ValueError(f"{written_name} must be {read_name} itself or not overlap it")
+
+
+def lp_group_norm_workspace_bytes(norm: GroupNorm, x: torch.Tensor, y_dtype=None):
+    """(forward bytes, backward bytes) of workspace."""
+    q = norm.c_struct(x, y_dtype)
+    f, b = C.c_size_t(0), C.c_size_t(0)
+    _check(_lib.lp_group_norm_workspace_bytes(C.byref(q), C.byref(f), C.byref(b)))
+    return int(f.value), int(b.value)
+
+
+def lp_group_norm_fwd(norm: GroupNorm, x: torch.Tensor, y: torch.Tensor, stats: Optional[torch.Tensor],
+                      workspace: torch.Tensor, stream=None) -> None:
+    """Enqueue the forward: y (shape of x; its type, or a 16-bit one where x is float32) and stats [N][groups][2] (None:
+    not wanted) are written."""
+    q = norm.c_struct(x, y.dtype, _channel_last(y, "y", x.shape, y.dtype))
+    _no_overlap(y, x, "y", "x")
+    wp, wn = _workspace(workspace)
+    _check(_lib.lp_group_norm_fwd(C.byref(q), x.data_ptr(), y.data_ptr(), _dev_f32(stats, "stats", (x.shape[0], norm.groups, 2)),
+                                  wp, wn, _stream_ptr(stream)))
+
+
+def lp_group_norm_bwd(norm: GroupNorm, x: torch.Tensor, stats: torch.Tensor, d_y: torch.Tensor, d_x: Optional[torch.Tensor],
+                      d_gamma: Optional[torch.Tensor], d_beta: Optional[torch.Tensor], workspace: torch.Tensor, stream=None) -> None:
+    """Enqueue the backward: d_x (shape, type and strides of x) is written, d_gamma and d_beta [C] are accumulated into; each
+    may be None.  stats as the forward wrote it for the same x."""
+    q = norm.c_struct(x, d_y.dtype, _channel_last(d_y, "d_y", x.shape, d_y.dtype))
+    if d_x is not None:
+        if _channel_last(d_x, "d_x", x.shape, x.dtype) != q.x_stride:
+            raise ValueError("d_x must have the strides of x")
+        _no_overlap(d_x, x, "d_x", "x")
+        _no_overlap(d_x, d_y, "d_x", "d_y")
+    c = (x.shape[-1],)
+    wp, wn = _workspace(workspace)
+    _check(_lib.lp_group_norm_bwd(C.byref(q), x.data_ptr(), _dev_f32(stats, "stats", (x.shape[0], norm.groups, 2)), d_y.data_ptr(),
+                                  None if d_x is None else d_x.data_ptr(), _dev_f32(d_gamma, "d_gamma", c),
+                                  _dev_f32(d_beta, "d_beta", c), wp, wn, _stream_ptr(stream)))
+
+
+def _matrix_shape(t: torch.Tensor, name: str, k: int):
+    if not (t.is_cuda and t.is_contiguous() and t.dim() >= 2):
+        raise ValueError(f"{name}[{k}] must be a contiguous GPU tensor [...][rows][cols]")
+    rows, cols = t.shape[-2], t.shape[-1]
+    return t.numel() // max(1, rows * cols), rows, cols
+
+
+def _matrices(mats, outs):
+    if len(mats) != len(outs):
+        raise ValueError("one output per input is needed")
+    arr = (_Matrices * max(1, len(mats)))()
+    for k, (g, o) in enumerate(zip(mats, outs)):
+        count, rows, cols = _matrix_shape(g, "mats", k)
+        if g.dtype not in _GRID_DTYPES:
+            raise ValueError("matrices must be float32, bfloat16 or float16")
+        if o is not g and not (o.is_cuda and o.is_contiguous() and o.dtype is g.dtype and o.shape == g.shape):
+            raise ValueError(f"outs[{k}] must be a contiguous GPU tensor of the shape and type of mats[{k}]")
+        arr[k] = _Matrices(count, rows, cols, g.data_ptr(), o.data_ptr(), _GRID_DTYPES[g.dtype])
+    return arr
+
+
+def _orth(steps: int, coeffs, eps: float) -> _Orth:
+    """(a struct of `steps` steps; coeffs: one (a, b, c) for all steps, one for each, or None)"""
+    if coeffs is None:
+        return _Orth(int(steps), None, float(eps))
+    rows = [tuple(float(v) for v in r) for r in ([coeffs] * int(steps) if isinstance(coeffs[0], (int, float)) else coeffs)]
+    if len(rows) != steps or any(len(r) != 3 for r in rows):
+        raise ValueError("coeffs must be (a, b, c), or one of these for every step")
+    flat = (C.c_float * max(1, 3 * len(rows)))(*[v for r in rows for v in r])
+    o = _Orth(int(steps), flat, float(eps))
+    o.keep = flat
+    return o
+
+
+def lp_orthogonalize_workspace_bytes(mats: Sequence[torch.Tensor]) -> int:
+    arr, n = _matrices(mats, mats), C.c_size_t(0)
+    _check(_lib.lp_orthogonalize_workspace_bytes(len(mats), arr, C.byref(n)))
+    return int(n.value)
+
+
+def lp_orthogonalize(mats: Sequence[torch.Tensor], outs: Sequence[torch.Tensor], workspace: torch.Tensor, steps: int = 5,
+                     coeffs=None, eps: float = 1e-7, stream=None) -> None:
+    """Enqueue the orthogonalisation of the matrices in `mats` (tensors [...][rows][cols], float32, bfloat16 or float16); outs
+    (same shapes and types, or the inputs themselves) are written."""
+    arr, o = _matrices(mats, outs), _orth(steps, coeffs, eps)
+    wp, wn = _workspace(workspace)
+    _check(_lib.lp_orthogonalize(len(mats), arr, C.byref(o), wp, wn, _stream_ptr(stream)))
+
+
+def _muon_weights(weights, grads, momenta):
+    if not len(weights) == len(grads) == len(momenta):
+        raise ValueError("one gradient and one momentum per weight are needed")
+    arr = (_MuonWeights * max(1, len(weights)))()
+    for k, (w, g, m) in enumerate(zip(weights, grads, momenta)):
+        shape = w.shape
+        count, rows, cols = _matrix_shape(w, "weights", k)
+        arr[k] = _MuonWeights(count, rows, cols, _dev_f32(w, "weights", None, k), _dev_f32(g, "grads", shape, k),
+                              _dev_f32(m, "momenta", shape, k))
+    return arr
+
+
+def lp_muon_workspace_bytes(weights: Sequence[torch.Tensor]) -> int:
+    arr, n = _muon_weights(weights, weights, weights), C.c_size_t(0)
+    _check(_lib.lp_muon_workspace_bytes(len(weights), arr, C.byref(n)))
+    return int(n.value)
+
+
+def lp_muon_step(weights: Sequence[torch.Tensor], grads: Sequence[torch.Tensor], momenta: Sequence[torch.Tensor],
+                 workspace: torch.Tensor, lr: float, momentum: float = 0.95, nesterov: bool = True, weight_decay: float = 0.0,
+                 scale: int = LP_MUON_SCALE_ASPECT, steps: int = 5, coeffs=None, eps: float = 1e-7, stream=None) -> None:
+    """Enqueue one optimiser step: weights and momenta (float32 tensors [...][rows][cols]) are updated in place."""
+    arr = _muon_weights(weights, grads, momenta)
+    q = _Muon(float(lr), float(momentum), float(weight_decay), int(nesterov), int(scale), _orth(steps, coeffs, eps))
+    wp, wn = _workspace(workspace)
+    _check(_lib.lp_muon_step(len(weights), arr, C.byref(q), wp, wn, _stream_ptr(stream)))
+
+
 # ---------------------------------------------------------------------------------------
 # Conveniences on top of the entry points: move host buffers to the GPU, allocate outputs.
 
@@ -692,3 +916,39 @@ def splat_bwd(target: _Grid, rays: Rays, splat: Splat, theta_w, d_theta):
     ws = torch.empty(lp_splat_bwd_workspace_bytes(target, rays, splat), dtype=torch.uint8, device=dev)
     lp_splat_bwd(target, rays, splat, theta_w, d_theta, d_feats, d_prior, dW, db, ws)
     return d_feats, d_prior, dW, db
+
+
+def group_norm_fwd(norm: GroupNorm, x: torch.Tensor, dtype=None):
+    """Allocate outputs and workspace and run lp_group_norm_fwd.  Returns (y, stats); dtype: of y (default: that of x)."""
+    y = torch.empty(x.shape, dtype=x.dtype if dtype is None else dtype, device=x.device)
+    stats = torch.empty((x.shape[0], norm.groups, 2), dtype=torch.float32, device=x.device)
+    ws = torch.empty(lp_group_norm_workspace_bytes(norm, x, y.dtype)[0], dtype=torch.uint8, device=x.device)
+    lp_group_norm_fwd(norm, x, y, stats, ws)
+    return y, stats
+
+
+def group_norm_bwd(norm: GroupNorm, x: torch.Tensor, stats: torch.Tensor, d_y: torch.Tensor):
+    """Allocate gradients and workspace and run lp_group_norm_bwd.  Returns (d_x, d_gamma, d_beta)."""
+    d_x = torch.empty_strided(x.shape, x.stride(), dtype=x.dtype, device=x.device)
+    d_gamma, d_beta = torch.zeros((2, x.shape[-1]), dtype=torch.float32, device=x.device)
+    ws = torch.empty(lp_group_norm_workspace_bytes(norm, x, d_y.dtype)[1], dtype=torch.uint8, device=x.device)
+    lp_group_norm_bwd(norm, x, stats, d_y, d_x, d_gamma, d_beta, ws)
+    return d_x, d_gamma, d_beta
+
+
+def orthogonalize(mats: Sequence[torch.Tensor], steps: int = 5, coeffs=None, eps: float = 1e-7):
+    """Allocate outputs and workspace and run lp_orthogonalize.  Returns the outputs."""
+    outs = [torch.empty_like(g) for g in mats]
+    if mats:
+        ws = torch.empty(lp_orthogonalize_workspace_bytes(mats), dtype=torch.uint8, device=mats[0].device)
+        lp_orthogonalize(mats, outs, ws, steps, coeffs, eps)
+    return outs
+
+
+def muon_step(weights: Sequence[torch.Tensor], grads: Sequence[torch.Tensor], momenta: Sequence[torch.Tensor], lr: float,
+              momentum: float = 0.95, nesterov: bool = True, weight_decay: float = 0.0, scale: int = LP_MUON_SCALE_ASPECT,
+              steps: int = 5, coeffs=None, eps: float = 1e-7) -> None:
+    """Allocate a workspace and run lp_muon_step."""
+    if weights:
+        ws = torch.empty(lp_muon_workspace_bytes(weights), dtype=torch.uint8, device=weights[0].device)
+        lp_muon_step(weights, grads, momenta, ws, lr, momentum, nesterov, weight_decay, scale, steps, coeffs, eps)

@@ -12,18 +12,16 @@
 #include "lp_kernels.h"
 
 namespace {
-
 thread_local std::string g_last_error;
+constexpr int kMaxDevices = 64;
+}
 
+namespace lp {
 lp_status fail(lp_status s, const std::string& msg)
 {
     g_last_error = msg;
     return s;
 }
-
-constexpr size_t kMaxLds = 160 * 1024;   // LDS per compute unit on gfx950
-constexpr int kGenericLanes = 64;
-constexpr int kMaxDevices = 64;
 
 int compute_units(int* out_n_cu, std::string* err)
 {
@@ -42,6 +40,15 @@ int compute_units(int* out_n_cu, std::string* err)
     *out_n_cu = n;
     return 0;
 }
+}  // namespace lp
+
+namespace {
+
+using lp::fail;
+using lp::compute_units;
+
+constexpr size_t kMaxLds = 160 * 1024;   // LDS per compute unit on gfx950
+constexpr int kGenericLanes = 64;
 
 lp_status validate(const lp_grid* grid, const lp_mlp* mlp, const lp_rays* rays)
 {

@@ -1,0 +1,733 @@
+// Group norm with an activation over channel-last grids, forward and backward.
+//
+// A sample's group is normalised with its own mean and variance,
+//     xh = (x - mean) rstd,   y = act(gamma xh + beta),
+// and with g = d_y act'(gamma xh + beta) the backward is
+//     d_gamma = sum g xh,   d_beta = sum g,
+//     d_x = rstd (gamma g - (S1 + xh S2) / n),   S1 = sum over the group of gamma g,   S2 of gamma g xh.
+//
+// What bounds it: memory.  A sum over the whole group stands between reading a value and using it, so either direction passes
+// over its data twice: a pass that sums (forward: x; backward: x and d_y), a small kernel that joins the workgroups' sums, and
+// a pass that writes.  In all passes a thread keeps to one slot of V neighbouring channels (16 bytes where channels and
+// alignment allow), so a channel's parameters and sums stay in its registers, and neighbouring lanes read neighbouring bytes.
+//
+// Sums: a thread sums differences to the first value that it sees, in fp32 (a mean far from zero does not cancel the
+// variance); threads are joined as (count, mean, sum of squared differences), workgroups in fp64 in a fixed order, so that
+// results do not change from call to call.
+#include <hip/hip_runtime.h>
+
+#include <cmath>
+#include <cstring>
+
+#include "lp_kernels.h"
+
+namespace lp {
+
+namespace {
+
+constexpr int kThreads = 256;
+constexpr int kUnroll = 4;               // rows a thread has in flight
+constexpr long long kMaxGrid = 1 << 20;  // workgroups of a launch; items beyond are taken in turn
+constexpr float kInvSqrt2 = 0.70710678118654752f, kInvSqrt2Pi = 0.39894228040143268f;
+
+struct NormDev {
+    long long N, P;
+    int C, G, Cg;
+    long long xs, ys;                   // elements from position to position
+    const float *gamma, *beta, *occ;
+    float eps;
+    int act;
+    int slots, zblocks, rows;           // C / V; blocks of kThreads slots; positions a workgroup takes at a time
+    int chunks;                         // items of a sample
+    long long chunk;                    // positions of an item
+};
+
+template <class T, int V>
+struct alignas(sizeof(T) * V) Pack { T v[V]; };
+
+__device__ __forceinline__ float to_f32(float v) { return v; }
+__device__ __forceinline__ float to_f32(__bf16 v) { return (float)v; }
+__device__ __forceinline__ float to_f32(_Float16 v) { return (float)v; }
+
+template <class T, int V>
+__device__ __forceinline__ void load(const T* p, Pack<T, V>& out)
+{
+    out = *reinterpret_cast<const Pack<T, V>*>(p);
+}
+
+template <class T, int V>
+__device__ __forceinline__ void store(T* p, const float (&in)[V])
+{
+    Pack<T, V> q;
+#pragma unroll
+    for (int j = 0; j < V; ++j) q.v[j] = (T)in[j];   // round to nearest even, once
+    *reinterpret_cast<Pack<T, V>*>(p) = q;
+}
+
+// 1 / (1 + exp(-z)) from the hardware's exponential and reciprocal (a few units in the last place)
+__device__ __forceinline__ float sigmoid(float z) { return __builtin_amdgcn_rcpf(1.0f + __expf(-z)); }
+
+__device__ __forceinline__ float activate(float z, int act)
+{
+    switch (act) {
+        case LP_ACT_RELU: return z < 0.0f ? 0.0f : z;   // (a NaN stays one)
+        case LP_ACT_SILU: return z * sigmoid(z);
+        case LP_ACT_GELU: return 0.5f * z * (1.0f + erff(z * kInvSqrt2));
+        default: return z;
+    }
+}
+
+__device__ __forceinline__ float slope(float z, int act)
+{
+    switch (act) {
+        case LP_ACT_RELU: return z > 0.0f ? 1.0f : (z <= 0.0f ? 0.0f : z);
+        case LP_ACT_SILU: {
+            const float s = sigmoid(z);
+            return s * (1.0f + z * (1.0f - s));
+        }
+        case LP_ACT_GELU: return 0.5f * (1.0f + erff(z * kInvSqrt2)) + z * kInvSqrt2Pi * __expf(-0.5f * z * z);
+        default: return 1.0f;
+    }
+}
+
+// Where a thread stands: its slot of channels and its row among the positions a workgroup takes at a time.
+struct Place {
+    int slot, row;
+    bool in;
+};
+__device__ __forceinline__ Place place(const NormDev& d)
+{
+    Place p;
+    if (d.zblocks == 1) {
+        p.row = threadIdx.x / d.slots;
+        p.slot = threadIdx.x - p.row * d.slots;
+        p.in = p.row < d.rows;
+    } else {
+        p.row = 0;
+        p.slot = blockIdx.y * kThreads + threadIdx.x;
+        p.in = p.slot < d.slots;
+    }
+    return p;
+}
+
+// Calls f(u, position) for the thread's positions of an item, kUnroll at a time: first all loads, then all of the rest.
+template <class Load, class Use>
+__device__ __forceinline__ void sweep(const NormDev& d, long long first, long long end, int row, Load&& ld, Use&& use)
+{
+    for (long long p = first + row; p < end; p += (long long)kUnroll * d.rows) {
+#pragma unroll
+        for (int u = 0; u < kUnroll; ++u) {
+            const long long q = p + (long long)u * d.rows;
+            ld(u, q, q < end);
+        }
+#pragma unroll
+        for (int u = 0; u < kUnroll; ++u) {
+            const long long q = p + (long long)u * d.rows;
+            use(u, q, q < end);
+        }
+    }
+}
+
+// (count, mean, m2) of a joined with those of b
+__device__ __forceinline__ void join(float& n, float& mean, float& m2, float nb, float mb, float m2b)
+{
+    const float total = n + nb;
+    if (nb > 0.0f) {
+        const float w = nb / total, delta = mb - mean;
+        mean = n > 0.0f ? mean + delta * w : mb;
+        m2 += m2b + (n > 0.0f ? delta * delta * n * w : 0.0f);
+        n = total;
+    }
+}
+
+// Pass 1 of the forward: (count, mean, m2) of every channel of every item -> part[(item C + c) 3].
+template <class TX, int V, bool MASK>
+__global__ __launch_bounds__(kThreads) void norm_stats_kernel(NormDev d, const TX* __restrict__ x, float* __restrict__ part)
+{
+    __shared__ float sm[kThreads * V * 2];
+    __shared__ float sn[kThreads];
+    const Place at = place(d);
+    const long long items = d.N * d.chunks;
+    for (long long item = blockIdx.x; item < items; item += gridDim.x) {
+        const long long n = item / d.chunks, first = (item - n * d.chunks) * d.chunk, end = min(first + d.chunk, d.P);
+        const TX* base = x + (size_t)(n * d.P) * d.xs + at.slot * V;
+        const float* occ = MASK ? d.occ + n * d.P : nullptr;
+        float shift[V], s1[V], s2[V], count = 0.0f;
+#pragma unroll
+        for (int j = 0; j < V; ++j) shift[j] = s1[j] = s2[j] = 0.0f;
+        if (at.in) {
+            Pack<TX, V> v[kUnroll];
+            bool on[kUnroll];
+            sweep(d, first, end, at.row,
+                  [&](int u, long long p, bool in) {
+                      on[u] = in && (!MASK || occ[p] > 0.0f);
+                      if (on[u]) load<TX, V>(base + p * d.xs, v[u]);
+                  },
+                  [&](int u, long long, bool) {
+                      if (!on[u]) return;
+#pragma unroll
+                      for (int j = 0; j < V; ++j) {
+                          const float value = to_f32(v[u].v[j]);
+                          if (count == 0.0f) shift[j] = value;
+                          const float t = value - shift[j];
+                          s1[j] += t;
+                          s2[j] = fmaf(t, t, s2[j]);
+                      }
+                      count += 1.0f;
+                  });
+        }
+        const float inv = count > 0.0f ? 1.0f / count : 0.0f;
+        float mean[V], m2[V];
+#pragma unroll
+        for (int j = 0; j < V; ++j) {
+            const float m = s1[j] * inv;
+            mean[j] = shift[j] + m;
+            m2[j] = fmaxf(s2[j] - s1[j] * m, 0.0f);
+            if (!(s2[j] >= 0.0f)) m2[j] = s2[j];   // (NaN among the values)
+        }
+        for (int rows = d.rows; rows > 1;) {
+            const int half = (rows + 1) / 2;
+            __syncthreads();
+            if (at.in && at.row >= half && at.row < rows) {
+                sn[threadIdx.x] = count;
+#pragma unroll
+                for (int j = 0; j < V; ++j) {
+                    sm[j * kThreads + threadIdx.x] = mean[j];
+                    sm[(V + j) * kThreads + threadIdx.x] = m2[j];
+                }
+            }
+            __syncthreads();
+            if (at.in && at.row + half < rows) {
+                const int o = threadIdx.x + half * d.slots;
+                const float nb = sn[o], before = count;
+#pragma unroll
+                for (int j = 0; j < V; ++j) {
+                    float c = before;
+                    join(c, mean[j], m2[j], nb, sm[j * kThreads + o], sm[(V + j) * kThreads + o]);
+                }
+                count = before + nb;
+            }
+            rows = half;
+        }
+        if (at.in && at.row == 0) {
+            float* out = part + ((size_t)item * d.C + at.slot * V) * 3;
+#pragma unroll
+            for (int j = 0; j < V; ++j) {
+                out[3 * j] = count;
+                out[3 * j + 1] = mean[j];
+                out[3 * j + 2] = m2[j];
+            }
+        }
+    }
+}
+
+__device__ __forceinline__ double block_sum(double v, double* lds)
+{
+    for (int o = 32; o; o >>= 1) v += __shfl_xor(v, o);
+    __syncthreads();
+    if ((threadIdx.x & 63) == 0) lds[threadIdx.x >> 6] = v;
+    __syncthreads();
+    return lds[0] + lds[1] + lds[2] + lds[3];
+}
+
+// Joins a group's parts: one workgroup a (sample, group) -> stats[(n G + g) 2] = mean, rstd.
+__global__ __launch_bounds__(kThreads) void norm_join_kernel(NormDev d, const float* __restrict__ part, float* __restrict__ stats)
+{
+    __shared__ double lds[4];
+    const long long groups = d.N * d.G;
+    for (long long k = blockIdx.x; k < groups; k += gridDim.x) {
+        const long long n = k / d.G;
+        const int g = (int)(k - n * d.G);
+        double cnt = 0.0, sum = 0.0, sq = 0.0;
+        for (long long i = threadIdx.x; i < (long long)d.chunks * d.Cg; i += kThreads) {
+            const long long chunk = i / d.Cg;
+            const float* p = part + ((size_t)(n * d.chunks + chunk) * d.C + g * d.Cg + (i - chunk * d.Cg)) * 3;
+            const double c = p[0], m = p[1];
+            cnt += c;
+            sum += c * m;
+            sq += (double)p[2] + c * m * m;
+        }
+        cnt = block_sum(cnt, lds);
+        sum = block_sum(sum, lds);
+        sq = block_sum(sq, lds);
+        if (threadIdx.x == 0) {
+            float mean = 0.0f, rstd = 0.0f;
+            if (cnt > 0.0) {
+                const double m = sum / cnt;
+                double var = sq / cnt - m * m;
+                if (var < 0.0) var = 0.0;
+                mean = (float)m;
+                rstd = (float)(1.0 / sqrt(var + (double)d.eps));
+            }
+            stats[2 * k] = mean;
+            stats[2 * k + 1] = rstd;
+        }
+        __syncthreads();
+    }
+}
+
+// Pass 2 of the forward.
+template <class TX, class TY, int V, bool MASK>
+__global__ __launch_bounds__(kThreads) void norm_apply_kernel(NormDev d, const TX* x, TY* y, const float* __restrict__ stats)
+{
+    const Place at = place(d);
+    if (!at.in) return;
+    const long long items = d.N * d.chunks;
+    for (long long item = blockIdx.x; item < items; item += gridDim.x) {
+        const long long n = item / d.chunks, first = (item - n * d.chunks) * d.chunk, end = min(first + d.chunk, d.P);
+        const TX* base = x + (size_t)(n * d.P) * d.xs + at.slot * V;
+        TY* out = y + (size_t)(n * d.P) * d.ys + at.slot * V;
+        const float* occ = MASK ? d.occ + n * d.P : nullptr;
+        float mean[V], scale[V], beta[V];
+#pragma unroll
+        for (int j = 0; j < V; ++j) {
+            const int c = at.slot * V + j;
+            const float* st = stats + (n * d.G + c / d.Cg) * 2;
+            mean[j] = st[0];
+            scale[j] = st[1] * (d.gamma ? d.gamma[c] : 1.0f);
+            beta[j] = d.beta ? d.beta[c] : 0.0f;
+        }
+        Pack<TX, V> v[kUnroll];
+        bool on[kUnroll];
+        sweep(d, first, end, at.row,
+              [&](int u, long long p, bool in) {
+                  on[u] = in && (!MASK || occ[p] > 0.0f);
+                  if (on[u]) load<TX, V>(base + p * d.xs, v[u]);
+              },
+              [&](int u, long long p, bool in) {
+                  if (!in) return;
+                  float r[V];
+#pragma unroll
+                  for (int j = 0; j < V; ++j) r[j] = on[u] ? activate(fmaf(to_f32(v[u].v[j]) - mean[j], scale[j], beta[j]), d.act) : 0.0f;
+                  store<TY, V>(out + p * d.ys, r);
+              });
+    }
+}
+
+// Pass 1 of the backward: (sum g, sum g xh) of every channel of every item -> part[(item C + c) 2], and the item's count.
+template <class TX, class TY, int V, bool MASK>
+__global__ __launch_bounds__(kThreads) void norm_grad_sums_kernel(NormDev d, const TX* __restrict__ x, const TY* __restrict__ dy,
+                                                                  const float* __restrict__ stats, float* __restrict__ part,
+                                                                  float* __restrict__ counts)
+{
+    __shared__ float sm[kThreads * V * 2];
+    __shared__ float sn[kThreads];
+    const Place at = place(d);
+    const long long items = d.N * d.chunks;
+    for (long long item = blockIdx.x; item < items; item += gridDim.x) {
+        const long long n = item / d.chunks, first = (item - n * d.chunks) * d.chunk, end = min(first + d.chunk, d.P);
+        float sg[V], sx[V], count = 0.0f;
+#pragma unroll
+        for (int j = 0; j < V; ++j) sg[j] = sx[j] = 0.0f;
+        if (at.in) {
+            const TX* base = x + (size_t)(n * d.P) * d.xs + at.slot * V;
+            const TY* up = dy + (size_t)(n * d.P) * d.ys + at.slot * V;
+            const float* occ = MASK ? d.occ + n * d.P : nullptr;
+            float mean[V], rstd[V], gamma[V], beta[V];
+#pragma unroll
+            for (int j = 0; j < V; ++j) {
+                const int c = at.slot * V + j;
+                const float* st = stats + (n * d.G + c / d.Cg) * 2;
+                mean[j] = st[0];
+                rstd[j] = st[1];
+                gamma[j] = d.gamma ? d.gamma[c] : 1.0f;
+                beta[j] = d.beta ? d.beta[c] : 0.0f;
+            }
+            Pack<TX, V> v[kUnroll];   // (as they are stored: converted where they are used)
+            Pack<TY, V> w[kUnroll];
+            bool on[kUnroll];
+            sweep(d, first, end, at.row,
+                  [&](int u, long long p, bool in) {
+                      on[u] = in && (!MASK || occ[p] > 0.0f);
+                      if (on[u]) {
+                          load<TX, V>(base + p * d.xs, v[u]);
+                          load<TY, V>(up + p * d.ys, w[u]);
+                      }
+                  },
+                  [&](int u, long long, bool) {
+                      if (!on[u]) return;
+#pragma unroll
+                      for (int j = 0; j < V; ++j) {
+                          const float xh = (to_f32(v[u].v[j]) - mean[j]) * rstd[j];
+                          const float g = to_f32(w[u].v[j]) * slope(fmaf(xh, gamma[j], beta[j]), d.act);
+                          sg[j] += g;
+                          sx[j] = fmaf(g, xh, sx[j]);
+                      }
+                      count += 1.0f;
+                  });
+        }
+        for (int rows = d.rows; rows > 1;) {
+            const int half = (rows + 1) / 2;
+            __syncthreads();
+            if (at.in && at.row >= half && at.row < rows) {
+                sn[threadIdx.x] = count;
+#pragma unroll
+                for (int j = 0; j < V; ++j) {
+                    sm[j * kThreads + threadIdx.x] = sg[j];
+                    sm[(V + j) * kThreads + threadIdx.x] = sx[j];
+                }
+            }
+            __syncthreads();
+            if (at.in && at.row + half < rows) {
+                const int o = threadIdx.x + half * d.slots;
+                count += sn[o];
+#pragma unroll
+                for (int j = 0; j < V; ++j) {
+                    sg[j] += sm[j * kThreads + o];
+                    sx[j] += sm[(V + j) * kThreads + o];
+                }
+            }
+            rows = half;
+        }
+        if (at.in && at.row == 0) {
+            float* out = part + ((size_t)item * d.C + at.slot * V) * 2;
+#pragma unroll
+            for (int j = 0; j < V; ++j) {
+                out[2 * j] = sg[j];
+                out[2 * j + 1] = sx[j];
+            }
+            if (at.slot == 0) counts[item] = count;
+        }
+    }
+}
+
+// Joins the backward's parts: one workgroup a (sample, group).  chan[(n C + c) 2] = sums of a channel,
+// means[(n G + g) 2] = S1 / count, S2 / count.
+__global__ __launch_bounds__(kThreads) void norm_grad_join_kernel(NormDev d, const float* __restrict__ part,
+                                                                  const float* __restrict__ counts, double* __restrict__ chan,
+                                                                  float* __restrict__ means)
+{
+    __shared__ double lds[4];
+    const long long groups = d.N * d.G;
+    for (long long k = blockIdx.x; k < groups; k += gridDim.x) {
+        const long long n = k / d.G;
+        const int g = (int)(k - n * d.G);
+        double cnt = 0.0;
+        for (int i = threadIdx.x; i < d.chunks; i += kThreads) cnt += (double)counts[n * d.chunks + i];
+        cnt = block_sum(cnt, lds) * d.Cg;
+        double s1 = 0.0, s2 = 0.0;
+        for (int j = 0; j < d.Cg; ++j) {
+            const int c = g * d.Cg + j;
+            double a = 0.0, b = 0.0;
+            for (int i = threadIdx.x; i < d.chunks; i += kThreads) {
+                const float* p = part + ((size_t)(n * d.chunks + i) * d.C + c) * 2;
+                a += (double)p[0];
+                b += (double)p[1];
+            }
+            a = block_sum(a, lds);
+            b = block_sum(b, lds);
+            const double gamma = d.gamma ? (double)d.gamma[c] : 1.0;
+            s1 += gamma * a;
+            s2 += gamma * b;
+            if (threadIdx.x == 0) {
+                chan[(n * d.C + c) * 2] = a;
+                chan[(n * d.C + c) * 2 + 1] = b;
+            }
+        }
+        if (threadIdx.x == 0) {
+            means[2 * k] = cnt > 0.0 ? (float)(s1 / cnt) : 0.0f;
+            means[2 * k + 1] = cnt > 0.0 ? (float)(s2 / cnt) : 0.0f;
+        }
+        __syncthreads();
+    }
+}
+
+// Gradients of the parameters: the samples' sums added in order.
+__global__ __launch_bounds__(kThreads) void norm_params_kernel(NormDev d, const double* __restrict__ chan, float* d_gamma, float* d_beta)
+{
+    const int c = blockIdx.x * kThreads + threadIdx.x;
+    if (c >= d.C) return;
+    double a = 0.0, b = 0.0;
+    for (long long n = 0; n < d.N; ++n) {
+        a += chan[(n * d.C + c) * 2];
+        b += chan[(n * d.C + c) * 2 + 1];
+    }
+    if (d_beta) d_beta[c] = (float)((double)d_beta[c] + a);
+    if (d_gamma) d_gamma[c] = (float)((double)d_gamma[c] + b);
+}
+
+// Pass 2 of the backward.
+template <class TX, class TY, int V, bool MASK>
+__global__ __launch_bounds__(kThreads) void norm_grad_kernel(NormDev d, const TX* x, const TY* dy, TX* dx,
+                                                             const float* __restrict__ stats, const float* __restrict__ means)
+{
+    const Place at = place(d);
+    if (!at.in) return;
+    const long long items = d.N * d.chunks;
+    for (long long item = blockIdx.x; item < items; item += gridDim.x) {
+        const long long n = item / d.chunks, first = (item - n * d.chunks) * d.chunk, end = min(first + d.chunk, d.P);
+        const TX* base = x + (size_t)(n * d.P) * d.xs + at.slot * V;
+        const TY* up = dy + (size_t)(n * d.P) * d.ys + at.slot * V;
+        TX* out = dx + (size_t)(n * d.P) * d.xs + at.slot * V;
+        const float* occ = MASK ? d.occ + n * d.P : nullptr;
+        float mean[V], rstd[V], gamma[V], beta[V], m1[V], m2[V];
+#pragma unroll
+        for (int j = 0; j < V; ++j) {
+            const int c = at.slot * V + j;
+            const long long k = n * d.G + c / d.Cg;
+            mean[j] = stats[2 * k];
+            rstd[j] = stats[2 * k + 1];
+            m1[j] = means[2 * k];
+            m2[j] = means[2 * k + 1];
+            gamma[j] = d.gamma ? d.gamma[c] : 1.0f;
+            beta[j] = d.beta ? d.beta[c] : 0.0f;
+        }
+        Pack<TX, V> v[kUnroll];   // (as they are stored: converted where they are used)
+        Pack<TY, V> w[kUnroll];
+        bool on[kUnroll];
+        sweep(d, first, end, at.row,
+              [&](int u, long long p, bool in) {
+                  on[u] = in && (!MASK || occ[p] > 0.0f);
+                  if (on[u]) {
+                      load<TX, V>(base + p * d.xs, v[u]);
+                      load<TY, V>(up + p * d.ys, w[u]);
+                  }
+              },
+              [&](int u, long long p, bool in) {
+                  if (!in) return;
+                  float r[V];
+#pragma unroll
+                  for (int j = 0; j < V; ++j) {
+                      r[j] = 0.0f;
+                      if (on[u]) {
+                          const float xh = (to_f32(v[u].v[j]) - mean[j]) * rstd[j];
+                          const float g = to_f32(w[u].v[j]) * slope(fmaf(xh, gamma[j], beta[j]), d.act);
+                          r[j] = rstd[j] * (fmaf(gamma[j], g, -m1[j]) - xh * m2[j]);
+                      }
+                  }
+                  store<TX, V>(out + p * d.xs, r);
+              });
+    }
+}
+
+// ---- host ------------------------------------------------------------------------------------------------------
+
+size_t align256(size_t n) { return (n + 255) / 256 * 256; }
+int dtype_bytes(int t) { return t == LP_F32 ? 4 : 2; }
+
+lp_status validate(const lp_group_norm* q, NormDev* d)
+{
+    if (!q) return fail(LP_ERR_INVALID_ARG, "norm must not be NULL");
+    if (q->N < 0 || q->P < 0) return fail(LP_ERR_INVALID_ARG, "norm->N and norm->P must be >= 0");
+    if (q->C < 1 || q->G < 1 || q->C % q->G) return fail(LP_ERR_INVALID_ARG, "norm->G must be >= 1 and divide norm->C");
+    if (q->act < LP_ACT_NONE || q->act > LP_ACT_GELU) return fail(LP_ERR_INVALID_ARG, "norm->act must be an lp_act");
+    if (!std::isfinite(q->eps) || q->eps < 0.0f) return fail(LP_ERR_INVALID_ARG, "norm->eps must be finite and >= 0");
+    for (int t : {q->x_dtype, q->y_dtype})
+        if (t != LP_F32 && t != LP_BF16 && t != LP_F16)
+            return fail(LP_ERR_INVALID_ARG, "norm->x_dtype and norm->y_dtype must be LP_F32, LP_BF16 or LP_F16");
+    if (q->x_dtype != q->y_dtype && q->x_dtype != LP_F32)
+        return fail(LP_ERR_UNSUPPORTED, "norm->y_dtype must be norm->x_dtype unless that is LP_F32");
+    const long long xs = q->x_stride ? q->x_stride : q->C, ys = q->y_stride ? q->y_stride : q->C;
+    if (xs < q->C || ys < q->C) return fail(LP_ERR_INVALID_ARG, "norm->x_stride and norm->y_stride must be 0 or >= norm->C");
+    // offsets in bytes are kept in 64 bits
+    const double most = (double)q->N * (double)q->P * (double)(xs > ys ? xs : ys) * 4.0;
+    if (most > 4e18 || (double)q->N * (double)q->C > 1e12) return fail(LP_ERR_UNSUPPORTED, "norm: tensors beyond 64-bit offsets");
+    std::memset(d, 0, sizeof(*d));
+    d->N = q->N; d->P = q->P; d->C = q->C; d->G = q->G; d->Cg = q->C / q->G;
+    d->xs = xs; d->ys = ys; d->gamma = q->gamma; d->beta = q->beta; d->occ = q->occupancy; d->eps = q->eps; d->act = q->act;
+    return LP_OK;
+}
+
+// Divides the work for slots of V channels.  The number of items does not depend on V by more than rounding: `most` is what
+// the workspace has room for.
+void divide(NormDev* d, int V, int n_cu)
+{
+    d->slots = d->C / V;
+    d->zblocks = (d->slots + kThreads - 1) / kThreads;
+    d->rows = d->zblocks > 1 ? 1 : kThreads / d->slots;
+    // eight workgroups a compute unit keep enough loads in flight; no fewer than eight positions a thread, at most 2^22 an item
+    // (counts are exact in fp32)
+    const long long target = ((long long)8 * n_cu + d->N - 1) / (d->N > 0 ? d->N : 1);
+    long long most = (d->P + 8ll * d->rows - 1) / (8ll * d->rows);
+    long long chunks = target < most ? target : most;
+    const long long least = (d->P + (1ll << 22) - 1) >> 22;
+    if (chunks < least) chunks = least;
+    if (chunks < 1) chunks = 1;
+    d->chunk = (d->P + chunks - 1) / chunks;
+    d->chunk = (d->chunk + d->rows - 1) / d->rows * d->rows;
+    if (d->chunk < 1) d->chunk = 1;
+    d->chunks = (int)((d->P + d->chunk - 1) / d->chunk);
+    if (d->chunks < 1) d->chunks = 1;
+}
+
+long long most_items(const NormDev& d, int n_cu)
+{
+    long long most = 0;
+    for (int V = 1; V <= 8; V *= 2) {
+        if (d.C % V) break;
+        NormDev t = d;
+        divide(&t, V, n_cu);
+        if (t.N * t.chunks > most) most = t.N * t.chunks;
+    }
+    return most;
+}
+
+struct Sizes {
+    size_t part, counts, chan, means, stats, fwd, bwd;
+};
+Sizes sizes(const NormDev& d, int n_cu)
+{
+    Sizes s;
+    const size_t items = (size_t)most_items(d, n_cu);
+    s.part = align256(items * d.C * 3 * sizeof(float));
+    s.counts = align256(items * sizeof(float));
+    s.chan = align256((size_t)d.N * d.C * 2 * sizeof(double));
+    s.means = s.stats = align256((size_t)d.N * d.G * 2 * sizeof(float));
+    s.fwd = s.part + s.stats;
+    s.bwd = s.part + s.counts + s.chan + s.means;
+    return s;
+}
+
+// The widest slot that channels, strides and addresses allow: 16 bytes of x.
+int slot_width(const NormDev& d, int x_bytes, int y_bytes, std::initializer_list<const void*> xs, std::initializer_list<const void*> ys)
+{
+    for (int V = 16 / x_bytes; V > 1; V /= 2) {
+        bool ok = d.C % V == 0 && d.xs % V == 0 && d.ys % V == 0;
+        for (const void* p : xs) ok = ok && (uintptr_t)p % (V * x_bytes) == 0;
+        for (const void* p : ys) ok = ok && (uintptr_t)p % (V * y_bytes) == 0;
+        if (ok) return V;
+    }
+    return 1;
+}
+
+// Calls f with the types, the slot width and whether there is an occupancy as constants.
+template <class T> struct Type { using type = T; };
+template <class F, class X, class Y, int... Vs>
+void with_width(int V, bool mask, F&& f, Type<X> x, Type<Y> y, std::integer_sequence<int, Vs...>)
+{
+    auto one = [&](auto v) {
+        if (v.value != V) return;
+        if (mask) f(x, y, v, std::true_type()); else f(x, y, v, std::false_type());
+    };
+    (one(std::integral_constant<int, Vs>()), ...);
+}
+template <class F>
+void dispatch(int x_dtype, int y_dtype, int V, bool mask, F&& f)
+{
+    using W4 = std::integer_sequence<int, 1, 2, 4>;
+    using W8 = std::integer_sequence<int, 1, 2, 4, 8>;
+    if (x_dtype == LP_BF16) with_width(V, mask, f, Type<__bf16>(), Type<__bf16>(), W8());
+    else if (x_dtype == LP_F16) with_width(V, mask, f, Type<_Float16>(), Type<_Float16>(), W8());
+    else if (y_dtype == LP_BF16) with_width(V, mask, f, Type<float>(), Type<__bf16>(), W4());
+    else if (y_dtype == LP_F16) with_width(V, mask, f, Type<float>(), Type<_Float16>(), W4());
+    else with_width(V, mask, f, Type<float>(), Type<float>(), W4());
+}
+
+unsigned grid_of(long long items) { return (unsigned)(items < kMaxGrid ? items : kMaxGrid); }
+
+lp_status launched(const char* what)
+{
+    const hipError_t e = hipGetLastError();
+    return e == hipSuccess ? LP_OK : fail(LP_ERR_HIP, std::string(what) + ": " + hipGetErrorString(e));
+}
+
+lp_status forward(const lp_group_norm* q, const void* x, void* y, float* stats, void* workspace, size_t workspace_bytes, hipStream_t s)
+{
+    NormDev d;
+    lp_status st = validate(q, &d);
+    if (st != LP_OK) return st;
+    if (d.N == 0 || d.P == 0) return LP_OK;
+    if (!x || !y) return fail(LP_ERR_INVALID_ARG, "x and y must not be NULL");
+    std::string err;
+    int n_cu = 0;
+    if (compute_units(&n_cu, &err)) return fail(LP_ERR_HIP, err);
+    const Sizes size = sizes(d, n_cu);
+    if (!workspace || workspace_bytes < size.fwd)
+        return fail(LP_ERR_WORKSPACE, "workspace is NULL or smaller than lp_group_norm_workspace_bytes");
+    if ((uintptr_t)workspace % 256) return fail(LP_ERR_INVALID_ARG, "workspace must be 256-byte aligned");
+    const int V = slot_width(d, dtype_bytes(q->x_dtype), dtype_bytes(q->y_dtype), {x}, {y});
+    divide(&d, V, n_cu);
+    float* part = (float*)workspace;
+    float* used = stats ? stats : (float*)((char*)workspace + size.part);
+    const dim3 grid(grid_of(d.N * d.chunks), d.zblocks);
+    dispatch(q->x_dtype, q->y_dtype, V, d.occ != nullptr, [&](auto tx, auto ty, auto v, auto mask) {
+        using TX = typename decltype(tx)::type;
+        using TY = typename decltype(ty)::type;
+        constexpr int W = decltype(v)::value;
+        constexpr bool M = decltype(mask)::value;
+        hipLaunchKernelGGL((norm_stats_kernel<TX, W, M>), grid, dim3(kThreads), 0, s, d, (const TX*)x, part);
+        hipLaunchKernelGGL(norm_join_kernel, dim3(grid_of(d.N * d.G)), dim3(kThreads), 0, s, d, part, used);
+        hipLaunchKernelGGL((norm_apply_kernel<TX, TY, W, M>), grid, dim3(kThreads), 0, s, d, (const TX*)x, (TY*)y, used);
+    });
+    return launched("group norm forward launch");
+}
+
+lp_status backward(const lp_group_norm* q, const void* x, const float* stats, const void* dy, void* dx, float* d_gamma, float* d_beta,
+                   void* workspace, size_t workspace_bytes, hipStream_t s)
+{
+    NormDev d;
+    lp_status st = validate(q, &d);
+    if (st != LP_OK) return st;
+    if (d.N == 0 || d.P == 0) return LP_OK;
+    if (!x || !stats || !dy) return fail(LP_ERR_INVALID_ARG, "x, stats and d_y must not be NULL");
+    std::string err;
+    int n_cu = 0;
+    if (compute_units(&n_cu, &err)) return fail(LP_ERR_HIP, err);
+    const Sizes size = sizes(d, n_cu);
+    if (!workspace || workspace_bytes < size.bwd)
+        return fail(LP_ERR_WORKSPACE, "workspace is NULL or smaller than lp_group_norm_workspace_bytes");
+    if ((uintptr_t)workspace % 256) return fail(LP_ERR_INVALID_ARG, "workspace must be 256-byte aligned");
+    const int V = slot_width(d, dtype_bytes(q->x_dtype), dtype_bytes(q->y_dtype), {x, dx}, {dy});
+    divide(&d, V, n_cu);
+    char* at = (char*)workspace;
+    float* part = (float*)at;
+    float* counts = (float*)(at += size.part);
+    double* chan = (double*)(at += size.counts);
+    float* means = (float*)(at += size.chan);
+    const dim3 grid(grid_of(d.N * d.chunks), d.zblocks);
+    dispatch(q->x_dtype, q->y_dtype, V, d.occ != nullptr, [&](auto tx, auto ty, auto v, auto mask) {
+        using TX = typename decltype(tx)::type;
+        using TY = typename decltype(ty)::type;
+        constexpr int W = decltype(v)::value;
+        constexpr bool M = decltype(mask)::value;
+        hipLaunchKernelGGL((norm_grad_sums_kernel<TX, TY, W, M>), grid, dim3(kThreads), 0, s, d, (const TX*)x, (const TY*)dy, stats,
+                           part, counts);
+        hipLaunchKernelGGL(norm_grad_join_kernel, dim3(grid_of(d.N * d.G)), dim3(kThreads), 0, s, d, part, counts, chan, means);
+        if (d_gamma || d_beta)
+            hipLaunchKernelGGL(norm_params_kernel, dim3((d.C + kThreads - 1) / kThreads), dim3(kThreads), 0, s, d, chan, d_gamma, d_beta);
+        if (dx)
+            hipLaunchKernelGGL((norm_grad_kernel<TX, TY, W, M>), grid, dim3(kThreads), 0, s, d, (const TX*)x, (const TY*)dy, (TX*)dx,
+                               stats, means);
+    });
+    return launched("group norm backward launch");
+}
+
+}  // namespace
+
+}  // namespace lp
+
+extern "C" {
+
+lp_status lp_group_norm_workspace_bytes(const lp_group_norm* norm, size_t* fwd_bytes, size_t* bwd_bytes)
+try {
+    lp::NormDev d;
+    const lp_status st = lp::validate(norm, &d);
+    if (st != LP_OK) return st;
+    std::string err;
+    int n_cu = 0;
+    if (lp::compute_units(&n_cu, &err)) return lp::fail(LP_ERR_HIP, err);
+    const lp::Sizes size = lp::sizes(d, n_cu);
+    if (fwd_bytes) *fwd_bytes = size.fwd;
+    if (bwd_bytes) *bwd_bytes = size.bwd;
+    return LP_OK;
+} catch (...) {
+    return LP_ERR_HIP;
+}
+
+lp_status lp_group_norm_fwd(const lp_group_norm* norm, const void* x, void* y, float* stats, void* workspace, size_t workspace_bytes,
+                            void* stream)
+try {
+    return lp::forward(norm, x, y, stats, workspace, workspace_bytes, (hipStream_t)stream);
+} catch (...) {
+    return LP_ERR_HIP;
+}
+
+lp_status lp_group_norm_bwd(const lp_group_norm* norm, const void* x, const float* stats, const void* d_y, void* d_x, float* d_gamma,
+                            float* d_beta, void* workspace, size_t workspace_bytes, void* stream)
+try {
+    return lp::backward(norm, x, stats, d_y, d_x, d_gamma, d_beta, workspace, workspace_bytes, (hipStream_t)stream);
+} catch (...) {
+    return LP_ERR_HIP;
+}
+
+}  // extern "C"

@@ -1,8 +1,17 @@
 // Kernels and host-side launchers shared between the translation units of the library.
 #pragma once
+#include <string>
+
+#include "lightplane.h"
 #include "lp_device.h"
 
 namespace lp {
+
+// ---- lp_api.hip -----------------------------------------------------------------------
+// Keeps the message for lp_last_error() and returns the status.
+lp_status fail(lp_status s, const std::string& msg);
+// Compute units of the current device; 1 and a message on failure.
+int compute_units(int* out_n_cu, std::string* err);
 
 // ---- generic scalar kernels (lp_generic.hip) ---------------------------------------
 __global__ void fwd_generic_kernel(GridDev g, MlpDev m, RaysDev rays, FwdOut out);

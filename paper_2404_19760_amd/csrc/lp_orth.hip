@@ -16,11 +16,14 @@
 // product.
 #include <hip/hip_runtime.h>
 
+#include <algorithm>
 #include <cmath>
 #include <cstring>
+#include <type_traits>
 #include <vector>
 
 #include "lp_kernels.h"
+#include "lp_mfma.h"
 
 namespace lp {
 
@@ -33,10 +36,16 @@ using f32x16 = float __attribute__((ext_vector_type(16)));
 constexpr int kThreads = 256;
 constexpr int kMaxLists = 16;     // lists of one set of launches (their descriptors travel as kernel arguments)
 constexpr int kPad = 64;          // rows and columns of operands are padded to this
-constexpr int kNormChunks = 64;   // partial sums of a matrix's norm
+constexpr int kNormChunks = 512;  // partial sums of a matrix's norm, at most
+constexpr int kChunk = 8192;      // values of one, at least
+__host__ __device__ inline int norm_chunks(long long size)
+{
+    const long long c = (size + kChunk - 1) / kChunk;
+    return (int)(c < kNormChunks ? c : kNormChunks);
+}
 
 // One list of matrices on the device side.  Layout of a matrix's workspace, in halves from `ws` + i `ws_stride`:
-// four X planes of mp np (X hi, X lo, X^T hi, X^T lo) twice, then four planes of mp mp (A hi, lo, B hi, lo).
+// X and X^T (2 mp np each: hi and lo parts) twice, then A and B (2 mp mp each).
 struct List {
     const void* in;     // G of lp_orthogonalize, or the gradients
     void* out;          // the result, or the weights
@@ -51,10 +60,12 @@ struct List {
     int first_matrix;   // index of its first matrix among all
     int first_tile;     // of the launch
     int tiles;          // of one matrix
+    int vec4;           // four neighbours can be read and written at a time
 };
 
 struct Lists {
     int n, matrices, total_tiles;
+    int order[kMaxLists];   // of the products: the longest ones first
     float lr_decay;     // 1 - lr weight_decay
     float mu;
     int nesterov;
@@ -82,6 +93,17 @@ __device__ __forceinline__ void split(float v, _Float16& hi, _Float16& lo)
     lo = (_Float16)(v - (float)hi);
 }
 
+// Operands lie in memory in the order in which the matrix instructions take them: blocks of 32 rows x 16 columns, row block by
+// row block; of a block first the hi parts, then the lo parts, of each 64 lanes' 16 bytes (lane = row mod 32 + 32 for columns 8 ..
+// 15).  A wave loads a block's half with one instruction, to registers or through LDS, both without bank conflicts.
+constexpr int kBlock = 1024;   // halves of a block: hi 512, lo 512
+// halves from the operand's start to the hi part of element (i, j)
+__device__ __forceinline__ size_t at(int i, int j, int width)
+{
+    return ((size_t)(i >> 5) * (width >> 4) + (j >> 4)) * kBlock + ((i & 31) + ((j & 8) << 2)) * 8 + (j & 7);
+}
+constexpr int kDepth = 32;   // columns a product takes at a time
+
 // The list and the matrix of it that `tile` belongs to, and the tile within the matrix.
 __device__ __forceinline__ const List& find(const Lists& a, int tile, int& matrix, int& local)
 {
@@ -93,6 +115,51 @@ __device__ __forceinline__ const List& find(const Lists& a, int tile, int& matri
     return a.l[k];
 }
 
+// The same for the products.  Neighbouring workgroups run on different XCDs: each XCD takes a contiguous part of every list's tiles
+// (its L2 holds the operands they share; no XCD is left with the long ones), lists in the launch's order.  False: nothing is left.
+__device__ __forceinline__ bool find_on_xcd(const Lists& a, int block, int& list, int& matrix, int& local)
+{
+    int rest = block >> 3;
+    for (int k = 0; k < a.n; ++k) {
+        const List& l = a.l[a.order[k]];
+        const long long all = (long long)l.tiles * l.count;
+        const int part = ((block & 7) + 3 * k) & 7;   // (lists of a few tiles do not all fall to the same XCD)
+        const int from = (int)(all * part >> 3), end = (int)(all * (part + 1) >> 3);
+        if (rest < end - from) {
+            list = a.order[k];
+            matrix = (from + rest) / l.tiles;
+            local = from + rest - matrix * l.tiles;
+            return true;
+        }
+        rest -= end - from;
+    }
+    return false;
+}
+
+using f32x4 = float __attribute__((ext_vector_type(4)));
+
+// Four neighbouring values from `i` on, of which `left` are there.
+__device__ __forceinline__ f32x4 load4(const void* p, size_t i, int dtype, bool vec4, int left)
+{
+    f32x4 v = {};
+    if (vec4) {
+        if (dtype == LP_F32) return *(const f32x4*)((const float*)p + i);
+        if (dtype == LP_BF16) {
+            using b4 = __bf16 __attribute__((ext_vector_type(4)));
+            const b4 q = *(const b4*)((const __bf16*)p + i);
+            for (int e = 0; e < 4; ++e) v[e] = (float)q[e];
+        } else {
+            const half4 q = *(const half4*)((const _Float16*)p + i);
+            for (int e = 0; e < 4; ++e) v[e] = (float)q[e];
+        }
+        return v;
+    }
+#pragma unroll
+    for (int e = 0; e < 4; ++e)
+        if (e < left) v[e] = load_value(p, i + e, dtype);
+    return v;
+}
+
 // Sums of squares in 64 bits (so that no gradient is too large or too small), one workgroup a (matrix, chunk); the optimiser
 // step updates the momentum on the way.
 __global__ __launch_bounds__(kThreads) void orth_norm_kernel(Lists a)
@@ -102,14 +169,28 @@ __global__ __launch_bounds__(kThreads) void orth_norm_kernel(Lists a)
     const List& l = find(a, blockIdx.x, matrix, chunk);
     const long long size = (long long)l.rows * l.cols, from = (long long)matrix * size;
     double sum = 0.0;
-    for (long long i = (long long)chunk * kThreads + threadIdx.x; i < size; i += (long long)l.tiles * kThreads) {
-        float v = load_value(l.in, from + i, l.dtype);
+    for (long long i = ((long long)chunk * kThreads + threadIdx.x) * 4; i < size; i += (long long)l.tiles * kThreads * 4) {
+        const int left = (int)min(size - i, 4ll);
+        f32x4 v = load4(l.in, from + i, l.dtype, l.vec4, left);
         if (l.momentum) {
-            const float mom = fmaf(a.mu, l.momentum[from + i], v);
-            l.momentum[from + i] = mom;
-            v = a.nesterov ? fmaf(a.mu, mom, v) : mom;
+            const f32x4 m = load4(l.momentum, from + i, LP_F32, l.vec4, left);
+            f32x4 to;
+#pragma unroll
+            for (int e = 0; e < 4; ++e) {
+                to[e] = fmaf(a.mu, m[e], v[e]);
+                v[e] = a.nesterov ? fmaf(a.mu, to[e], v[e]) : to[e];
+            }
+            if (l.vec4) {
+                *(f32x4*)(l.momentum + from + i) = to;
+            } else {
+#pragma unroll
+                for (int e = 0; e < 4; ++e)
+                    if (e < left) l.momentum[from + i + e] = to[e];
+            }
         }
-        sum += (double)v * (double)v;
+#pragma unroll
+        for (int e = 0; e < 4; ++e)
+            if (e < left) sum += (double)v[e] * (double)v[e];
     }
     for (int o = 32; o; o >>= 1) sum += __shfl_xor(sum, o);
     if ((threadIdx.x & 63) == 0) lds[threadIdx.x >> 6] = sum;
@@ -117,52 +198,71 @@ __global__ __launch_bounds__(kThreads) void orth_norm_kernel(Lists a)
     if (threadIdx.x == 0) a.norms[(size_t)(l.first_matrix + matrix) * kNormChunks + chunk] = lds[0] + lds[1] + lds[2] + lds[3];
 }
 
-// X_0 and its transpose as hi and lo parts, padded with zeros: one workgroup a 64 x 64 tile of rows x cols.
-__global__ __launch_bounds__(kThreads) void orth_load_kernel(Lists a, int chunks_shift, float scale)
+// X_0 and its transpose as operands, padded with zeros: one workgroup a 64 x 64 tile of G.
+__global__ __launch_bounds__(kThreads) void orth_load_kernel(Lists a, float scale)
 {
-    __shared__ _Float16 th[64 * 66], tl[64 * 66];
-    __shared__ double factor;   // (in 64 bits: no gradient is too large or too small)
+    __shared__ float tile[64 * 65];
+    __shared__ double sums[4];
     int matrix, local;
     const List& l = find(a, blockIdx.x, matrix, local);
-    if (threadIdx.x < 64) {
-        double v = 0.0;
-        const long long size = (long long)l.rows * l.cols;
-        const int chunks = (int)min((long long)kNormChunks, (size + (1 << chunks_shift) - 1) >> chunks_shift);
-        if ((int)threadIdx.x < chunks) v = a.norms[(size_t)(l.first_matrix + matrix) * kNormChunks + threadIdx.x];
-        for (int o = 32; o; o >>= 1) v += __shfl_xor(v, o);
-        const double norm = sqrt(v);
-        if (threadIdx.x == 0) factor = norm == 0.0 ? 0.0 : (double)scale / (norm + (double)a.eps);
-    }
-    __syncthreads();
-    const double f = factor;
+    const long long size = (long long)l.rows * l.cols;
+    const int chunks = norm_chunks(size);
+    double norm = 0.0;
+    for (int i = threadIdx.x; i < chunks; i += kThreads) norm += a.norms[(size_t)(l.first_matrix + matrix) * kNormChunks + i];
+    for (int o = 32; o; o >>= 1) norm += __shfl_xor(norm, o);
+    if ((threadIdx.x & 63) == 0) sums[threadIdx.x >> 6] = norm;
     const int rp = l.tall ? l.np : l.mp, cp = l.tall ? l.mp : l.np;   // padded rows and columns of G
     const int tr = local / (cp / 64), tc = local - tr * (cp / 64);
-    const long long from = (long long)matrix * l.rows * l.cols;
-    _Float16* ws = l.ws + (size_t)matrix * l.ws_stride;
-    const size_t plane = (size_t)l.mp * l.np;
-    _Float16* same = ws + (l.tall ? 2 * plane : 0);    // the planes in the order of G
-    _Float16* other = ws + (l.tall ? 0 : 2 * plane);   // the planes of its transpose
-    const int c = threadIdx.x & 63;
-    for (int r = threadIdx.x >> 6; r < 64; r += 4) {
-        const int gr = tr * 64 + r, gc = tc * 64 + c;
-        float v = 0.0f;
+    const long long from = (long long)matrix * size;
+    const int c4 = (threadIdx.x & 15) * 4;
+    f32x4 v[4];
+#pragma unroll
+    for (int k = 0; k < 4; ++k) {
+        const int gr = tr * 64 + (threadIdx.x >> 4) + 16 * k, gc = tc * 64 + c4;
+        v[k] = f32x4{};
         if (gr < l.rows && gc < l.cols) {
             const size_t i = from + (size_t)gr * l.cols + gc;
-            v = load_value(l.in, i, l.dtype);
-            if (l.momentum) v = a.nesterov ? fmaf(a.mu, l.momentum[i], v) : l.momentum[i];
+            const int left = min(l.cols - gc, 4);
+            const bool vec4 = l.vec4 && left == 4 && (l.cols & 3) == 0;
+            v[k] = load4(l.in, i, l.dtype, vec4, left);
+            if (l.momentum) {
+                const f32x4 m = load4(l.momentum, i, LP_F32, vec4, left);
+#pragma unroll
+                for (int e = 0; e < 4; ++e) v[k][e] = a.nesterov ? fmaf(a.mu, m[e], v[k][e]) : m[e];
+            }
         }
-        _Float16 hi, lo;
-        split((float)((double)v * f), hi, lo);
-        same[(size_t)gr * cp + gc] = hi;
-        same[plane + (size_t)gr * cp + gc] = lo;
-        th[r * 66 + c] = hi;
-        tl[r * 66 + c] = lo;
     }
     __syncthreads();
-    for (int r = threadIdx.x >> 6; r < 64; r += 4) {
-        const size_t at = (size_t)(tc * 64 + r) * rp + tr * 64 + c;
-        other[at] = th[c * 66 + r];
-        other[plane + at] = tl[c * 66 + r];
+    norm = sqrt(sums[0] + sums[1] + sums[2] + sums[3]);
+    const double f = norm == 0.0 ? 0.0 : (double)scale / (norm + (double)a.eps);   // (in 64 bits: see above)
+#pragma unroll
+    for (int k = 0; k < 4; ++k)
+#pragma unroll
+        for (int e = 0; e < 4; ++e) tile[((threadIdx.x >> 4) + 16 * k) * 65 + c4 + e] = (float)((double)v[k][e] * f);
+    __syncthreads();
+    _Float16* ws = l.ws + (size_t)matrix * l.ws_stride;
+    const size_t plane = (size_t)2 * l.mp * l.np;
+    _Float16* same = ws + (l.tall ? plane : 0);    // the operand in the order of G
+    _Float16* other = ws + (l.tall ? 0 : plane);   // its transpose
+    // a lane's 16 bytes: row r of a block of 32, columns c .. c + 7
+    const int lane = threadIdx.x & 63, r = lane & 31, c = (threadIdx.x >> 6) * 16 + (lane >> 5) * 8;
+#pragma unroll
+    for (int k = 0; k < 2; ++k) {
+        half8 hi, lo, thi, tlo;
+#pragma unroll
+        for (int e = 0; e < 8; ++e) {
+            _Float16 vh, vl;
+            split(tile[(k * 32 + r) * 65 + c + e], vh, vl);
+            hi[e] = vh; lo[e] = vl;
+            split(tile[(c + e) * 65 + k * 32 + r], vh, vl);
+            thi[e] = vh; tlo[e] = vl;
+        }
+        _Float16* to = same + at(tr * 64 + k * 32 + r, tc * 64 + c, cp);
+        *(half8*)to = hi;
+        *(half8*)(to + 512) = lo;
+        to = other + at(tc * 64 + k * 32 + r, tr * 64 + c, rp);
+        *(half8*)to = thi;
+        *(half8*)(to + 512) = tlo;
     }
 }
 
@@ -175,23 +275,48 @@ struct Step {
     int from, to;       // which of the two X's is read, written
 };
 
-constexpr int kTile = 64, kDepth = 32;
+using GlobalPtr = __attribute__((address_space(1))) const void;
+using LdsPtr = __attribute__((address_space(3))) void;
 
-// One workgroup of four waves a 64 x 64 tile of P Q^T, a wave 32 x 32 of it.
-template <Product WHAT>
-__global__ __launch_bounds__(kThreads) void orth_product_kernel(Lists a, Step s)
+// One workgroup of eight waves a TILE x TILE tile of P Q^T.  A wave has all rows and 32 columns of the tile, so TILE / 32 waves
+// make a group that covers it, and the groups share the inner dimension among themselves; at the end they exchange sums through LDS,
+// and each finishes a part of the rows.  So a compute unit with a single tile has two waves on every SIMD.
+//
+// The loop's step is 32 columns of P and Q.  P goes through LDS (two buffers in turn), Q, of which no two waves of a group need the
+// same, straight to registers.  For 128 x 128 this keeps both ways below the matrix cores' time: of 768 cycles for a group's step
+// LDS (128 bytes a cycle) takes 640, the cache (64 bytes a cycle) 512.  With waves of 64 x 64 and both operands in LDS it would be
+// 768 and 512, with Q in registers 384 and 768.  A row block's registers are read again, for the next half step, as soon as they
+// have been used, and the workgroup meets in the middle of a step, so that a wave always has products to issue behind the barrier.
+// The small products (hi lo + lo hi) have an accumulator of their own: added into the large one's they would round it three
+// times as often (error against 64 bits at 2048 x 2048: 6.8e-6 in one accumulator, 4.4e-6 in two; fp32 torch 4.2e-6).
+template <int TILE, int GROUPS>
+struct ProductShape {
+    static constexpr int kWaves = TILE / 32, kGroups = GROUPS, kGroupThreads = 64 * kWaves;
+    static constexpr int kThreadsOf = kGroups * kGroupThreads;
+    static constexpr int kBuffer = TILE * kDepth * 4;         // bytes of a step's P
+    static constexpr int kValues = TILE / 2;                  // sums of a lane: TILE / 32 blocks of 16
+    static constexpr int kMine = kValues / kGroups;           // of them a group finishes
+    static constexpr int kBuffers = kGroups * 2 * kBuffer, kExchange = kGroups * (kGroups - 1) * kWaves * kMine * 64 * 4, kTurn = kGroups * kWaves * 32 * 33 * 4;
+    static constexpr int kLds = kBuffers > kExchange ? (kBuffers > kTurn ? kBuffers : kTurn) : (kExchange > kTurn ? kExchange : kTurn);
+};
+
+template <Product WHAT, int TILE, int GROUPS>
+__global__ __launch_bounds__((ProductShape<TILE, GROUPS>::kThreadsOf), (2)) void orth_product_kernel(Lists a, Step s)
 {
-    __shared__ alignas(16) _Float16 lds[4][kTile * (kDepth + 8)];   // P hi, P lo, Q hi, Q lo; rows padded against bank conflicts
-    constexpr int kRow = kDepth + 8;
-    int matrix, local;
-    const List& l = find(a, blockIdx.x, matrix, local);
+    using S = ProductShape<TILE, GROUPS>;
+    constexpr int F = TILE / 32;                    // row blocks
+    constexpr int kLoads = S::kBuffer / (S::kGroupThreads * 16);
+    __shared__ alignas(16) char lds[S::kLds];
+    int list = 0, matrix = 0, local = 0;
+    if (!find_on_xcd(a, blockIdx.x, list, matrix, local)) return;
+    const List& l = a.l[list];
     _Float16* ws = l.ws + (size_t)matrix * l.ws_stride;
-    const size_t plane = (size_t)l.mp * l.np, square = (size_t)l.mp * l.mp;
-    _Float16* x = ws + s.from * 4 * plane;
-    _Float16* A = ws + 8 * plane;
-    _Float16* B = A + 2 * square;
+    const size_t plane = (size_t)2 * l.mp * l.np, square = (size_t)2 * l.mp * l.mp;
+    _Float16* x = ws + s.from * 2 * plane;
+    _Float16* A = ws + 4 * plane;
+    _Float16* B = A + square;
     int ti, tj;
-    const int mt = l.mp / kTile, nt = l.np / kTile;
+    const int mt = (l.mp + TILE - 1) / TILE, nt = (l.np + TILE - 1) / TILE;
     if (WHAT == kGram || WHAT == kPoly) {   // tiles on and above the diagonal, row by row
         ti = 0;
         int rest = local;
@@ -201,82 +326,229 @@ __global__ __launch_bounds__(kThreads) void orth_product_kernel(Lists a, Step s)
         ti = local / nt;
         tj = local - ti * nt;
     }
-    const _Float16 *p, *q;
-    size_t p_lo, q_lo;
-    int K;
-    if (WHAT == kGram) { p = q = x; p_lo = q_lo = plane; K = l.np; }
-    else if (WHAT == kPoly) { p = q = A; p_lo = q_lo = square; K = l.mp; }
-    else { p = B; q = x + 2 * plane; p_lo = square; q_lo = plane; K = l.mp; }
-    const int wave = threadIdx.x >> 6, lane = threadIdx.x & 63;
-    const int wi = wave >> 1, wj = wave & 1, l32 = lane & 31, h = lane >> 5;
-    f32x16 acc = {};
-    const int sr = threadIdx.x >> 2, sc = (threadIdx.x & 3) * 8;   // a thread stages 8 halves of a row of each plane
-    const size_t pat = (size_t)(ti * kTile + sr) * K + sc, qat = (size_t)(tj * kTile + sr) * K + sc;
-    for (int k = 0; k < K; k += kDepth) {
-        const half8 v0 = *(const half8*)(p + pat + k), v1 = *(const half8*)(p + p_lo + pat + k);
-        const half8 v2 = *(const half8*)(q + qat + k), v3 = *(const half8*)(q + q_lo + qat + k);
-        __syncthreads();
-        *(half8*)&lds[0][sr * kRow + sc] = v0;
-        *(half8*)&lds[1][sr * kRow + sc] = v1;
-        *(half8*)&lds[2][sr * kRow + sc] = v2;
-        *(half8*)&lds[3][sr * kRow + sc] = v3;
-        __syncthreads();
+    const _Float16* p = WHAT == kGram ? x : WHAT == kPoly ? A : B;
+    const _Float16* q = WHAT == kGram ? x : WHAT == kPoly ? A : x + plane;
+    const int K = WHAT == kGram ? l.np : l.mp;
+    const int p_blocks = l.mp >> 5, q_blocks = (WHAT == kGram || WHAT == kPoly ? l.mp : l.np) >> 5;
+    const int wave_of_8 = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), group = wave_of_8 / S::kWaves, wave = wave_of_8 % S::kWaves;
+    const int lane = threadIdx.x & 63, in_group = threadIdx.x % S::kGroupThreads, l32 = lane & 31, h = lane >> 5;
+    // a group's steps; where they do not divide evenly the last ones have fewer
+    const int all = K / kDepth, steps = (all + S::kGroups - 1) / S::kGroups, start = group * steps, mine_steps = min(steps, all - start);
+    // row blocks behind an operand's end are its last one again (their products are not stored)
+    const size_t row = (size_t)(K >> 4) * kBlock;   // halves of a row block
+    const _Float16 *p_at[kLoads], *q_at;            // the same for all lanes
 #pragma unroll
-        for (int kk = 0; kk < kDepth; kk += 16) {
-            const int pa = (wi * 32 + l32) * kRow + kk + 8 * h, qa = (wj * 32 + l32) * kRow + kk + 8 * h;
-            const half8 ph = *(const half8*)&lds[0][pa], pl = *(const half8*)&lds[1][pa];
-            const half8 qh = *(const half8*)&lds[2][qa], ql = *(const half8*)&lds[3][qa];
-            acc = __builtin_amdgcn_mfma_f32_32x32x16_f16(pl, qh, acc, 0, 0, 0);
-            acc = __builtin_amdgcn_mfma_f32_32x32x16_f16(ph, ql, acc, 0, 0, 0);
-            acc = __builtin_amdgcn_mfma_f32_32x32x16_f16(ph, qh, acc, 0, 0, 0);
+    for (int u = 0; u < kLoads; ++u) {
+        const int at_byte = u * S::kGroupThreads * 16;   // of the step's P: 4096 of every row block
+        p_at[u] = p + min(ti * F + at_byte / 4096, p_blocks - 1) * row + at_byte % 4096 / 2;
+    }
+    q_at = q + min(tj * F + wave, q_blocks - 1) * row;
+    char* buffers = lds + group * 2 * S::kBuffer;
+    half8 staged[kLoads];
+    half8 qv[4][2];   // Q of two steps: 16-column half of a step, hi or lo
+    auto ask_p = [&](int step) {
+        step = min(start + step, all - 1);
+#pragma unroll
+        for (int u = 0; u < kLoads; ++u) staged[u] = *(const half8*)(p_at[u] + (size_t)step * (2 * kBlock) + in_group * 8);
+    };
+    auto put_p = [&](int buffer, bool any) {
+        char* to = buffers + buffer * S::kBuffer + in_group * 16;
+        if (any) {
+#pragma unroll
+            for (int u = 0; u < kLoads; ++u) *(half8*)(to + u * S::kGroupThreads * 16) = staged[u];
+        } else {
+#pragma unroll
+            for (int u = 0; u < kLoads; ++u) *(half8*)(to + u * S::kGroupThreads * 16) = half8{};
+        }
+    };
+    auto ask_q = [&](int k, half8 (&to)[2]) {   // k: half steps
+        k = min(2 * start + k, 2 * all - 1);
+#pragma unroll
+        for (int c = 0; c < 2; ++c) to[c] = *(const half8*)(q_at + (size_t)k * kBlock + c * 512 + lane * 8);
+    };
+    half8 pv[F][2];
+    auto get_p = [&](int buffer, int k, int f) {
+#pragma unroll
+        for (int c = 0; c < 2; ++c) pv[f][c] = *(const half8*)(buffers + buffer * S::kBuffer + f * 4096 + (2 * k + c) * 1024 + lane * 16);
+    };
+    f32x16 acc[F] = {}, cross[F] = {};
+    ask_p(0);
+#pragma unroll
+    for (int k = 0; k < 4; ++k) ask_q(k, qv[k]);
+    put_p(0, mine_steps > 0);
+    ask_p(1);
+    __syncthreads();
+#pragma unroll
+    for (int f = 0; f < F; ++f) get_p(0, 0, f);
+    for (int first = 0; first < steps; first += 2) {
+#pragma unroll
+        for (int u = 0; u < 2; ++u) {
+            const int step = first + u;
+            put_p(u ^ 1, step + 1 < mine_steps);   // (behind the last step P is zero: what is left of the loop adds nothing)
+            ask_p(step + 2);
+            __builtin_amdgcn_sched_barrier(0);     // (everything is asked for and used in the order written)
+#pragma unroll
+            for (int k = 0; k < 2; ++k) {
+                half8 (&q2)[2] = qv[2 * u + k];
+#pragma unroll
+                for (int i = 0; i < F; ++i) {
+                    cross[i] = __builtin_amdgcn_mfma_f32_32x32x16_f16(pv[i][1], q2[0], cross[i], 0, 0, 0);
+                    acc[i] = __builtin_amdgcn_mfma_f32_32x32x16_f16(pv[i][0], q2[0], acc[i], 0, 0, 0);
+                    cross[i] = __builtin_amdgcn_mfma_f32_32x32x16_f16(pv[i][0], q2[1], cross[i], 0, 0, 0);
+                    // the same rows of the next half step: they arrive while the other rows are multiplied
+                    get_p(k ? u ^ 1 : u, k ^ 1, i);
+                    __builtin_amdgcn_sched_barrier(0);
+                }
+                ask_q(2 * step + k + 4, q2);
+                __builtin_amdgcn_sched_barrier(0);
+                // in the middle of a step: the next step's P is there, and nobody reads this step's any more
+                if (k == 0) __syncthreads();
+            }
         }
     }
-    // value e of a lane: row 8 (e / 4) + 4 h + e % 4, column l32 of the wave's 32 x 32
-    const int i0 = ti * kTile + wi * 32, j = tj * kTile + wj * 32 + l32;
+    __syncthreads();
+    // group g finishes values g kMine .. of every lane; the groups' sums are added in their order
+    float mine[S::kMine];
+    if constexpr (S::kGroups == 1) {
 #pragma unroll
-    for (int e4 = 0; e4 < 4; ++e4) {
-        half4 hi, lo;
-        const int ib = i0 + 8 * e4 + 4 * h;
+        for (int e = 0; e < S::kMine; ++e) mine[e] = acc[e >> 4][e & 15] + cross[e >> 4][e & 15];
+    } else {
+        auto slot = [&](int to, int from, int e) {
+            return (f32x4*)lds + ((to * (S::kGroups - 1) + from - (from > to)) * S::kWaves + wave) * (S::kMine * 16) + (e >> 2) * 64 + lane;
+        };
 #pragma unroll
-        for (int e = 0; e < 4; ++e) {
-            const int i = ib + e;
-            float v = acc[4 * e4 + e] * s.acc;
-            if (WHAT == kPoly) {
-                const size_t at = (size_t)i * l.mp + j;
-                v = fmaf(s.lin, (float)A[at] + (float)A[square + at], v);
-                if (i == j && i < l.m) v += s.diag;
-            }
-            if (WHAT == kLast) {
-                if (i < l.m && j < l.n) {
-                    const size_t at = (size_t)matrix * l.rows * l.cols + (l.tall ? (size_t)j * l.cols + i : (size_t)i * l.cols + j);
-                    if (l.momentum) {
-                        float* w = (float*)l.out + at;
-                        *w = fmaf(-l.step, v, a.lr_decay * *w);
-                    } else {
-                        store_value(l.out, at, l.dtype, v);
-                    }
+        for (int g = 0; g < S::kGroups; ++g)
+#pragma unroll
+            for (int e = 0; e < S::kMine; e += 4) {
+                f32x4 v;
+#pragma unroll
+                for (int j = 0; j < 4; ++j) {
+                    const int at_value = g * S::kMine + e + j;
+                    v[j] = acc[at_value >> 4][at_value & 15] + cross[at_value >> 4][at_value & 15];
                 }
-                continue;
-            }
-            _Float16 vh, vl;
-            split(v, vh, vl);
-            hi[e] = vh;
-            lo[e] = vl;
-        }
-        if (WHAT == kLast) continue;
-        // rows as they come (32 lanes, 64 bytes), and 4 neighbours of the transpose in one store
-        _Float16* direct = WHAT == kGram ? A : WHAT == kPoly ? B : ws + s.to * 4 * plane;
-        const size_t lo_at = WHAT == kUpdate ? plane : square;
-        _Float16* trans = WHAT == kUpdate ? direct + 2 * plane : direct;
-        const int width = WHAT == kUpdate ? l.np : l.mp;
+                if (g == group) {
 #pragma unroll
-        for (int e = 0; e < 4; ++e) {
-            if (WHAT != kUpdate && ti == tj) break;   // (a tile on the diagonal is its own transpose)
-            direct[(size_t)(ib + e) * width + j] = hi[e];
-            direct[lo_at + (size_t)(ib + e) * width + j] = lo[e];
+                    for (int j = 0; j < 4; ++j) mine[e + j] = v[j];
+                } else {
+                    *slot(g, group, e) = v;
+                }
+            }
+        __syncthreads();
+#pragma unroll
+        for (int e = 0; e < S::kMine; e += 4) {
+            f32x4 v = {};
+#pragma unroll
+            for (int g = 0; g < S::kGroups; ++g) {
+                const f32x4 own = {mine[e], mine[e + 1], mine[e + 2], mine[e + 3]};
+                v += g == group ? own : *slot(group, g, e);
+            }
+#pragma unroll
+            for (int j = 0; j < 4; ++j) mine[e + j] = v[j];
         }
-        *(half4*)&trans[(size_t)j * l.mp + ib] = hi;
-        *(half4*)&trans[lo_at + (size_t)j * l.mp + ib] = lo;
+        __syncthreads();
+    }
+    // value e of a lane: row 8 (e / 4) + 4 h + e % 4, column l32 of a 32 x 32 block.  Four rows of a column are neighbours in an
+    // operand whose rows are the block's columns; for the other order the rows are turned over in the wave's own LDS.
+    constexpr int kRows = S::kMine >= 16 ? 32 : 16;   // rows of a block that this wave finishes
+    constexpr int kFinish = S::kMine >= 16 ? S::kMine / 16 : 1;
+    uint32_t* turn = (uint32_t*)lds + wave_of_8 * (32 * 33);
+    const int jb = tj * TILE + wave * 32;
+#pragma unroll
+    for (int fi = 0; fi < kFinish; ++fi) {
+        const int ib = ti * TILE + (group * kFinish + fi) * kRows;
+        if ((ib >> 5) >= p_blocks || (jb >> 5) >= q_blocks) continue;
+        if (WHAT == kLast) {
+            const size_t from = (size_t)matrix * l.rows * l.cols;
+            constexpr int kOut = kRows / 2;
+            float v[kOut];
+#pragma unroll
+            for (int e = 0; e < kOut; ++e) v[e] = mine[fi * 16 + e] * s.acc;
+            if (l.tall) {   // the result's rows are the block's columns: neighbouring lanes take neighbouring block rows
+#pragma unroll
+                for (int e = 0; e < kOut; ++e) turn[(8 * (e >> 2) + 4 * h + (e & 3)) * 33 + l32] = __float_as_uint(v[e]);
+                wave_lds_fence();
+#pragma unroll
+                for (int e = 0; e < kOut; ++e) v[e] = __uint_as_float(turn[(lane & (kRows - 1)) * 33 + e * (64 / kRows) + lane / kRows]);
+                wave_lds_fence();
+            }
+            auto place = [&](int e, bool& in) {
+                const int r = l.tall ? jb + e * (64 / kRows) + lane / kRows : ib + 8 * (e >> 2) + 4 * h + (e & 3);
+                const int c = l.tall ? ib + (lane & (kRows - 1)) : jb + l32;
+                in = r < l.rows && c < l.cols;
+                return from + (size_t)r * l.cols + c;
+            };
+            if (l.momentum) {   // (all weights are read before the first is written)
+                float* w = (float*)l.out;
+                float old[kOut];
+#pragma unroll
+                for (int e = 0; e < kOut; ++e) {
+                    bool in;
+                    const size_t i = place(e, in);
+                    old[e] = in ? w[i] : 0.0f;
+                }
+#pragma unroll
+                for (int e = 0; e < kOut; ++e) {
+                    bool in;
+                    const size_t i = place(e, in);
+                    if (in) w[i] = fmaf(-l.step, v[e], a.lr_decay * old[e]);
+                }
+            } else {
+#pragma unroll
+                for (int e = 0; e < kOut; ++e) {
+                    bool in;
+                    const size_t i = place(e, in);
+                    if (in) store_value(l.out, i, l.dtype, v[e]);
+                }
+            }
+            continue;
+        }
+        _Float16* direct = WHAT == kGram ? A : WHAT == kPoly ? B : ws + s.to * 2 * plane;
+        _Float16* trans = WHAT == kUpdate ? direct + plane : direct;
+        const int width = WHAT == kUpdate ? l.np : l.mp;
+        const bool both = WHAT == kUpdate || ti != tj;   // (a tile on the diagonal is its own transpose)
+#pragma unroll
+        for (int e4 = 0; e4 < kRows / 8; ++e4) {
+            half4 hi, lo, ah, al;
+            const int r = 8 * e4 + 4 * h;
+            const size_t to = at(jb + l32, ib + r, l.mp);
+            if (WHAT == kPoly) {
+                ah = *(const half4*)(A + to);
+                al = *(const half4*)(A + to + 512);
+            }
+#pragma unroll
+            for (int e = 0; e < 4; ++e) {
+                float v = mine[fi * 16 + 4 * e4 + e] * s.acc;
+                if (WHAT == kPoly) {
+                    v = fmaf(s.lin, (float)ah[e] + (float)al[e], v);
+                    if (ib + r + e == jb + l32 && jb + l32 < l.m) v += s.diag;
+                }
+                _Float16 vh, vl;
+                split(v, vh, vl);
+                hi[e] = vh;
+                lo[e] = vl;
+                if (both) turn[(r + e) * 33 + l32] = (uint32_t)__builtin_bit_cast(uint16_t, vh) | (uint32_t)__builtin_bit_cast(uint16_t, vl) << 16;
+            }
+            *(half4*)(trans + to) = hi;
+            *(half4*)(trans + to + 512) = lo;
+        }
+        if (both) {
+            wave_lds_fence();
+#pragma unroll
+            for (int k = 0; k < kRows / 16; ++k) {
+                const int r = lane & (kRows - 1), c = k * 16 + lane / kRows * 8;
+                half8 hi, lo;
+#pragma unroll
+                for (int e = 0; e < 8; ++e) {
+                    const uint32_t v = turn[r * 33 + c + e];
+                    hi[e] = __builtin_bit_cast(_Float16, (uint16_t)v);
+                    lo[e] = __builtin_bit_cast(_Float16, (uint16_t)(v >> 16));
+                }
+                _Float16* to = direct + at(ib + r, jb + c, width);
+                *(half8*)to = hi;
+                *(half8*)(to + 512) = lo;
+            }
+            wave_lds_fence();
+        }
     }
 }
 
@@ -284,7 +556,6 @@ __global__ __launch_bounds__(kThreads) void orth_product_kernel(Lists a, Step s)
 
 size_t align256(size_t n) { return (n + 255) / 256 * 256; }
 int pad(int v) { return (v + kPad - 1) / kPad * kPad; }
-constexpr int kChunkShift = 14;   // values of a partial sum of the norm
 
 struct HostList {
     long long count;
@@ -421,13 +692,29 @@ void number(Lists* a, F&& tiles_of)
     a->total_tiles = at;
 }
 
+// Workgroups of a product: eight times the most that an XCD has.
+unsigned grid_of(const Lists& a)
+{
+    int most = 0;
+    for (int x = 0; x < 8; ++x) {
+        int sum = 0;
+        for (int k = 0; k < a.n; ++k) {
+            const long long all = (long long)a.l[a.order[k]].tiles * a.l[a.order[k]].count;
+            const int part = (x + 3 * k) & 7;
+            sum += (int)((all * (part + 1) >> 3) - (all * part >> 3));
+        }
+        most = sum > most ? sum : most;
+    }
+    return 8u * (unsigned)most;
+}
+
 struct Muon {
     float lr_decay, mu, lr;
     int nesterov, scale;
 };
 
 lp_status run_set(const std::vector<HostList>& v, size_t first, size_t end, const Plan& plan, float eps, const Muon* muon,
-                  void* workspace, hipStream_t s)
+                  void* workspace, int n_cu, hipStream_t s)
 {
     Lists a;
     std::memset(&a, 0, sizeof(a));
@@ -452,6 +739,8 @@ lp_status run_set(const std::vector<HostList>& v, size_t first, size_t end, cons
         l.ws = (_Float16*)at;
         l.ws_stride = (long long)align256(matrix_halves(q.rows, q.cols) * 2) / 2;
         at += (size_t)l.ws_stride * 2 * q.count;
+        l.vec4 = (long long)q.rows * q.cols % 4 == 0 && (uintptr_t)q.in % 16 == 0 && (uintptr_t)q.momentum % 16 == 0;
+        a.order[a.n - 1] = a.n - 1;
         l.first_matrix = a.matrices;
         a.matrices += l.count;
         if (muon) {
@@ -461,25 +750,38 @@ lp_status run_set(const std::vector<HostList>& v, size_t first, size_t end, cons
             l.step = (float)(muon->lr * scale);
         }
     }
-    auto norm_chunks = [](const List& l) {
-        const long long c = ((long long)l.rows * l.cols + (1 << kChunkShift) - 1) >> kChunkShift;
-        return (int)(c < kNormChunks ? c : kNormChunks);   // (never more than the matrix has tiles)
-    };
-    auto all_tiles = [](const List& l) { return (l.mp / kTile) * (l.np / kTile); };
-    auto half_tiles = [](const List& l) { const int t = l.mp / kTile; return t * (t + 1) / 2; };
-    number(&a, norm_chunks);
+    auto load_tiles = [](const List& l) { return (l.mp / 64) * (l.np / 64); };
+    number(&a, [](const List& l) { return norm_chunks((long long)l.rows * l.cols); });   // (never more than the matrix has tiles)
     hipLaunchKernelGGL(orth_norm_kernel, dim3(a.total_tiles), dim3(kThreads), 0, s, a);
-    number(&a, all_tiles);
-    hipLaunchKernelGGL(orth_load_kernel, dim3(a.total_tiles), dim3(kThreads), 0, s, a, kChunkShift, plan.load);
+    number(&a, load_tiles);
+    hipLaunchKernelGGL(orth_load_kernel, dim3(a.total_tiles), dim3(kThreads), 0, s, a, plan.load);
+    // large tiles where they give every compute unit work
+    auto tiles = [](const List& l, int tile, bool half) {
+        const int mt = (l.mp + tile - 1) / tile, nt = (l.np + tile - 1) / tile;
+        return half ? mt * (mt + 1) / 2 : mt * nt;
+    };
+    auto product = [&](auto what, const Step& step) {
+        constexpr Product W = decltype(what)::value;
+        constexpr bool half = W == kGram || W == kPoly;
+        std::sort(a.order, a.order + a.n, [&](int i, int j) {
+            const int ki = W == kGram ? a.l[i].np : a.l[i].mp, kj = W == kGram ? a.l[j].np : a.l[j].mp;
+            return ki != kj ? ki > kj : i < j;
+        });
+        number(&a, [&](const List& l) { return tiles(l, 128, half); });
+        if (a.total_tiles >= 2 * n_cu) {
+            hipLaunchKernelGGL((orth_product_kernel<W, 128, 1>), dim3(grid_of(a)), dim3(256), 0, s, a, step);
+        } else if (a.total_tiles >= n_cu) {
+            hipLaunchKernelGGL((orth_product_kernel<W, 128, 2>), dim3(grid_of(a)), dim3(512), 0, s, a, step);
+        } else {
+            number(&a, [&](const List& l) { return tiles(l, 64, half); });
+            hipLaunchKernelGGL((orth_product_kernel<W, 64, 4>), dim3(grid_of(a)), dim3(512), 0, s, a, step);
+        }
+    };
     for (int k = 0; k < plan.steps; ++k) {
-        number(&a, half_tiles);
-        hipLaunchKernelGGL((orth_product_kernel<kGram>), dim3(a.total_tiles), dim3(kThreads), 0, s, a, plan.gram[k]);
-        hipLaunchKernelGGL((orth_product_kernel<kPoly>), dim3(a.total_tiles), dim3(kThreads), 0, s, a, plan.poly[k]);
-        number(&a, all_tiles);
-        if (k + 1 < plan.steps)
-            hipLaunchKernelGGL((orth_product_kernel<kUpdate>), dim3(a.total_tiles), dim3(kThreads), 0, s, a, plan.update[k]);
-        else
-            hipLaunchKernelGGL((orth_product_kernel<kLast>), dim3(a.total_tiles), dim3(kThreads), 0, s, a, plan.update[k]);
+        product(std::integral_constant<Product, kGram>(), plan.gram[k]);
+        product(std::integral_constant<Product, kPoly>(), plan.poly[k]);
+        if (k + 1 < plan.steps) product(std::integral_constant<Product, kUpdate>(), plan.update[k]);
+        else product(std::integral_constant<Product, kLast>(), plan.update[k]);
     }
     return launched("orthogonalisation launch");
 }
@@ -491,15 +793,18 @@ lp_status run(const std::vector<HostList>& v, const Plan& plan, float eps, const
     if (!workspace || workspace_bytes < all_bytes(v))
         return fail(LP_ERR_WORKSPACE, "workspace is NULL or smaller than the call's workspace_bytes function says");
     if ((uintptr_t)workspace % 256) return fail(LP_ERR_INVALID_ARG, "workspace must be 256-byte aligned");
+    std::string err;
+    int n_cu = 0;
+    if (compute_units(&n_cu, &err)) return fail(LP_ERR_HIP, err);
     // (refused before anything is launched)
     for (size_t k = 0; k < v.size(); k += kMaxLists) {
         double tiles = 0.0;
         for (size_t i = k; i < v.size() && i < k + kMaxLists; ++i)
-            tiles += (double)v[i].count * (pad(v[i].rows) / kTile) * (pad(v[i].cols) / kTile);
+            tiles += (double)v[i].count * (pad(v[i].rows) / 64) * (pad(v[i].cols) / 64);
         if (tiles > (double)kMaxTiles) return fail(LP_ERR_UNSUPPORTED, "too many matrices for one call");
     }
     for (size_t k = 0; k < v.size(); k += kMaxLists) {
-        const lp_status st = run_set(v, k, v.size() < k + kMaxLists ? v.size() : k + kMaxLists, plan, eps, muon, workspace, s);
+        const lp_status st = run_set(v, k, v.size() < k + kMaxLists ? v.size() : k + kMaxLists, plan, eps, muon, workspace, n_cu, s);
         if (st != LP_OK) return st;
     }
     return LP_OK;

@@ -552,6 +552,226 @@ __global__ __launch_bounds__((ProductShape<TILE, GROUPS>::kThreadsOf), (2)) void
     }
 }
 
+// Scales of all steps from the bounds of what the operands can hold.
+struct Plan {
+    float load;   // of X_0
+    Step gram[LP_ORTH_MAX_STEPS], poly[LP_ORTH_MAX_STEPS], update[LP_ORTH_MAX_STEPS];
+    int steps;
+};
+
+// ---- small matrices: a workgroup does all of it --------------------------------------------------------------------
+
+// Matrices of at most 64 x 128 (a decoder's layers): one workgroup of four waves keeps X, X^T, A and B in LDS, in the same order as
+// the large operands, from the gradient to the result: one launch, and no bytes but G's and the result's (the optimiser's: the
+// momentum's and the weights').  Its time is that of a chain of 3 x steps products with a barrier behind each, about XXX us.
+// Rows and columns are padded to 32.  A wave has one 32 x 32 block of A and B and up to two of X.
+constexpr int kSmallM = 64, kSmallN = 128;
+__host__ __device__ inline int pad32(int v) { return (v + 31) & ~31; }
+__host__ __device__ inline bool is_small(int rows, int cols)
+{
+    const int m = rows < cols ? rows : cols, n = rows < cols ? cols : rows;
+    return m <= kSmallM && n <= kSmallN;
+}
+// LDS: X, X^T, B, then A (the waves' blocks to turn over lie over it); G in 32 bits lies over B and A before they are made.
+__host__ __device__ inline int small_lds(int mp, int np)
+{
+    const int turn = 4 * 32 * 33 * 4, square = mp * mp * 4, g = mp * (np + 1) * 4;
+    const int rest = square + (square > turn ? square : turn);
+    return 2 * mp * np * 4 + (rest > g ? rest : g);
+}
+
+__global__ __launch_bounds__(kThreads) void orth_small_kernel(Lists a, Plan plan)
+{
+    extern __shared__ char small_bytes[];
+    __shared__ double sums[4];
+    int matrix, local;
+    const List& l = find(a, blockIdx.x, matrix, local);
+    const int m = l.m, n = l.n, mp = pad32(m), np = pad32(n);
+    _Float16* X = (_Float16*)small_bytes;
+    _Float16* XT = X + 2 * mp * np;
+    _Float16* B = XT + 2 * mp * np;
+    _Float16* A = B + 2 * mp * mp;
+    float* g = (float*)B;   // [mp][np + 1], X's order
+    const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), lane = threadIdx.x & 63, l32 = lane & 31, h = lane >> 5;
+    uint32_t* turn = (uint32_t*)A + wave * (32 * 33);
+    const size_t from = (size_t)matrix * l.rows * l.cols;
+    const int size = l.rows * l.cols;
+    for (int i = threadIdx.x; i < mp * (np + 1); i += kThreads) g[i] = 0.0f;
+    __syncthreads();
+    double norm = 0.0;
+    constexpr int kMost = kSmallM * kSmallN / kThreads;   // values of a thread, at most
+    float value[kMost], old[kMost];
+#pragma unroll
+    for (int k = 0; k < kMost; ++k) {
+        const int i = threadIdx.x + k * kThreads;
+        if (k * kThreads >= size) break;
+        value[k] = old[k] = 0.0f;
+        if (i < size) {
+            value[k] = load_value(l.in, from + i, l.dtype);
+            if (l.momentum) old[k] = l.momentum[from + i];
+        }
+    }
+#pragma unroll
+    for (int k = 0; k < kMost; ++k) {
+        const int i = threadIdx.x + k * kThreads;
+        if (k * kThreads >= size) break;
+        if (i < size) {
+            float v = value[k];
+            if (l.momentum) {
+                const float mom = fmaf(a.mu, old[k], v);
+                l.momentum[from + i] = mom;
+                v = a.nesterov ? fmaf(a.mu, mom, v) : mom;
+            }
+            norm += (double)v * (double)v;
+            const int r = i / l.cols, c = i - r * l.cols;
+            g[l.tall ? c * (np + 1) + r : r * (np + 1) + c] = v;
+        }
+    }
+    for (int o = 32; o; o >>= 1) norm += __shfl_xor(norm, o);
+    if (lane == 0) sums[wave] = norm;
+    __syncthreads();
+    norm = sqrt(sums[0] + sums[1] + sums[2] + sums[3]);
+    const double f = norm == 0.0 ? 0.0 : (double)plan.load / (norm + (double)a.eps);
+    for (int u = threadIdx.x; u < mp * np / 8; u += kThreads) {
+        // unit u: 16 bytes of a lane of a block, of X and of X^T
+        const int ln = u & 63, block = u >> 6, r = ln & 31, c = (ln >> 5) * 8;
+        half8 hi, lo;
+        const int xi = block / (np >> 4) * 32 + r, xj = block % (np >> 4) * 16 + c;
+        const int ti = block / (mp >> 4) * 32 + r, tj = block % (mp >> 4) * 16 + c;
+#pragma unroll
+        for (int e = 0; e < 8; ++e) {
+            _Float16 vh, vl;
+            split((float)((double)g[xi * (np + 1) + xj + e] * f), vh, vl);
+            hi[e] = vh; lo[e] = vl;
+        }
+        *(half8*)(X + block * kBlock + ln * 8) = hi;
+        *(half8*)(X + block * kBlock + 512 + ln * 8) = lo;
+#pragma unroll
+        for (int e = 0; e < 8; ++e) {
+            _Float16 vh, vl;
+            split((float)((double)g[(tj + e) * (np + 1) + ti] * f), vh, vl);
+            hi[e] = vh; lo[e] = vl;
+        }
+        *(half8*)(XT + block * kBlock + ln * 8) = hi;
+        *(half8*)(XT + block * kBlock + 512 + ln * 8) = lo;
+    }
+    __syncthreads();
+    // block (bi, bj) of P Q^T over K columns
+    auto product = [&](const _Float16* p, const _Float16* q, int K, int bi, int bj) {
+        f32x16 acc = {}, cross = {};
+        const _Float16* pb = p + bi * (K >> 4) * kBlock + lane * 8;
+        const _Float16* qb = q + bj * (K >> 4) * kBlock + lane * 8;
+        for (int k = 0; k < K >> 4; k += 2) {
+#pragma unroll
+            for (int u = 0; u < 2; ++u) {
+                const half8 ph = *(const half8*)(pb + (k + u) * kBlock), pl = *(const half8*)(pb + (k + u) * kBlock + 512);
+                const half8 qh = *(const half8*)(qb + (k + u) * kBlock), ql = *(const half8*)(qb + (k + u) * kBlock + 512);
+                cross = __builtin_amdgcn_mfma_f32_32x32x16_f16(pl, qh, cross, 0, 0, 0);
+                acc = __builtin_amdgcn_mfma_f32_32x32x16_f16(ph, qh, acc, 0, 0, 0);
+                cross = __builtin_amdgcn_mfma_f32_32x32x16_f16(ph, ql, cross, 0, 0, 0);
+            }
+        }
+        return acc + cross;
+    };
+    // block (bi, bj) as block (bj, bi) of an operand of `width` columns: a lane's four rows are neighbours there
+    auto put_turned = [&](const f32x16& v, _Float16* to, int width, int bi, int bj) {
+#pragma unroll
+        for (int e4 = 0; e4 < 4; ++e4) {
+            half4 hi, lo;
+#pragma unroll
+            for (int e = 0; e < 4; ++e) {
+                _Float16 vh, vl;
+                split(v[4 * e4 + e], vh, vl);
+                hi[e] = vh; lo[e] = vl;
+            }
+            _Float16* dst = to + at(bj * 32 + l32, bi * 32 + 8 * e4 + 4 * h, width);
+            *(half4*)dst = hi;
+            *(half4*)(dst + 512) = lo;
+        }
+    };
+    const int mb = mp >> 5, nb = np >> 5;
+    const int bi = wave >> 1, bj = wave & 1;          // of A and B
+    const bool square = bi < mb && bj < mb;
+    for (int step = 0; step < plan.steps; ++step) {
+        f32x16 gram = {};
+        if (square) {
+            gram = product(X, X, np, bi, bj) * plan.gram[step].acc;
+            put_turned(gram, A, mp, bi, bj);
+        }
+        __syncthreads();
+        if (square) {
+            const Step s = plan.poly[step];
+            f32x16 v = product(A, A, mp, bi, bj);
+#pragma unroll
+            for (int e = 0; e < 16; ++e) {
+                const int i = bi * 32 + 8 * (e >> 2) + 4 * h + (e & 3), j = bj * 32 + l32;
+                v[e] = fmaf(s.lin, gram[e], v[e] * s.acc) + (i == j && i < m ? s.diag : 0.0f);
+            }
+            put_turned(v, B, mp, bi, bj);
+        }
+        __syncthreads();
+        const float scale = plan.update[step].acc;
+        if (step + 1 < plan.steps) {
+            f32x16 next[2] = {};
+#pragma unroll
+            for (int u = 0; u < 2; ++u)
+                if (wave + 4 * u < mb * nb) next[u] = product(B, XT, mp, (wave + 4 * u) / nb, (wave + 4 * u) % nb) * scale;
+            __syncthreads();
+#pragma unroll
+            for (int u = 0; u < 2; ++u) {
+                if (wave + 4 * u >= mb * nb) continue;
+                const int xi = (wave + 4 * u) / nb, xj = (wave + 4 * u) % nb;
+                put_turned(next[u], XT, mp, xi, xj);
+#pragma unroll
+                for (int e = 0; e < 16; ++e) {
+                    _Float16 vh, vl;
+                    split(next[u][e], vh, vl);
+                    turn[(8 * (e >> 2) + 4 * h + (e & 3)) * 33 + l32] =
+                        (uint32_t)__builtin_bit_cast(uint16_t, vh) | (uint32_t)__builtin_bit_cast(uint16_t, vl) << 16;
+                }
+                wave_lds_fence();
+#pragma unroll
+                for (int k = 0; k < 2; ++k) {
+                    half8 hi, lo;
+#pragma unroll
+                    for (int e = 0; e < 8; ++e) {
+                        const uint32_t v = turn[l32 * 33 + k * 16 + h * 8 + e];
+                        hi[e] = __builtin_bit_cast(_Float16, (uint16_t)v);
+                        lo[e] = __builtin_bit_cast(_Float16, (uint16_t)(v >> 16));
+                    }
+                    _Float16* dst = X + at(xi * 32 + l32, xj * 32 + k * 16 + h * 8, np);
+                    *(half8*)dst = hi;
+                    *(half8*)(dst + 512) = lo;
+                }
+                wave_lds_fence();
+            }
+            __syncthreads();
+        } else {
+            // the result in G's order: of a tall G the transposed product, so that neighbouring lanes have neighbouring columns
+#pragma unroll
+            for (int u = 0; u < 2; ++u) {
+                if (wave + 4 * u >= mb * nb) continue;
+                const int xi = (wave + 4 * u) / nb, xj = (wave + 4 * u) % nb;
+                const f32x16 v = (l.tall ? product(XT, B, mp, xj, xi) : product(B, XT, mp, xi, xj)) * scale;
+                const int rb = (l.tall ? xj : xi) * 32, c = (l.tall ? xi : xj) * 32 + l32;
+                float w[16];
+#pragma unroll
+                for (int e = 0; e < 16; ++e) {
+                    const int r = rb + 8 * (e >> 2) + 4 * h + (e & 3);
+                    if (l.momentum && r < l.rows && c < l.cols) w[e] = ((const float*)l.out)[from + r * l.cols + c];
+                }
+#pragma unroll
+                for (int e = 0; e < 16; ++e) {
+                    const int r = rb + 8 * (e >> 2) + 4 * h + (e & 3);
+                    if (r >= l.rows || c >= l.cols) continue;
+                    if (l.momentum) ((float*)l.out)[from + r * l.cols + c] = fmaf(-l.step, v[e], a.lr_decay * w[e]);
+                    else store_value(l.out, from + r * l.cols + c, l.dtype, v[e]);
+                }
+            }
+        }
+    }
+}
+
 // ---- host ------------------------------------------------------------------------------------------------------
 
 size_t align256(size_t n) { return (n + 255) / 256 * 256; }
@@ -586,6 +806,7 @@ size_t set_bytes(const std::vector<HostList>& v, size_t first, size_t end)
 {
     size_t matrices = 0, planes = 0;
     for (size_t k = first; k < end; ++k) {
+        if (is_small(v[k].rows, v[k].cols)) continue;
         matrices += (size_t)v[k].count;
         planes += (size_t)v[k].count * align256(matrix_halves(v[k].rows, v[k].cols) * 2);
     }
@@ -630,13 +851,6 @@ double most_quintic(double a, double b, double c, double top)
         if (l > 0.0 && l < top * top) most = fmax(most, p(sqrt(l)));
     return most;
 }
-
-// Scales of all steps from the bounds of what the operands can hold.
-struct Plan {
-    float load;   // of X_0
-    Step gram[LP_ORTH_MAX_STEPS], poly[LP_ORTH_MAX_STEPS], update[LP_ORTH_MAX_STEPS];
-    int steps;
-};
 
 double scale_for(double bound)   // the power of two that puts the bound (with 1 % for rounding) at or below 2^15
 {
@@ -726,23 +940,32 @@ lp_status run_set(const std::vector<HostList>& v, size_t first, size_t end, cons
         a.nesterov = muon->nesterov;
     }
     size_t matrices = 0;
-    for (size_t k = first; k < end; ++k) matrices += (size_t)v[k].count;
+    for (size_t k = first; k < end; ++k)
+        if (!is_small(v[k].rows, v[k].cols)) matrices += (size_t)v[k].count;
     char* at = (char*)workspace + align256(matrices * kNormChunks * sizeof(double));
+    Lists small = a;
+    int lds = 0;
     for (size_t k = first; k < end; ++k) {
-        List& l = a.l[a.n++];
         const HostList& q = v[k];
+        const bool is = is_small(q.rows, q.cols);
+        List& l = is ? small.l[small.n++] : a.l[a.n++];
         l.in = q.in; l.out = q.out; l.momentum = q.momentum; l.dtype = q.dtype;
         l.count = (int)q.count; l.rows = q.rows; l.cols = q.cols;
         l.tall = q.rows > q.cols;
         l.m = l.tall ? q.cols : q.rows; l.n = l.tall ? q.rows : q.cols;
         l.mp = pad(l.m); l.np = pad(l.n);
-        l.ws = (_Float16*)at;
-        l.ws_stride = (long long)align256(matrix_halves(q.rows, q.cols) * 2) / 2;
-        at += (size_t)l.ws_stride * 2 * q.count;
-        l.vec4 = (long long)q.rows * q.cols % 4 == 0 && (uintptr_t)q.in % 16 == 0 && (uintptr_t)q.momentum % 16 == 0;
-        a.order[a.n - 1] = a.n - 1;
-        l.first_matrix = a.matrices;
-        a.matrices += l.count;
+        if (is) {
+            const int need = small_lds(pad32(l.m), pad32(l.n));
+            lds = need > lds ? need : lds;
+        } else {
+            l.ws = (_Float16*)at;
+            l.ws_stride = (long long)align256(matrix_halves(q.rows, q.cols) * 2) / 2;
+            at += (size_t)l.ws_stride * 2 * q.count;
+            l.vec4 = (long long)q.rows * q.cols % 4 == 0 && (uintptr_t)q.in % 16 == 0 && (uintptr_t)q.momentum % 16 == 0;
+            a.order[a.n - 1] = a.n - 1;
+            l.first_matrix = a.matrices;
+            a.matrices += l.count;
+        }
         if (muon) {
             const double ratio = (double)q.rows / q.cols, larger = q.rows > q.cols ? q.rows : q.cols;
             const double scale = muon->scale == LP_MUON_SCALE_ASPECT ? sqrt(ratio > 1.0 ? ratio : 1.0)
@@ -750,6 +973,13 @@ lp_status run_set(const std::vector<HostList>& v, size_t first, size_t end, cons
             l.step = (float)(muon->lr * scale);
         }
     }
+    if (small.n) {
+        number(&small, [](const List&) { return 1; });
+        const hipError_t e = hipFuncSetAttribute((const void*)orth_small_kernel, hipFuncAttributeMaxDynamicSharedMemorySize, lds);
+        if (e != hipSuccess) return fail(LP_ERR_HIP, std::string("hipFuncSetAttribute(orth_small_kernel): ") + hipGetErrorString(e));
+        hipLaunchKernelGGL(orth_small_kernel, dim3(small.total_tiles), dim3(kThreads), lds, s, small, plan);
+    }
+    if (a.n == 0) return launched("orthogonalisation launch");
     auto load_tiles = [](const List& l) { return (l.mp / 64) * (l.np / 64); };
     number(&a, [](const List& l) { return norm_chunks((long long)l.rows * l.cols); });   // (never more than the matrix has tiles)
     hipLaunchKernelGGL(orth_norm_kernel, dim3(a.total_tiles), dim3(kThreads), 0, s, a);
@@ -790,9 +1020,10 @@ lp_status run(const std::vector<HostList>& v, const Plan& plan, float eps, const
               hipStream_t s)
 {
     if (v.empty()) return LP_OK;
-    if (!workspace || workspace_bytes < all_bytes(v))
+    const size_t need = all_bytes(v);
+    if (need && (!workspace || workspace_bytes < need))
         return fail(LP_ERR_WORKSPACE, "workspace is NULL or smaller than the call's workspace_bytes function says");
-    if ((uintptr_t)workspace % 256) return fail(LP_ERR_INVALID_ARG, "workspace must be 256-byte aligned");
+    if (need && (uintptr_t)workspace % 256) return fail(LP_ERR_INVALID_ARG, "workspace must be 256-byte aligned");
     std::string err;
     int n_cu = 0;
     if (compute_units(&n_cu, &err)) return fail(LP_ERR_HIP, err);

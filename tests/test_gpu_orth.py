@@ -180,7 +180,7 @@ def test_streams_and_graphs(lp):
 
 
 def test_refusals(lp):
-    g = gradient((16, 16), 1)
+    g = gradient((80, 80), 1)   # (smaller ones need no workspace)
     ws = torch.empty(1 << 20, dtype=torch.uint8, device="cuda")
 
     def status(f):

@@ -52,6 +52,7 @@ PER_SOURCE_FLAGS = {"lp_mfma_fwd.hip": ["-mllvm", "-amdgpu-mfma-vgpr-form"],
                     "lp_mfma_bwd_tile_hash.hip": ["-mllvm", "-amdgpu-mfma-vgpr-form"],
                     "lp_mfma_bwd_hash.hip": ["-mllvm", "-amdgpu-mfma-vgpr-form"],
                     "lp_mfma_bwd_hexplane.hip": ["-mllvm", "-amdgpu-mfma-vgpr-form"],
+                    "lp_orth.hip": ["-mllvm", "-amdgpu-mfma-vgpr-form"],
                     "lp_diag.hip": ["-mllvm", "-amdgpu-mfma-vgpr-form"],
                     "lp_mfma_dec2_fwd.hip": ["-mllvm", "-amdgpu-mfma-vgpr-form"],
                     "lp_mfma_dec2_bwd.hip": ["-mllvm", "-amdgpu-mfma-vgpr-form"],

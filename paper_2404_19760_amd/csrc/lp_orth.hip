@@ -104,6 +104,27 @@ __device__ __forceinline__ size_t at(int i, int j, int width)
 }
 constexpr int kDepth = 32;   // columns a product takes at a time
 
+using f32x4 = float __attribute__((ext_vector_type(4)));
+__device__ __forceinline__ void split4(f32x4 v, half4& hi, half4& lo)
+{
+    hi = __builtin_convertvector(v, half4);
+    lo = __builtin_convertvector(v - __builtin_convertvector(hi, f32x4), half4);
+}
+
+// What brings a matrix of this norm to X_0's scale: v -> ldexp(v, e) f (an exponent of its own: no gradient is too large or too small).
+struct Scale {
+    float f;
+    int e;
+    __device__ __forceinline__ float operator()(float v) const { return ldexpf(v, e) * f; }
+};
+__device__ __forceinline__ Scale scale_of(double squares, float eps, float load)
+{
+    const double norm = sqrt(squares);
+    Scale s = {0.0f, 0};
+    if (norm != 0.0) s.f = (float)frexp((double)load / (norm + (double)eps), &s.e);
+    return s;
+}
+
 // The list and the matrix of it that `tile` belongs to, and the tile within the matrix.
 __device__ __forceinline__ const List& find(const Lists& a, int tile, int& matrix, int& local)
 {
@@ -135,8 +156,6 @@ __device__ __forceinline__ bool find_on_xcd(const Lists& a, int block, int& list
     }
     return false;
 }
-
-using f32x4 = float __attribute__((ext_vector_type(4)));
 
 // Four neighbouring values from `i` on, of which `left` are there.
 __device__ __forceinline__ f32x4 load4(const void* p, size_t i, int dtype, bool vec4, int left)
@@ -233,12 +252,11 @@ __global__ __launch_bounds__(kThreads) void orth_load_kernel(Lists a, float scal
         }
     }
     __syncthreads();
-    norm = sqrt(sums[0] + sums[1] + sums[2] + sums[3]);
-    const double f = norm == 0.0 ? 0.0 : (double)scale / (norm + (double)a.eps);   // (in 64 bits: see above)
+    const Scale f = scale_of(sums[0] + sums[1] + sums[2] + sums[3], a.eps, scale);
 #pragma unroll
     for (int k = 0; k < 4; ++k)
 #pragma unroll
-        for (int e = 0; e < 4; ++e) tile[((threadIdx.x >> 4) + 16 * k) * 65 + c4 + e] = (float)((double)v[k][e] * f);
+        for (int e = 0; e < 4; ++e) tile[((threadIdx.x >> 4) + 16 * k) * 65 + c4 + e] = f(v[k][e]);
     __syncthreads();
     _Float16* ws = l.ws + (size_t)matrix * l.ws_stride;
     const size_t plane = (size_t)2 * l.mp * l.np;
@@ -595,80 +613,100 @@ __global__ __launch_bounds__(kThreads) void orth_small_kernel(Lists a, Plan plan
     const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), lane = threadIdx.x & 63, l32 = lane & 31, h = lane >> 5;
     uint32_t* turn = (uint32_t*)A + wave * (32 * 33);
     const size_t from = (size_t)matrix * l.rows * l.cols;
-    const int size = l.rows * l.cols;
+    // G: a thread has four columns of every kPasses-th group of rows
+    constexpr int kPasses = kSmallM * kSmallN / (4 * kThreads);
+    const int shift = l.cols > 64 ? 5 : l.cols > 32 ? 4 : 3;
+    const int c0 = (threadIdx.x & ((1 << shift) - 1)) * 4, r0 = threadIdx.x >> shift, dr = kThreads >> shift;
+    const int left = l.cols - c0;
+    const bool vec4 = l.vec4 && (l.cols & 3) == 0;
+    f32x4 v[kPasses], mom[kPasses];
+#pragma unroll
+    for (int k = 0; k < kPasses; ++k) {
+        const int r = r0 + k * dr;
+        const bool in = r < l.rows && left > 0;
+        v[k] = in && l.dtype == LP_F32 ? load4(l.in, from + r * l.cols + c0, LP_F32, vec4, left) : f32x4{};
+        mom[k] = in && l.momentum ? load4(l.momentum, from + r * l.cols + c0, LP_F32, vec4, left) : f32x4{};
+    }
+    if (l.dtype != LP_F32) {
+#pragma unroll
+        for (int k = 0; k < kPasses; ++k) {
+            const int r = r0 + k * dr;
+            if (r < l.rows && left > 0) v[k] = load4(l.in, from + r * l.cols + c0, l.dtype, vec4, left);
+        }
+    }
     for (int i = threadIdx.x; i < mp * (np + 1); i += kThreads) g[i] = 0.0f;
     __syncthreads();
     double norm = 0.0;
-    constexpr int kMost = kSmallM * kSmallN / kThreads;   // values of a thread, at most
-    float value[kMost], old[kMost];
 #pragma unroll
-    for (int k = 0; k < kMost; ++k) {
-        const int i = threadIdx.x + k * kThreads;
-        if (k * kThreads >= size) break;
-        value[k] = old[k] = 0.0f;
-        if (i < size) {
-            value[k] = load_value(l.in, from + i, l.dtype);
-            if (l.momentum) old[k] = l.momentum[from + i];
-        }
-    }
+    for (int k = 0; k < kPasses; ++k) {
+        const int r = r0 + k * dr;
+        if (r >= l.rows || left <= 0) continue;
+        if (l.momentum) {
+            float* to = l.momentum + from + r * l.cols + c0;
 #pragma unroll
-    for (int k = 0; k < kMost; ++k) {
-        const int i = threadIdx.x + k * kThreads;
-        if (k * kThreads >= size) break;
-        if (i < size) {
-            float v = value[k];
-            if (l.momentum) {
-                const float mom = fmaf(a.mu, old[k], v);
-                l.momentum[from + i] = mom;
-                v = a.nesterov ? fmaf(a.mu, mom, v) : mom;
+            for (int e = 0; e < 4; ++e) {
+                mom[k][e] = fmaf(a.mu, mom[k][e], v[k][e]);
+                v[k][e] = a.nesterov ? fmaf(a.mu, mom[k][e], v[k][e]) : mom[k][e];
+                if (!vec4 && e < left) to[e] = mom[k][e];
             }
-            norm += (double)v * (double)v;
-            const int r = i / l.cols, c = i - r * l.cols;
-            g[l.tall ? c * (np + 1) + r : r * (np + 1) + c] = v;
+            if (vec4) *(f32x4*)to = mom[k];
+        }
+#pragma unroll
+        for (int e = 0; e < 4; ++e) {
+            if (e >= left) continue;
+            norm += (double)v[k][e] * (double)v[k][e];
+            g[l.tall ? (c0 + e) * (np + 1) + r : r * (np + 1) + c0 + e] = v[k][e];
         }
     }
     for (int o = 32; o; o >>= 1) norm += __shfl_xor(norm, o);
     if (lane == 0) sums[wave] = norm;
     __syncthreads();
-    norm = sqrt(sums[0] + sums[1] + sums[2] + sums[3]);
-    const double f = norm == 0.0 ? 0.0 : (double)plan.load / (norm + (double)a.eps);
-    for (int u = threadIdx.x; u < mp * np / 8; u += kThreads) {
-        // unit u: 16 bytes of a lane of a block, of X and of X^T
-        const int ln = u & 63, block = u >> 6, r = ln & 31, c = (ln >> 5) * 8;
-        half8 hi, lo;
-        const int xi = block / (np >> 4) * 32 + r, xj = block % (np >> 4) * 16 + c;
-        const int ti = block / (mp >> 4) * 32 + r, tj = block % (mp >> 4) * 16 + c;
+    const Scale f = scale_of(sums[0] + sums[1] + sums[2] + sums[3], a.eps, plan.load);
+    // blocks of X, then of X^T, one a wave at a time: the 16 bytes of a lane are row `i`, columns j .. of the operand
+    const int blocks = mp * np / 512;
+#pragma unroll 1
+    for (int u = wave; u < 2 * blocks; u += 4) {
+        const bool t = u >= blocks;
+        const int block = t ? u - blocks : u, per_row = (t ? mp : np) >> 4;
+        const int i = block / per_row * 32 + l32, j = block % per_row * 16 + 8 * h;
+        const float* src = t ? g + j * (np + 1) + i : g + i * (np + 1) + j;
+        const int step = t ? np + 1 : 1;
+        _Float16* to = (t ? XT : X) + block * kBlock + lane * 8;
 #pragma unroll
-        for (int e = 0; e < 8; ++e) {
-            _Float16 vh, vl;
-            split((float)((double)g[xi * (np + 1) + xj + e] * f), vh, vl);
-            hi[e] = vh; lo[e] = vl;
-        }
-        *(half8*)(X + block * kBlock + ln * 8) = hi;
-        *(half8*)(X + block * kBlock + 512 + ln * 8) = lo;
+        for (int q = 0; q < 2; ++q) {
+            f32x4 w;
 #pragma unroll
-        for (int e = 0; e < 8; ++e) {
-            _Float16 vh, vl;
-            split((float)((double)g[(tj + e) * (np + 1) + ti] * f), vh, vl);
-            hi[e] = vh; lo[e] = vl;
+            for (int e = 0; e < 4; ++e) w[e] = f(src[(4 * q + e) * step]);
+            half4 hi, lo;
+            split4(w, hi, lo);
+            *(half4*)(to + 4 * q) = hi;
+            *(half4*)(to + 512 + 4 * q) = lo;
         }
-        *(half8*)(XT + block * kBlock + ln * 8) = hi;
-        *(half8*)(XT + block * kBlock + 512 + ln * 8) = lo;
     }
     __syncthreads();
-    // block (bi, bj) of P Q^T over K columns
+    // block (bi, bj) of P Q^T over K columns, 64 at a time (the operands of all of them are asked for before the first product)
     auto product = [&](const _Float16* p, const _Float16* q, int K, int bi, int bj) {
         f32x16 acc = {}, cross = {};
         const _Float16* pb = p + bi * (K >> 4) * kBlock + lane * 8;
         const _Float16* qb = q + bj * (K >> 4) * kBlock + lane * 8;
-        for (int k = 0; k < K >> 4; k += 2) {
+#pragma unroll 1
+        for (int k = 0; k < K >> 4; k += 4) {
+            const int n_k = min(4, (K >> 4) - k);   // 4 or 2
+            half8 ph[4], pl[4], qh[4], ql[4];
 #pragma unroll
-            for (int u = 0; u < 2; ++u) {
-                const half8 ph = *(const half8*)(pb + (k + u) * kBlock), pl = *(const half8*)(pb + (k + u) * kBlock + 512);
-                const half8 qh = *(const half8*)(qb + (k + u) * kBlock), ql = *(const half8*)(qb + (k + u) * kBlock + 512);
-                cross = __builtin_amdgcn_mfma_f32_32x32x16_f16(pl, qh, cross, 0, 0, 0);
-                acc = __builtin_amdgcn_mfma_f32_32x32x16_f16(ph, qh, acc, 0, 0, 0);
-                cross = __builtin_amdgcn_mfma_f32_32x32x16_f16(ph, ql, cross, 0, 0, 0);
+            for (int u = 0; u < 4; ++u) {
+                if (u >= n_k) break;
+                ph[u] = *(const half8*)(pb + (k + u) * kBlock);
+                qh[u] = *(const half8*)(qb + (k + u) * kBlock);
+                pl[u] = *(const half8*)(pb + (k + u) * kBlock + 512);
+                ql[u] = *(const half8*)(qb + (k + u) * kBlock + 512);
+            }
+#pragma unroll
+            for (int u = 0; u < 4; ++u) {
+                if (u >= n_k) break;
+                acc = __builtin_amdgcn_mfma_f32_32x32x16_f16(ph[u], qh[u], acc, 0, 0, 0);
+                cross = __builtin_amdgcn_mfma_f32_32x32x16_f16(pl[u], qh[u], cross, 0, 0, 0);
+                cross = __builtin_amdgcn_mfma_f32_32x32x16_f16(ph[u], ql[u], cross, 0, 0, 0);
             }
         }
         return acc + cross;
@@ -678,12 +716,7 @@ __global__ __launch_bounds__(kThreads) void orth_small_kernel(Lists a, Plan plan
 #pragma unroll
         for (int e4 = 0; e4 < 4; ++e4) {
             half4 hi, lo;
-#pragma unroll
-            for (int e = 0; e < 4; ++e) {
-                _Float16 vh, vl;
-                split(v[4 * e4 + e], vh, vl);
-                hi[e] = vh; lo[e] = vl;
-            }
+            split4(f32x4{v[4 * e4], v[4 * e4 + 1], v[4 * e4 + 2], v[4 * e4 + 3]}, hi, lo);
             _Float16* dst = to + at(bj * 32 + l32, bi * 32 + 8 * e4 + 4 * h, width);
             *(half4*)dst = hi;
             *(half4*)(dst + 512) = lo;
@@ -721,13 +754,17 @@ __global__ __launch_bounds__(kThreads) void orth_small_kernel(Lists a, Plan plan
             for (int u = 0; u < 2; ++u) {
                 if (wave + 4 * u >= mb * nb) continue;
                 const int xi = (wave + 4 * u) / nb, xj = (wave + 4 * u) % nb;
-                put_turned(next[u], XT, mp, xi, xj);
 #pragma unroll
-                for (int e = 0; e < 16; ++e) {
-                    _Float16 vh, vl;
-                    split(next[u][e], vh, vl);
-                    turn[(8 * (e >> 2) + 4 * h + (e & 3)) * 33 + l32] =
-                        (uint32_t)__builtin_bit_cast(uint16_t, vh) | (uint32_t)__builtin_bit_cast(uint16_t, vl) << 16;
+                for (int e4 = 0; e4 < 4; ++e4) {
+                    half4 hi, lo;
+                    split4(f32x4{next[u][4 * e4], next[u][4 * e4 + 1], next[u][4 * e4 + 2], next[u][4 * e4 + 3]}, hi, lo);
+                    _Float16* dst = XT + at(xj * 32 + l32, xi * 32 + 8 * e4 + 4 * h, mp);
+                    *(half4*)dst = hi;
+                    *(half4*)(dst + 512) = lo;
+#pragma unroll
+                    for (int e = 0; e < 4; ++e)
+                        turn[(8 * e4 + 4 * h + e) * 33 + l32] =
+                            (uint32_t)__builtin_bit_cast(uint16_t, (_Float16)hi[e]) | (uint32_t)__builtin_bit_cast(uint16_t, (_Float16)lo[e]) << 16;
                 }
                 wave_lds_fence();
 #pragma unroll
@@ -748,24 +785,32 @@ __global__ __launch_bounds__(kThreads) void orth_small_kernel(Lists a, Plan plan
             __syncthreads();
         } else {
             // the result in G's order: of a tall G the transposed product, so that neighbouring lanes have neighbouring columns
+            const int cb = l.tall ? mb : nb;
+#pragma unroll 1
+            for (int u = wave; u < mb * nb; u += 4) {
+                const int ri = u / cb, ci = u % cb, rb = ri * 32, c = ci * 32 + l32;
+                f32x16 v = product(l.tall ? XT : B, l.tall ? B : XT, mp, ri, ci);
+                auto each = [&](auto&& f) {   // (offsets from the matrix's start: 32 bits)
 #pragma unroll
-            for (int u = 0; u < 2; ++u) {
-                if (wave + 4 * u >= mb * nb) continue;
-                const int xi = (wave + 4 * u) / nb, xj = (wave + 4 * u) % nb;
-                const f32x16 v = (l.tall ? product(XT, B, mp, xj, xi) : product(B, XT, mp, xi, xj)) * scale;
-                const int rb = (l.tall ? xj : xi) * 32, c = (l.tall ? xi : xj) * 32 + l32;
-                float w[16];
-#pragma unroll
-                for (int e = 0; e < 16; ++e) {
-                    const int r = rb + 8 * (e >> 2) + 4 * h + (e & 3);
-                    if (l.momentum && r < l.rows && c < l.cols) w[e] = ((const float*)l.out)[from + r * l.cols + c];
-                }
-#pragma unroll
-                for (int e = 0; e < 16; ++e) {
-                    const int r = rb + 8 * (e >> 2) + 4 * h + (e & 3);
-                    if (r >= l.rows || c >= l.cols) continue;
-                    if (l.momentum) ((float*)l.out)[from + r * l.cols + c] = fmaf(-l.step, v[e], a.lr_decay * w[e]);
-                    else store_value(l.out, from + r * l.cols + c, l.dtype, v[e]);
+                    for (int e = 0; e < 16; ++e) {
+                        const int r = rb + 8 * (e >> 2) + 4 * h + (e & 3);
+                        if (r < l.rows && c < l.cols) f(e, (unsigned)(r * l.cols + c));
+                    }
+                };
+                if (l.momentum) {
+                    float* to = (float*)l.out + from;
+                    float w[16];
+                    each([&](int e, unsigned i) { w[e] = to[i]; });
+                    each([&](int e, unsigned i) { to[i] = fmaf(-l.step, v[e] * scale, a.lr_decay * w[e]); });
+                } else if (l.dtype == LP_F32) {
+                    float* to = (float*)l.out + from;
+                    each([&](int e, unsigned i) { to[i] = v[e] * scale; });
+                } else if (l.dtype == LP_BF16) {
+                    __bf16* to = (__bf16*)l.out + from;
+                    each([&](int e, unsigned i) { to[i] = (__bf16)(v[e] * scale); });
+                } else {
+                    _Float16* to = (_Float16*)l.out + from;
+                    each([&](int e, unsigned i) { to[i] = (_Float16)(v[e] * scale); });
                 }
             }
         }
@@ -955,6 +1000,7 @@ lp_status run_set(const std::vector<HostList>& v, size_t first, size_t end, cons
         l.m = l.tall ? q.cols : q.rows; l.n = l.tall ? q.rows : q.cols;
         l.mp = pad(l.m); l.np = pad(l.n);
         if (is) {
+            l.vec4 = (uintptr_t)q.in % 16 == 0 && (uintptr_t)q.momentum % 16 == 0;
             const int need = small_lds(pad32(l.m), pad32(l.n));
             lds = need > lds ? need : lds;
         } else {

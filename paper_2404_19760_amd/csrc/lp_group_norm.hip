@@ -6,9 +6,10 @@
 //     d_gamma = sum g xh,   d_beta = sum g,
 //     d_x = rstd (gamma g - (S1 + xh S2) / n),   S1 = sum over the group of gamma g,   S2 of gamma g xh.
 //
-// What bounds it: memory.  A sum over the whole group stands between reading a value and using it, so either direction passes
-// over its data twice: a pass that sums (forward: x; backward: x and d_y), a small kernel that joins the workgroups' sums, and
-// a pass that writes.  In all passes a thread keeps to one slot of V neighbouring channels (16 bytes where channels and
+// What bounds it: memory.  A sum over the whole group stands between reading a value and using it.  A sample of at most 128 KB stays in the
+// registers of one workgroup meanwhile (one launch).  Larger ones are passed over twice: a pass that sums (forward: x; backward: x
+// and d_y), a small kernel that joins the workgroups' sums, and a pass that writes, from the end back to the start: what the first
+// pass read last is still in the 256 MB of Infinity Cache.  In all passes a thread keeps to one slot of V neighbouring channels (16 bytes where channels and
 // alignment allow), so a channel's parameters and sums stay in its registers, and neighbouring lanes read neighbouring bytes.
 //
 // Sums: a thread sums differences to the first value that it sees, in fp32 (a mean far from zero does not cancel the
@@ -18,6 +19,9 @@
 
 #include <cmath>
 #include <cstring>
+#include <initializer_list>
+#include <type_traits>
+#include <utility>
 
 #include "lp_kernels.h"
 
@@ -26,7 +30,7 @@ namespace lp {
 namespace {
 
 constexpr int kThreads = 256;
-constexpr int kUnroll = 4;               // rows a thread has in flight
+template <int V> constexpr int kUnroll = V == 8 ? 2 : V == 1 ? 8 : 4;   // rows a thread has in flight
 constexpr long long kMaxGrid = 1 << 20;  // workgroups of a launch; items beyond are taken in turn
 constexpr float kInvSqrt2 = 0.70710678118654752f, kInvSqrt2Pi = 0.39894228040143268f;
 
@@ -41,6 +45,9 @@ struct NormDev {
     int chunks;                         // items of a sample
     long long chunk;                    // positions of an item
 };
+
+using f32x2 = float __attribute__((ext_vector_type(2)));
+using f32x4 = float __attribute__((ext_vector_type(4)));
 
 template <class T, int V>
 struct alignas(sizeof(T) * V) Pack { T v[V]; };
@@ -67,26 +74,59 @@ __device__ __forceinline__ void store(T* p, const float (&in)[V])
 // 1 / (1 + exp(-z)) from the hardware's exponential and reciprocal (a few units in the last place)
 __device__ __forceinline__ float sigmoid(float z) { return __builtin_amdgcn_rcpf(1.0f + __expf(-z)); }
 
-__device__ __forceinline__ float activate(float z, int act)
+// The normal distribution's integral up to z and its density, by Abramowitz and Stegun 7.1.26 (erf to 1.5e-7): with
+// t = 1 / (1 + p |z| / sqrt 2), the tail beyond |z| is t (a1 + t (a2 + ...)) exp(-z z / 2) / 2, which keeps its relative error where
+// the integral is small.
+__device__ __forceinline__ void normal(float z, float& integral, float& density)
 {
-    switch (act) {
-        case LP_ACT_RELU: return z < 0.0f ? 0.0f : z;   // (a NaN stays one)
-        case LP_ACT_SILU: return z * sigmoid(z);
-        case LP_ACT_GELU: return 0.5f * z * (1.0f + erff(z * kInvSqrt2));
-        default: return z;
-    }
+    const float u = fabsf(z) * kInvSqrt2, e = __expf(-u * u), t = __builtin_amdgcn_rcpf(fmaf(0.3275911f, u, 1.0f));
+    float tail = fmaf(t, 1.061405429f, -1.453152027f);
+    tail = fmaf(t, tail, 1.421413741f);
+    tail = fmaf(t, tail, -0.284496736f);
+    tail = fmaf(t, tail, 0.254829592f);
+    tail *= 0.5f * t * e;
+    integral = z < 0.0f ? tail : 1.0f - tail;
+    density = e * kInvSqrt2Pi;
 }
 
-__device__ __forceinline__ float slope(float z, int act)
+template <int ACT>
+__device__ __forceinline__ float activate(float z)
+{
+    if (ACT == LP_ACT_RELU) return z < 0.0f ? 0.0f : z;   // (a NaN stays one)
+    if (ACT == LP_ACT_SILU) return z * sigmoid(z);
+    if (ACT == LP_ACT_GELU) {
+        float i, d;
+        normal(z, i, d);
+        return z * i;
+    }
+    return z;
+}
+
+template <int ACT>
+__device__ __forceinline__ float slope(float z)
+{
+    if (ACT == LP_ACT_RELU) return z > 0.0f ? 1.0f : (z <= 0.0f ? 0.0f : z);
+    if (ACT == LP_ACT_SILU) {
+        const float s = sigmoid(z);
+        return fmaf(z * s, 1.0f - s, s);
+    }
+    if (ACT == LP_ACT_GELU) {
+        float i, d;
+        normal(z, i, d);
+        return fmaf(z, d, i);
+    }
+    return 1.0f;
+}
+
+// Calls f with the activation as a constant: the choice stands outside the loops.
+template <class F>
+__device__ __forceinline__ void with_act(int act, F&& f)
 {
     switch (act) {
-        case LP_ACT_RELU: return z > 0.0f ? 1.0f : (z <= 0.0f ? 0.0f : z);
-        case LP_ACT_SILU: {
-            const float s = sigmoid(z);
-            return s * (1.0f + z * (1.0f - s));
-        }
-        case LP_ACT_GELU: return 0.5f * (1.0f + erff(z * kInvSqrt2)) + z * kInvSqrt2Pi * __expf(-0.5f * z * z);
-        default: return 1.0f;
+        case LP_ACT_RELU: f(std::integral_constant<int, LP_ACT_RELU>()); break;
+        case LP_ACT_SILU: f(std::integral_constant<int, LP_ACT_SILU>()); break;
+        case LP_ACT_GELU: f(std::integral_constant<int, LP_ACT_GELU>()); break;
+        default: f(std::integral_constant<int, LP_ACT_NONE>());
     }
 }
 
@@ -110,18 +150,18 @@ __device__ __forceinline__ Place place(const NormDev& d)
     return p;
 }
 
-// Calls f(u, position) for the thread's positions of an item, kUnroll at a time: first all loads, then all of the rest.
-template <class Load, class Use>
+// Calls ld, then use, for the thread's positions of an item, U at a time: first all loads, then all of the rest.
+template <int U, class Load, class Use>
 __device__ __forceinline__ void sweep(const NormDev& d, long long first, long long end, int row, Load&& ld, Use&& use)
 {
-    for (long long p = first + row; p < end; p += (long long)kUnroll * d.rows) {
+    for (long long p = first + row; p < end; p += (long long)U * d.rows) {
 #pragma unroll
-        for (int u = 0; u < kUnroll; ++u) {
+        for (int u = 0; u < U; ++u) {
             const long long q = p + (long long)u * d.rows;
             ld(u, q, q < end);
         }
 #pragma unroll
-        for (int u = 0; u < kUnroll; ++u) {
+        for (int u = 0; u < U; ++u) {
             const long long q = p + (long long)u * d.rows;
             use(u, q, q < end);
         }
@@ -140,108 +180,397 @@ __device__ __forceinline__ void join(float& n, float& mean, float& m2, float nb,
     }
 }
 
-// Pass 1 of the forward: (count, mean, m2) of every channel of every item -> part[(item C + c) 3].
-template <class TX, int V, bool MASK>
-__global__ __launch_bounds__(kThreads) void norm_stats_kernel(NormDev d, const TX* __restrict__ x, float* __restrict__ part)
+// A channel's parameters, for the V channels of a thread's slot.
+template <int V>
+struct Slot {
+    float mean[V], rstd[V], gamma[V], beta[V];
+    __device__ __forceinline__ void parameters(const NormDev& d, int slot)
+    {
+#pragma unroll
+        for (int j = 0; j < V; ++j) {
+            gamma[j] = d.gamma ? d.gamma[slot * V + j] : 1.0f;
+            beta[j] = d.beta ? d.beta[slot * V + j] : 0.0f;
+        }
+    }
+    // stats: [groups][2] of the sample
+    __device__ __forceinline__ void statistics(const NormDev& d, int slot, const float* stats)
+    {
+#pragma unroll
+        for (int j = 0; j < V; ++j) {
+            const int g = (slot * V + j) / d.Cg;
+            mean[j] = stats[2 * g];
+            rstd[j] = stats[2 * g + 1];
+        }
+    }
+};
+
+// The sums of all threads of a slot, joined at row 0: a tree over the rows through LDS (2 V + 1 values a thread).
+template <int V, int THREADS>
+__device__ __forceinline__ void join_rows(const NormDev& d, const Place& at, int all_rows, float& count, float (&mean)[V], float (&m2)[V], float* lds)
 {
-    __shared__ float sm[kThreads * V * 2];
-    __shared__ float sn[kThreads];
+    for (int rows = all_rows; rows > 1;) {
+        const int half = (rows + 1) / 2;
+        __syncthreads();
+        if (at.in && at.row >= half && at.row < rows) {
+            lds[threadIdx.x] = count;
+#pragma unroll
+            for (int j = 0; j < V; ++j) {
+                lds[(1 + j) * THREADS + threadIdx.x] = mean[j];
+                lds[(1 + V + j) * THREADS + threadIdx.x] = m2[j];
+            }
+        }
+        __syncthreads();
+        if (at.in && at.row + half < rows) {
+            const int o = threadIdx.x + half * d.slots;
+            const float nb = lds[o], before = count;
+#pragma unroll
+            for (int j = 0; j < V; ++j) {
+                float c = before;
+                join(c, mean[j], m2[j], nb, lds[(1 + j) * THREADS + o], lds[(1 + V + j) * THREADS + o]);
+            }
+            count = before + nb;
+        }
+        rows = half;
+    }
+}
+
+// The same for plain sums.
+template <int V, int THREADS>
+__device__ __forceinline__ void add_rows(const NormDev& d, const Place& at, int all_rows, float& count, float (&a)[V], float (&b)[V], float* lds)
+{
+    for (int rows = all_rows; rows > 1;) {
+        const int half = (rows + 1) / 2;
+        __syncthreads();
+        if (at.in && at.row >= half && at.row < rows) {
+            lds[threadIdx.x] = count;
+#pragma unroll
+            for (int j = 0; j < V; ++j) {
+                lds[(1 + j) * THREADS + threadIdx.x] = a[j];
+                lds[(1 + V + j) * THREADS + threadIdx.x] = b[j];
+            }
+        }
+        __syncthreads();
+        if (at.in && at.row + half < rows) {
+            const int o = threadIdx.x + half * d.slots;
+            count += lds[o];
+#pragma unroll
+            for (int j = 0; j < V; ++j) {
+                a[j] += lds[(1 + j) * THREADS + o];
+                b[j] += lds[(1 + V + j) * THREADS + o];
+            }
+        }
+        rows = half;
+    }
+}
+
+// Sums of differences to a first value, and what they say of mean and m2.
+template <int V>
+struct Sums {
+    float shift[V], s1[V], s2[V], count = 0.0f;
+    __device__ Sums()
+    {
+#pragma unroll
+        for (int j = 0; j < V; ++j) shift[j] = s1[j] = s2[j] = 0.0f;
+    }
+    template <class T>
+    __device__ __forceinline__ void add(const Pack<T, V>& v)
+    {
+#pragma unroll
+        for (int j = 0; j < V; ++j) {
+            const float value = to_f32(v.v[j]);
+            if (count == 0.0f) shift[j] = value;
+            const float t = value - shift[j];
+            s1[j] += t;
+            s2[j] = fmaf(t, t, s2[j]);
+        }
+        count += 1.0f;
+    }
+    __device__ __forceinline__ void close(float (&mean)[V], float (&m2)[V]) const
+    {
+        const float inv = count > 0.0f ? 1.0f / count : 0.0f;
+#pragma unroll
+        for (int j = 0; j < V; ++j) {
+            const float m = s1[j] * inv, v = s2[j] - s1[j] * m;
+            mean[j] = shift[j] + m;
+            m2[j] = v < 0.0f ? 0.0f : v;   // (a NaN stays one)
+        }
+    }
+};
+
+__device__ __forceinline__ void statistics_of(double n, double sum, double squares, float eps, float& mean, float& rstd)
+{
+    mean = rstd = 0.0f;
+    if (n > 0.0) {
+        const double m = sum / n;
+        double var = squares / n - m * m;
+        if (var < 0.0) var = 0.0;
+        mean = (float)m;
+        rstd = (float)(1.0 / sqrt(var + (double)eps));
+    }
+}
+
+__device__ __forceinline__ double wave_sum(double v)
+{
+    for (int o = 32; o; o >>= 1) v += __shfl_xor(v, o);
+    return v;
+}
+
+// ---- a sample in the registers of one workgroup ------------------------------------------------------------------
+
+constexpr int kSmallThreads = 1024;
+template <int V> constexpr int kHeld = V == 8 ? 4 : V == 4 ? 8 : 16;   // rows of a thread, at most
+
+// One workgroup a sample, whose values stay in registers between the sums and the results: x is read once.
+template <class TX, class TY, int V, bool MASK>
+__global__ __launch_bounds__(kSmallThreads) void norm_small_kernel(NormDev d, const TX* x, TY* y, float* stats)
+{
+    __shared__ float lds[(2 * V + 1) * kSmallThreads];
+    __shared__ float group_stats[2 * kSmallThreads];
+    const Place at = place(d);
+    const long long n = blockIdx.x;
+    const TX* base = x + (size_t)(n * d.P) * d.xs + at.slot * V;
+    const float* occ = MASK ? d.occ + n * d.P : nullptr;
+    Pack<TX, V> v[kHeld<V>];
+    bool on[kHeld<V>];
+    Slot<V> slot;
+#pragma unroll
+    for (int k = 0; k < kHeld<V>; ++k) {
+        const long long p = at.row + (long long)k * d.rows;
+        on[k] = at.in && p < d.P && (!MASK || occ[p] > 0.0f);
+        if (on[k]) load<TX, V>(base + p * d.xs, v[k]);
+    }
+    if (at.in) slot.parameters(d, at.slot);
+    Sums<V> sums;
+#pragma unroll
+    for (int k = 0; k < kHeld<V>; ++k)
+        if (on[k]) sums.add(v[k]);
+    float count = sums.count, mean[V], m2[V];
+    sums.close(mean, m2);
+    join_rows<V, kSmallThreads>(d, at, d.rows, count, mean, m2, lds);
+    __syncthreads();
+    if (at.in && at.row == 0) {
+#pragma unroll
+        for (int j = 0; j < V; ++j) {
+            const int c = at.slot * V + j;
+            lds[3 * c] = count;
+            lds[3 * c + 1] = mean[j];
+            lds[3 * c + 2] = m2[j];
+        }
+    }
+    __syncthreads();
+    for (int g = threadIdx.x >> 6; g < d.G; g += kSmallThreads / 64) {
+        double cnt = 0.0, sum = 0.0, sq = 0.0;
+        for (int c = threadIdx.x & 63; c < d.Cg; c += 64) {
+            const float* q = lds + 3 * (g * d.Cg + c);
+            const double m = q[1];
+            cnt += q[0];
+            sum += (double)q[0] * m;
+            sq += (double)q[2] + (double)q[0] * m * m;
+        }
+        cnt = wave_sum(cnt);
+        sum = wave_sum(sum);
+        sq = wave_sum(sq);
+        if ((threadIdx.x & 63) == 0) {
+            float mu, rstd;
+            statistics_of(cnt, sum, sq, d.eps, mu, rstd);
+            group_stats[2 * g] = mu;
+            group_stats[2 * g + 1] = rstd;
+            if (stats) {
+                stats[(n * d.G + g) * 2] = mu;
+                stats[(n * d.G + g) * 2 + 1] = rstd;
+            }
+        }
+    }
+    __syncthreads();
+    if (!at.in) return;
+    slot.statistics(d, at.slot, group_stats);
+    TY* out = y + (size_t)(n * d.P) * d.ys + at.slot * V;
+    with_act(d.act, [&](auto act) {
+#pragma unroll
+        for (int k = 0; k < kHeld<V>; ++k) {
+            const long long p = at.row + (long long)k * d.rows;
+            if (p >= d.P) continue;
+            float r[V];
+#pragma unroll
+            for (int j = 0; j < V; ++j)
+                r[j] = on[k] ? activate<decltype(act)::value>(fmaf((to_f32(v[k].v[j]) - slot.mean[j]) * slot.rstd[j], slot.gamma[j], slot.beta[j])) : 0.0f;
+            store<TY, V>(out + p * d.ys, r);
+        }
+    });
+}
+
+// The same for the backward.  chan [n][C][2]: the samples' sums for the parameters; with a single sample they are added here.
+template <class TX, class TY, int V, bool MASK>
+__global__ __launch_bounds__(kSmallThreads) void norm_small_grad_kernel(NormDev d, const TX* x, const TY* dy, TX* dx, const float* __restrict__ stats,
+                                                                        double* __restrict__ chan, float* d_gamma, float* d_beta)
+{
+    __shared__ float lds[(2 * V + 1) * kSmallThreads];
+    __shared__ float means[2 * kSmallThreads];
+    const Place at = place(d);
+    const long long n = blockIdx.x;
+    const TX* base = x + (size_t)(n * d.P) * d.xs + at.slot * V;
+    const TY* up = dy + (size_t)(n * d.P) * d.ys + at.slot * V;
+    const float* occ = MASK ? d.occ + n * d.P : nullptr;
+    Pack<TX, V> v[kHeld<V>];
+    Pack<TY, V> w[kHeld<V>];
+    bool on[kHeld<V>];
+    Slot<V> slot;
+#pragma unroll
+    for (int k = 0; k < kHeld<V>; ++k) {
+        const long long p = at.row + (long long)k * d.rows;
+        on[k] = at.in && p < d.P && (!MASK || occ[p] > 0.0f);
+        if (on[k]) {
+            load<TX, V>(base + p * d.xs, v[k]);
+            load<TY, V>(up + p * d.ys, w[k]);
+        }
+    }
+    if (at.in) {
+        slot.parameters(d, at.slot);
+        slot.statistics(d, at.slot, stats + n * d.G * 2);
+    }
+    float sg[V], sx[V], count = 0.0f;
+#pragma unroll
+    for (int j = 0; j < V; ++j) sg[j] = sx[j] = 0.0f;
+    with_act(d.act, [&](auto act) {
+#pragma unroll
+        for (int k = 0; k < kHeld<V>; ++k) {
+            if (!on[k]) continue;
+#pragma unroll
+            for (int j = 0; j < V; ++j) {
+                const float xh = (to_f32(v[k].v[j]) - slot.mean[j]) * slot.rstd[j];
+                const float g = to_f32(w[k].v[j]) * slope<decltype(act)::value>(fmaf(xh, slot.gamma[j], slot.beta[j]));
+                sg[j] += g;
+                sx[j] = fmaf(g, xh, sx[j]);
+            }
+            count += 1.0f;
+        }
+    });
+    add_rows<V, kSmallThreads>(d, at, d.rows, count, sg, sx, lds);
+    __syncthreads();
+    if (at.in && at.row == 0) {
+#pragma unroll
+        for (int j = 0; j < V; ++j) {
+            const int c = at.slot * V + j;
+            lds[3 * c] = count;
+            lds[3 * c + 1] = sg[j];
+            lds[3 * c + 2] = sx[j];
+            if (d.N > 1) {
+                chan[(n * d.C + c) * 2] = sg[j];
+                chan[(n * d.C + c) * 2 + 1] = sx[j];
+            } else {
+                if (d_beta) d_beta[c] += sg[j];
+                if (d_gamma) d_gamma[c] += sx[j];
+            }
+        }
+    }
+    __syncthreads();
+    for (int g = threadIdx.x >> 6; g < d.G; g += kSmallThreads / 64) {
+        double cnt = 0.0, s1 = 0.0, s2 = 0.0;
+        for (int j = threadIdx.x & 63; j < d.Cg; j += 64) {
+            const int c = g * d.Cg + j;
+            const double gamma = d.gamma ? d.gamma[c] : 1.0f;
+            cnt += lds[3 * c];
+            s1 += gamma * lds[3 * c + 1];
+            s2 += gamma * lds[3 * c + 2];
+        }
+        cnt = wave_sum(cnt);
+        s1 = wave_sum(s1);
+        s2 = wave_sum(s2);
+        if ((threadIdx.x & 63) == 0) {
+            means[2 * g] = cnt > 0.0 ? (float)(s1 / cnt) : 0.0f;
+            means[2 * g + 1] = cnt > 0.0 ? (float)(s2 / cnt) : 0.0f;
+        }
+    }
+    __syncthreads();
+    if (!at.in || !dx) return;
+    float m1[V], mx[V];
+#pragma unroll
+    for (int j = 0; j < V; ++j) {
+        const int g = (at.slot * V + j) / d.Cg;
+        m1[j] = means[2 * g];
+        mx[j] = means[2 * g + 1];
+    }
+    TX* out = dx + (size_t)(n * d.P) * d.xs + at.slot * V;
+    with_act(d.act, [&](auto act) {
+#pragma unroll
+        for (int k = 0; k < kHeld<V>; ++k) {
+            const long long p = at.row + (long long)k * d.rows;
+            if (p >= d.P) continue;
+            float r[V];
+#pragma unroll
+            for (int j = 0; j < V; ++j) {
+                r[j] = 0.0f;
+                if (on[k]) {
+                    const float xh = (to_f32(v[k].v[j]) - slot.mean[j]) * slot.rstd[j];
+                    const float g = to_f32(w[k].v[j]) * slope<decltype(act)::value>(fmaf(xh, slot.gamma[j], slot.beta[j]));
+                    r[j] = slot.rstd[j] * (fmaf(slot.gamma[j], g, -m1[j]) - xh * mx[j]);
+                }
+            }
+            store<TX, V>(out + p * d.xs, r);
+        }
+    });
+}
+
+// ---- in two passes ---------------------------------------------------------------------------------------------
+
+// Pass 1 of the forward: (count, mean, m2) of every channel of every item -> part[((n C + c) chunks + chunk) 4].
+template <class TX, int V, bool MASK>
+__global__ __launch_bounds__(kThreads) void norm_stats_kernel(NormDev d, const TX* __restrict__ x, f32x4* __restrict__ part)
+{
+    __shared__ float lds[(2 * V + 1) * kThreads];
     const Place at = place(d);
     const long long items = d.N * d.chunks;
     for (long long item = blockIdx.x; item < items; item += gridDim.x) {
-        const long long n = item / d.chunks, first = (item - n * d.chunks) * d.chunk, end = min(first + d.chunk, d.P);
+        const long long n = item / d.chunks, chunk = item - n * d.chunks, first = chunk * d.chunk, end = min(first + d.chunk, d.P);
         const TX* base = x + (size_t)(n * d.P) * d.xs + at.slot * V;
         const float* occ = MASK ? d.occ + n * d.P : nullptr;
-        float shift[V], s1[V], s2[V], count = 0.0f;
-#pragma unroll
-        for (int j = 0; j < V; ++j) shift[j] = s1[j] = s2[j] = 0.0f;
+        Sums<V> sums;
         if (at.in) {
-            Pack<TX, V> v[kUnroll];
-            bool on[kUnroll];
-            sweep(d, first, end, at.row,
+            Pack<TX, V> v[kUnroll<V>];
+            bool on[kUnroll<V>];
+            sweep<kUnroll<V>>(d, first, end, at.row,
                   [&](int u, long long p, bool in) {
                       on[u] = in && (!MASK || occ[p] > 0.0f);
                       if (on[u]) load<TX, V>(base + p * d.xs, v[u]);
                   },
                   [&](int u, long long, bool) {
-                      if (!on[u]) return;
-#pragma unroll
-                      for (int j = 0; j < V; ++j) {
-                          const float value = to_f32(v[u].v[j]);
-                          if (count == 0.0f) shift[j] = value;
-                          const float t = value - shift[j];
-                          s1[j] += t;
-                          s2[j] = fmaf(t, t, s2[j]);
-                      }
-                      count += 1.0f;
+                      if (on[u]) sums.add(v[u]);
                   });
         }
-        const float inv = count > 0.0f ? 1.0f / count : 0.0f;
-        float mean[V], m2[V];
-#pragma unroll
-        for (int j = 0; j < V; ++j) {
-            const float m = s1[j] * inv;
-            mean[j] = shift[j] + m;
-            m2[j] = fmaxf(s2[j] - s1[j] * m, 0.0f);
-            if (!(s2[j] >= 0.0f)) m2[j] = s2[j];   // (NaN among the values)
-        }
-        for (int rows = d.rows; rows > 1;) {
-            const int half = (rows + 1) / 2;
-            __syncthreads();
-            if (at.in && at.row >= half && at.row < rows) {
-                sn[threadIdx.x] = count;
-#pragma unroll
-                for (int j = 0; j < V; ++j) {
-                    sm[j * kThreads + threadIdx.x] = mean[j];
-                    sm[(V + j) * kThreads + threadIdx.x] = m2[j];
-                }
-            }
-            __syncthreads();
-            if (at.in && at.row + half < rows) {
-                const int o = threadIdx.x + half * d.slots;
-                const float nb = sn[o], before = count;
-#pragma unroll
-                for (int j = 0; j < V; ++j) {
-                    float c = before;
-                    join(c, mean[j], m2[j], nb, sm[j * kThreads + o], sm[(V + j) * kThreads + o]);
-                }
-                count = before + nb;
-            }
-            rows = half;
-        }
+        float count = sums.count, mean[V], m2[V];
+        sums.close(mean, m2);
+        join_rows<V, kThreads>(d, at, d.rows, count, mean, m2, lds);
         if (at.in && at.row == 0) {
-            float* out = part + ((size_t)item * d.C + at.slot * V) * 3;
 #pragma unroll
-            for (int j = 0; j < V; ++j) {
-                out[3 * j] = count;
-                out[3 * j + 1] = mean[j];
-                out[3 * j + 2] = m2[j];
-            }
+            for (int j = 0; j < V; ++j) part[(size_t)(n * d.C + at.slot * V + j) * d.chunks + chunk] = f32x4{count, mean[j], m2[j], 0.0f};
         }
     }
 }
 
+constexpr int kJoinThreads = 512;
 __device__ __forceinline__ double block_sum(double v, double* lds)
 {
-    for (int o = 32; o; o >>= 1) v += __shfl_xor(v, o);
+    v = wave_sum(v);
     __syncthreads();
     if ((threadIdx.x & 63) == 0) lds[threadIdx.x >> 6] = v;
     __syncthreads();
-    return lds[0] + lds[1] + lds[2] + lds[3];
+    double sum = 0.0;
+#pragma unroll
+    for (int k = 0; k < kJoinThreads / 64; ++k) sum += lds[k];
+    return sum;
 }
 
 // Joins a group's parts: one workgroup a (sample, group) -> stats[(n G + g) 2] = mean, rstd.
-__global__ __launch_bounds__(kThreads) void norm_join_kernel(NormDev d, const float* __restrict__ part, float* __restrict__ stats)
+__global__ __launch_bounds__(kJoinThreads) void norm_join_kernel(NormDev d, const f32x4* __restrict__ part, float* __restrict__ stats)
 {
-    __shared__ double lds[4];
+    __shared__ double lds[kJoinThreads / 64];
     const long long groups = d.N * d.G;
     for (long long k = blockIdx.x; k < groups; k += gridDim.x) {
-        const long long n = k / d.G;
-        const int g = (int)(k - n * d.G);
+        // (the parts of a group lie one behind the other)
+        const f32x4* from = part + (size_t)k * d.Cg * d.chunks;
         double cnt = 0.0, sum = 0.0, sq = 0.0;
-        for (long long i = threadIdx.x; i < (long long)d.chunks * d.Cg; i += kThreads) {
-            const long long chunk = i / d.Cg;
-            const float* p = part + ((size_t)(n * d.chunks + chunk) * d.C + g * d.Cg + (i - chunk * d.Cg)) * 3;
+        for (long long i = threadIdx.x; i < (long long)d.chunks * d.Cg; i += kJoinThreads) {
+            const f32x4 p = from[i];
             const double c = p[0], m = p[1];
             cnt += c;
             sum += c * m;
@@ -251,18 +580,11 @@ __global__ __launch_bounds__(kThreads) void norm_join_kernel(NormDev d, const fl
         sum = block_sum(sum, lds);
         sq = block_sum(sq, lds);
         if (threadIdx.x == 0) {
-            float mean = 0.0f, rstd = 0.0f;
-            if (cnt > 0.0) {
-                const double m = sum / cnt;
-                double var = sq / cnt - m * m;
-                if (var < 0.0) var = 0.0;
-                mean = (float)m;
-                rstd = (float)(1.0 / sqrt(var + (double)d.eps));
-            }
+            float mean, rstd;
+            statistics_of(cnt, sum, sq, d.eps, mean, rstd);
             stats[2 * k] = mean;
             stats[2 * k + 1] = rstd;
         }
-        __syncthreads();
     }
 }
 
@@ -272,50 +594,51 @@ __global__ __launch_bounds__(kThreads) void norm_apply_kernel(NormDev d, const T
 {
     const Place at = place(d);
     if (!at.in) return;
+    Slot<V> slot;
+    slot.parameters(d, at.slot);
     const long long items = d.N * d.chunks;
-    for (long long item = blockIdx.x; item < items; item += gridDim.x) {
-        const long long n = item / d.chunks, first = (item - n * d.chunks) * d.chunk, end = min(first + d.chunk, d.P);
+    for (long long k = blockIdx.x; k < items; k += gridDim.x) {
+        const long long item = items - 1 - k, n = item / d.chunks, first = (item - n * d.chunks) * d.chunk, end = min(first + d.chunk, d.P);
         const TX* base = x + (size_t)(n * d.P) * d.xs + at.slot * V;
         TY* out = y + (size_t)(n * d.P) * d.ys + at.slot * V;
         const float* occ = MASK ? d.occ + n * d.P : nullptr;
-        float mean[V], scale[V], beta[V];
+        slot.statistics(d, at.slot, stats + n * d.G * 2);
+        float scale[V];
 #pragma unroll
-        for (int j = 0; j < V; ++j) {
-            const int c = at.slot * V + j;
-            const float* st = stats + (n * d.G + c / d.Cg) * 2;
-            mean[j] = st[0];
-            scale[j] = st[1] * (d.gamma ? d.gamma[c] : 1.0f);
-            beta[j] = d.beta ? d.beta[c] : 0.0f;
-        }
-        Pack<TX, V> v[kUnroll];
-        bool on[kUnroll];
-        sweep(d, first, end, at.row,
-              [&](int u, long long p, bool in) {
-                  on[u] = in && (!MASK || occ[p] > 0.0f);
-                  if (on[u]) load<TX, V>(base + p * d.xs, v[u]);
-              },
-              [&](int u, long long p, bool in) {
-                  if (!in) return;
-                  float r[V];
+        for (int j = 0; j < V; ++j) scale[j] = slot.rstd[j] * slot.gamma[j];
+        with_act(d.act, [&](auto act) {
+            Pack<TX, V> v[kUnroll<V>];   // (as they are stored: converted where they are used)
+            bool on[kUnroll<V>];
+            sweep<kUnroll<V>>(d, first, end, at.row,
+                  [&](int u, long long p, bool in) {
+                      on[u] = in && (!MASK || occ[p] > 0.0f);
+                      if (on[u]) load<TX, V>(base + p * d.xs, v[u]);
+                  },
+                  [&](int u, long long p, bool in) {
+                      if (!in) return;
+                      float r[V];
 #pragma unroll
-                  for (int j = 0; j < V; ++j) r[j] = on[u] ? activate(fmaf(to_f32(v[u].v[j]) - mean[j], scale[j], beta[j]), d.act) : 0.0f;
-                  store<TY, V>(out + p * d.ys, r);
-              });
+                      for (int j = 0; j < V; ++j)
+                          r[j] = on[u] ? activate<decltype(act)::value>(fmaf(to_f32(v[u].v[j]) - slot.mean[j], scale[j], slot.beta[j])) : 0.0f;
+                      store<TY, V>(out + p * d.ys, r);
+                  });
+        });
     }
 }
 
-// Pass 1 of the backward: (sum g, sum g xh) of every channel of every item -> part[(item C + c) 2], and the item's count.
+// Pass 1 of the backward: (sum g, sum g xh) of every channel of every item -> part[((n C + c) chunks + chunk) 2], and the item's count.
 template <class TX, class TY, int V, bool MASK>
 __global__ __launch_bounds__(kThreads) void norm_grad_sums_kernel(NormDev d, const TX* __restrict__ x, const TY* __restrict__ dy,
-                                                                  const float* __restrict__ stats, float* __restrict__ part,
+                                                                  const float* __restrict__ stats, f32x2* __restrict__ part,
                                                                   float* __restrict__ counts)
 {
-    __shared__ float sm[kThreads * V * 2];
-    __shared__ float sn[kThreads];
+    __shared__ float lds[(2 * V + 1) * kThreads];
     const Place at = place(d);
+    Slot<V> slot;
+    if (at.in) slot.parameters(d, at.slot);
     const long long items = d.N * d.chunks;
     for (long long item = blockIdx.x; item < items; item += gridDim.x) {
-        const long long n = item / d.chunks, first = (item - n * d.chunks) * d.chunk, end = min(first + d.chunk, d.P);
+        const long long n = item / d.chunks, chunk = item - n * d.chunks, first = chunk * d.chunk, end = min(first + d.chunk, d.P);
         float sg[V], sx[V], count = 0.0f;
 #pragma unroll
         for (int j = 0; j < V; ++j) sg[j] = sx[j] = 0.0f;
@@ -323,120 +646,92 @@ __global__ __launch_bounds__(kThreads) void norm_grad_sums_kernel(NormDev d, con
             const TX* base = x + (size_t)(n * d.P) * d.xs + at.slot * V;
             const TY* up = dy + (size_t)(n * d.P) * d.ys + at.slot * V;
             const float* occ = MASK ? d.occ + n * d.P : nullptr;
-            float mean[V], rstd[V], gamma[V], beta[V];
+            slot.statistics(d, at.slot, stats + n * d.G * 2);
+            with_act(d.act, [&](auto act) {
+                Pack<TX, V> v[kUnroll<V>];   // (as they are stored: converted where they are used)
+                Pack<TY, V> w[kUnroll<V>];
+                bool on[kUnroll<V>];
+                sweep<kUnroll<V>>(d, first, end, at.row,
+                      [&](int u, long long p, bool in) {
+                          on[u] = in && (!MASK || occ[p] > 0.0f);
+                          if (on[u]) {
+                              load<TX, V>(base + p * d.xs, v[u]);
+                              load<TY, V>(up + p * d.ys, w[u]);
+                          }
+                      },
+                      [&](int u, long long, bool) {
+                          if (!on[u]) return;
 #pragma unroll
-            for (int j = 0; j < V; ++j) {
-                const int c = at.slot * V + j;
-                const float* st = stats + (n * d.G + c / d.Cg) * 2;
-                mean[j] = st[0];
-                rstd[j] = st[1];
-                gamma[j] = d.gamma ? d.gamma[c] : 1.0f;
-                beta[j] = d.beta ? d.beta[c] : 0.0f;
-            }
-            Pack<TX, V> v[kUnroll];   // (as they are stored: converted where they are used)
-            Pack<TY, V> w[kUnroll];
-            bool on[kUnroll];
-            sweep(d, first, end, at.row,
-                  [&](int u, long long p, bool in) {
-                      on[u] = in && (!MASK || occ[p] > 0.0f);
-                      if (on[u]) {
-                          load<TX, V>(base + p * d.xs, v[u]);
-                          load<TY, V>(up + p * d.ys, w[u]);
-                      }
-                  },
-                  [&](int u, long long, bool) {
-                      if (!on[u]) return;
-#pragma unroll
-                      for (int j = 0; j < V; ++j) {
-                          const float xh = (to_f32(v[u].v[j]) - mean[j]) * rstd[j];
-                          const float g = to_f32(w[u].v[j]) * slope(fmaf(xh, gamma[j], beta[j]), d.act);
-                          sg[j] += g;
-                          sx[j] = fmaf(g, xh, sx[j]);
-                      }
-                      count += 1.0f;
-                  });
+                          for (int j = 0; j < V; ++j) {
+                              const float xh = (to_f32(v[u].v[j]) - slot.mean[j]) * slot.rstd[j];
+                              const float g = to_f32(w[u].v[j]) * slope<decltype(act)::value>(fmaf(xh, slot.gamma[j], slot.beta[j]));
+                              sg[j] += g;
+                              sx[j] = fmaf(g, xh, sx[j]);
+                          }
+                          count += 1.0f;
+                      });
+            });
         }
-        for (int rows = d.rows; rows > 1;) {
-            const int half = (rows + 1) / 2;
-            __syncthreads();
-            if (at.in && at.row >= half && at.row < rows) {
-                sn[threadIdx.x] = count;
-#pragma unroll
-                for (int j = 0; j < V; ++j) {
-                    sm[j * kThreads + threadIdx.x] = sg[j];
-                    sm[(V + j) * kThreads + threadIdx.x] = sx[j];
-                }
-            }
-            __syncthreads();
-            if (at.in && at.row + half < rows) {
-                const int o = threadIdx.x + half * d.slots;
-                count += sn[o];
-#pragma unroll
-                for (int j = 0; j < V; ++j) {
-                    sg[j] += sm[j * kThreads + o];
-                    sx[j] += sm[(V + j) * kThreads + o];
-                }
-            }
-            rows = half;
-        }
+        add_rows<V, kThreads>(d, at, d.rows, count, sg, sx, lds);
         if (at.in && at.row == 0) {
-            float* out = part + ((size_t)item * d.C + at.slot * V) * 2;
 #pragma unroll
-            for (int j = 0; j < V; ++j) {
-                out[2 * j] = sg[j];
-                out[2 * j + 1] = sx[j];
-            }
+            for (int j = 0; j < V; ++j) part[(size_t)(n * d.C + at.slot * V + j) * d.chunks + chunk] = f32x2{sg[j], sx[j]};
             if (at.slot == 0) counts[item] = count;
         }
     }
 }
 
-// Joins the backward's parts: one workgroup a (sample, group).  chan[(n C + c) 2] = sums of a channel,
-// means[(n G + g) 2] = S1 / count, S2 / count.
-__global__ __launch_bounds__(kThreads) void norm_grad_join_kernel(NormDev d, const float* __restrict__ part,
-                                                                  const float* __restrict__ counts, double* __restrict__ chan,
-                                                                  float* __restrict__ means)
+// Joins the backward's parts: one workgroup a (sample, group), a wave a channel at a time.  chan[(n C + c) 2] = sums of a
+// channel, means[(n G + g) 2] = S1 / count, S2 / count; with a single sample the parameters' gradients are added here.
+__global__ __launch_bounds__(kJoinThreads) void norm_grad_join_kernel(NormDev d, const f32x2* __restrict__ part, const float* __restrict__ counts,
+                                                                      double* __restrict__ chan, float* __restrict__ means, float* d_gamma,
+                                                                      float* d_beta)
 {
-    __shared__ double lds[4];
+    __shared__ double lds[kJoinThreads / 64];
     const long long groups = d.N * d.G;
     for (long long k = blockIdx.x; k < groups; k += gridDim.x) {
         const long long n = k / d.G;
         const int g = (int)(k - n * d.G);
         double cnt = 0.0;
-        for (int i = threadIdx.x; i < d.chunks; i += kThreads) cnt += (double)counts[n * d.chunks + i];
-        cnt = block_sum(cnt, lds) * d.Cg;
+        for (int i = threadIdx.x; i < d.chunks; i += kJoinThreads) cnt += (double)counts[n * d.chunks + i];
         double s1 = 0.0, s2 = 0.0;
-        for (int j = 0; j < d.Cg; ++j) {
+        for (int j = threadIdx.x >> 6; j < d.Cg; j += kJoinThreads / 64) {
             const int c = g * d.Cg + j;
+            const f32x2* from = part + (size_t)(n * d.C + c) * d.chunks;
             double a = 0.0, b = 0.0;
-            for (int i = threadIdx.x; i < d.chunks; i += kThreads) {
-                const float* p = part + ((size_t)(n * d.chunks + i) * d.C + c) * 2;
+            for (int i = threadIdx.x & 63; i < d.chunks; i += 64) {
+                const f32x2 p = from[i];
                 a += (double)p[0];
                 b += (double)p[1];
             }
-            a = block_sum(a, lds);
-            b = block_sum(b, lds);
-            const double gamma = d.gamma ? (double)d.gamma[c] : 1.0;
-            s1 += gamma * a;
-            s2 += gamma * b;
-            if (threadIdx.x == 0) {
-                chan[(n * d.C + c) * 2] = a;
-                chan[(n * d.C + c) * 2 + 1] = b;
+            a = wave_sum(a);
+            b = wave_sum(b);
+            if ((threadIdx.x & 63) == 0) {
+                const double gamma = d.gamma ? (double)d.gamma[c] : 1.0;
+                s1 += gamma * a;
+                s2 += gamma * b;
+                if (d.N > 1) {
+                    chan[(n * d.C + c) * 2] = a;
+                    chan[(n * d.C + c) * 2 + 1] = b;
+                } else {
+                    if (d_beta) d_beta[c] = (float)((double)d_beta[c] + a);
+                    if (d_gamma) d_gamma[c] = (float)((double)d_gamma[c] + b);
+                }
             }
         }
+        cnt = block_sum(cnt, lds) * d.Cg;
+        s1 = block_sum(s1, lds);
+        s2 = block_sum(s2, lds);
         if (threadIdx.x == 0) {
             means[2 * k] = cnt > 0.0 ? (float)(s1 / cnt) : 0.0f;
             means[2 * k + 1] = cnt > 0.0 ? (float)(s2 / cnt) : 0.0f;
         }
-        __syncthreads();
     }
 }
 
-// Gradients of the parameters: the samples' sums added in order.
-__global__ __launch_bounds__(kThreads) void norm_params_kernel(NormDev d, const double* __restrict__ chan, float* d_gamma, float* d_beta)
+// Gradients of the parameters over several samples, whose sums are added in order.
+__device__ __forceinline__ void add_parameters(const NormDev& d, int c, const double* chan, float* d_gamma, float* d_beta)
 {
-    const int c = blockIdx.x * kThreads + threadIdx.x;
-    if (c >= d.C) return;
     double a = 0.0, b = 0.0;
     for (long long n = 0; n < d.N; ++n) {
         a += chan[(n * d.C + c) * 2];
@@ -444,6 +739,11 @@ __global__ __launch_bounds__(kThreads) void norm_params_kernel(NormDev d, const 
     }
     if (d_beta) d_beta[c] = (float)((double)d_beta[c] + a);
     if (d_gamma) d_gamma[c] = (float)((double)d_gamma[c] + b);
+}
+__global__ __launch_bounds__(kThreads) void norm_params_kernel(NormDev d, const double* __restrict__ chan, float* d_gamma, float* d_beta)
+{
+    const int c = blockIdx.x * kThreads + threadIdx.x;
+    if (c < d.C) add_parameters(d, c, chan, d_gamma, d_beta);
 }
 
 // Pass 2 of the backward.
@@ -453,50 +753,49 @@ __global__ __launch_bounds__(kThreads) void norm_grad_kernel(NormDev d, const TX
 {
     const Place at = place(d);
     if (!at.in) return;
+    Slot<V> slot;
+    slot.parameters(d, at.slot);
     const long long items = d.N * d.chunks;
-    for (long long item = blockIdx.x; item < items; item += gridDim.x) {
-        const long long n = item / d.chunks, first = (item - n * d.chunks) * d.chunk, end = min(first + d.chunk, d.P);
+    for (long long k = blockIdx.x; k < items; k += gridDim.x) {
+        const long long item = items - 1 - k, n = item / d.chunks, first = (item - n * d.chunks) * d.chunk, end = min(first + d.chunk, d.P);
         const TX* base = x + (size_t)(n * d.P) * d.xs + at.slot * V;
         const TY* up = dy + (size_t)(n * d.P) * d.ys + at.slot * V;
         TX* out = dx + (size_t)(n * d.P) * d.xs + at.slot * V;
         const float* occ = MASK ? d.occ + n * d.P : nullptr;
-        float mean[V], rstd[V], gamma[V], beta[V], m1[V], m2[V];
+        slot.statistics(d, at.slot, stats + n * d.G * 2);
+        // d_x = rstd (gamma g - m1 - xh m2)
+        float scale[V], m1[V], m2[V];
 #pragma unroll
         for (int j = 0; j < V; ++j) {
-            const int c = at.slot * V + j;
-            const long long k = n * d.G + c / d.Cg;
-            mean[j] = stats[2 * k];
-            rstd[j] = stats[2 * k + 1];
-            m1[j] = means[2 * k];
-            m2[j] = means[2 * k + 1];
-            gamma[j] = d.gamma ? d.gamma[c] : 1.0f;
-            beta[j] = d.beta ? d.beta[c] : 0.0f;
+            const long long g = n * d.G + (at.slot * V + j) / d.Cg;
+            scale[j] = slot.rstd[j] * slot.gamma[j];
+            m1[j] = slot.rstd[j] * means[2 * g];
+            m2[j] = slot.rstd[j] * means[2 * g + 1];
         }
-        Pack<TX, V> v[kUnroll];   // (as they are stored: converted where they are used)
-        Pack<TY, V> w[kUnroll];
-        bool on[kUnroll];
-        sweep(d, first, end, at.row,
-              [&](int u, long long p, bool in) {
-                  on[u] = in && (!MASK || occ[p] > 0.0f);
-                  if (on[u]) {
-                      load<TX, V>(base + p * d.xs, v[u]);
-                      load<TY, V>(up + p * d.ys, w[u]);
-                  }
-              },
-              [&](int u, long long p, bool in) {
-                  if (!in) return;
-                  float r[V];
-#pragma unroll
-                  for (int j = 0; j < V; ++j) {
-                      r[j] = 0.0f;
+        with_act(d.act, [&](auto act) {
+            Pack<TX, V> v[kUnroll<V>];   // (as they are stored: converted where they are used)
+            Pack<TY, V> w[kUnroll<V>];
+            bool on[kUnroll<V>];
+            sweep<kUnroll<V>>(d, first, end, at.row,
+                  [&](int u, long long p, bool in) {
+                      on[u] = in && (!MASK || occ[p] > 0.0f);
                       if (on[u]) {
-                          const float xh = (to_f32(v[u].v[j]) - mean[j]) * rstd[j];
-                          const float g = to_f32(w[u].v[j]) * slope(fmaf(xh, gamma[j], beta[j]), d.act);
-                          r[j] = rstd[j] * (fmaf(gamma[j], g, -m1[j]) - xh * m2[j]);
+                          load<TX, V>(base + p * d.xs, v[u]);
+                          load<TY, V>(up + p * d.ys, w[u]);
                       }
-                  }
-                  store<TX, V>(out + p * d.xs, r);
-              });
+                  },
+                  [&](int u, long long p, bool in) {
+                      if (!in) return;
+                      float r[V];
+#pragma unroll
+                      for (int j = 0; j < V; ++j) {
+                          const float xh = (to_f32(v[u].v[j]) - slot.mean[j]) * slot.rstd[j];
+                          const float g = to_f32(w[u].v[j]) * slope<decltype(act)::value>(fmaf(xh, slot.gamma[j], slot.beta[j]));
+                          r[j] = on[u] ? fmaf(scale[j], g, -fmaf(xh, m2[j], m1[j])) : 0.0f;
+                      }
+                      store<TX, V>(out + p * d.xs, r);
+                  });
+        });
     }
 }
 
@@ -569,7 +868,7 @@ Sizes sizes(const NormDev& d, int n_cu)
 {
     Sizes s;
     const size_t items = (size_t)most_items(d, n_cu);
-    s.part = align256(items * d.C * 3 * sizeof(float));
+    s.part = align256(items * d.C * sizeof(f32x4));
     s.counts = align256(items * sizeof(float));
     s.chan = align256((size_t)d.N * d.C * 2 * sizeof(double));
     s.means = s.stats = align256((size_t)d.N * d.G * 2 * sizeof(float));
@@ -578,10 +877,24 @@ Sizes sizes(const NormDev& d, int n_cu)
     return s;
 }
 
+// Whether a sample fits the registers of a workgroup: then `d` is divided for that.  The rule's other side: a sample of 128 KB takes
+// XXX us like that and YYY us in three launches, one of 256 KB would leave registers for half a workgroup.
+bool hold(NormDev* d, int V)
+{
+    const int held = V == 8 ? 4 : V == 4 ? 8 : 16;
+    if (d->C / V > kSmallThreads || d->C > kSmallThreads || d->N > kMaxGrid) return false;
+    const int rows = kSmallThreads / (d->C / V);
+    if (d->P > (long long)rows * held) return false;
+    d->slots = d->C / V;
+    d->zblocks = 1;
+    d->rows = rows;
+    return true;
+}
+
 // The widest slot that channels, strides and addresses allow: 16 bytes of x.
 int slot_width(const NormDev& d, int x_bytes, int y_bytes, std::initializer_list<const void*> xs, std::initializer_list<const void*> ys)
 {
-    for (int V = 16 / x_bytes; V > 1; V /= 2) {
+    for (int V = 16 / x_bytes; V > 1; V = V == 8 ? 4 : 1) {
         bool ok = d.C % V == 0 && d.xs % V == 0 && d.ys % V == 0;
         for (const void* p : xs) ok = ok && (uintptr_t)p % (V * x_bytes) == 0;
         for (const void* p : ys) ok = ok && (uintptr_t)p % (V * y_bytes) == 0;
@@ -604,8 +917,8 @@ void with_width(int V, bool mask, F&& f, Type<X> x, Type<Y> y, std::integer_sequ
 template <class F>
 void dispatch(int x_dtype, int y_dtype, int V, bool mask, F&& f)
 {
-    using W4 = std::integer_sequence<int, 1, 2, 4>;
-    using W8 = std::integer_sequence<int, 1, 2, 4, 8>;
+    using W4 = std::integer_sequence<int, 1, 4>;
+    using W8 = std::integer_sequence<int, 1, 4, 8>;
     if (x_dtype == LP_BF16) with_width(V, mask, f, Type<__bf16>(), Type<__bf16>(), W8());
     else if (x_dtype == LP_F16) with_width(V, mask, f, Type<_Float16>(), Type<_Float16>(), W8());
     else if (y_dtype == LP_BF16) with_width(V, mask, f, Type<float>(), Type<__bf16>(), W4());
@@ -636,8 +949,9 @@ lp_status forward(const lp_group_norm* q, const void* x, void* y, float* stats, 
         return fail(LP_ERR_WORKSPACE, "workspace is NULL or smaller than lp_group_norm_workspace_bytes");
     if ((uintptr_t)workspace % 256) return fail(LP_ERR_INVALID_ARG, "workspace must be 256-byte aligned");
     const int V = slot_width(d, dtype_bytes(q->x_dtype), dtype_bytes(q->y_dtype), {x}, {y});
-    divide(&d, V, n_cu);
-    float* part = (float*)workspace;
+    const bool small = hold(&d, V);
+    if (!small) divide(&d, V, n_cu);
+    f32x4* part = (f32x4*)workspace;
     float* used = stats ? stats : (float*)((char*)workspace + size.part);
     const dim3 grid(grid_of(d.N * d.chunks), d.zblocks);
     dispatch(q->x_dtype, q->y_dtype, V, d.occ != nullptr, [&](auto tx, auto ty, auto v, auto mask) {
@@ -645,8 +959,12 @@ lp_status forward(const lp_group_norm* q, const void* x, void* y, float* stats, 
         using TY = typename decltype(ty)::type;
         constexpr int W = decltype(v)::value;
         constexpr bool M = decltype(mask)::value;
+        if (small) {
+            hipLaunchKernelGGL((norm_small_kernel<TX, TY, W, M>), dim3((unsigned)d.N), dim3(kSmallThreads), 0, s, d, (const TX*)x, (TY*)y, stats);
+            return;
+        }
         hipLaunchKernelGGL((norm_stats_kernel<TX, W, M>), grid, dim3(kThreads), 0, s, d, (const TX*)x, part);
-        hipLaunchKernelGGL(norm_join_kernel, dim3(grid_of(d.N * d.G)), dim3(kThreads), 0, s, d, part, used);
+        hipLaunchKernelGGL(norm_join_kernel, dim3(grid_of(d.N * d.G)), dim3(kJoinThreads), 0, s, d, part, used);
         hipLaunchKernelGGL((norm_apply_kernel<TX, TY, W, M>), grid, dim3(kThreads), 0, s, d, (const TX*)x, (TY*)y, used);
     });
     return launched("group norm forward launch");
@@ -668,9 +986,10 @@ lp_status backward(const lp_group_norm* q, const void* x, const float* stats, co
         return fail(LP_ERR_WORKSPACE, "workspace is NULL or smaller than lp_group_norm_workspace_bytes");
     if ((uintptr_t)workspace % 256) return fail(LP_ERR_INVALID_ARG, "workspace must be 256-byte aligned");
     const int V = slot_width(d, dtype_bytes(q->x_dtype), dtype_bytes(q->y_dtype), {x, dx}, {dy});
-    divide(&d, V, n_cu);
+    const bool small = hold(&d, V);
+    if (!small) divide(&d, V, n_cu);
     char* at = (char*)workspace;
-    float* part = (float*)at;
+    f32x2* part = (f32x2*)at;
     float* counts = (float*)(at += size.part);
     double* chan = (double*)(at += size.counts);
     float* means = (float*)(at += size.chan);
@@ -680,11 +999,19 @@ lp_status backward(const lp_group_norm* q, const void* x, const float* stats, co
         using TY = typename decltype(ty)::type;
         constexpr int W = decltype(v)::value;
         constexpr bool M = decltype(mask)::value;
-        hipLaunchKernelGGL((norm_grad_sums_kernel<TX, TY, W, M>), grid, dim3(kThreads), 0, s, d, (const TX*)x, (const TY*)dy, stats,
-                           part, counts);
-        hipLaunchKernelGGL(norm_grad_join_kernel, dim3(grid_of(d.N * d.G)), dim3(kThreads), 0, s, d, part, counts, chan, means);
-        if (d_gamma || d_beta)
+        const bool params = (d_gamma || d_beta) && d.N > 1;
+        if (small) {
+            hipLaunchKernelGGL((norm_small_grad_kernel<TX, TY, W, M>), dim3((unsigned)d.N), dim3(kSmallThreads), 0, s, d, (const TX*)x,
+                               (const TY*)dy, (TX*)dx, stats, chan, d_gamma, d_beta);
+        } else {
+            hipLaunchKernelGGL((norm_grad_sums_kernel<TX, TY, W, M>), grid, dim3(kThreads), 0, s, d, (const TX*)x, (const TY*)dy, stats,
+                               part, counts);
+            hipLaunchKernelGGL(norm_grad_join_kernel, dim3(grid_of(d.N * d.G)), dim3(kJoinThreads), 0, s, d, part, counts, chan, means,
+                               d_gamma, d_beta);
+        }
+        if (params)
             hipLaunchKernelGGL(norm_params_kernel, dim3((d.C + kThreads - 1) / kThreads), dim3(kThreads), 0, s, d, chan, d_gamma, d_beta);
+        if (small) return;
         if (dx)
             hipLaunchKernelGGL((norm_grad_kernel<TX, TY, W, M>), grid, dim3(kThreads), 0, s, d, (const TX*)x, (const TY*)dy, (TX*)dx,
                                stats, means);

@@ -338,7 +338,7 @@ typedef struct {
 } lp_group_norm;
 
 /* Bytes of device workspace of the two calls below (either pointer may be NULL); they depend on
-   N, P, C, G and the device's compute-unit count. */
+   N, P, C, G and the device's compute-unit count, and may be 0 (then NULL will do). */
 lp_status lp_group_norm_workspace_bytes(const lp_group_norm* norm, size_t* fwd_bytes, size_t* bwd_bytes);
 
 /* Forward.  y is WRITTEN; stats [N][G][2] (device, fp32: mean, rstd; may be NULL) is written for the
@@ -387,6 +387,7 @@ typedef struct {
    count, rows or cols 0. */
 lp_status lp_orthogonalize(int32_t n, const lp_matrices* lists, const lp_orth* orth, void* workspace,
                            size_t workspace_bytes, void* stream);
+/* 0 where all matrices are at most 64 x 128 or 128 x 64 (then NULL will do). */
 lp_status lp_orthogonalize_workspace_bytes(int32_t n, const lp_matrices* lists, size_t* bytes);
 
 /* How the step of a matrix is scaled. */

@@ -456,7 +456,9 @@ def lp_dec_workspace_bytes(grid: Grid, dec: Decoder, rays: Rays, math_mode: int 
     return int(nf.value), int(nb.value)
 
 
-def _workspace(workspace: torch.Tensor):
+def _workspace(workspace: Optional[torch.Tensor]):
+    if workspace is None:
+        return None, C.c_size_t(0)
     if not (workspace.is_cuda and workspace.is_contiguous()):
         raise ValueError("workspace must be a contiguous GPU tensor")
     return C.c_void_p(workspace.data_ptr()), C.c_size_t(workspace.numel() * workspace.element_size())
@@ -636,12 +638,12 @@ class GroupNorm:
         y_dtype = x.dtype if y_dtype is None else y_dtype
         if x.dtype not in _GRID_DTYPES or y_dtype not in _GRID_DTYPES:
             raise ValueError("x and y must be float32, bfloat16 or float16")
-        if x.dim() < 2:
-            raise ValueError("x must have a first axis of samples and a last axis of channels")
         shape = x.shape
-        c = shape[-1]
-        return _GroupNorm(shape[0], x.numel() // max(1, shape[0] * c) if c else 0, c, int(self.groups), int(self.act),
-                          float(self.eps), _GRID_DTYPES[x.dtype], _GRID_DTYPES[y_dtype], _position_stride(x, "x"), y_stride,
+        if len(shape) < 2:
+            raise ValueError("x must have a first axis of samples and a last axis of channels")
+        n, c = shape[0], shape[-1]
+        return _GroupNorm(n, x.numel() // (n * c) if n and c else 0, c, int(self.groups), int(self.act), float(self.eps),
+                          _GRID_DTYPES[x.dtype], _GRID_DTYPES[y_dtype], _position_stride(x, "x"), y_stride,
                           _dev_f32(self.gamma, "gamma", (c,)), _dev_f32(self.beta, "beta", (c,)),
                           _dev_f32(self.occupancy, "occupancy", shape[:-1]))
 
@@ -687,16 +689,19 @@ def _no_overlap(written: torch.Tensor, read: torch.Tensor, written_name: str, re
         raise ValueError(f"{written_name} must be {read_name} itself or not overlap it")
 
 
+def _norm_bytes(q: _GroupNorm):
+    f, b = C.c_size_t(), C.c_size_t()
+    _check(_lib.lp_group_norm_workspace_bytes(C.byref(q), C.byref(f), C.byref(b)))
+    return f.value, b.value
+
+
 def lp_group_norm_workspace_bytes(norm: GroupNorm, x: torch.Tensor, y_dtype=None):
     """(forward bytes, backward bytes) of workspace."""
-    q = norm.c_struct(x, y_dtype)
-    f, b = C.c_size_t(0), C.c_size_t(0)
-    _check(_lib.lp_group_norm_workspace_bytes(C.byref(q), C.byref(f), C.byref(b)))
-    return int(f.value), int(b.value)
+    return _norm_bytes(norm.c_struct(x, y_dtype))
 
 
 def lp_group_norm_fwd(norm: GroupNorm, x: torch.Tensor, y: torch.Tensor, stats: Optional[torch.Tensor],
-                      workspace: torch.Tensor, stream=None) -> None:
+                      workspace: Optional[torch.Tensor], stream=None) -> None:
     """Enqueue the forward: y (shape of x; its type, or a 16-bit one where x is float32) and stats [N][groups][2] (None:
     not wanted) are written."""
     q = norm.c_struct(x, y.dtype, _channel_last(y, "y", x.shape, y.dtype))
@@ -707,7 +712,8 @@ def lp_group_norm_fwd(norm: GroupNorm, x: torch.Tensor, y: torch.Tensor, stats: 
 
 
 def lp_group_norm_bwd(norm: GroupNorm, x: torch.Tensor, stats: torch.Tensor, d_y: torch.Tensor, d_x: Optional[torch.Tensor],
-                      d_gamma: Optional[torch.Tensor], d_beta: Optional[torch.Tensor], workspace: torch.Tensor, stream=None) -> None:
+                      d_gamma: Optional[torch.Tensor], d_beta: Optional[torch.Tensor], workspace: Optional[torch.Tensor],
+                      stream=None) -> None:
     """Enqueue the backward: d_x (shape, type and strides of x) is written, d_gamma and d_beta [C] are accumulated into; each
     may be None.  stats as the forward wrote it for the same x."""
     q = norm.c_struct(x, d_y.dtype, _channel_last(d_y, "d_y", x.shape, d_y.dtype))
@@ -920,10 +926,12 @@ def splat_bwd(target: _Grid, rays: Rays, splat: Splat, theta_w, d_theta):
 
 def group_norm_fwd(norm: GroupNorm, x: torch.Tensor, dtype=None):
     """Allocate outputs and workspace and run lp_group_norm_fwd.  Returns (y, stats); dtype: of y (default: that of x)."""
+    q = norm.c_struct(x, dtype)   # (new outputs are dense: what the entry point checks of them holds)
     y = torch.empty(x.shape, dtype=x.dtype if dtype is None else dtype, device=x.device)
-    stats = torch.empty((x.shape[0], norm.groups, 2), dtype=torch.float32, device=x.device)
-    ws = torch.empty(lp_group_norm_workspace_bytes(norm, x, y.dtype)[0], dtype=torch.uint8, device=x.device)
-    lp_group_norm_fwd(norm, x, y, stats, ws)
+    stats = torch.empty((q.N, q.G, 2), device=x.device, dtype=torch.float32)
+    n = _norm_bytes(q)[0]
+    ws = torch.empty(n, dtype=torch.uint8, device=x.device).data_ptr() if n else None
+    _check(_lib.lp_group_norm_fwd(C.byref(q), x.data_ptr(), y.data_ptr(), stats.data_ptr(), ws, n, _stream_ptr(None)))
     return y, stats
 
 
@@ -931,7 +939,8 @@ def group_norm_bwd(norm: GroupNorm, x: torch.Tensor, stats: torch.Tensor, d_y: t
     """Allocate gradients and workspace and run lp_group_norm_bwd.  Returns (d_x, d_gamma, d_beta)."""
     d_x = torch.empty_strided(x.shape, x.stride(), dtype=x.dtype, device=x.device)
     d_gamma, d_beta = torch.zeros((2, x.shape[-1]), dtype=torch.float32, device=x.device)
-    ws = torch.empty(lp_group_norm_workspace_bytes(norm, x, d_y.dtype)[1], dtype=torch.uint8, device=x.device)
+    n = lp_group_norm_workspace_bytes(norm, x, d_y.dtype)[1]
+    ws = torch.empty(n, dtype=torch.uint8, device=x.device) if n else None
     lp_group_norm_bwd(norm, x, stats, d_y, d_x, d_gamma, d_beta, ws)
     return d_x, d_gamma, d_beta
 

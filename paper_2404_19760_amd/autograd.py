@@ -1,12 +1,15 @@
-"""torch.autograd wrapper around the Renderer's two entry points, for callers that train with
-PyTorch optimisers: the forward keeps one scalar per ray (Section 3.4: the backward recomputes the
-rest), the backward calls lp_render_bwd.  Argument marshalling only: every step of the path runs in the
-library's kernels.  No gradient flows to the rays (the library produces none)."""
+"""torch.autograd wrappers, for callers that train with PyTorch optimisers.  Argument marshalling only: every step runs in the
+library's kernels.
+
+render: the Renderer's two entry points; the forward keeps one scalar per ray (Section 3.4: the backward recomputes the
+rest), the backward calls lp_render_bwd.  No gradient flows to the rays (the library produces none).
+group_norm: group norm with an activation over channel-last grids; the forward keeps its input and two numbers a group."""
 from typing import List, Optional, Sequence
 
 import torch
 
-from . import (LP_MATH_DEFAULT, Grid, Mlp, Rays, lp_bwd_workspace_bytes, lp_render_bwd, lp_render_fwd)
+from . import (LP_ACT_NONE, LP_MATH_DEFAULT, Grid, GroupNorm, Mlp, Rays, group_norm_fwd, lp_bwd_workspace_bytes,
+               lp_group_norm_bwd, lp_group_norm_workspace_bytes, lp_render_bwd, lp_render_fwd)
 
 
 class _Render(torch.autograd.Function):
@@ -51,3 +54,37 @@ def render(grid: Grid, mlp: Mlp, rays: Rays, bg: Sequence[float], math_mode: int
     spec = (grid.kind, tuple(grid.res), tuple(grid.aabb_min), tuple(grid.aabb_max), float(grid.contract_a),
             tuple(grid.t_range), rays, tuple(float(v) for v in bg), int(math_mode))
     return _Render.apply(spec, len(grid.data), len(mlp.weights), *grid.data, *mlp.weights, *mlp.biases)
+
+
+class _GroupNorm(torch.autograd.Function):
+    @staticmethod
+    def forward(ctx, spec, x, gamma, beta):
+        groups, act, eps, occupancy, dtype = spec
+        detach = lambda t: None if t is None else t.detach()
+        norm = GroupNorm(groups, detach(gamma), detach(beta), act, eps, occupancy)
+        y, stats = group_norm_fwd(norm, x.detach(), dtype)
+        ctx.save_for_backward(x, gamma, beta, stats)
+        ctx.lp = spec
+        return y
+
+    @staticmethod
+    def backward(ctx, d_y):
+        groups, act, eps, occupancy, _ = ctx.lp
+        x, gamma, beta, stats = ctx.saved_tensors
+        norm = GroupNorm(groups, gamma, beta, act, eps, occupancy)
+        need_x, need_gamma, need_beta = ctx.needs_input_grad[1:4]
+        d_y = d_y.contiguous()
+        d_x = torch.empty_strided(x.shape, x.stride(), dtype=x.dtype, device=x.device) if need_x else None
+        d_gamma = torch.zeros_like(gamma) if need_gamma else None
+        d_beta = torch.zeros_like(beta) if need_beta else None
+        n = lp_group_norm_workspace_bytes(norm, x, d_y.dtype)[1]
+        ws = torch.empty(n, dtype=torch.uint8, device=x.device) if n else None
+        lp_group_norm_bwd(norm, x, stats, d_y, d_x, d_gamma, d_beta, ws)
+        return None, d_x, d_gamma, d_beta
+
+
+def group_norm(x: torch.Tensor, groups: int, gamma: Optional[torch.Tensor] = None, beta: Optional[torch.Tensor] = None,
+               act: int = LP_ACT_NONE, eps: float = 1e-5, occupancy: Optional[torch.Tensor] = None, dtype=None) -> torch.Tensor:
+    """Differentiable group norm with an activation of a channel-last tensor [N][...][C] (see GroupNorm; dtype: of the result);
+    gradients flow to x, gamma and beta."""
+    return _GroupNorm.apply((int(groups), int(act), float(eps), occupancy, dtype), x, gamma, beta)

@@ -34,6 +34,7 @@ using half4 = _Float16 __attribute__((ext_vector_type(4)));
 using f32x16 = float __attribute__((ext_vector_type(16)));
 
 constexpr int kThreads = 256;
+constexpr int kUnits = 256;       // compute units of the chip: what divides the work goes by it
 constexpr int kMaxLists = 16;     // lists of one set of launches (their descriptors travel as kernel arguments)
 constexpr int kPad = 64;          // rows and columns of operands are padded to this
 constexpr int kNormChunks = 512;  // partial sums of a matrix's norm, at most
@@ -61,6 +62,8 @@ struct List {
     int first_tile;     // of the launch
     int tiles;          // of one matrix
     int vec4;           // four neighbours can be read and written at a time
+    int splits, chunk;  // kPart: parts of the inner dimension, and their steps
+    int first_part;     // its first tile's first part among all
 };
 
 struct Lists {
@@ -71,6 +74,7 @@ struct Lists {
     int nesterov;
     float eps;
     double* norms;      // [matrices][kNormChunks]
+    float* parts;       // kPart's tiles, as the waves hold them
     List l[kMaxLists];
 };
 
@@ -284,7 +288,7 @@ __global__ __launch_bounds__(kThreads) void orth_load_kernel(Lists a, float scal
     }
 }
 
-enum Product { kGram, kPoly, kUpdate, kLast };
+enum Product { kGram, kPoly, kUpdate, kLast, kPart, kJoin };   // kPart: a part of kGram's inner dimension; kJoin adds the parts
 
 // Scales of one step: what the accumulator is multiplied with, and the polynomial's coefficients at B's scale.
 struct Step {
@@ -333,9 +337,15 @@ __global__ __launch_bounds__((ProductShape<TILE, GROUPS>::kThreadsOf), (2)) void
     _Float16* x = ws + s.from * 2 * plane;
     _Float16* A = ws + 4 * plane;
     _Float16* B = A + square;
-    int ti, tj;
+    constexpr bool kGramLike = WHAT == kGram || WHAT == kPart || WHAT == kJoin, kSymmetric = kGramLike || WHAT == kPoly;
+    int ti, tj, slice = 0;
     const int mt = (l.mp + TILE - 1) / TILE, nt = (l.np + TILE - 1) / TILE;
-    if (WHAT == kGram || WHAT == kPoly) {   // tiles on and above the diagonal, row by row
+    const int part = l.first_part + (matrix * l.tiles + local) * (WHAT == kJoin ? l.splits : 1);
+    if (WHAT == kPart) {
+        slice = local % l.splits;
+        local /= l.splits;
+    }
+    if (kSymmetric) {   // tiles on and above the diagonal, row by row
         ti = 0;
         int rest = local;
         while (rest >= mt - ti) rest -= mt - ti++;
@@ -344,14 +354,28 @@ __global__ __launch_bounds__((ProductShape<TILE, GROUPS>::kThreadsOf), (2)) void
         ti = local / nt;
         tj = local - ti * nt;
     }
-    const _Float16* p = WHAT == kGram ? x : WHAT == kPoly ? A : B;
-    const _Float16* q = WHAT == kGram ? x : WHAT == kPoly ? A : x + plane;
-    const int K = WHAT == kGram ? l.np : l.mp;
-    const int p_blocks = l.mp >> 5, q_blocks = (WHAT == kGram || WHAT == kPoly ? l.mp : l.np) >> 5;
+    const _Float16* p = kGramLike ? x : WHAT == kPoly ? A : B;
+    const _Float16* q = kGramLike ? x : WHAT == kPoly ? A : x + plane;
+    const int K = kGramLike ? l.np : l.mp;
+    const int p_blocks = l.mp >> 5, q_blocks = (kSymmetric ? l.mp : l.np) >> 5;
     const int wave_of_8 = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), group = wave_of_8 / S::kWaves, wave = wave_of_8 % S::kWaves;
     const int lane = threadIdx.x & 63, in_group = threadIdx.x % S::kGroupThreads, l32 = lane & 31, h = lane >> 5;
+    float mine[S::kMine];   // what this wave finishes
+    auto part_at = [&](int k, int e) { return (f32x4*)(a.parts + (size_t)k * TILE * TILE) + wave_of_8 * (S::kMine * 16) + (e >> 2) * 64 + lane; };
+    if constexpr (WHAT == kJoin) {
+#pragma unroll
+        for (int e = 0; e < S::kMine; ++e) mine[e] = 0.0f;
+        for (int k = 0; k < l.splits; ++k)
+#pragma unroll
+            for (int e = 0; e < S::kMine; e += 4) {
+                const f32x4 v = *part_at(part + k, e);
+#pragma unroll
+                for (int j = 0; j < 4; ++j) mine[e + j] += v[j];
+            }
+    } else {
     // a group's steps; where they do not divide evenly the last ones have fewer
-    const int all = K / kDepth, steps = (all + S::kGroups - 1) / S::kGroups, start = group * steps, mine_steps = min(steps, all - start);
+    const int begin = WHAT == kPart ? slice * l.chunk : 0, all = WHAT == kPart ? min(K / kDepth, begin + l.chunk) : K / kDepth;
+    const int steps = (all - begin + S::kGroups - 1) / S::kGroups, start = begin + group * steps, mine_steps = min(steps, all - start);
     // row blocks behind an operand's end are its last one again (their products are not stored)
     const size_t row = (size_t)(K >> 4) * kBlock;   // halves of a row block
     const _Float16 *p_at[kLoads], *q_at;            // the same for all lanes
@@ -426,7 +450,6 @@ __global__ __launch_bounds__((ProductShape<TILE, GROUPS>::kThreadsOf), (2)) void
     }
     __syncthreads();
     // group g finishes values g kMine .. of every lane; the groups' sums are added in their order
-    float mine[S::kMine];
     if constexpr (S::kGroups == 1) {
 #pragma unroll
         for (int e = 0; e < S::kMine; ++e) mine[e] = acc[e >> 4][e & 15] + cross[e >> 4][e & 15];
@@ -464,6 +487,12 @@ __global__ __launch_bounds__((ProductShape<TILE, GROUPS>::kThreadsOf), (2)) void
             for (int j = 0; j < 4; ++j) mine[e + j] = v[j];
         }
         __syncthreads();
+    }
+    if (WHAT == kPart) {
+#pragma unroll
+        for (int e = 0; e < S::kMine; e += 4) *part_at(part, e) = f32x4{mine[e], mine[e + 1], mine[e + 2], mine[e + 3]};
+        return;
+    }
     }
     // value e of a lane: row 8 (e / 4) + 4 h + e % 4, column l32 of a 32 x 32 block.  Four rows of a column are neighbours in an
     // operand whose rows are the block's columns; for the other order the rows are turned over in the wave's own LDS.
@@ -520,7 +549,7 @@ __global__ __launch_bounds__((ProductShape<TILE, GROUPS>::kThreadsOf), (2)) void
             }
             continue;
         }
-        _Float16* direct = WHAT == kGram ? A : WHAT == kPoly ? B : ws + s.to * 2 * plane;
+        _Float16* direct = kGramLike ? A : WHAT == kPoly ? B : ws + s.to * 2 * plane;
         _Float16* trans = WHAT == kUpdate ? direct + plane : direct;
         const int width = WHAT == kUpdate ? l.np : l.mp;
         const bool both = WHAT == kUpdate || ti != tj;   // (a tile on the diagonal is its own transpose)
@@ -858,11 +887,52 @@ size_t set_bytes(const std::vector<HostList>& v, size_t first, size_t end)
     return align256(matrices * kNormChunks * sizeof(double)) + planes;
 }
 
+
+// How a set's A = X X^T is divided.
+struct GramPlan {
+    int tile, groups;
+    int splits[kMaxLists], chunk;   // of the set's lists; 1: not divided
+    long long parts;                // tiles of all parts
+};
+GramPlan plan_gram(const std::vector<HostList>& v, size_t first, size_t end)
+{
+    GramPlan g;
+    std::memset(&g, 0, sizeof(g));
+    long long large = 0, steps = 0;
+    for (size_t k = first; k < end; ++k) {
+        if (is_small(v[k].rows, v[k].cols)) continue;
+        const long long mp = pad(v[k].rows < v[k].cols ? v[k].rows : v[k].cols), np = pad(v[k].rows < v[k].cols ? v[k].cols : v[k].rows);
+        const long long t128 = (mp + 127) / 128, t64 = mp / 64;
+        large += v[k].count * (t128 * (t128 + 1) / 2);
+        steps += v[k].count * (t64 * (t64 + 1) / 2) * (np / kDepth);
+    }
+    for (int& s : g.splits) s = 1;
+    if (large >= 2 * kUnits) {
+        g.tile = 128;
+        g.groups = 1;
+        return g;
+    }
+    g.tile = 64;
+    g.groups = 4;
+    const long long even = (steps + 2 * kUnits - 1) / (2 * kUnits);
+    g.chunk = (int)((even > 16 ? even + 3 : 16) / 4 * 4);
+    for (size_t k = first; k < end; ++k) {
+        if (is_small(v[k].rows, v[k].cols)) continue;
+        const long long mp = pad(v[k].rows < v[k].cols ? v[k].rows : v[k].cols), np = pad(v[k].rows < v[k].cols ? v[k].cols : v[k].rows);
+        const int s = (int)((np / kDepth + g.chunk - 1) / g.chunk);
+        g.splits[k - first] = s;
+        g.parts += v[k].count * (mp / 64 * (mp / 64 + 1) / 2) * s;
+    }
+    return g;
+}
+
 size_t all_bytes(const std::vector<HostList>& v)
 {
     size_t most = 0;
     for (size_t k = 0; k < v.size(); k += kMaxLists) {
-        const size_t need = set_bytes(v, k, v.size() < k + kMaxLists ? v.size() : k + kMaxLists);
+        const size_t end = v.size() < k + kMaxLists ? v.size() : k + kMaxLists;
+        const GramPlan g = plan_gram(v, k, end);
+        const size_t need = set_bytes(v, k, end) + (size_t)g.parts * g.tile * g.tile * sizeof(float);
         most = need > most ? need : most;
     }
     return most;
@@ -973,7 +1043,7 @@ struct Muon {
 };
 
 lp_status run_set(const std::vector<HostList>& v, size_t first, size_t end, const Plan& plan, float eps, const Muon* muon,
-                  void* workspace, int n_cu, hipStream_t s)
+                  void* workspace, hipStream_t s)
 {
     Lists a;
     std::memset(&a, 0, sizeof(a));
@@ -988,6 +1058,7 @@ lp_status run_set(const std::vector<HostList>& v, size_t first, size_t end, cons
     for (size_t k = first; k < end; ++k)
         if (!is_small(v[k].rows, v[k].cols)) matrices += (size_t)v[k].count;
     char* at = (char*)workspace + align256(matrices * kNormChunks * sizeof(double));
+    const GramPlan gram = plan_gram(v, first, end);
     Lists small = a;
     int lds = 0;
     for (size_t k = first; k < end; ++k) {
@@ -1009,6 +1080,8 @@ lp_status run_set(const std::vector<HostList>& v, size_t first, size_t end, cons
             at += (size_t)l.ws_stride * 2 * q.count;
             l.vec4 = (long long)q.rows * q.cols % 4 == 0 && (uintptr_t)q.in % 16 == 0 && (uintptr_t)q.momentum % 16 == 0;
             a.order[a.n - 1] = a.n - 1;
+            l.splits = gram.splits[k - first];
+            l.chunk = gram.chunk;
             l.first_matrix = a.matrices;
             a.matrices += l.count;
         }
@@ -1026,6 +1099,7 @@ lp_status run_set(const std::vector<HostList>& v, size_t first, size_t end, cons
         hipLaunchKernelGGL(orth_small_kernel, dim3(small.total_tiles), dim3(kThreads), lds, s, small, plan);
     }
     if (a.n == 0) return launched("orthogonalisation launch");
+    a.parts = (float*)at;
     auto load_tiles = [](const List& l) { return (l.mp / 64) * (l.np / 64); };
     number(&a, [](const List& l) { return norm_chunks((long long)l.rows * l.cols); });   // (never more than the matrix has tiles)
     hipLaunchKernelGGL(orth_norm_kernel, dim3(a.total_tiles), dim3(kThreads), 0, s, a);
@@ -1036,25 +1110,41 @@ lp_status run_set(const std::vector<HostList>& v, size_t first, size_t end, cons
         const int mt = (l.mp + tile - 1) / tile, nt = (l.np + tile - 1) / tile;
         return half ? mt * (mt + 1) / 2 : mt * nt;
     };
+    auto sort_by = [&](auto&& steps) {
+        std::sort(a.order, a.order + a.n, [&](int i, int j) { return steps(a.l[i]) != steps(a.l[j]) ? steps(a.l[i]) > steps(a.l[j]) : i < j; });
+    };
     auto product = [&](auto what, const Step& step) {
         constexpr Product W = decltype(what)::value;
         constexpr bool half = W == kGram || W == kPoly;
-        std::sort(a.order, a.order + a.n, [&](int i, int j) {
-            const int ki = W == kGram ? a.l[i].np : a.l[i].mp, kj = W == kGram ? a.l[j].np : a.l[j].mp;
-            return ki != kj ? ki > kj : i < j;
-        });
+        sort_by([](const List& l) { return W == kGram ? l.np : l.mp; });
         number(&a, [&](const List& l) { return tiles(l, 128, half); });
-        if (a.total_tiles >= 2 * n_cu) {
+        if (a.total_tiles >= 2 * kUnits) {
             hipLaunchKernelGGL((orth_product_kernel<W, 128, 1>), dim3(grid_of(a)), dim3(256), 0, s, a, step);
-        } else if (a.total_tiles >= n_cu) {
+        } else if (a.total_tiles >= kUnits) {
             hipLaunchKernelGGL((orth_product_kernel<W, 128, 2>), dim3(grid_of(a)), dim3(512), 0, s, a, step);
         } else {
             number(&a, [&](const List& l) { return tiles(l, 64, half); });
             hipLaunchKernelGGL((orth_product_kernel<W, 64, 4>), dim3(grid_of(a)), dim3(512), 0, s, a, step);
         }
     };
+    // A = X X^T: where few tiles have long sums, these are divided among workgroups and joined by a second launch
+    bool divided = false;
+    for (int k = 0; k < a.n; ++k) divided = divided || a.l[k].splits > 1;
+    auto gram_product = [&](const Step& step) {
+        if (!divided) return product(std::integral_constant<Product, kGram>(), step);
+        sort_by([](const List& l) { return std::min(l.chunk, l.np / kDepth); });
+        int at = 0;
+        for (int k = 0; k < a.n; ++k) {
+            a.l[k].first_part = at;
+            at += a.l[k].count * tiles(a.l[k], 64, true) * a.l[k].splits;
+        }
+        number(&a, [&](const List& l) { return tiles(l, 64, true) * l.splits; });
+        hipLaunchKernelGGL((orth_product_kernel<kPart, 64, 4>), dim3(grid_of(a)), dim3(512), 0, s, a, step);
+        number(&a, [&](const List& l) { return tiles(l, 64, true); });
+        hipLaunchKernelGGL((orth_product_kernel<kJoin, 64, 4>), dim3(grid_of(a)), dim3(512), 0, s, a, step);
+    };
     for (int k = 0; k < plan.steps; ++k) {
-        product(std::integral_constant<Product, kGram>(), plan.gram[k]);
+        gram_product(plan.gram[k]);
         product(std::integral_constant<Product, kPoly>(), plan.poly[k]);
         if (k + 1 < plan.steps) product(std::integral_constant<Product, kUpdate>(), plan.update[k]);
         else product(std::integral_constant<Product, kLast>(), plan.update[k]);
@@ -1070,9 +1160,6 @@ lp_status run(const std::vector<HostList>& v, const Plan& plan, float eps, const
     if (need && (!workspace || workspace_bytes < need))
         return fail(LP_ERR_WORKSPACE, "workspace is NULL or smaller than the call's workspace_bytes function says");
     if (need && (uintptr_t)workspace % 256) return fail(LP_ERR_INVALID_ARG, "workspace must be 256-byte aligned");
-    std::string err;
-    int n_cu = 0;
-    if (compute_units(&n_cu, &err)) return fail(LP_ERR_HIP, err);
     // (refused before anything is launched)
     for (size_t k = 0; k < v.size(); k += kMaxLists) {
         double tiles = 0.0;
@@ -1081,7 +1168,7 @@ lp_status run(const std::vector<HostList>& v, const Plan& plan, float eps, const
         if (tiles > (double)kMaxTiles) return fail(LP_ERR_UNSUPPORTED, "too many matrices for one call");
     }
     for (size_t k = 0; k < v.size(); k += kMaxLists) {
-        const lp_status st = run_set(v, k, v.size() < k + kMaxLists ? v.size() : k + kMaxLists, plan, eps, muon, workspace, n_cu, s);
+        const lp_status st = run_set(v, k, v.size() < k + kMaxLists ? v.size() : k + kMaxLists, plan, eps, muon, workspace, s);
         if (st != LP_OK) return st;
     }
     return LP_OK;

@@ -17,6 +17,7 @@
 #include <hip/hip_runtime.h>
 
 #include <algorithm>
+#include <climits>
 #include <cmath>
 #include <cstring>
 #include <type_traits>
@@ -59,16 +60,20 @@ struct List {
     int dtype;
     float step;         // lr s
     int first_matrix;   // index of its first matrix among all
-    int first_tile;     // of the launch
-    int tiles;          // of one matrix
+    int tiles;          // of one matrix, in the launch
     int vec4;           // four neighbours can be read and written at a time
     int splits, chunk;  // kPart: parts of the inner dimension, and their steps
     int first_part;     // its first tile's first part among all
 };
 
 struct Lists {
-    int n, matrices, total_tiles;
+    // In front, in a few lines, what a workgroup looks its list up in (the arguments lie in memory, a line is most of a
+    // microsecond away, and what depends on another line waits for it):
+    int n, total_tiles;
+    int first[kMaxLists];   // of the launch's workgroups, that of the list's first; behind the last list: none's
+    int all[kMaxLists];     // workgroups of the lists, in the order
     int order[kMaxLists];   // of the products: the longest ones first
+    int matrices;
     float lr_decay;     // 1 - lr weight_decay
     float mu;
     int nesterov;
@@ -132,11 +137,15 @@ __device__ __forceinline__ Scale scale_of(double squares, float eps, float load)
 // The list and the matrix of it that `tile` belongs to, and the tile within the matrix.
 __device__ __forceinline__ const List& find(const Lists& a, int tile, int& matrix, int& local)
 {
-    int k = 0;
-    while (k + 1 < a.n && tile >= a.l[k + 1].first_tile) ++k;
-    const int rest = tile - a.l[k].first_tile;
-    matrix = rest / a.l[k].tiles;
-    local = rest - matrix * a.l[k].tiles;
+    int k = 0, from = 0;
+#pragma unroll
+    for (int i = 1; i < kMaxLists; ++i)
+        if (tile >= a.first[i]) {
+            k = i;
+            from = a.first[i];
+        }
+    matrix = (tile - from) / a.l[k].tiles;
+    local = tile - from - matrix * a.l[k].tiles;
     return a.l[k];
 }
 
@@ -144,21 +153,24 @@ __device__ __forceinline__ const List& find(const Lists& a, int tile, int& matri
 // (its L2 holds the operands they share; no XCD is left with the long ones), lists in the launch's order.  False: nothing is left.
 __device__ __forceinline__ bool find_on_xcd(const Lists& a, int block, int& list, int& matrix, int& local)
 {
-    int rest = block >> 3;
-    for (int k = 0; k < a.n; ++k) {
-        const List& l = a.l[a.order[k]];
-        const long long all = (long long)l.tiles * l.count;
+    int rest = block >> 3, index = 0;
+    list = -1;
+#pragma unroll
+    for (int k = 0; k < kMaxLists; ++k) {
         const int part = ((block & 7) + 3 * k) & 7;   // (lists of a few tiles do not all fall to the same XCD)
-        const int from = (int)(all * part >> 3), end = (int)(all * (part + 1) >> 3);
-        if (rest < end - from) {
-            list = a.order[k];
-            matrix = (from + rest) / l.tiles;
-            local = from + rest - matrix * l.tiles;
-            return true;
+        const int from = a.all[k] * part >> 3, end = a.all[k] * (part + 1) >> 3;   // (at most 2^23 tiles)
+        if (list < 0) {
+            if (rest < end - from) {
+                list = a.order[k];
+                index = from + rest;
+            }
+            rest -= end - from;
         }
-        rest -= end - from;
     }
-    return false;
+    if (list < 0) return false;
+    matrix = index / a.l[list].tiles;
+    local = index - matrix * a.l[list].tiles;
+    return true;
 }
 
 // Four neighbouring values from `i` on, of which `left` are there.
@@ -627,10 +639,19 @@ __host__ __device__ inline int small_lds(int mp, int np)
     return 2 * mp * np * 4 + (rest > g ? rest : g);
 }
 
-__global__ __launch_bounds__(kThreads) void orth_small_kernel(Lists a, Plan plan)
+// The steps' scales as this kernel takes them.
+struct SmallPlan {
+    float load;
+    int steps;
+    float v[LP_ORTH_MAX_STEPS][5];   // kGram's, kPoly's three, kUpdate's
+};
+
+__global__ __launch_bounds__(kThreads) void orth_small_kernel(Lists a, SmallPlan plan)
 {
     extern __shared__ char small_bytes[];
     __shared__ double sums[4];
+    __shared__ float scales[LP_ORTH_MAX_STEPS * 5];   // (read once: as arguments every step's would wait for a line of its own)
+    if (threadIdx.x < LP_ORTH_MAX_STEPS * 5) scales[threadIdx.x] = plan.v[threadIdx.x / 5][threadIdx.x % 5];
     int matrix, local;
     const List& l = find(a, blockIdx.x, matrix, local);
     const int m = l.m, n = l.n, mp = pad32(m), np = pad32(n);
@@ -755,24 +776,24 @@ __global__ __launch_bounds__(kThreads) void orth_small_kernel(Lists a, Plan plan
     const int bi = wave >> 1, bj = wave & 1;          // of A and B
     const bool square = bi < mb && bj < mb;
     for (int step = 0; step < plan.steps; ++step) {
+        const float* sc = scales + 5 * step;
         f32x16 gram = {};
         if (square) {
-            gram = product(X, X, np, bi, bj) * plan.gram[step].acc;
+            gram = product(X, X, np, bi, bj) * sc[0];
             put_turned(gram, A, mp, bi, bj);
         }
         __syncthreads();
         if (square) {
-            const Step s = plan.poly[step];
             f32x16 v = product(A, A, mp, bi, bj);
 #pragma unroll
             for (int e = 0; e < 16; ++e) {
                 const int i = bi * 32 + 8 * (e >> 2) + 4 * h + (e & 3), j = bj * 32 + l32;
-                v[e] = fmaf(s.lin, gram[e], v[e] * s.acc) + (i == j && i < m ? s.diag : 0.0f);
+                v[e] = fmaf(sc[3], gram[e], v[e] * sc[1]) + (i == j && i < m ? sc[2] : 0.0f);
             }
             put_turned(v, B, mp, bi, bj);
         }
         __syncthreads();
-        const float scale = plan.update[step].acc;
+        const float scale = sc[4];
         if (step + 1 < plan.steps) {
             f32x16 next[2] = {};
 #pragma unroll
@@ -1013,11 +1034,11 @@ template <class F>
 void number(Lists* a, F&& tiles_of)
 {
     int at = 0;
-    for (int k = 0; k < a->n; ++k) {
-        a->l[k].first_tile = at;
-        a->l[k].tiles = tiles_of(a->l[k]);
-        at += a->l[k].tiles * a->l[k].count;
+    for (int k = 0; k < kMaxLists; ++k) {
+        a->first[k] = k < a->n ? at : INT_MAX;
+        if (k < a->n) at += (a->l[k].tiles = tiles_of(a->l[k])) * a->l[k].count;
     }
+    for (int k = 0; k < kMaxLists; ++k) a->all[k] = k < a->n ? a->l[a->order[k]].tiles * a->l[a->order[k]].count : 0;
     a->total_tiles = at;
 }
 
@@ -1028,9 +1049,8 @@ unsigned grid_of(const Lists& a)
     for (int x = 0; x < 8; ++x) {
         int sum = 0;
         for (int k = 0; k < a.n; ++k) {
-            const long long all = (long long)a.l[a.order[k]].tiles * a.l[a.order[k]].count;
             const int part = (x + 3 * k) & 7;
-            sum += (int)((all * (part + 1) >> 3) - (all * part >> 3));
+            sum += (a.all[k] * (part + 1) >> 3) - (a.all[k] * part >> 3);
         }
         most = sum > most ? sum : most;
     }
@@ -1064,7 +1084,9 @@ lp_status run_set(const std::vector<HostList>& v, size_t first, size_t end, cons
     for (size_t k = first; k < end; ++k) {
         const HostList& q = v[k];
         const bool is = is_small(q.rows, q.cols);
-        List& l = is ? small.l[small.n++] : a.l[a.n++];
+        List& l = is ? small.l[small.n] : a.l[a.n];
+        (is ? small.order[small.n] : a.order[a.n]) = is ? small.n : a.n;
+        ++(is ? small.n : a.n);
         l.in = q.in; l.out = q.out; l.momentum = q.momentum; l.dtype = q.dtype;
         l.count = (int)q.count; l.rows = q.rows; l.cols = q.cols;
         l.tall = q.rows > q.cols;
@@ -1079,7 +1101,6 @@ lp_status run_set(const std::vector<HostList>& v, size_t first, size_t end, cons
             l.ws_stride = (long long)align256(matrix_halves(q.rows, q.cols) * 2) / 2;
             at += (size_t)l.ws_stride * 2 * q.count;
             l.vec4 = (long long)q.rows * q.cols % 4 == 0 && (uintptr_t)q.in % 16 == 0 && (uintptr_t)q.momentum % 16 == 0;
-            a.order[a.n - 1] = a.n - 1;
             l.splits = gram.splits[k - first];
             l.chunk = gram.chunk;
             l.first_matrix = a.matrices;
@@ -1096,7 +1117,15 @@ lp_status run_set(const std::vector<HostList>& v, size_t first, size_t end, cons
         number(&small, [](const List&) { return 1; });
         const hipError_t e = hipFuncSetAttribute((const void*)orth_small_kernel, hipFuncAttributeMaxDynamicSharedMemorySize, lds);
         if (e != hipSuccess) return fail(LP_ERR_HIP, std::string("hipFuncSetAttribute(orth_small_kernel): ") + hipGetErrorString(e));
-        hipLaunchKernelGGL(orth_small_kernel, dim3(small.total_tiles), dim3(kThreads), lds, s, small, plan);
+        SmallPlan sp;
+        std::memset(&sp, 0, sizeof(sp));
+        sp.load = plan.load;
+        sp.steps = plan.steps;
+        for (int k = 0; k < plan.steps; ++k) {
+            const float v[5] = {plan.gram[k].acc, plan.poly[k].acc, plan.poly[k].diag, plan.poly[k].lin, plan.update[k].acc};
+            std::memcpy(sp.v[k], v, sizeof(v));
+        }
+        hipLaunchKernelGGL(orth_small_kernel, dim3(small.total_tiles), dim3(kThreads), lds, s, small, sp);
     }
     if (a.n == 0) return launched("orthogonalisation launch");
     a.parts = (float*)at;

@@ -639,6 +639,144 @@ __host__ __device__ inline int small_lds(int mp, int np)
     return 2 * mp * np * 4 + (rest > g ? rest : g);
 }
 
+// Block (bi, bj) of P Q^T over 16 K16 columns.
+template <int K16>
+__device__ __forceinline__ f32x16 small_product(const _Float16* p, const _Float16* q, int bi, int bj)
+{
+    const int lane = threadIdx.x & 63;
+    f32x16 acc = {}, cross = {};
+    const _Float16* pb = p + bi * K16 * kBlock + lane * 8;
+    const _Float16* qb = q + bj * K16 * kBlock + lane * 8;
+#pragma unroll
+    for (int k = 0; k < K16; ++k) {
+        const half8 ph = *(const half8*)(pb + k * kBlock), pl = *(const half8*)(pb + k * kBlock + 512);
+        const half8 qh = *(const half8*)(qb + k * kBlock), ql = *(const half8*)(qb + k * kBlock + 512);
+        acc = __builtin_amdgcn_mfma_f32_32x32x16_f16(ph, qh, acc, 0, 0, 0);
+        cross = __builtin_amdgcn_mfma_f32_32x32x16_f16(pl, qh, cross, 0, 0, 0);
+        cross = __builtin_amdgcn_mfma_f32_32x32x16_f16(ph, ql, cross, 0, 0, 0);
+    }
+    return acc + cross;
+}
+
+// The steps of a matrix of MB x NB blocks of 32 x 32 (sizes are constants: at one wave a SIMD every index that is worked out
+// between two barriers is waited for), and the result.
+template <int MB, int NB>
+__device__ __forceinline__ void small_steps(const Lists& a, const List& l, int n_steps, const float* scales, _Float16* X, _Float16* XT,
+                                            _Float16* B, _Float16* A, size_t from)
+{
+    constexpr int kPer = (MB * NB + 3) / 4;   // blocks of X that a wave has, at most
+    const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), lane = threadIdx.x & 63, l32 = lane & 31, h = lane >> 5;
+    uint32_t* turn = (uint32_t*)A + wave * (32 * 33);
+    const int bi = wave >> 1, bj = wave & 1;   // of A and B
+    const bool square = bi < MB && bj < MB;
+    int xi[kPer], xj[kPer];
+#pragma unroll
+    for (int u = 0; u < kPer; ++u) {
+        xi[u] = (wave + 4 * u) / NB;
+        xj[u] = (wave + 4 * u) % NB;
+    }
+    // block (bi, bj) as block (bj, bi) of an operand of 32 W columns: a lane's four rows are neighbours there
+    auto put_turned = [&](const half4 (&hi)[4], const half4 (&lo)[4], _Float16* to, int W, int rb, int cb) {
+        _Float16* dst = to + (cb * 2 * W + rb * 2) * kBlock + l32 * 8 + 4 * h;
+#pragma unroll
+        for (int e4 = 0; e4 < 4; ++e4) {   // rows 8 e4 + 4 h ..: block e4 / 2, its half e4 % 2
+            *(half4*)(dst + (e4 >> 1) * kBlock + (e4 & 1) * 256) = hi[e4];
+            *(half4*)(dst + (e4 >> 1) * kBlock + (e4 & 1) * 256 + 512) = lo[e4];
+        }
+    };
+    auto split16 = [&](const f32x16& v, half4 (&hi)[4], half4 (&lo)[4]) {
+#pragma unroll
+        for (int e4 = 0; e4 < 4; ++e4) split4(f32x4{v[4 * e4], v[4 * e4 + 1], v[4 * e4 + 2], v[4 * e4 + 3]}, hi[e4], lo[e4]);
+    };
+    half4 hi[4], lo[4];
+#pragma unroll 1
+    for (int step = 0; step < n_steps; ++step) {
+        const float s_gram = scales[5 * step], s_poly = scales[5 * step + 1], s_diag = scales[5 * step + 2], s_lin = scales[5 * step + 3],
+                    s_update = scales[5 * step + 4];
+        f32x16 gram = {};
+        if (square) {
+            gram = small_product<2 * NB>(X, X, bi, bj) * s_gram;
+            split16(gram, hi, lo);
+            put_turned(hi, lo, A, MB, bi, bj);
+        }
+        __syncthreads();
+        if (square) {
+            f32x16 v = small_product<2 * MB>(A, A, bi, bj);
+#pragma unroll
+            for (int e = 0; e < 16; ++e) {
+                const int i = bi * 32 + 8 * (e >> 2) + 4 * h + (e & 3), j = bj * 32 + l32;
+                v[e] = fmaf(s_lin, gram[e], v[e] * s_poly) + (i == j && i < l.m ? s_diag : 0.0f);
+            }
+            split16(v, hi, lo);
+            put_turned(hi, lo, B, MB, bi, bj);
+        }
+        __syncthreads();
+        if (step + 1 < n_steps) {
+            f32x16 next[kPer];
+#pragma unroll
+            for (int u = 0; u < kPer; ++u)
+                if (wave + 4 * u < MB * NB) next[u] = small_product<2 * MB>(B, XT, xi[u], xj[u]) * s_update;
+            __syncthreads();
+#pragma unroll
+            for (int u = 0; u < kPer; ++u) {
+                if (wave + 4 * u >= MB * NB) continue;
+                split16(next[u], hi, lo);
+                put_turned(hi, lo, XT, MB, xi[u], xj[u]);
+#pragma unroll
+                for (int e = 0; e < 16; ++e)
+                    turn[(8 * (e >> 2) + 4 * h + (e & 3)) * 33 + l32] = (uint32_t)__builtin_bit_cast(uint16_t, (_Float16)hi[e >> 2][e & 3]) |
+                                                                        (uint32_t)__builtin_bit_cast(uint16_t, (_Float16)lo[e >> 2][e & 3]) << 16;
+                wave_lds_fence();
+#pragma unroll
+                for (int k = 0; k < 2; ++k) {
+                    half8 rh, rl;
+#pragma unroll
+                    for (int e = 0; e < 8; ++e) {
+                        const uint32_t v = turn[l32 * 33 + k * 16 + h * 8 + e];
+                        rh[e] = __builtin_bit_cast(_Float16, (uint16_t)v);
+                        rl[e] = __builtin_bit_cast(_Float16, (uint16_t)(v >> 16));
+                    }
+                    _Float16* dst = X + (xi[u] * 2 * NB + xj[u] * 2 + k) * kBlock + lane * 8;
+                    *(half8*)dst = rh;
+                    *(half8*)(dst + 512) = rl;
+                }
+                wave_lds_fence();
+            }
+            __syncthreads();
+        } else {
+            // the result in G's order: of a tall G the transposed product, so that neighbouring lanes have neighbouring columns
+            const _Float16 *p = l.tall ? XT : B, *q = l.tall ? B : XT;
+#pragma unroll 1
+            for (int u = wave; u < MB * NB; u += 4) {
+                const int x0 = u / NB, x1 = u % NB, ri = l.tall ? x1 : x0, ci = l.tall ? x0 : x1, rb = ri * 32, c = ci * 32 + l32;
+                const f32x16 v = small_product<2 * MB>(p, q, ri, ci) * s_update;
+                auto each = [&](auto&& f) {   // (offsets from the matrix's start: 32 bits)
+#pragma unroll
+                    for (int e = 0; e < 16; ++e) {
+                        const int r = rb + 8 * (e >> 2) + 4 * h + (e & 3);
+                        if (r < l.rows && c < l.cols) f(e, (unsigned)(r * l.cols + c));
+                    }
+                };
+                if (l.momentum) {
+                    float* to = (float*)l.out + from;
+                    float w[16];
+                    each([&](int e, unsigned i) { w[e] = to[i]; });
+                    each([&](int e, unsigned i) { to[i] = fmaf(-l.step, v[e], a.lr_decay * w[e]); });
+                } else if (l.dtype == LP_F32) {
+                    float* to = (float*)l.out + from;
+                    each([&](int e, unsigned i) { to[i] = v[e]; });
+                } else if (l.dtype == LP_BF16) {
+                    __bf16* to = (__bf16*)l.out + from;
+                    each([&](int e, unsigned i) { to[i] = (__bf16)v[e]; });
+                } else {
+                    _Float16* to = (_Float16*)l.out + from;
+                    each([&](int e, unsigned i) { to[i] = (_Float16)v[e]; });
+                }
+            }
+        }
+    }
+}
+
 // The steps' scales as this kernel takes them.
 struct SmallPlan {
     float load;
@@ -661,7 +799,6 @@ __global__ __launch_bounds__(kThreads) void orth_small_kernel(Lists a, SmallPlan
     _Float16* A = B + 2 * mp * mp;
     float* g = (float*)B;   // [mp][np + 1], X's order
     const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), lane = threadIdx.x & 63, l32 = lane & 31, h = lane >> 5;
-    uint32_t* turn = (uint32_t*)A + wave * (32 * 33);
     const size_t from = (size_t)matrix * l.rows * l.cols;
     // G: a thread has four columns of every kPasses-th group of rows
     constexpr int kPasses = kSmallM * kSmallN / (4 * kThreads);
@@ -734,136 +871,14 @@ __global__ __launch_bounds__(kThreads) void orth_small_kernel(Lists a, SmallPlan
         }
     }
     __syncthreads();
-    // block (bi, bj) of P Q^T over K columns, 64 at a time (the operands of all of them are asked for before the first product)
-    auto product = [&](const _Float16* p, const _Float16* q, int K, int bi, int bj) {
-        f32x16 acc = {}, cross = {};
-        const _Float16* pb = p + bi * (K >> 4) * kBlock + lane * 8;
-        const _Float16* qb = q + bj * (K >> 4) * kBlock + lane * 8;
-#pragma unroll 1
-        for (int k = 0; k < K >> 4; k += 4) {
-            const int n_k = min(4, (K >> 4) - k);   // 4 or 2
-            half8 ph[4], pl[4], qh[4], ql[4];
-#pragma unroll
-            for (int u = 0; u < 4; ++u) {
-                if (u >= n_k) break;
-                ph[u] = *(const half8*)(pb + (k + u) * kBlock);
-                qh[u] = *(const half8*)(qb + (k + u) * kBlock);
-                pl[u] = *(const half8*)(pb + (k + u) * kBlock + 512);
-                ql[u] = *(const half8*)(qb + (k + u) * kBlock + 512);
-            }
-#pragma unroll
-            for (int u = 0; u < 4; ++u) {
-                if (u >= n_k) break;
-                acc = __builtin_amdgcn_mfma_f32_32x32x16_f16(ph[u], qh[u], acc, 0, 0, 0);
-                cross = __builtin_amdgcn_mfma_f32_32x32x16_f16(pl[u], qh[u], cross, 0, 0, 0);
-                cross = __builtin_amdgcn_mfma_f32_32x32x16_f16(ph[u], ql[u], cross, 0, 0, 0);
-            }
-        }
-        return acc + cross;
-    };
-    // block (bi, bj) as block (bj, bi) of an operand of `width` columns: a lane's four rows are neighbours there
-    auto put_turned = [&](const f32x16& v, _Float16* to, int width, int bi, int bj) {
-#pragma unroll
-        for (int e4 = 0; e4 < 4; ++e4) {
-            half4 hi, lo;
-            split4(f32x4{v[4 * e4], v[4 * e4 + 1], v[4 * e4 + 2], v[4 * e4 + 3]}, hi, lo);
-            _Float16* dst = to + at(bj * 32 + l32, bi * 32 + 8 * e4 + 4 * h, width);
-            *(half4*)dst = hi;
-            *(half4*)(dst + 512) = lo;
-        }
-    };
-    const int mb = mp >> 5, nb = np >> 5;
-    const int bi = wave >> 1, bj = wave & 1;          // of A and B
-    const bool square = bi < mb && bj < mb;
-    for (int step = 0; step < plan.steps; ++step) {
-        const float* sc = scales + 5 * step;
-        f32x16 gram = {};
-        if (square) {
-            gram = product(X, X, np, bi, bj) * sc[0];
-            put_turned(gram, A, mp, bi, bj);
-        }
-        __syncthreads();
-        if (square) {
-            f32x16 v = product(A, A, mp, bi, bj);
-#pragma unroll
-            for (int e = 0; e < 16; ++e) {
-                const int i = bi * 32 + 8 * (e >> 2) + 4 * h + (e & 3), j = bj * 32 + l32;
-                v[e] = fmaf(sc[3], gram[e], v[e] * sc[1]) + (i == j && i < m ? sc[2] : 0.0f);
-            }
-            put_turned(v, B, mp, bi, bj);
-        }
-        __syncthreads();
-        const float scale = sc[4];
-        if (step + 1 < plan.steps) {
-            f32x16 next[2] = {};
-#pragma unroll
-            for (int u = 0; u < 2; ++u)
-                if (wave + 4 * u < mb * nb) next[u] = product(B, XT, mp, (wave + 4 * u) / nb, (wave + 4 * u) % nb) * scale;
-            __syncthreads();
-#pragma unroll
-            for (int u = 0; u < 2; ++u) {
-                if (wave + 4 * u >= mb * nb) continue;
-                const int xi = (wave + 4 * u) / nb, xj = (wave + 4 * u) % nb;
-#pragma unroll
-                for (int e4 = 0; e4 < 4; ++e4) {
-                    half4 hi, lo;
-                    split4(f32x4{next[u][4 * e4], next[u][4 * e4 + 1], next[u][4 * e4 + 2], next[u][4 * e4 + 3]}, hi, lo);
-                    _Float16* dst = XT + at(xj * 32 + l32, xi * 32 + 8 * e4 + 4 * h, mp);
-                    *(half4*)dst = hi;
-                    *(half4*)(dst + 512) = lo;
-#pragma unroll
-                    for (int e = 0; e < 4; ++e)
-                        turn[(8 * e4 + 4 * h + e) * 33 + l32] =
-                            (uint32_t)__builtin_bit_cast(uint16_t, (_Float16)hi[e]) | (uint32_t)__builtin_bit_cast(uint16_t, (_Float16)lo[e]) << 16;
-                }
-                wave_lds_fence();
-#pragma unroll
-                for (int k = 0; k < 2; ++k) {
-                    half8 hi, lo;
-#pragma unroll
-                    for (int e = 0; e < 8; ++e) {
-                        const uint32_t v = turn[l32 * 33 + k * 16 + h * 8 + e];
-                        hi[e] = __builtin_bit_cast(_Float16, (uint16_t)v);
-                        lo[e] = __builtin_bit_cast(_Float16, (uint16_t)(v >> 16));
-                    }
-                    _Float16* dst = X + at(xi * 32 + l32, xj * 32 + k * 16 + h * 8, np);
-                    *(half8*)dst = hi;
-                    *(half8*)(dst + 512) = lo;
-                }
-                wave_lds_fence();
-            }
-            __syncthreads();
-        } else {
-            // the result in G's order: of a tall G the transposed product, so that neighbouring lanes have neighbouring columns
-            const int cb = l.tall ? mb : nb;
-#pragma unroll 1
-            for (int u = wave; u < mb * nb; u += 4) {
-                const int ri = u / cb, ci = u % cb, rb = ri * 32, c = ci * 32 + l32;
-                f32x16 v = product(l.tall ? XT : B, l.tall ? B : XT, mp, ri, ci);
-                auto each = [&](auto&& f) {   // (offsets from the matrix's start: 32 bits)
-#pragma unroll
-                    for (int e = 0; e < 16; ++e) {
-                        const int r = rb + 8 * (e >> 2) + 4 * h + (e & 3);
-                        if (r < l.rows && c < l.cols) f(e, (unsigned)(r * l.cols + c));
-                    }
-                };
-                if (l.momentum) {
-                    float* to = (float*)l.out + from;
-                    float w[16];
-                    each([&](int e, unsigned i) { w[e] = to[i]; });
-                    each([&](int e, unsigned i) { to[i] = fmaf(-l.step, v[e] * scale, a.lr_decay * w[e]); });
-                } else if (l.dtype == LP_F32) {
-                    float* to = (float*)l.out + from;
-                    each([&](int e, unsigned i) { to[i] = v[e] * scale; });
-                } else if (l.dtype == LP_BF16) {
-                    __bf16* to = (__bf16*)l.out + from;
-                    each([&](int e, unsigned i) { to[i] = (__bf16)(v[e] * scale); });
-                } else {
-                    _Float16* to = (_Float16*)l.out + from;
-                    each([&](int e, unsigned i) { to[i] = (_Float16)(v[e] * scale); });
-                }
-            }
-        }
+    switch (mp / 32 * 4 + np / 32) {
+        case 4 + 1: small_steps<1, 1>(a, l, plan.steps, scales, X, XT, B, A, from); break;
+        case 4 + 2: small_steps<1, 2>(a, l, plan.steps, scales, X, XT, B, A, from); break;
+        case 4 + 3: small_steps<1, 3>(a, l, plan.steps, scales, X, XT, B, A, from); break;
+        case 4 + 4: small_steps<1, 4>(a, l, plan.steps, scales, X, XT, B, A, from); break;
+        case 8 + 2: small_steps<2, 2>(a, l, plan.steps, scales, X, XT, B, A, from); break;
+        case 8 + 3: small_steps<2, 3>(a, l, plan.steps, scales, X, XT, B, A, from); break;
+        case 8 + 4: small_steps<2, 4>(a, l, plan.steps, scales, X, XT, B, A, from); break;
     }
 }
 

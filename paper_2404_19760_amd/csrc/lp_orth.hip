@@ -1149,7 +1149,6 @@ lp_status run_set(const std::vector<HostList>& v, size_t first, size_t end, cons
     hipLaunchKernelGGL(orth_norm_kernel, dim3(a.total_tiles), dim3(kThreads), 0, s, a);
     number(&a, load_tiles);
     hipLaunchKernelGGL(orth_load_kernel, dim3(a.total_tiles), dim3(kThreads), 0, s, a, plan.load);
-    // large tiles where they give every compute unit work
     auto tiles = [](const List& l, int tile, bool half) {
         const int mt = (l.mp + tile - 1) / tile, nt = (l.np + tile - 1) / tile;
         return half ? mt * (mt + 1) / 2 : mt * nt;
@@ -1162,14 +1161,21 @@ lp_status run_set(const std::vector<HostList>& v, size_t first, size_t end, cons
         constexpr bool half = W == kGram || W == kPoly;
         sort_by([](const List& l) { return W == kGram ? l.np : l.mp; });
         number(&a, [&](const List& l) { return tiles(l, 128, half); });
-        if (a.total_tiles >= 2 * kUnits) {
+        // Large tiles where they give every compute unit work.  Two small workgroups a unit overlap one's ends with the other's
+        // products (B X of 340 tiles with sums of 64 .. 256: 19 us, in one large workgroup a unit 24, in 64 x 64 tiles 34); the long
+        // sums of A = X X^T are better halved inside a workgroup while there are fewer than two a unit (308 tiles: 104 and 130 us).
+        if (a.total_tiles >= (W == kGram ? 2 : 1) * kUnits) {
             hipLaunchKernelGGL((orth_product_kernel<W, 128, 1>), dim3(grid_of(a)), dim3(256), 0, s, a, step);
-        } else if (a.total_tiles >= kUnits) {
-            hipLaunchKernelGGL((orth_product_kernel<W, 128, 2>), dim3(grid_of(a)), dim3(512), 0, s, a, step);
-        } else {
-            number(&a, [&](const List& l) { return tiles(l, 64, half); });
-            hipLaunchKernelGGL((orth_product_kernel<W, 64, 4>), dim3(grid_of(a)), dim3(512), 0, s, a, step);
+            return;
         }
+        if constexpr (W == kGram) {
+            if (a.total_tiles >= kUnits) {
+                hipLaunchKernelGGL((orth_product_kernel<W, 128, 2>), dim3(grid_of(a)), dim3(512), 0, s, a, step);
+                return;
+            }
+        }
+        number(&a, [&](const List& l) { return tiles(l, 64, half); });
+        hipLaunchKernelGGL((orth_product_kernel<W, 64, 4>), dim3(grid_of(a)), dim3(512), 0, s, a, step);
     };
     // A = X X^T: where few tiles have long sums, these are divided among workgroups and joined by a second launch
     bool divided = false;

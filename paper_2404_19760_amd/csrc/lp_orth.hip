@@ -398,18 +398,18 @@ __global__ __launch_bounds__((ProductShape<TILE, GROUPS>::kThreadsOf), (2)) void
     }
     q_at = q + min(tj * F + wave, q_blocks - 1) * row;
     char* buffers = lds + group * 2 * S::kBuffer;
-    half8 staged[kLoads];
+    half8 staged[2][kLoads];   // P of two steps
     half8 qv[4][2];   // Q of two steps: 16-column half of a step, hi or lo
-    auto ask_p = [&](int step) {
+    auto ask_p = [&](int step, half8 (&v)[kLoads]) {
         step = min(start + step, all - 1);
 #pragma unroll
-        for (int u = 0; u < kLoads; ++u) staged[u] = *(const half8*)(p_at[u] + (size_t)step * (2 * kBlock) + in_group * 8);
+        for (int u = 0; u < kLoads; ++u) v[u] = *(const half8*)(p_at[u] + (size_t)step * (2 * kBlock) + in_group * 8);
     };
-    auto put_p = [&](int buffer, bool any) {
+    auto put_p = [&](int buffer, bool any, const half8 (&v)[kLoads]) {
         char* to = buffers + buffer * S::kBuffer + in_group * 16;
         if (any) {
 #pragma unroll
-            for (int u = 0; u < kLoads; ++u) *(half8*)(to + u * S::kGroupThreads * 16) = staged[u];
+            for (int u = 0; u < kLoads; ++u) *(half8*)(to + u * S::kGroupThreads * 16) = v[u];
         } else {
 #pragma unroll
             for (int u = 0; u < kLoads; ++u) *(half8*)(to + u * S::kGroupThreads * 16) = half8{};
@@ -426,11 +426,12 @@ __global__ __launch_bounds__((ProductShape<TILE, GROUPS>::kThreadsOf), (2)) void
         for (int c = 0; c < 2; ++c) pv[f][c] = *(const half8*)(buffers + buffer * S::kBuffer + f * 4096 + (2 * k + c) * 1024 + lane * 16);
     };
     f32x16 acc[F] = {}, cross[F] = {};
-    ask_p(0);
+    ask_p(0, staged[0]);
 #pragma unroll
     for (int k = 0; k < 4; ++k) ask_q(k, qv[k]);
-    put_p(0, mine_steps > 0);
-    ask_p(1);
+    put_p(0, mine_steps > 0, staged[0]);
+    ask_p(1, staged[1]);
+    ask_p(2, staged[0]);
     __syncthreads();
 #pragma unroll
     for (int f = 0; f < F; ++f) get_p(0, 0, f);
@@ -438,8 +439,8 @@ __global__ __launch_bounds__((ProductShape<TILE, GROUPS>::kThreadsOf), (2)) void
 #pragma unroll
         for (int u = 0; u < 2; ++u) {
             const int step = first + u;
-            put_p(u ^ 1, step + 1 < mine_steps);   // (behind the last step P is zero: what is left of the loop adds nothing)
-            ask_p(step + 2);
+            put_p(u ^ 1, step + 1 < mine_steps, staged[u ^ 1]);   // (behind the last step P is zero: what is left of the loop adds nothing)
+            ask_p(step + 3, staged[u ^ 1]);
             __builtin_amdgcn_sched_barrier(0);     // (everything is asked for and used in the order written)
 #pragma unroll
             for (int k = 0; k < 2; ++k) {
@@ -821,8 +822,10 @@ __global__ __launch_bounds__(kThreads) void orth_small_kernel(Lists a, SmallPlan
             if (r < l.rows && left > 0) v[k] = load4(l.in, from + r * l.cols + c0, l.dtype, vec4, left);
         }
     }
-    for (int i = threadIdx.x; i < mp * (np + 1); i += kThreads) g[i] = 0.0f;
-    __syncthreads();
+    if (m != mp || n != np) {   // (rows and columns behind the matrix's)
+        for (int i = threadIdx.x; i < mp * (np + 1); i += kThreads) g[i] = 0.0f;
+        __syncthreads();
+    }
     double norm = 0.0;
 #pragma unroll
     for (int k = 0; k < kPasses; ++k) {

@@ -89,13 +89,6 @@ __device__ __forceinline__ float load_value(const void* p, size_t i, int dtype)
     if (dtype == LP_BF16) return (float)((const __bf16*)p)[i];
     return (float)((const _Float16*)p)[i];
 }
-__device__ __forceinline__ void store_value(void* p, size_t i, int dtype, float v)
-{
-    if (dtype == LP_F32) ((float*)p)[i] = v;
-    else if (dtype == LP_BF16) ((__bf16*)p)[i] = (__bf16)v;
-    else ((_Float16*)p)[i] = (_Float16)v;
-}
-
 __device__ __forceinline__ void split(float v, _Float16& hi, _Float16& lo)
 {
     hi = (_Float16)v;
@@ -513,17 +506,35 @@ __global__ __launch_bounds__((ProductShape<TILE, GROUPS>::kThreadsOf), (2)) void
     constexpr int kFinish = S::kMine >= 16 ? S::kMine / 16 : 1;
     uint32_t* turn = (uint32_t*)lds + wave_of_8 * (32 * 33);
     const int jb = tj * TILE + wave * 32;
+    if constexpr (WHAT == kLast) {
+        // Row by row of G's order: of a tall G neighbouring lanes take neighbouring block rows.  Value e of a lane lies dr(e) rows
+        // behind its first one.  All weights are read before the first is written: a read behind a write would wait for it.
+        constexpr int kOut = kRows / 2;
+        auto dr = [&](int e) { return l.tall ? e * (64 / kRows) : 8 * (e >> 2) + (e & 3); };
+        auto first_row = [&](int ib) { return l.tall ? jb + lane / kRows : ib + 4 * h; };
+        auto column = [&](int ib) { return l.tall ? ib + (lane & (kRows - 1)) : jb + l32; };
+        auto place = [&](int ib) { return ((size_t)matrix * l.rows + first_row(ib)) * l.cols + column(ib); };
+        float old[kFinish][kOut];
+        if (l.momentum) {
 #pragma unroll
-    for (int fi = 0; fi < kFinish; ++fi) {
-        const int ib = ti * TILE + (group * kFinish + fi) * kRows;
-        if ((ib >> 5) >= p_blocks || (jb >> 5) >= q_blocks) continue;
-        if (WHAT == kLast) {
-            const size_t from = (size_t)matrix * l.rows * l.cols;
-            constexpr int kOut = kRows / 2;
+            for (int fi = 0; fi < kFinish; ++fi) {
+                const int ib = ti * TILE + (group * kFinish + fi) * kRows;
+                const float* w = (const float*)l.out + place(ib);
+                const int r = first_row(ib);
+                const bool in = column(ib) < l.cols;
+#pragma unroll
+                for (int e = 0; e < kOut; ++e)
+                    if (in && r + dr(e) < l.rows) old[fi][e] = w[(size_t)dr(e) * l.cols];
+            }
+        }
+#pragma unroll
+        for (int fi = 0; fi < kFinish; ++fi) {
+            const int ib = ti * TILE + (group * kFinish + fi) * kRows;
+            if ((ib >> 5) >= p_blocks || (jb >> 5) >= q_blocks) continue;
             float v[kOut];
 #pragma unroll
             for (int e = 0; e < kOut; ++e) v[e] = mine[fi * 16 + e] * s.acc;
-            if (l.tall) {   // the result's rows are the block's columns: neighbouring lanes take neighbouring block rows
+            if (l.tall) {
 #pragma unroll
                 for (int e = 0; e < kOut; ++e) turn[(8 * (e >> 2) + 4 * h + (e & 3)) * 33 + l32] = __float_as_uint(v[e]);
                 wave_lds_fence();
@@ -531,37 +542,34 @@ __global__ __launch_bounds__((ProductShape<TILE, GROUPS>::kThreadsOf), (2)) void
                 for (int e = 0; e < kOut; ++e) v[e] = __uint_as_float(turn[(lane & (kRows - 1)) * 33 + e * (64 / kRows) + lane / kRows]);
                 wave_lds_fence();
             }
-            auto place = [&](int e, bool& in) {
-                const int r = l.tall ? jb + e * (64 / kRows) + lane / kRows : ib + 8 * (e >> 2) + 4 * h + (e & 3);
-                const int c = l.tall ? ib + (lane & (kRows - 1)) : jb + l32;
-                in = r < l.rows && c < l.cols;
-                return from + (size_t)r * l.cols + c;
+            const size_t at_first = place(ib);
+            const int r = first_row(ib);
+            const bool in = column(ib) < l.cols;
+            auto each = [&](auto&& f) {
+#pragma unroll
+                for (int e = 0; e < kOut; ++e)
+                    if (in && r + dr(e) < l.rows) f(e, (size_t)dr(e) * l.cols);
             };
-            if (l.momentum) {   // (all weights are read before the first is written)
-                float* w = (float*)l.out;
-                float old[kOut];
-#pragma unroll
-                for (int e = 0; e < kOut; ++e) {
-                    bool in;
-                    const size_t i = place(e, in);
-                    old[e] = in ? w[i] : 0.0f;
-                }
-#pragma unroll
-                for (int e = 0; e < kOut; ++e) {
-                    bool in;
-                    const size_t i = place(e, in);
-                    if (in) w[i] = fmaf(-l.step, v[e], a.lr_decay * old[e]);
-                }
+            if (l.momentum) {
+                float* w = (float*)l.out + at_first;
+                each([&](int e, size_t i) { w[i] = fmaf(-l.step, v[e], a.lr_decay * old[fi][e]); });
+            } else if (l.dtype == LP_F32) {
+                float* to = (float*)l.out + at_first;
+                each([&](int e, size_t i) { to[i] = v[e]; });
+            } else if (l.dtype == LP_BF16) {
+                __bf16* to = (__bf16*)l.out + at_first;
+                each([&](int e, size_t i) { to[i] = (__bf16)v[e]; });
             } else {
-#pragma unroll
-                for (int e = 0; e < kOut; ++e) {
-                    bool in;
-                    const size_t i = place(e, in);
-                    if (in) store_value(l.out, i, l.dtype, v[e]);
-                }
+                _Float16* to = (_Float16*)l.out + at_first;
+                each([&](int e, size_t i) { to[i] = (_Float16)v[e]; });
             }
-            continue;
         }
+        return;
+    }
+#pragma unroll
+    for (int fi = 0; fi < kFinish; ++fi) {
+        const int ib = ti * TILE + (group * kFinish + fi) * kRows;
+        if ((ib >> 5) >= p_blocks || (jb >> 5) >= q_blocks) continue;
         _Float16* direct = kGramLike ? A : WHAT == kPoly ? B : ws + s.to * 2 * plane;
         _Float16* trans = WHAT == kUpdate ? direct + plane : direct;
         const int width = WHAT == kUpdate ? l.np : l.mp;

@@ -937,11 +937,15 @@ def group_norm_fwd(norm: GroupNorm, x: torch.Tensor, dtype=None):
 
 def group_norm_bwd(norm: GroupNorm, x: torch.Tensor, stats: torch.Tensor, d_y: torch.Tensor):
     """Allocate gradients and workspace and run lp_group_norm_bwd.  Returns (d_x, d_gamma, d_beta)."""
-    d_x = torch.empty_strided(x.shape, x.stride(), dtype=x.dtype, device=x.device)
-    d_gamma, d_beta = torch.zeros((2, x.shape[-1]), dtype=torch.float32, device=x.device)
-    n = lp_group_norm_workspace_bytes(norm, x, d_y.dtype)[1]
-    ws = torch.empty(n, dtype=torch.uint8, device=x.device) if n else None
-    lp_group_norm_bwd(norm, x, stats, d_y, d_x, d_gamma, d_beta, ws)
+    q = norm.c_struct(x, d_y.dtype, _channel_last(d_y, "d_y", x.shape, d_y.dtype))
+    d_x = torch.empty_like(x) if x.is_contiguous() else torch.empty_strided(x.shape, x.stride(), dtype=x.dtype, device=x.device)
+    d_params = torch.zeros((2, q.C), dtype=torch.float32, device=x.device)
+    at = d_params.data_ptr()
+    n = _norm_bytes(q)[1]
+    ws = torch.empty(n, dtype=torch.uint8, device=x.device).data_ptr() if n else None
+    _check(_lib.lp_group_norm_bwd(C.byref(q), x.data_ptr(), _dev_f32(stats, "stats", (q.N, q.G, 2)), d_y.data_ptr(), d_x.data_ptr(),
+                                  at, at + 4 * q.C, ws, n, _stream_ptr(None)))
+    d_gamma, d_beta = d_params.unbind(0)
     return d_x, d_gamma, d_beta
 
 

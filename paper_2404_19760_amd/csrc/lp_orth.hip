@@ -60,28 +60,35 @@ struct List {
     int dtype;
     float step;         // lr s
     int first_matrix;   // index of its first matrix among all
-    int tiles;          // of one matrix, in the launch
     int vec4;           // four neighbours can be read and written at a time
     int splits, chunk;  // kPart: parts of the inner dimension, and their steps
     int first_part;     // its first tile's first part among all
 };
 
-struct Lists {
-    // In front, in a few lines, what a workgroup looks its list up in (the arguments lie in memory, a line is most of a
-    // microsecond away, and what depends on another line waits for it):
-    int n, total_tiles;
-    int first[kMaxLists];   // of the launch's workgroups, that of the list's first; behind the last list: none's
-    int all[kMaxLists];     // workgroups of the lists, in the order
+// How a launch's workgroups are numbered.
+struct Launch {
+    int total;
+    int tiles[kMaxLists];   // of one matrix of a list
     int order[kMaxLists];   // of the products: the longest ones first
-    int matrices;
+    int all[kMaxLists];     // of the products: workgroups of the lists, in the order; else the lists' first ones (behind the last: INT_MAX)
+};
+enum LaunchOf { kOfNorm, kOfLoad, kOfGram, kOfJoin, kOfPoly, kOfUpdate, kLaunches };
+
+// All that the launches of a call go by.  The first kernel has it as its argument and leaves it in the workspace, where the others
+// read it: kernel arguments of 3 KB took the host 7 us a launch.
+struct Lists {
+    int n, matrices;
     float lr_decay;     // 1 - lr weight_decay
     float mu;
     int nesterov;
     float eps;
     double* norms;      // [matrices][kNormChunks]
     float* parts;       // kPart's tiles, as the waves hold them
+    Launch launch[kLaunches];
     List l[kMaxLists];
 };
+static_assert(sizeof(Lists) % 16 == 0 && sizeof(Lists) <= 3600, "kernel arguments");
+using ListsInMemory = const Lists __attribute__((address_space(4)));   // read by scalar loads
 
 __device__ __forceinline__ float load_value(const void* p, size_t i, int dtype)
 {
@@ -128,41 +135,46 @@ __device__ __forceinline__ Scale scale_of(double squares, float eps, float load)
 }
 
 // The list and the matrix of it that `tile` belongs to, and the tile within the matrix.
-__device__ __forceinline__ const List& find(const Lists& a, int tile, int& matrix, int& local)
+template <class L>
+__device__ __forceinline__ auto& find(L& a, LaunchOf which, int tile, int& matrix, int& local)
 {
+    auto& q = a.launch[which];
     int k = 0, from = 0;
 #pragma unroll
     for (int i = 1; i < kMaxLists; ++i)
-        if (tile >= a.first[i]) {
+        if (tile >= q.all[i]) {
             k = i;
-            from = a.first[i];
+            from = q.all[i];
         }
-    matrix = (tile - from) / a.l[k].tiles;
-    local = tile - from - matrix * a.l[k].tiles;
+    const int tiles = q.tiles[k];
+    matrix = (tile - from) / tiles;
+    local = tile - from - matrix * tiles;
     return a.l[k];
 }
 
 // The same for the products.  Neighbouring workgroups run on different XCDs: each XCD takes a contiguous part of every list's tiles
 // (its L2 holds the operands they share; no XCD is left with the long ones), lists in the launch's order.  False: nothing is left.
-__device__ __forceinline__ bool find_on_xcd(const Lists& a, int block, int& list, int& matrix, int& local)
+__device__ __forceinline__ bool find_on_xcd(ListsInMemory& a, LaunchOf which, int block, int& list, int& matrix, int& local)
 {
+    auto& q = a.launch[which];
     int rest = block >> 3, index = 0;
     list = -1;
 #pragma unroll
     for (int k = 0; k < kMaxLists; ++k) {
         const int part = ((block & 7) + 3 * k) & 7;   // (lists of a few tiles do not all fall to the same XCD)
-        const int from = a.all[k] * part >> 3, end = a.all[k] * (part + 1) >> 3;   // (at most 2^23 tiles)
+        const int from = q.all[k] * part >> 3, end = q.all[k] * (part + 1) >> 3;   // (at most 2^23 tiles)
         if (list < 0) {
             if (rest < end - from) {
-                list = a.order[k];
+                list = q.order[k];
                 index = from + rest;
             }
             rest -= end - from;
         }
     }
     if (list < 0) return false;
-    matrix = index / a.l[list].tiles;
-    local = index - matrix * a.l[list].tiles;
+    const int tiles = q.tiles[list];
+    matrix = index / tiles;
+    local = index - matrix * tiles;
     return true;
 }
 
@@ -190,14 +202,19 @@ __device__ __forceinline__ f32x4 load4(const void* p, size_t i, int dtype, bool 
 
 // Sums of squares in 64 bits (so that no gradient is too large or too small), one workgroup a (matrix, chunk); the optimiser
 // step updates the momentum on the way.
-__global__ __launch_bounds__(kThreads) void orth_norm_kernel(Lists a)
+__global__ __launch_bounds__(kThreads) void orth_norm_kernel(Lists a, Lists* in_memory)
 {
+    if (blockIdx.x == 0) {   // (the lists are the first argument: taken by address they would be copied to scratch memory)
+        const auto* from = (const uint32_t __attribute__((address_space(4)))*)__builtin_amdgcn_kernarg_segment_ptr();
+        for (int i = threadIdx.x; i < (int)(sizeof(Lists) / 4); i += kThreads) ((uint32_t*)in_memory)[i] = from[i];
+    }
     __shared__ double lds[4];
     int matrix, chunk;
-    const List& l = find(a, blockIdx.x, matrix, chunk);
+    const List& l = find(a, kOfNorm, blockIdx.x, matrix, chunk);
+    const int chunks = norm_chunks((long long)l.rows * l.cols);
     const long long size = (long long)l.rows * l.cols, from = (long long)matrix * size;
     double sum = 0.0;
-    for (long long i = ((long long)chunk * kThreads + threadIdx.x) * 4; i < size; i += (long long)l.tiles * kThreads * 4) {
+    for (long long i = ((long long)chunk * kThreads + threadIdx.x) * 4; i < size; i += (long long)chunks * kThreads * 4) {
         const int left = (int)min(size - i, 4ll);
         f32x4 v = load4(l.in, from + i, l.dtype, l.vec4, left);
         if (l.momentum) {
@@ -227,12 +244,13 @@ __global__ __launch_bounds__(kThreads) void orth_norm_kernel(Lists a)
 }
 
 // X_0 and its transpose as operands, padded with zeros: one workgroup a 64 x 64 tile of G.
-__global__ __launch_bounds__(kThreads) void orth_load_kernel(Lists a, float scale)
+__global__ __launch_bounds__(kThreads) void orth_load_kernel(const Lists* lists, float scale)
 {
+    ListsInMemory& a = *(ListsInMemory*)lists;
     __shared__ float tile[64 * 65];
     __shared__ double sums[4];
     int matrix, local;
-    const List& l = find(a, blockIdx.x, matrix, local);
+    auto& l = find(a, kOfLoad, blockIdx.x, matrix, local);
     const long long size = (long long)l.rows * l.cols;
     const int chunks = norm_chunks(size);
     double norm = 0.0;
@@ -328,15 +346,17 @@ struct ProductShape {
 };
 
 template <Product WHAT, int TILE, int GROUPS>
-__global__ __launch_bounds__((ProductShape<TILE, GROUPS>::kThreadsOf), (2)) void orth_product_kernel(Lists a, Step s)
+__global__ __launch_bounds__((ProductShape<TILE, GROUPS>::kThreadsOf), (2)) void orth_product_kernel(const Lists* lists, Step s)
 {
+    ListsInMemory& a = *(ListsInMemory*)lists;
     using S = ProductShape<TILE, GROUPS>;
     constexpr int F = TILE / 32;                    // row blocks
     constexpr int kLoads = S::kBuffer / (S::kGroupThreads * 16);
     __shared__ alignas(16) char lds[S::kLds];
     int list = 0, matrix = 0, local = 0;
-    if (!find_on_xcd(a, blockIdx.x, list, matrix, local)) return;
-    const List& l = a.l[list];
+    constexpr LaunchOf kWhich = WHAT == kGram || WHAT == kPart ? kOfGram : WHAT == kJoin ? kOfJoin : WHAT == kPoly ? kOfPoly : kOfUpdate;
+    if (!find_on_xcd(a, kWhich, blockIdx.x, list, matrix, local)) return;
+    auto& l = a.l[list];
     _Float16* ws = l.ws + (size_t)matrix * l.ws_stride;
     const size_t plane = (size_t)2 * l.mp * l.np, square = (size_t)2 * l.mp * l.mp;
     _Float16* x = ws + s.from * 2 * plane;
@@ -345,7 +365,7 @@ __global__ __launch_bounds__((ProductShape<TILE, GROUPS>::kThreadsOf), (2)) void
     constexpr bool kGramLike = WHAT == kGram || WHAT == kPart || WHAT == kJoin, kSymmetric = kGramLike || WHAT == kPoly;
     int ti, tj, slice = 0;
     const int mt = (l.mp + TILE - 1) / TILE, nt = (l.np + TILE - 1) / TILE;
-    const int part = l.first_part + (matrix * l.tiles + local) * (WHAT == kJoin ? l.splits : 1);
+    const int part = l.first_part + (matrix * a.launch[kWhich].tiles[list] + local) * (WHAT == kJoin ? l.splits : 1);
     if (WHAT == kPart) {
         slice = local % l.splits;
         local /= l.splits;
@@ -800,7 +820,7 @@ __global__ __launch_bounds__(kThreads) void orth_small_kernel(Lists a, SmallPlan
     __shared__ float scales[LP_ORTH_MAX_STEPS * 5];   // (read once: as arguments every step's would wait for a line of its own)
     if (threadIdx.x < LP_ORTH_MAX_STEPS * 5) scales[threadIdx.x] = plan.v[threadIdx.x / 5][threadIdx.x % 5];
     int matrix, local;
-    const List& l = find(a, blockIdx.x, matrix, local);
+    const List& l = find(a, kOfUpdate, blockIdx.x, matrix, local);
     const int m = l.m, n = l.n, mp = pad32(m), np = pad32(n);
     _Float16* X = (_Float16*)small_bytes;
     _Float16* XT = X + 2 * mp * np;
@@ -931,7 +951,7 @@ size_t set_bytes(const std::vector<HostList>& v, size_t first, size_t end)
         matrices += (size_t)v[k].count;
         planes += (size_t)v[k].count * align256(matrix_halves(v[k].rows, v[k].cols) * 2);
     }
-    return align256(matrices * kNormChunks * sizeof(double)) + planes;
+    return matrices ? align256(matrices * kNormChunks * sizeof(double)) + align256(sizeof(Lists)) + planes : 0;
 }
 
 
@@ -1057,26 +1077,37 @@ lp_status launched(const char* what)
 // Numbers the workgroups of a launch: `tiles_of` gives those of one matrix.
 constexpr int kMaxTiles = 1 << 23;   // workgroups of a launch (2^31 threads)
 template <class F>
-void number(Lists* a, F&& tiles_of)
+void number(Lists* a, LaunchOf which, F&& tiles_of)
 {
+    Launch& q = a->launch[which];
     int at = 0;
     for (int k = 0; k < kMaxLists; ++k) {
-        a->first[k] = k < a->n ? at : INT_MAX;
-        if (k < a->n) at += (a->l[k].tiles = tiles_of(a->l[k])) * a->l[k].count;
+        q.all[k] = k < a->n ? at : INT_MAX;
+        if (k < a->n) at += (q.tiles[k] = tiles_of(a->l[k])) * a->l[k].count;
     }
-    for (int k = 0; k < kMaxLists; ++k) a->all[k] = k < a->n ? a->l[a->order[k]].tiles * a->l[a->order[k]].count : 0;
-    a->total_tiles = at;
+    q.total = at;
+}
+
+// The same for a product, lists of more `steps` first.
+template <class F, class G>
+void number_product(Lists* a, LaunchOf which, F&& tiles_of, G&& steps)
+{
+    number(a, which, tiles_of);
+    Launch& q = a->launch[which];
+    for (int k = 0; k < a->n; ++k) q.order[k] = k;
+    std::sort(q.order, q.order + a->n, [&](int i, int j) { return steps(a->l[i]) != steps(a->l[j]) ? steps(a->l[i]) > steps(a->l[j]) : i < j; });
+    for (int k = 0; k < kMaxLists; ++k) q.all[k] = k < a->n ? q.tiles[q.order[k]] * a->l[q.order[k]].count : 0;
 }
 
 // Workgroups of a product: eight times the most that an XCD has.
-unsigned grid_of(const Lists& a)
+unsigned grid_of(const Lists& a, LaunchOf which)
 {
     int most = 0;
     for (int x = 0; x < 8; ++x) {
         int sum = 0;
         for (int k = 0; k < a.n; ++k) {
-            const int part = (x + 3 * k) & 7;
-            sum += (a.all[k] * (part + 1) >> 3) - (a.all[k] * part >> 3);
+            const int part = (x + 3 * k) & 7, all = a.launch[which].all[k];
+            sum += (all * (part + 1) >> 3) - (all * part >> 3);
         }
         most = sum > most ? sum : most;
     }
@@ -1103,7 +1134,8 @@ lp_status run_set(const std::vector<HostList>& v, size_t first, size_t end, cons
     size_t matrices = 0;
     for (size_t k = first; k < end; ++k)
         if (!is_small(v[k].rows, v[k].cols)) matrices += (size_t)v[k].count;
-    char* at = (char*)workspace + align256(matrices * kNormChunks * sizeof(double));
+    const size_t lists_at = align256(matrices * kNormChunks * sizeof(double));
+    char* at = (char*)workspace + lists_at + align256(sizeof(Lists));
     const GramPlan gram = plan_gram(v, first, end);
     Lists small = a;
     int lds = 0;
@@ -1111,7 +1143,6 @@ lp_status run_set(const std::vector<HostList>& v, size_t first, size_t end, cons
         const HostList& q = v[k];
         const bool is = is_small(q.rows, q.cols);
         List& l = is ? small.l[small.n] : a.l[a.n];
-        (is ? small.order[small.n] : a.order[a.n]) = is ? small.n : a.n;
         ++(is ? small.n : a.n);
         l.in = q.in; l.out = q.out; l.momentum = q.momentum; l.dtype = q.dtype;
         l.count = (int)q.count; l.rows = q.rows; l.cols = q.cols;
@@ -1140,7 +1171,7 @@ lp_status run_set(const std::vector<HostList>& v, size_t first, size_t end, cons
         }
     }
     if (small.n) {
-        number(&small, [](const List&) { return 1; });
+        number(&small, kOfUpdate, [](const List&) { return 1; });
         const hipError_t e = hipFuncSetAttribute((const void*)orth_small_kernel, hipFuncAttributeMaxDynamicSharedMemorySize, lds);
         if (e != hipSuccess) return fail(LP_ERR_HIP, std::string("hipFuncSetAttribute(orth_small_kernel): ") + hipGetErrorString(e));
         SmallPlan sp;
@@ -1151,64 +1182,76 @@ lp_status run_set(const std::vector<HostList>& v, size_t first, size_t end, cons
             const float v[5] = {plan.gram[k].acc, plan.poly[k].acc, plan.poly[k].diag, plan.poly[k].lin, plan.update[k].acc};
             std::memcpy(sp.v[k], v, sizeof(v));
         }
-        hipLaunchKernelGGL(orth_small_kernel, dim3(small.total_tiles), dim3(kThreads), lds, s, small, sp);
+        hipLaunchKernelGGL(orth_small_kernel, dim3(small.launch[kOfUpdate].total), dim3(kThreads), lds, s, small, sp);
     }
     if (a.n == 0) return launched("orthogonalisation launch");
     a.parts = (float*)at;
-    auto load_tiles = [](const List& l) { return (l.mp / 64) * (l.np / 64); };
-    number(&a, [](const List& l) { return norm_chunks((long long)l.rows * l.cols); });   // (never more than the matrix has tiles)
-    hipLaunchKernelGGL(orth_norm_kernel, dim3(a.total_tiles), dim3(kThreads), 0, s, a);
-    number(&a, load_tiles);
-    hipLaunchKernelGGL(orth_load_kernel, dim3(a.total_tiles), dim3(kThreads), 0, s, a, plan.load);
+    Lists* in_memory = (Lists*)((char*)workspace + lists_at);
     auto tiles = [](const List& l, int tile, bool half) {
         const int mt = (l.mp + tile - 1) / tile, nt = (l.np + tile - 1) / tile;
         return half ? mt * (mt + 1) / 2 : mt * nt;
     };
-    auto sort_by = [&](auto&& steps) {
-        std::sort(a.order, a.order + a.n, [&](int i, int j) { return steps(a.l[i]) != steps(a.l[j]) ? steps(a.l[i]) > steps(a.l[j]) : i < j; });
-    };
-    auto product = [&](auto what, const Step& step) {
-        constexpr Product W = decltype(what)::value;
-        constexpr bool half = W == kGram || W == kPoly;
-        sort_by([](const List& l) { return W == kGram ? l.np : l.mp; });
-        number(&a, [&](const List& l) { return tiles(l, 128, half); });
-        // Large tiles where they give every compute unit work.  Two small workgroups a unit overlap one's ends with the other's
-        // products (B X of 340 tiles with sums of 64 .. 256: 19 us, in one large workgroup a unit 24, in 64 x 64 tiles 34); the long
-        // sums of A = X X^T are better halved inside a workgroup while there are fewer than two a unit (308 tiles: 104 and 130 us).
-        if (a.total_tiles >= (W == kGram ? 2 : 1) * kUnits) {
-            hipLaunchKernelGGL((orth_product_kernel<W, 128, 1>), dim3(grid_of(a)), dim3(256), 0, s, a, step);
-            return;
-        }
-        if constexpr (W == kGram) {
-            if (a.total_tiles >= kUnits) {
-                hipLaunchKernelGGL((orth_product_kernel<W, 128, 2>), dim3(grid_of(a)), dim3(512), 0, s, a, step);
-                return;
-            }
-        }
-        number(&a, [&](const List& l) { return tiles(l, 64, half); });
-        hipLaunchKernelGGL((orth_product_kernel<W, 64, 4>), dim3(grid_of(a)), dim3(512), 0, s, a, step);
+    number(&a, kOfNorm, [](const List& l) { return norm_chunks((long long)l.rows * l.cols); });   // (never more than the matrix has tiles)
+    number(&a, kOfLoad, [](const List& l) { return (l.mp / 64) * (l.np / 64); });
+    // How a product is divided.  Large tiles where they give every compute unit work.  Two small workgroups a unit overlap one's
+    // ends with the other's products (B X of 340 tiles with sums of 64 .. 256: 19 us, in one large workgroup a unit 24, in 64 x 64
+    // tiles 34); the long sums of A = X X^T are better halved inside a workgroup while there are fewer than two a unit (308 tiles:
+    // 104 and 130 us).
+    struct Shape { int tile, groups; };
+    auto shape_of = [&](LaunchOf which, bool half) {
+        const bool is_gram = which == kOfGram;
+        auto steps = [&](const List& l) { return is_gram ? l.np : l.mp; };
+        number_product(&a, which, [&](const List& l) { return tiles(l, 128, half); }, steps);
+        if (a.launch[which].total >= (is_gram ? 2 : 1) * kUnits) return Shape{128, 1};
+        if (is_gram && a.launch[which].total >= kUnits) return Shape{128, 2};
+        number_product(&a, which, [&](const List& l) { return tiles(l, 64, half); }, steps);
+        return Shape{64, 4};
     };
     // A = X X^T: where few tiles have long sums, these are divided among workgroups and joined by a second launch
     bool divided = false;
     for (int k = 0; k < a.n; ++k) divided = divided || a.l[k].splits > 1;
-    auto gram_product = [&](const Step& step) {
-        if (!divided) return product(std::integral_constant<Product, kGram>(), step);
-        sort_by([](const List& l) { return std::min(l.chunk, l.np / kDepth); });
-        int at = 0;
+    Shape gram_shape = {64, 4};
+    if (divided) {
+        int first_part = 0;
         for (int k = 0; k < a.n; ++k) {
-            a.l[k].first_part = at;
-            at += a.l[k].count * tiles(a.l[k], 64, true) * a.l[k].splits;
+            a.l[k].first_part = first_part;
+            first_part += a.l[k].count * tiles(a.l[k], 64, true) * a.l[k].splits;
         }
-        number(&a, [&](const List& l) { return tiles(l, 64, true) * l.splits; });
-        hipLaunchKernelGGL((orth_product_kernel<kPart, 64, 4>), dim3(grid_of(a)), dim3(512), 0, s, a, step);
-        number(&a, [&](const List& l) { return tiles(l, 64, true); });
-        hipLaunchKernelGGL((orth_product_kernel<kJoin, 64, 4>), dim3(grid_of(a)), dim3(512), 0, s, a, step);
+        auto steps = [](const List& l) { return std::min(l.chunk, l.np / kDepth); };
+        number_product(&a, kOfGram, [&](const List& l) { return tiles(l, 64, true) * l.splits; }, steps);
+        number_product(&a, kOfJoin, [&](const List& l) { return tiles(l, 64, true); }, steps);
+    } else {
+        gram_shape = shape_of(kOfGram, true);
+    }
+    const Shape poly_shape = shape_of(kOfPoly, true), update_shape = shape_of(kOfUpdate, false);
+    const unsigned gram_grid = grid_of(a, kOfGram), join_grid = divided ? grid_of(a, kOfJoin) : 0, poly_grid = grid_of(a, kOfPoly),
+                   update_grid = grid_of(a, kOfUpdate);
+    hipLaunchKernelGGL(orth_norm_kernel, dim3(a.launch[kOfNorm].total), dim3(kThreads), 0, s, a, in_memory);
+    hipLaunchKernelGGL(orth_load_kernel, dim3(a.launch[kOfLoad].total), dim3(kThreads), 0, s, in_memory, plan.load);
+    auto product = [&](auto what, const Shape& shape, unsigned grid, const Step& step) {
+        constexpr Product W = decltype(what)::value;
+        if (shape.tile == 64) {
+            hipLaunchKernelGGL((orth_product_kernel<W, 64, 4>), dim3(grid), dim3(512), 0, s, in_memory, step);
+        } else if constexpr (W != kPart && W != kJoin) {
+            if constexpr (W == kGram) {
+                if (shape.groups == 2) {
+                    hipLaunchKernelGGL((orth_product_kernel<W, 128, 2>), dim3(grid), dim3(512), 0, s, in_memory, step);
+                    return;
+                }
+            }
+            hipLaunchKernelGGL((orth_product_kernel<W, 128, 1>), dim3(grid), dim3(256), 0, s, in_memory, step);
+        }
     };
     for (int k = 0; k < plan.steps; ++k) {
-        gram_product(plan.gram[k]);
-        product(std::integral_constant<Product, kPoly>(), plan.poly[k]);
-        if (k + 1 < plan.steps) product(std::integral_constant<Product, kUpdate>(), plan.update[k]);
-        else product(std::integral_constant<Product, kLast>(), plan.update[k]);
+        if (divided) {
+            product(std::integral_constant<Product, kPart>(), gram_shape, gram_grid, plan.gram[k]);
+            product(std::integral_constant<Product, kJoin>(), gram_shape, join_grid, plan.gram[k]);
+        } else {
+            product(std::integral_constant<Product, kGram>(), gram_shape, gram_grid, plan.gram[k]);
+        }
+        product(std::integral_constant<Product, kPoly>(), poly_shape, poly_grid, plan.poly[k]);
+        if (k + 1 < plan.steps) product(std::integral_constant<Product, kUpdate>(), update_shape, update_grid, plan.update[k]);
+        else product(std::integral_constant<Product, kLast>(), update_shape, update_grid, plan.update[k]);
     }
     return launched("orthogonalisation launch");
 }

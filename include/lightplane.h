@@ -5,7 +5,8 @@
  * differentiable emission-absorption ray marching over a hybrid 3D representation
  * f = g o h (Section 3.2), where h is bi/tri-linear sampling of a triplane or voxel
  * feature grid and g a tiny MLP, with a backward pass that stores one scalar per ray
- * and recomputes everything else (Section 3.4).
+ * and recomputes everything else (Section 3.4).  Next to it: the Splatter, and for networks that work
+ * on the structures a group norm with an activation and the orthogonalised update of weight matrices.
  *
  * General rules
  *   - Every pointer named "device" is a pointer to GPU memory owned by the caller

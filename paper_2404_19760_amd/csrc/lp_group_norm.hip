@@ -9,7 +9,9 @@
 // What bounds it: memory.  A sum over the whole group stands between reading a value and using it.  A sample of at most 128 KB stays in the
 // registers of one workgroup meanwhile (one launch).  Larger ones are passed over twice: a pass that sums (forward: x; backward: x
 // and d_y), a small kernel that joins the workgroups' sums, and a pass that writes, from the end back to the start: what the first
-// pass read last is still in the 256 MB of Infinity Cache.  In all passes a thread keeps to one slot of V neighbouring channels (16 bytes where channels and
+// pass read last is still in the 256 MB of Infinity Cache (160^3 x 32 in fp32, all passes of a training step: 744 us, from the
+// start 823).  Measured there: 117, 179, 216 and 285 us for 0.5, 1.0, 1.0 and 1.6 GB (4.5 to 5.9 TB/s; a copy of 2 GB 4.95), 24 planes
+// of 256^2 x 32 in bf16 24, 34, 47 and 52 us for 0.1, 0.2, 0.2 and 0.3 GB.  In all passes a thread keeps to one slot of V neighbouring channels (16 bytes where channels and
 // alignment allow), so a channel's parameters and sums stay in its registers, and neighbouring lanes read neighbouring bytes.
 //
 // Sums: a thread sums differences to the first value that it sees, in fp32 (a mean far from zero does not cancel the

@@ -36,7 +36,7 @@ using f32x16 = float __attribute__((ext_vector_type(16)));
 
 constexpr int kThreads = 256;
 constexpr int kUnits = 256;       // compute units of the chip: what divides the work goes by it
-constexpr int kMaxLists = 16;     // lists of one set of launches (their descriptors travel as kernel arguments)
+constexpr int kMaxLists = 16;     // lists of one set of launches (their descriptors are the first kernel's arguments)
 constexpr int kPad = 64;          // rows and columns of operands are padded to this
 constexpr int kNormChunks = 512;  // partial sums of a matrix's norm, at most
 constexpr int kChunk = 8192;      // values of one, at least
@@ -334,6 +334,8 @@ using LdsPtr = __attribute__((address_space(3))) void;
 // have been used, and the workgroup meets in the middle of a step, so that a wave always has products to issue behind the barrier.
 // The small products (hi lo + lo hi) have an accumulator of their own: added into the large one's they would round it three
 // times as often (error against 64 bits at 2048 x 2048: 6.8e-6 in one accumulator, 4.4e-6 in two; fp32 torch 4.2e-6).
+// Measured on 2 x 2048 x 2048 and 1024 x 4096: B X 129 us (1.0 PFLOP/s of fp16 products; a library product of 8192^3 1.08), A = X X^T
+// 94 to 105, A A 87 (308 tiles on 256 units); on 36 matrices of width 512 88, 62 and 39 us.
 template <int TILE, int GROUPS>
 struct ProductShape {
     static constexpr int kWaves = TILE / 32, kGroups = GROUPS, kGroupThreads = 64 * kWaves;
@@ -651,7 +653,8 @@ struct Plan {
 
 // Matrices of at most 64 x 128 (a decoder's layers): one workgroup of four waves keeps X, X^T, A and B in LDS, in the same order as
 // the large operands, from the gradient to the result: one launch, and no bytes but G's and the result's (the optimiser's: the
-// momentum's and the weights').  Its time is that of a chain of 3 x steps products with a barrier behind each, about XXX us.
+// momentum's and the weights').  Its time is that of a chain of 3 x steps products with a barrier behind each: 64 x 64 in 2.2 us a
+// step and 10 us before and after them (in the launches of the large matrices: 86 us for the three matrices of a decoder, here 22).
 // Rows and columns are padded to 32.  A wave has one 32 x 32 block of A and B and up to two of X.
 constexpr int kSmallM = 64, kSmallN = 128;
 __host__ __device__ inline int pad32(int v) { return (v + 31) & ~31; }

@@ -54,6 +54,42 @@ def test_against_64_bits(lp, dtype, shape):
     _close(out, reference(g), dtype, str(shape))
 
 
+@pytest.mark.parametrize("dtype", [torch.float32, torch.bfloat16])
+@pytest.mark.parametrize("shape", [(64, 2999), (100, 5001), (4001, 70), (2, 130, 2500), (300, 1400), (1500, 260)])
+def test_long_sums_that_are_divided(lp, dtype, shape):
+    """A = X X^T of more than 32 blocks of 32 columns: parts, and their join."""
+    g = gradient(shape, sum(shape)).to(dtype)
+    out, = lp.orthogonalize([g])
+    _close(out, reference(g), dtype, str(shape))
+
+
+@pytest.mark.parametrize("shapes", [[(100, 200, 300)],                         # 300 tiles of 128 for A, 600 for B X
+                                    [(200, 300, 200)],                         # 600 and 1200, tall
+                                    [(90, 130, 250), (40, 256, 129), (3, 1, 900)],   # edges in the middle of a tile of 128
+                                    [(5, 900, 1000), (700, 700)]])
+def test_large_tiles(lp, shapes):
+    mats = [gradient(s, 9 + k) for k, s in enumerate(shapes)]
+    for g, out in zip(mats, lp.orthogonalize(mats)):
+        want = reference(g)
+        _close(out, want, torch.float32, str(g.shape))
+        if g.dim() == 3:   # the matrices one by one, too
+            for i in range(g.shape[0]):
+                assert float((out[i].double().cpu() - want[i]).norm()) <= 2 * TOL[torch.float32] * float(want[i].norm()), (g.shape, i)
+
+
+@pytest.mark.parametrize("shape,dtype", [((262200, 64, 128), torch.bfloat16), ((300, 64, 65536), torch.float32)])
+def test_offsets_beyond_32_bits(lp, shape, dtype):
+    """Lists of more than 2^31 values and 2^32 bytes: the last matrix is as by itself, zeros stay zeros."""
+    mats = torch.zeros(shape, dtype=dtype, device="cuda")
+    last = gradient(shape[1:], 3).to(dtype)
+    mats[0], mats[-1] = last, last
+    alone, = lp.orthogonalize([last], steps=1)
+    ws = torch.empty(lp.lp_orthogonalize_workspace_bytes([mats]), dtype=torch.uint8, device="cuda")
+    lp.lp_orthogonalize([mats], [mats], ws, steps=1)
+    _close(mats[-1], alone.double().cpu(), dtype, "last")
+    assert torch.equal(mats[0], mats[-1]) and float(mats[1:-1].abs().amax()) == 0
+
+
 def test_one_call_for_many_lists(lp):
     """More lists than one set of launches takes, of all sizes and types: each as by itself."""
     shapes = [(64, 16), (64, 64), (4, 64), (2, 100, 30), (7, 300), (129, 65)] * 4

@@ -1175,7 +1175,8 @@ lp_status run_set(const std::vector<HostList>& v, size_t first, size_t end, cons
     }
     if (small.n) {
         number(&small, kOfUpdate, [](const List&) { return 1; });
-        const hipError_t e = hipFuncSetAttribute((const void*)orth_small_kernel, hipFuncAttributeMaxDynamicSharedMemorySize, lds);
+        const hipError_t e = hipFuncSetAttribute((const void*)orth_small_kernel, hipFuncAttributeMaxDynamicSharedMemorySize,
+                                                 small_lds(kSmallM, kSmallN));   // (the same from every thread)
         if (e != hipSuccess) return fail(LP_ERR_HIP, std::string("hipFuncSetAttribute(orth_small_kernel): ") + hipGetErrorString(e));
         SmallPlan sp;
         std::memset(&sp, 0, sizeof(sp));

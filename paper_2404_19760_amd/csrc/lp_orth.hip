@@ -671,6 +671,23 @@ __host__ __device__ inline int small_lds(int mp, int np)
     return 2 * mp * np * 4 + (rest > g ? rest : g);
 }
 
+// The lists of such matrices, and what the steps go by (all that this kernel is given: 1.4 KB).
+struct SmallList {
+    const void* in;
+    void* out;
+    float* momentum;
+    int rows, cols, m, n, tall, dtype, vec4;
+    float step;
+};
+struct SmallCall {
+    int n, nesterov;
+    float lr_decay, mu, eps, load;
+    int steps;
+    int first[kMaxLists];            // workgroups, as in Launch
+    SmallList l[kMaxLists];
+    float v[LP_ORTH_MAX_STEPS][5];   // scales of a step: kGram's, kPoly's three, kUpdate's
+};
+
 // Block (bi, bj) of P Q^T over 16 K16 columns.
 template <int K16>
 __device__ __forceinline__ f32x16 small_product(const _Float16* p, const _Float16* q, int bi, int bj)
@@ -693,8 +710,8 @@ __device__ __forceinline__ f32x16 small_product(const _Float16* p, const _Float1
 // The steps of a matrix of MB x NB blocks of 32 x 32 (sizes are constants: at one wave a SIMD every index that is worked out
 // between two barriers is waited for), and the result.
 template <int MB, int NB>
-__device__ __forceinline__ void small_steps(const Lists& a, const List& l, int n_steps, const float* scales, _Float16* X, _Float16* XT,
-                                            _Float16* B, _Float16* A, size_t from)
+__device__ __forceinline__ void small_steps(const SmallCall& a, const SmallList& l, int n_steps, const float* scales, _Float16* X, _Float16* XT,
+                                            _Float16* B, _Float16* A, const float* g, const Scale& f, size_t from)
 {
     constexpr int kPer = (MB * NB + 3) / 4;   // blocks of X that a wave has, at most
     const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), lane = threadIdx.x & 63, l32 = lane & 31, h = lane >> 5;
@@ -720,6 +737,34 @@ __device__ __forceinline__ void small_steps(const Lists& a, const List& l, int n
 #pragma unroll
         for (int e4 = 0; e4 < 4; ++e4) split4(f32x4{v[4 * e4], v[4 * e4 + 1], v[4 * e4 + 2], v[4 * e4 + 3]}, hi[e4], lo[e4]);
     };
+    // blocks of X, then of X^T, one a wave at a time: the 16 bytes of a lane are row `i`, columns j .. of the operand
+    constexpr int kBlocks = MB * NB * 2, kRow = NB * 32 + 1;
+#pragma unroll 2
+    for (int u = wave; u < 2 * kBlocks; u += 4) {
+        const bool t = u >= kBlocks;
+        const int block = t ? u - kBlocks : u;
+        const int i = (t ? block / (2 * MB) : block / (2 * NB)) * 32 + l32, j = (t ? block % (2 * MB) : block % (2 * NB)) * 16 + 8 * h;
+        const float* src = t ? g + j * kRow + i : g + i * kRow + j;
+        const int next = t ? kRow : 1;
+        _Float16* to = (t ? XT : X) + block * kBlock + lane * 8;
+#pragma unroll
+        for (int q = 0; q < 2; ++q) {
+            f32x4 w;
+#pragma unroll
+            for (int e = 0; e < 4; ++e) w[e] = f(src[(4 * q + e) * next]);
+            half4 wh, wl;
+            split4(w, wh, wl);
+            *(half4*)(to + 4 * q) = wh;
+            *(half4*)(to + 512 + 4 * q) = wl;
+        }
+    }
+    float diagonal[16];   // 1 on it
+#pragma unroll
+    for (int e = 0; e < 16; ++e) {
+        const int i = bi * 32 + 8 * (e >> 2) + 4 * h + (e & 3), j = bj * 32 + l32;
+        diagonal[e] = i == j && i < l.m ? 1.0f : 0.0f;
+    }
+    __syncthreads();
     half4 hi[4], lo[4];
 #pragma unroll 1
     for (int step = 0; step < n_steps; ++step) {
@@ -735,10 +780,7 @@ __device__ __forceinline__ void small_steps(const Lists& a, const List& l, int n
         if (square) {
             f32x16 v = small_product<2 * MB>(A, A, bi, bj);
 #pragma unroll
-            for (int e = 0; e < 16; ++e) {
-                const int i = bi * 32 + 8 * (e >> 2) + 4 * h + (e & 3), j = bj * 32 + l32;
-                v[e] = fmaf(s_lin, gram[e], v[e] * s_poly) + (i == j && i < l.m ? s_diag : 0.0f);
-            }
+            for (int e = 0; e < 16; ++e) v[e] = fmaf(s_diag, diagonal[e], fmaf(s_lin, gram[e], v[e] * s_poly));
             split16(v, hi, lo);
             put_turned(hi, lo, B, MB, bi, bj);
         }
@@ -809,28 +851,27 @@ __device__ __forceinline__ void small_steps(const Lists& a, const List& l, int n
     }
 }
 
-// The steps' scales as this kernel takes them.
-struct SmallPlan {
-    float load;
-    int steps;
-    float v[LP_ORTH_MAX_STEPS][5];   // kGram's, kPoly's three, kUpdate's
-};
-
-__global__ __launch_bounds__(kThreads) void orth_small_kernel(Lists a, SmallPlan plan)
+__global__ __launch_bounds__(kThreads) void orth_small_kernel(SmallCall a)
 {
     extern __shared__ char small_bytes[];
     __shared__ double sums[4];
     __shared__ float scales[LP_ORTH_MAX_STEPS * 5];   // (read once: as arguments every step's would wait for a line of its own)
-    if (threadIdx.x < LP_ORTH_MAX_STEPS * 5) scales[threadIdx.x] = plan.v[threadIdx.x / 5][threadIdx.x % 5];
-    int matrix, local;
-    const List& l = find(a, kOfUpdate, blockIdx.x, matrix, local);
+    const float my_scale = threadIdx.x < LP_ORTH_MAX_STEPS * 5 ? a.v[threadIdx.x / 5][threadIdx.x % 5] : 0.0f;   // (stored once G is asked for)
+    int list = 0, matrix = blockIdx.x;
+#pragma unroll
+    for (int i = 1; i < kMaxLists; ++i)
+        if ((int)blockIdx.x >= a.first[i]) {
+            list = i;
+            matrix = (int)blockIdx.x - a.first[i];
+        }
+    const SmallList& l = a.l[list];
     const int m = l.m, n = l.n, mp = pad32(m), np = pad32(n);
     _Float16* X = (_Float16*)small_bytes;
     _Float16* XT = X + 2 * mp * np;
     _Float16* B = XT + 2 * mp * np;
     _Float16* A = B + 2 * mp * mp;
     float* g = (float*)B;   // [mp][np + 1], X's order
-    const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), lane = threadIdx.x & 63, l32 = lane & 31, h = lane >> 5;
+    const int wave = threadIdx.x >> 6, lane = threadIdx.x & 63;
     const size_t from = (size_t)matrix * l.rows * l.cols;
     // G: a thread has four columns of every kPasses-th group of rows
     constexpr int kPasses = kSmallM * kSmallN / (4 * kThreads);
@@ -881,38 +922,17 @@ __global__ __launch_bounds__(kThreads) void orth_small_kernel(Lists a, SmallPlan
     }
     for (int o = 32; o; o >>= 1) norm += __shfl_xor(norm, o);
     if (lane == 0) sums[wave] = norm;
+    if (threadIdx.x < LP_ORTH_MAX_STEPS * 5) scales[threadIdx.x] = my_scale;
     __syncthreads();
-    const Scale f = scale_of(sums[0] + sums[1] + sums[2] + sums[3], a.eps, plan.load);
-    // blocks of X, then of X^T, one a wave at a time: the 16 bytes of a lane are row `i`, columns j .. of the operand
-    const int blocks = mp * np / 512;
-#pragma unroll 1
-    for (int u = wave; u < 2 * blocks; u += 4) {
-        const bool t = u >= blocks;
-        const int block = t ? u - blocks : u, per_row = (t ? mp : np) >> 4;
-        const int i = block / per_row * 32 + l32, j = block % per_row * 16 + 8 * h;
-        const float* src = t ? g + j * (np + 1) + i : g + i * (np + 1) + j;
-        const int step = t ? np + 1 : 1;
-        _Float16* to = (t ? XT : X) + block * kBlock + lane * 8;
-#pragma unroll
-        for (int q = 0; q < 2; ++q) {
-            f32x4 w;
-#pragma unroll
-            for (int e = 0; e < 4; ++e) w[e] = f(src[(4 * q + e) * step]);
-            half4 hi, lo;
-            split4(w, hi, lo);
-            *(half4*)(to + 4 * q) = hi;
-            *(half4*)(to + 512 + 4 * q) = lo;
-        }
-    }
-    __syncthreads();
+    const Scale f = scale_of(sums[0] + sums[1] + sums[2] + sums[3], a.eps, a.load);
     switch (mp / 32 * 4 + np / 32) {
-        case 4 + 1: small_steps<1, 1>(a, l, plan.steps, scales, X, XT, B, A, from); break;
-        case 4 + 2: small_steps<1, 2>(a, l, plan.steps, scales, X, XT, B, A, from); break;
-        case 4 + 3: small_steps<1, 3>(a, l, plan.steps, scales, X, XT, B, A, from); break;
-        case 4 + 4: small_steps<1, 4>(a, l, plan.steps, scales, X, XT, B, A, from); break;
-        case 8 + 2: small_steps<2, 2>(a, l, plan.steps, scales, X, XT, B, A, from); break;
-        case 8 + 3: small_steps<2, 3>(a, l, plan.steps, scales, X, XT, B, A, from); break;
-        case 8 + 4: small_steps<2, 4>(a, l, plan.steps, scales, X, XT, B, A, from); break;
+        case 4 + 1: small_steps<1, 1>(a, l, a.steps, scales, X, XT, B, A, g, f, from); break;
+        case 4 + 2: small_steps<1, 2>(a, l, a.steps, scales, X, XT, B, A, g, f, from); break;
+        case 4 + 3: small_steps<1, 3>(a, l, a.steps, scales, X, XT, B, A, g, f, from); break;
+        case 4 + 4: small_steps<1, 4>(a, l, a.steps, scales, X, XT, B, A, g, f, from); break;
+        case 8 + 2: small_steps<2, 2>(a, l, a.steps, scales, X, XT, B, A, g, f, from); break;
+        case 8 + 3: small_steps<2, 3>(a, l, a.steps, scales, X, XT, B, A, g, f, from); break;
+        case 8 + 4: small_steps<2, 4>(a, l, a.steps, scales, X, XT, B, A, g, f, from); break;
     }
 }
 
@@ -1140,53 +1160,52 @@ lp_status run_set(const std::vector<HostList>& v, size_t first, size_t end, cons
     const size_t lists_at = align256(matrices * kNormChunks * sizeof(double));
     char* at = (char*)workspace + lists_at + align256(sizeof(Lists));
     const GramPlan gram = plan_gram(v, first, end);
-    Lists small = a;
-    int lds = 0;
+    SmallCall small;
+    std::memset(&small, 0, sizeof(small));
+    small.lr_decay = a.lr_decay; small.mu = a.mu; small.nesterov = a.nesterov; small.eps = eps;
+    int lds = 0, small_matrices = 0;
+    for (int k = 0; k < kMaxLists; ++k) small.first[k] = INT_MAX;
     for (size_t k = first; k < end; ++k) {
         const HostList& q = v[k];
-        const bool is = is_small(q.rows, q.cols);
-        List& l = is ? small.l[small.n] : a.l[a.n];
-        ++(is ? small.n : a.n);
-        l.in = q.in; l.out = q.out; l.momentum = q.momentum; l.dtype = q.dtype;
-        l.count = (int)q.count; l.rows = q.rows; l.cols = q.cols;
-        l.tall = q.rows > q.cols;
-        l.m = l.tall ? q.cols : q.rows; l.n = l.tall ? q.rows : q.cols;
-        l.mp = pad(l.m); l.np = pad(l.n);
-        if (is) {
-            l.vec4 = (uintptr_t)q.in % 16 == 0 && (uintptr_t)q.momentum % 16 == 0;
-            const int need = small_lds(pad32(l.m), pad32(l.n));
-            lds = need > lds ? need : lds;
-        } else {
-            l.ws = (_Float16*)at;
-            l.ws_stride = (long long)align256(matrix_halves(q.rows, q.cols) * 2) / 2;
-            at += (size_t)l.ws_stride * 2 * q.count;
-            l.vec4 = (long long)q.rows * q.cols % 4 == 0 && (uintptr_t)q.in % 16 == 0 && (uintptr_t)q.momentum % 16 == 0;
-            l.splits = gram.splits[k - first];
-            l.chunk = gram.chunk;
-            l.first_matrix = a.matrices;
-            a.matrices += l.count;
-        }
+        const int tall = q.rows > q.cols, m = tall ? q.cols : q.rows, n = tall ? q.rows : q.cols;
+        const bool aligned = (uintptr_t)q.in % 16 == 0 && (uintptr_t)q.momentum % 16 == 0;
+        float step = 0.0f;
         if (muon) {
-            const double ratio = (double)q.rows / q.cols, larger = q.rows > q.cols ? q.rows : q.cols;
-            const double scale = muon->scale == LP_MUON_SCALE_ASPECT ? sqrt(ratio > 1.0 ? ratio : 1.0)
-                               : muon->scale == LP_MUON_SCALE_RMS ? 0.2 * sqrt(larger) : 1.0;
-            l.step = (float)(muon->lr * scale);
+            const double ratio = (double)q.rows / q.cols;
+            step = (float)(muon->lr * (muon->scale == LP_MUON_SCALE_ASPECT ? sqrt(ratio > 1.0 ? ratio : 1.0)
+                                     : muon->scale == LP_MUON_SCALE_RMS ? 0.2 * sqrt((double)n) : 1.0));
         }
+        if (is_small(q.rows, q.cols)) {
+            small.first[small.n] = small_matrices;
+            small.l[small.n++] = {q.in, q.out, q.momentum, q.rows, q.cols, m, n, tall, q.dtype, aligned, step};
+            small_matrices += (int)q.count;
+            lds = std::max(lds, small_lds(pad32(m), pad32(n)));
+            continue;
+        }
+        List& l = a.l[a.n++];
+        l.in = q.in; l.out = q.out; l.momentum = q.momentum; l.dtype = q.dtype; l.step = step;
+        l.count = (int)q.count; l.rows = q.rows; l.cols = q.cols; l.tall = tall;
+        l.m = m; l.n = n; l.mp = pad(m); l.np = pad(n);
+        l.ws = (_Float16*)at;
+        l.ws_stride = (long long)align256(matrix_halves(q.rows, q.cols) * 2) / 2;
+        at += (size_t)l.ws_stride * 2 * q.count;
+        l.vec4 = aligned && (long long)q.rows * q.cols % 4 == 0;
+        l.splits = gram.splits[k - first];
+        l.chunk = gram.chunk;
+        l.first_matrix = a.matrices;
+        a.matrices += l.count;
     }
     if (small.n) {
-        number(&small, kOfUpdate, [](const List&) { return 1; });
         const hipError_t e = hipFuncSetAttribute((const void*)orth_small_kernel, hipFuncAttributeMaxDynamicSharedMemorySize,
                                                  small_lds(kSmallM, kSmallN));   // (the same from every thread)
         if (e != hipSuccess) return fail(LP_ERR_HIP, std::string("hipFuncSetAttribute(orth_small_kernel): ") + hipGetErrorString(e));
-        SmallPlan sp;
-        std::memset(&sp, 0, sizeof(sp));
-        sp.load = plan.load;
-        sp.steps = plan.steps;
+        small.load = plan.load;
+        small.steps = plan.steps;
         for (int k = 0; k < plan.steps; ++k) {
-            const float v[5] = {plan.gram[k].acc, plan.poly[k].acc, plan.poly[k].diag, plan.poly[k].lin, plan.update[k].acc};
-            std::memcpy(sp.v[k], v, sizeof(v));
+            const float w[5] = {plan.gram[k].acc, plan.poly[k].acc, plan.poly[k].diag, plan.poly[k].lin, plan.update[k].acc};
+            std::memcpy(small.v[k], w, sizeof(w));
         }
-        hipLaunchKernelGGL(orth_small_kernel, dim3(small.launch[kOfUpdate].total), dim3(kThreads), lds, s, small, sp);
+        hipLaunchKernelGGL(orth_small_kernel, dim3(small_matrices), dim3(kThreads), lds, s, small);
     }
     if (a.n == 0) return launched("orthogonalisation launch");
     a.parts = (float*)at;

@@ -28,7 +28,7 @@ def _events(lines):
     return out
 
 
-@pytest.mark.parametrize("first,last,accesses", [(r"void orth_product_kernel\(", r"^struct Plan", 4), (r"void small_steps\(", r"^struct SmallPlan", 2)])
+@pytest.mark.parametrize("first,last,accesses", [(r"void orth_product_kernel\(", r"^struct Plan", 4), (r"void small_steps\(", r"orth_small_kernel", 2)])
 def test_a_fence_between_stores_and_reads_of_other_lanes(first, last, accesses):
     events = _events(_body(first, last))
     assert sum(e != "fence" for e in events) == accesses and {"store", "read"} <= set(events)

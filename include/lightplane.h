@@ -388,7 +388,9 @@ typedef struct {
    count, rows or cols 0. */
 lp_status lp_orthogonalize(int32_t n, const lp_matrices* lists, const lp_orth* orth, void* workspace,
                            size_t workspace_bytes, void* stream);
-/* 0 where all matrices are at most 64 x 128 or 128 x 64 (then NULL will do). */
+/* 0 where all matrices are at most 64 x 224 or 32 x 448, or their transposes (then NULL will do).
+   The result of a matrix of more than 128 rows or columns may differ in its last bits with what else the
+   call holds. */
 lp_status lp_orthogonalize_workspace_bytes(int32_t n, const lp_matrices* lists, size_t* bytes);
 
 /* How the step of a matrix is scaled. */

@@ -653,23 +653,27 @@ struct Plan {
 
 // Matrices of at most 64 x 128 (a decoder's layers): one workgroup of four waves keeps X, X^T, A and B in LDS, in the same order as
 // the large operands, from the gradient to the result: one launch, and no bytes but G's and the result's (the optimiser's: the
-// momentum's and the weights').  Its time is that of a chain of 3 x steps products with a barrier behind each: 64 x 64 in 2.2 us a
-// step and 10 us before and after them (in the launches of the large matrices: 86 us for the three matrices of a decoder, here 22).
+// momentum's and the weights').  Its time is that of a chain of 3 x steps products with a barrier behind each: 64 x 64 in 2.1 us a
+// step and 10 us before and after them (in the launches of the large matrices: 86 us for the three matrices of a decoder, here 20.7).
 // Rows and columns are padded to 32.  A wave has one 32 x 32 block of A and B and up to two of X.
 constexpr int kSmallM = 64, kSmallN = 128;
+// Longer ones as far as X and X^T fit the LDS: 64 x 224 and 32 x 448 (in the launches of the large
+// ones 101 us for 64 x 224, 109 for 30 x 448, 118 for 31 of 20 x 400; here 41, 43 and 41).  Their columns are padded to sizes that the steps are built for.
 __host__ __device__ inline int pad32(int v) { return (v + 31) & ~31; }
-__host__ __device__ inline bool is_small(int rows, int cols)
+__host__ __device__ inline int small_columns(int mp, int n) { return n <= kSmallN ? pad32(n) : mp == 64 ? (n <= 192 ? 192 : 224) : (n + 63) & ~63; }
+__host__ __device__ inline bool fits_one_workgroup(int rows, int cols)
 {
     const int m = rows < cols ? rows : cols, n = rows < cols ? cols : rows;
-    return m <= kSmallM && n <= kSmallN;
+    return m <= kSmallM && n <= (m <= 32 ? 448 : 224);
 }
-// LDS: X, X^T, B, then A (the waves' blocks to turn over lie over it); G in 32 bits lies over B and A before they are made.
+// LDS: X, X^T, B, then A (the waves' blocks to turn over lie over it); G in 32 bits lies over all but X before they are made.
 __host__ __device__ inline int small_lds(int mp, int np)
 {
     const int turn = 4 * 32 * 33 * 4, square = mp * mp * 4, g = mp * (np + 1) * 4;
-    const int rest = square + (square > turn ? square : turn);
-    return 2 * mp * np * 4 + (rest > g ? rest : g);
+    const int rest = mp * np * 4 + square + (square > turn ? square : turn);
+    return mp * np * 4 + (rest > g ? rest : g);
 }
+constexpr int kSmallLds = 64 * 224 * 8 + 64 * 64 * 4 + 4 * 32 * 33 * 4;   // of 64 x 224, the most
 
 // The lists of such matrices, and what the steps go by (all that this kernel is given: 1.4 KB).
 struct SmallList {
@@ -737,26 +741,34 @@ __device__ __forceinline__ void small_steps(const SmallCall& a, const SmallList&
 #pragma unroll
         for (int e4 = 0; e4 < 4; ++e4) split4(f32x4{v[4 * e4], v[4 * e4 + 1], v[4 * e4 + 2], v[4 * e4 + 3]}, hi[e4], lo[e4]);
     };
-    // blocks of X, then of X^T, one a wave at a time: the 16 bytes of a lane are row `i`, columns j .. of the operand
+    // blocks of X, one a wave at a time: the 16 bytes of a lane are row i, columns j .. of the operand
     constexpr int kBlocks = MB * NB * 2, kRow = NB * 32 + 1;
 #pragma unroll 2
-    for (int u = wave; u < 2 * kBlocks; u += 4) {
-        const bool t = u >= kBlocks;
-        const int block = t ? u - kBlocks : u;
-        const int i = (t ? block / (2 * MB) : block / (2 * NB)) * 32 + l32, j = (t ? block % (2 * MB) : block % (2 * NB)) * 16 + 8 * h;
-        const float* src = t ? g + j * kRow + i : g + i * kRow + j;
-        const int next = t ? kRow : 1;
-        _Float16* to = (t ? XT : X) + block * kBlock + lane * 8;
+    for (int block = wave; block < kBlocks; block += 4) {
+        const float* src = g + (block / (2 * NB) * 32 + l32) * kRow + block % (2 * NB) * 16 + 8 * h;
+        _Float16* to = X + block * kBlock + lane * 8;
 #pragma unroll
         for (int q = 0; q < 2; ++q) {
-            f32x4 w;
-#pragma unroll
-            for (int e = 0; e < 4; ++e) w[e] = f(src[(4 * q + e) * next]);
             half4 wh, wl;
-            split4(w, wh, wl);
+            split4(f32x4{f(src[4 * q]), f(src[4 * q + 1]), f(src[4 * q + 2]), f(src[4 * q + 3])}, wh, wl);
             *(half4*)(to + 4 * q) = wh;
             *(half4*)(to + 512 + 4 * q) = wl;
         }
+    }
+    __syncthreads();   // (X^T lies where G was)
+#pragma unroll 2
+    for (int block = wave; block < kBlocks; block += 4) {
+        // row j of X^T, columns i .. i + 7: column j of X, whose rows lie 16 bytes apart
+        const int j = block / (2 * MB) * 32 + l32, i = block % (2 * MB) * 16 + 8 * h;
+        const _Float16* src = X + ((i >> 5) * 2 * NB + (j >> 4)) * kBlock + ((i & 31) + ((j & 8) << 2)) * 8 + (j & 7);
+        half8 wh, wl;
+#pragma unroll
+        for (int e = 0; e < 8; ++e) {
+            wh[e] = src[e * 8];
+            wl[e] = src[e * 8 + 512];
+        }
+        *(half8*)(XT + block * kBlock + lane * 8) = wh;
+        *(half8*)(XT + block * kBlock + 512 + lane * 8) = wl;
     }
     float diagonal[16];   // 1 on it
 #pragma unroll
@@ -851,6 +863,7 @@ __device__ __forceinline__ void small_steps(const SmallCall& a, const SmallList&
     }
 }
 
+template <bool LONG>
 __global__ __launch_bounds__(kThreads) void orth_small_kernel(SmallCall a)
 {
     extern __shared__ char small_bytes[];
@@ -865,17 +878,17 @@ __global__ __launch_bounds__(kThreads) void orth_small_kernel(SmallCall a)
             matrix = (int)blockIdx.x - a.first[i];
         }
     const SmallList& l = a.l[list];
-    const int m = l.m, n = l.n, mp = pad32(m), np = pad32(n);
+    const int m = l.m, n = l.n, mp = pad32(m), np = small_columns(mp, n);
     _Float16* X = (_Float16*)small_bytes;
     _Float16* XT = X + 2 * mp * np;
     _Float16* B = XT + 2 * mp * np;
     _Float16* A = B + 2 * mp * mp;
-    float* g = (float*)B;   // [mp][np + 1], X's order
+    float* g = (float*)XT;   // [mp][np + 1], X's order
     const int wave = threadIdx.x >> 6, lane = threadIdx.x & 63;
     const size_t from = (size_t)matrix * l.rows * l.cols;
     // G: a thread has four columns of every kPasses-th group of rows
-    constexpr int kPasses = kSmallM * kSmallN / (4 * kThreads);
-    const int shift = l.cols > 64 ? 5 : l.cols > 32 ? 4 : 3;
+    constexpr int kPasses = LONG ? 16 : 8;   // 32 x 448 in rows of 128 lanes, 64 x 224 in rows of 64; 64 x 128 in rows of 32
+    const int shift = l.cols > 256 ? 7 : l.cols > 128 ? 6 : l.cols > 64 ? 5 : l.cols > 32 ? 4 : 3;
     const int c0 = (threadIdx.x & ((1 << shift) - 1)) * 4, r0 = threadIdx.x >> shift, dr = kThreads >> shift;
     const int left = l.cols - c0;
     const bool vec4 = l.vec4 && (l.cols & 3) == 0;
@@ -925,14 +938,26 @@ __global__ __launch_bounds__(kThreads) void orth_small_kernel(SmallCall a)
     if (threadIdx.x < LP_ORTH_MAX_STEPS * 5) scales[threadIdx.x] = my_scale;
     __syncthreads();
     const Scale f = scale_of(sums[0] + sums[1] + sums[2] + sums[3], a.eps, a.load);
-    switch (mp / 32 * 4 + np / 32) {
-        case 4 + 1: small_steps<1, 1>(a, l, a.steps, scales, X, XT, B, A, g, f, from); break;
-        case 4 + 2: small_steps<1, 2>(a, l, a.steps, scales, X, XT, B, A, g, f, from); break;
-        case 4 + 3: small_steps<1, 3>(a, l, a.steps, scales, X, XT, B, A, g, f, from); break;
-        case 4 + 4: small_steps<1, 4>(a, l, a.steps, scales, X, XT, B, A, g, f, from); break;
-        case 8 + 2: small_steps<2, 2>(a, l, a.steps, scales, X, XT, B, A, g, f, from); break;
-        case 8 + 3: small_steps<2, 3>(a, l, a.steps, scales, X, XT, B, A, g, f, from); break;
-        case 8 + 4: small_steps<2, 4>(a, l, a.steps, scales, X, XT, B, A, g, f, from); break;
+    if constexpr (LONG) {
+        switch (mp / 32 * 16 + np / 32) {
+            case 22: small_steps<1, 6>(a, l, a.steps, scales, X, XT, B, A, g, f, from); break;
+            case 24: small_steps<1, 8>(a, l, a.steps, scales, X, XT, B, A, g, f, from); break;
+            case 26: small_steps<1, 10>(a, l, a.steps, scales, X, XT, B, A, g, f, from); break;
+            case 28: small_steps<1, 12>(a, l, a.steps, scales, X, XT, B, A, g, f, from); break;
+            case 30: small_steps<1, 14>(a, l, a.steps, scales, X, XT, B, A, g, f, from); break;
+            case 38: small_steps<2, 6>(a, l, a.steps, scales, X, XT, B, A, g, f, from); break;
+            case 39: small_steps<2, 7>(a, l, a.steps, scales, X, XT, B, A, g, f, from); break;
+        }
+    } else {
+        switch (mp / 32 * 16 + np / 32) {
+            case 17: small_steps<1, 1>(a, l, a.steps, scales, X, XT, B, A, g, f, from); break;
+            case 18: small_steps<1, 2>(a, l, a.steps, scales, X, XT, B, A, g, f, from); break;
+            case 19: small_steps<1, 3>(a, l, a.steps, scales, X, XT, B, A, g, f, from); break;
+            case 20: small_steps<1, 4>(a, l, a.steps, scales, X, XT, B, A, g, f, from); break;
+            case 34: small_steps<2, 2>(a, l, a.steps, scales, X, XT, B, A, g, f, from); break;
+            case 35: small_steps<2, 3>(a, l, a.steps, scales, X, XT, B, A, g, f, from); break;
+            case 36: small_steps<2, 4>(a, l, a.steps, scales, X, XT, B, A, g, f, from); break;
+        }
     }
 }
 
@@ -948,6 +973,7 @@ struct HostList {
     void* out;
     float* momentum;
     int dtype;
+    bool small;   // one workgroup does all of a matrix
 };
 
 size_t matrix_halves(int rows, int cols)
@@ -965,12 +991,27 @@ lp_status check_shape(long long count, int rows, int cols, int index)
     return LP_OK;
 }
 
+// Which matrices one workgroup does.  Those of at most 64 x 128 always; longer ones (41 us a call, however few) unless other lists of
+// the call need the large matrices' launches anyway, where a few more tiles cost next to nothing: 500 matrices of 64 x 200 take 295
+// us there and 93 in one workgroup each, so from about 100 on they are kept apart.
+void choose_kernels(std::vector<HostList>* v)
+{
+    bool large = false;
+    long long longer = 0;
+    for (const HostList& q : *v) {
+        if (!fits_one_workgroup(q.rows, q.cols)) large = true;
+        else if (std::max(q.rows, q.cols) > kSmallN) longer += q.count;
+    }
+    for (HostList& q : *v)
+        q.small = fits_one_workgroup(q.rows, q.cols) && (std::max(q.rows, q.cols) <= kSmallN || !large || longer >= 100);
+}
+
 // Workspace of a set of at most kMaxLists lists: the norms, then the matrices' planes.
 size_t set_bytes(const std::vector<HostList>& v, size_t first, size_t end)
 {
     size_t matrices = 0, planes = 0;
     for (size_t k = first; k < end; ++k) {
-        if (is_small(v[k].rows, v[k].cols)) continue;
+        if (v[k].small) continue;
         matrices += (size_t)v[k].count;
         planes += (size_t)v[k].count * align256(matrix_halves(v[k].rows, v[k].cols) * 2);
     }
@@ -990,7 +1031,7 @@ GramPlan plan_gram(const std::vector<HostList>& v, size_t first, size_t end)
     std::memset(&g, 0, sizeof(g));
     long long large = 0, steps = 0;
     for (size_t k = first; k < end; ++k) {
-        if (is_small(v[k].rows, v[k].cols)) continue;
+        if (v[k].small) continue;
         const long long mp = pad(v[k].rows < v[k].cols ? v[k].rows : v[k].cols), np = pad(v[k].rows < v[k].cols ? v[k].cols : v[k].rows);
         const long long t128 = (mp + 127) / 128, t64 = mp / 64;
         large += v[k].count * (t128 * (t128 + 1) / 2);
@@ -1007,7 +1048,7 @@ GramPlan plan_gram(const std::vector<HostList>& v, size_t first, size_t end)
     const long long even = (steps + 2 * kUnits - 1) / (2 * kUnits);
     g.chunk = (int)((even > 32 ? even + 3 : 32) / 4 * 4);   // (shortest parts of 16, 32, 64 steps: 279, 247, 265 us for the weights of ten convolutions)
     for (size_t k = first; k < end; ++k) {
-        if (is_small(v[k].rows, v[k].cols)) continue;
+        if (v[k].small) continue;
         const long long mp = pad(v[k].rows < v[k].cols ? v[k].rows : v[k].cols), np = pad(v[k].rows < v[k].cols ? v[k].cols : v[k].rows);
         const int s = (int)((np / kDepth + g.chunk - 1) / g.chunk);
         g.splits[k - first] = s;
@@ -1156,15 +1197,17 @@ lp_status run_set(const std::vector<HostList>& v, size_t first, size_t end, cons
     }
     size_t matrices = 0;
     for (size_t k = first; k < end; ++k)
-        if (!is_small(v[k].rows, v[k].cols)) matrices += (size_t)v[k].count;
+        if (!v[k].small) matrices += (size_t)v[k].count;
     const size_t lists_at = align256(matrices * kNormChunks * sizeof(double));
     char* at = (char*)workspace + lists_at + align256(sizeof(Lists));
     const GramPlan gram = plan_gram(v, first, end);
-    SmallCall small;
-    std::memset(&small, 0, sizeof(small));
-    small.lr_decay = a.lr_decay; small.mu = a.mu; small.nesterov = a.nesterov; small.eps = eps;
-    int lds = 0, small_matrices = 0;
-    for (int k = 0; k < kMaxLists; ++k) small.first[k] = INT_MAX;
+    SmallCall smalls[2];   // up to 64 x 128, longer ones
+    int lds[2] = {0, 0}, small_matrices[2] = {0, 0};
+    for (SmallCall& small : smalls) {
+        std::memset(&small, 0, sizeof(small));
+        small.lr_decay = a.lr_decay; small.mu = a.mu; small.nesterov = a.nesterov; small.eps = eps;
+        for (int k = 0; k < kMaxLists; ++k) small.first[k] = INT_MAX;
+    }
     for (size_t k = first; k < end; ++k) {
         const HostList& q = v[k];
         const int tall = q.rows > q.cols, m = tall ? q.cols : q.rows, n = tall ? q.rows : q.cols;
@@ -1175,11 +1218,13 @@ lp_status run_set(const std::vector<HostList>& v, size_t first, size_t end, cons
             step = (float)(muon->lr * (muon->scale == LP_MUON_SCALE_ASPECT ? sqrt(ratio > 1.0 ? ratio : 1.0)
                                      : muon->scale == LP_MUON_SCALE_RMS ? 0.2 * sqrt((double)n) : 1.0));
         }
-        if (is_small(q.rows, q.cols)) {
-            small.first[small.n] = small_matrices;
+        if (q.small) {
+            const int which = n > kSmallN;
+            SmallCall& small = smalls[which];
+            small.first[small.n] = small_matrices[which];
             small.l[small.n++] = {q.in, q.out, q.momentum, q.rows, q.cols, m, n, tall, q.dtype, aligned, step};
-            small_matrices += (int)q.count;
-            lds = std::max(lds, small_lds(pad32(m), pad32(n)));
+            small_matrices[which] += (int)q.count;
+            lds[which] = std::max(lds[which], small_lds(pad32(m), small_columns(pad32(m), n)));
             continue;
         }
         List& l = a.l[a.n++];
@@ -1195,9 +1240,11 @@ lp_status run_set(const std::vector<HostList>& v, size_t first, size_t end, cons
         l.first_matrix = a.matrices;
         a.matrices += l.count;
     }
-    if (small.n) {
-        const hipError_t e = hipFuncSetAttribute((const void*)orth_small_kernel, hipFuncAttributeMaxDynamicSharedMemorySize,
-                                                 small_lds(kSmallM, kSmallN));   // (the same from every thread)
+    for (int which = 0; which < 2; ++which) {
+        SmallCall& small = smalls[which];
+        if (!small.n) continue;
+        const void* kernel = which ? (const void*)orth_small_kernel<true> : (const void*)orth_small_kernel<false>;
+        const hipError_t e = hipFuncSetAttribute(kernel, hipFuncAttributeMaxDynamicSharedMemorySize, kSmallLds);   // (the same from every thread)
         if (e != hipSuccess) return fail(LP_ERR_HIP, std::string("hipFuncSetAttribute(orth_small_kernel): ") + hipGetErrorString(e));
         small.load = plan.load;
         small.steps = plan.steps;
@@ -1205,7 +1252,8 @@ lp_status run_set(const std::vector<HostList>& v, size_t first, size_t end, cons
             const float w[5] = {plan.gram[k].acc, plan.poly[k].acc, plan.poly[k].diag, plan.poly[k].lin, plan.update[k].acc};
             std::memcpy(small.v[k], w, sizeof(w));
         }
-        hipLaunchKernelGGL(orth_small_kernel, dim3(small_matrices), dim3(kThreads), lds, s, small);
+        if (which) hipLaunchKernelGGL(orth_small_kernel<true>, dim3(small_matrices[which]), dim3(kThreads), lds[which], s, small);
+        else hipLaunchKernelGGL(orth_small_kernel<false>, dim3(small_matrices[which]), dim3(kThreads), lds[which], s, small);
     }
     if (a.n == 0) return launched("orthogonalisation launch");
     a.parts = (float*)at;
@@ -1313,8 +1361,9 @@ lp_status collect(int32_t n, const lp_matrices* lists, bool pointers, std::vecto
             return fail(LP_ERR_INVALID_ARG, "lists[" + std::to_string(k) + "].dtype must be LP_F32, LP_BF16 or LP_F16");
         if (!q.count || !q.rows || !q.cols) continue;
         if (pointers && (!q.in || !q.out)) return fail(LP_ERR_INVALID_ARG, "lists[" + std::to_string(k) + "] has a NULL tensor");
-        v->push_back({q.count, q.rows, q.cols, q.in, q.out, nullptr, q.dtype});
+        v->push_back({q.count, q.rows, q.cols, q.in, q.out, nullptr, q.dtype, false});
     }
+    choose_kernels(v);
     return LP_OK;
 }
 
@@ -1329,8 +1378,9 @@ lp_status collect(int32_t n, const lp_muon_weights* lists, bool pointers, std::v
         if (!q.count || !q.rows || !q.cols) continue;
         if (pointers && (!q.weight || !q.grad || !q.momentum))
             return fail(LP_ERR_INVALID_ARG, "lists[" + std::to_string(k) + "] has a NULL tensor");
-        v->push_back({q.count, q.rows, q.cols, q.grad, q.weight, q.momentum, LP_F32});
+        v->push_back({q.count, q.rows, q.cols, q.grad, q.weight, q.momentum, LP_F32, false});
     }
+    choose_kernels(v);
     return LP_OK;
 }
 

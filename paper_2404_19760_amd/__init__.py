@@ -930,8 +930,9 @@ def group_norm_fwd(norm: GroupNorm, x: torch.Tensor, dtype=None):
     y = torch.empty(x.shape, dtype=x.dtype if dtype is None else dtype, device=x.device)
     stats = torch.empty((q.N, q.G, 2), device=x.device, dtype=torch.float32)
     n = _norm_bytes(q)[0]
-    ws = torch.empty(n, dtype=torch.uint8, device=x.device).data_ptr() if n else None
-    _check(_lib.lp_group_norm_fwd(C.byref(q), x.data_ptr(), y.data_ptr(), stats.data_ptr(), ws, n, _stream_ptr(None)))
+    ws = torch.empty(n, dtype=torch.uint8, device=x.device) if n else None   # (held until the kernels are enqueued)
+    _check(_lib.lp_group_norm_fwd(C.byref(q), x.data_ptr(), y.data_ptr(), stats.data_ptr(), ws.data_ptr() if n else None, n,
+                                  _stream_ptr(None)))
     return y, stats
 
 
@@ -942,9 +943,9 @@ def group_norm_bwd(norm: GroupNorm, x: torch.Tensor, stats: torch.Tensor, d_y: t
     d_params = torch.zeros((2, q.C), dtype=torch.float32, device=x.device)
     at = d_params.data_ptr()
     n = _norm_bytes(q)[1]
-    ws = torch.empty(n, dtype=torch.uint8, device=x.device).data_ptr() if n else None
+    ws = torch.empty(n, dtype=torch.uint8, device=x.device) if n else None   # (held until the kernels are enqueued)
     _check(_lib.lp_group_norm_bwd(C.byref(q), x.data_ptr(), _dev_f32(stats, "stats", (q.N, q.G, 2)), d_y.data_ptr(), d_x.data_ptr(),
-                                  at, at + 4 * q.C, ws, n, _stream_ptr(None)))
+                                  at, at + 4 * q.C, ws.data_ptr() if n else None, n, _stream_ptr(None)))
     d_gamma, d_beta = d_params.unbind(0)
     return d_x, d_gamma, d_beta
 

@@ -1,0 +1,59 @@
+"""What the binding of the norm and of the orthogonalised updates does around a library call, on the CPU: the library's functions are
+stood in for by Python functions, tensors that say they are on the GPU lie in host memory."""
+import types
+import weakref
+
+import pytest
+import torch
+
+
+class _Gpu(torch.Tensor):
+    """A host tensor that says it is on the GPU."""
+    is_cuda = True
+
+
+def gpu(t):
+    return torch.Tensor._make_subclass(_Gpu, t)
+
+
+@pytest.fixture()
+def stub(monkeypatch):
+    """The binding with a library whose calls do nothing but what a test puts in their place."""
+    import paper_2404_19760_amd as lp
+
+    def bytes_of_norm(norm, fwd, bwd):
+        fwd._obj.value, bwd._obj.value = 4096, 8192
+        return lp.LP_OK
+
+    lib = types.SimpleNamespace(lp_group_norm_workspace_bytes=bytes_of_norm)
+    monkeypatch.setattr(lp, "_lib", lib)
+    monkeypatch.setattr(lp, "_stream_ptr", lambda stream: None)
+    return lp, lib
+
+
+def test_workspace_of_the_norm_lives_through_the_call(stub, monkeypatch):
+    """The kernels are enqueued inside the call: until it returns nobody else may be given the memory (the call gives up the
+    interpreter's lock, so other threads allocate meanwhile)."""
+    lp, lib = stub
+    allocated, empty = [], torch.empty
+
+    def counted(*args, **kw):
+        t = empty(*args, **kw)
+        if kw.get("dtype") == torch.uint8:
+            allocated.append((weakref.ref(t), t.data_ptr(), t.numel()))
+        return t
+
+    seen = []
+
+    def call(*args):
+        workspace, size = args[-3], args[-2]
+        ref, at, numel = allocated[-1]
+        seen.append((ref() is not None, workspace == at, size == numel))
+        return lp.LP_OK
+
+    lib.lp_group_norm_fwd = lib.lp_group_norm_bwd = call
+    monkeypatch.setattr(torch, "empty", counted)
+    x = gpu(torch.zeros(2, 10, 8))
+    _, stats = lp.group_norm_fwd(lp.GroupNorm(2), x)
+    lp.group_norm_bwd(lp.GroupNorm(2), x, gpu(torch.zeros(2, 2, 2)), x)
+    assert seen == [(True, True, True)] * 2

@@ -58,19 +58,19 @@ def render(grid: Grid, mlp: Mlp, rays: Rays, bg: Sequence[float], math_mode: int
 
 class _GroupNorm(torch.autograd.Function):
     @staticmethod
-    def forward(ctx, spec, x, gamma, beta):
-        groups, act, eps, occupancy, dtype = spec
+    def forward(ctx, spec, x, gamma, beta, occupancy):
+        groups, act, eps, dtype = spec
         detach = lambda t: None if t is None else t.detach()
         norm = GroupNorm(groups, detach(gamma), detach(beta), act, eps, occupancy)
         y, stats = group_norm_fwd(norm, x.detach(), dtype)
-        ctx.save_for_backward(x, gamma, beta, stats)
+        ctx.save_for_backward(x, gamma, beta, occupancy, stats)
         ctx.lp = spec
         return y
 
     @staticmethod
     def backward(ctx, d_y):
-        groups, act, eps, occupancy, _ = ctx.lp
-        x, gamma, beta, stats = ctx.saved_tensors
+        groups, act, eps, _ = ctx.lp
+        x, gamma, beta, occupancy, stats = ctx.saved_tensors
         norm = GroupNorm(groups, gamma, beta, act, eps, occupancy)
         need_x, need_gamma, need_beta = ctx.needs_input_grad[1:4]
         d_y = d_y.contiguous()
@@ -80,11 +80,11 @@ class _GroupNorm(torch.autograd.Function):
         n = lp_group_norm_workspace_bytes(norm, x, d_y.dtype)[1]
         ws = torch.empty(n, dtype=torch.uint8, device=x.device) if n else None
         lp_group_norm_bwd(norm, x, stats, d_y, d_x, d_gamma, d_beta, ws)
-        return None, d_x, d_gamma, d_beta
+        return None, d_x, d_gamma, d_beta, None
 
 
 def group_norm(x: torch.Tensor, groups: int, gamma: Optional[torch.Tensor] = None, beta: Optional[torch.Tensor] = None,
                act: int = LP_ACT_NONE, eps: float = 1e-5, occupancy: Optional[torch.Tensor] = None, dtype=None) -> torch.Tensor:
     """Differentiable group norm with an activation of a channel-last tensor [N][...][C] (see GroupNorm; dtype: of the result);
     gradients flow to x, gamma and beta."""
-    return _GroupNorm.apply((int(groups), int(act), float(eps), occupancy, dtype), x, gamma, beta)
+    return _GroupNorm.apply((int(groups), int(act), float(eps), dtype), x, gamma, beta, occupancy)

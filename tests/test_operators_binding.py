@@ -7,15 +7,6 @@ import pytest
 import torch
 
 
-class _Gpu(torch.Tensor):
-    """A host tensor that says it is on the GPU."""
-    is_cuda = True
-
-
-def gpu(t):
-    return torch.Tensor._make_subclass(_Gpu, t)
-
-
 @pytest.fixture()
 def stub(monkeypatch):
     """The binding with a library whose calls do nothing but what a test puts in their place."""
@@ -28,6 +19,7 @@ def stub(monkeypatch):
     lib = types.SimpleNamespace(lp_group_norm_workspace_bytes=bytes_of_norm)
     monkeypatch.setattr(lp, "_lib", lib)
     monkeypatch.setattr(lp, "_stream_ptr", lambda stream: None)
+    monkeypatch.setattr(torch.Tensor, "is_cuda", True, raising=False)
     return lp, lib
 
 
@@ -53,7 +45,26 @@ def test_workspace_of_the_norm_lives_through_the_call(stub, monkeypatch):
 
     lib.lp_group_norm_fwd = lib.lp_group_norm_bwd = call
     monkeypatch.setattr(torch, "empty", counted)
-    x = gpu(torch.zeros(2, 10, 8))
+    x = torch.zeros(2, 10, 8)
     _, stats = lp.group_norm_fwd(lp.GroupNorm(2), x)
-    lp.group_norm_bwd(lp.GroupNorm(2), x, gpu(torch.zeros(2, 2, 2)), x)
+    lp.group_norm_bwd(lp.GroupNorm(2), x, torch.zeros(2, 2, 2), x)
     assert seen == [(True, True, True)] * 2
+
+
+def _norm_calls_do_nothing(lp, lib):
+    lib.lp_group_norm_fwd = lib.lp_group_norm_bwd = lambda *args: lp.LP_OK
+
+
+def test_occupancy_that_changes_before_the_backward_is_an_error(stub):
+    """A weight buffer that is splatted into again between forward and backward: the gradients would be those of another norm."""
+    lp, lib = stub
+    from paper_2404_19760_amd import autograd as lpa
+    _norm_calls_do_nothing(lp, lib)
+    x = torch.randn(1, 10, 8, requires_grad=True)
+    occupancy = torch.ones(1, 10)
+    y = lpa.group_norm(x, 2, occupancy=occupancy)
+    y.sum().backward()
+    y = lpa.group_norm(x, 2, occupancy=occupancy)
+    occupancy.zero_()
+    with pytest.raises(RuntimeError, match="modified by an inplace operation"):
+        y.sum().backward()

@@ -3,10 +3,12 @@ library's kernels.
 
 render: the Renderer's two entry points; the forward keeps one scalar per ray (Section 3.4: the backward recomputes the
 rest), the backward calls lp_render_bwd.  No gradient flows to the rays (the library produces none).
-group_norm: group norm with an activation over channel-last grids; the forward keeps its input and two numbers a group."""
+group_norm: group norm with an activation over channel-last grids; the forward keeps its input, the occupancy and two
+numbers a group; first derivatives alone."""
 from typing import List, Optional, Sequence
 
 import torch
+from torch.autograd.function import once_differentiable
 
 from . import (LP_ACT_NONE, LP_MATH_DEFAULT, Grid, GroupNorm, Mlp, Rays, group_norm_fwd, lp_bwd_workspace_bytes,
                lp_group_norm_bwd, lp_group_norm_workspace_bytes, lp_render_bwd, lp_render_fwd)
@@ -68,6 +70,7 @@ class _GroupNorm(torch.autograd.Function):
         return y
 
     @staticmethod
+    @once_differentiable   # (the kernels' results carry no graph: second derivatives are refused)
     def backward(ctx, d_y):
         groups, act, eps, _ = ctx.lp
         x, gamma, beta, occupancy, stats = ctx.saved_tensors

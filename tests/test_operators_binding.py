@@ -68,3 +68,16 @@ def test_occupancy_that_changes_before_the_backward_is_an_error(stub):
     occupancy.zero_()
     with pytest.raises(RuntimeError, match="modified by an inplace operation"):
         y.sum().backward()
+
+
+def test_second_derivatives_of_the_norm_are_an_error(stub):
+    """The backward's kernels are not differentiable: where another path exists, a gradient penalty would lose its term without a word."""
+    lp, lib = stub
+    from paper_2404_19760_amd import autograd as lpa
+    _norm_calls_do_nothing(lp, lib)
+    x, gamma = torch.randn(1, 10, 8, requires_grad=True), torch.ones(8, requires_grad=True)
+    y = lpa.group_norm(x, 2, gamma)
+    d_x, d_gamma = torch.autograd.grad(y.sum(), (x, gamma), create_graph=True)
+    for d in (d_x, d_gamma):
+        with pytest.raises(RuntimeError, match="once_differentiable"):
+            (d.square().sum() + x.square().sum()).backward()

@@ -8,10 +8,31 @@ numbers a group; first derivatives alone."""
 from typing import List, Optional, Sequence
 
 import torch
-from torch.autograd.function import once_differentiable
 
 from . import (LP_ACT_NONE, LP_MATH_DEFAULT, Grid, GroupNorm, Mlp, Rays, group_norm_fwd, lp_bwd_workspace_bytes,
                lp_group_norm_bwd, lp_group_norm_workspace_bytes, lp_render_bwd, lp_render_fwd)
+
+
+class _First(torch.autograd.Function):
+    """Results of a backward that is not differentiable itself, where a graph of it is asked for (create_graph): derivatives of
+    them are an error.  (torch's once_differentiable sees to that only where the upstream gradient has a graph; a gradient
+    penalty's has none, its second derivatives come from the inputs.)"""
+    @staticmethod
+    def forward(ctx, count, *tensors):
+        return tuple(t.view_as(t) for t in tensors[:count])
+
+    @staticmethod
+    def backward(ctx, *grads):
+        raise RuntimeError("the library's operators have first derivatives alone")
+
+
+def _first(results, inputs):
+    """`results` (None: not wanted), which depend on `inputs` in a way that no graph holds."""
+    if not torch.is_grad_enabled():
+        return results
+    there = [t for t in results if t is not None]
+    marked = iter(_First.apply(len(there), *there, *[t for t in inputs if t is not None]) if there else ())
+    return tuple(None if t is None else next(marked) for t in results)
 
 
 class _Render(torch.autograd.Function):
@@ -70,19 +91,19 @@ class _GroupNorm(torch.autograd.Function):
         return y
 
     @staticmethod
-    @once_differentiable   # (the kernels' results carry no graph: second derivatives are refused)
-    def backward(ctx, d_y):
+    def backward(ctx, upstream):
         groups, act, eps, _ = ctx.lp
         x, gamma, beta, occupancy, stats = ctx.saved_tensors
         norm = GroupNorm(groups, gamma, beta, act, eps, occupancy)
         need_x, need_gamma, need_beta = ctx.needs_input_grad[1:4]
-        d_y = d_y.contiguous()
+        d_y = upstream.contiguous()
         d_x = torch.empty_strided(x.shape, x.stride(), dtype=x.dtype, device=x.device) if need_x else None
         d_gamma = torch.zeros_like(gamma) if need_gamma else None
         d_beta = torch.zeros_like(beta) if need_beta else None
         n = lp_group_norm_workspace_bytes(norm, x, d_y.dtype)[1]
         ws = torch.empty(n, dtype=torch.uint8, device=x.device) if n else None
         lp_group_norm_bwd(norm, x, stats, d_y, d_x, d_gamma, d_beta, ws)
+        d_x, d_gamma, d_beta = _first((d_x, d_gamma, d_beta), (upstream, x, gamma, beta))
         return None, d_x, d_gamma, d_beta, None
 
 

@@ -79,5 +79,5 @@ def test_second_derivatives_of_the_norm_are_an_error(stub):
     y = lpa.group_norm(x, 2, gamma)
     d_x, d_gamma = torch.autograd.grad(y.sum(), (x, gamma), create_graph=True)
     for d in (d_x, d_gamma):
-        with pytest.raises(RuntimeError, match="once_differentiable"):
+        with pytest.raises(RuntimeError, match="first derivatives"):
             (d.square().sum() + x.square().sum()).backward()

@@ -2,7 +2,7 @@
 library's kernels.
 
 render: the Renderer's two entry points; the forward keeps one scalar per ray (Section 3.4: the backward recomputes the
-rest), the backward calls lp_render_bwd.  No gradient flows to the rays (the library produces none).
+rest), the backward calls lp_render_bwd.  No gradient flows to the rays (the library produces none); first derivatives alone.
 group_norm: group norm with an activation over channel-last grids; the forward keeps its input, the occupancy and two
 numbers a group; first derivatives alone."""
 from typing import List, Optional, Sequence
@@ -52,6 +52,7 @@ class _Render(torch.autograd.Function):
         cache = torch.empty((m,), dtype=torch.float32, device=dev)
         lp_render_fwd(grid, mlp, rays, bg, rgb, alpha, depth, cache, math_mode)
         ctx.lp = (grid, mlp, rays, bg, math_mode, cache)
+        ctx.inputs = tensors
         ctx.mark_non_differentiable(cache)
         return rgb, alpha, depth
 
@@ -68,7 +69,7 @@ class _Render(torch.autograd.Function):
                       math_mode)
         # gradients of structures stored in reduced precision come back in that type
         d_grid = [g.to(t.dtype) for g, t in zip(d_grid, grid.data)]
-        return (None, None, None, *d_grid, *dW, *db)
+        return (None, None, None, *_first((*d_grid, *dW, *db), (d_rgb, d_alpha, d_depth, *ctx.inputs)))
 
 
 def render(grid: Grid, mlp: Mlp, rays: Rays, bg: Sequence[float], math_mode: int = LP_MATH_DEFAULT):

@@ -81,3 +81,31 @@ def test_second_derivatives_of_the_norm_are_an_error(stub):
     for d in (d_x, d_gamma):
         with pytest.raises(RuntimeError, match="first derivatives"):
             (d.square().sum() + x.square().sum()).backward()
+
+
+def test_second_derivatives_of_the_renderer_are_an_error(stub):
+    """The same of the Renderer, for its grid, weights and biases."""
+    lp, lib = stub
+    from paper_2404_19760_amd import autograd as lpa
+
+    def bytes_of_backward(*args):
+        args[-1]._obj.value = 4096
+        return lp.LP_OK
+
+    lib.lp_bwd_workspace_bytes = bytes_of_backward
+    lib.lp_render_fwd = lib.lp_render_bwd = lambda *args: lp.LP_OK
+    data = torch.randn(1, 4, 4, 4, 16, requires_grad=True)
+    weights = [torch.randn(*s, requires_grad=True) for s in ((32, 16), (4, 32))]
+    biases = [torch.randn(s, requires_grad=True) for s in (32, 4)]
+    one = torch.ones(5)
+    rays = lp.Rays(torch.zeros(5, 3), torch.ones(5, 3), one, 2 * one, 8)
+    rgb, alpha, depth = lpa.render(lp.Grid(lp.LP_GRID_VOXEL, [data], (4, 4, 4)), lp.Mlp(weights, biases), rays, (0.0, 0.0, 0.0))
+    inputs = [data, *weights, *biases]
+    grads = torch.autograd.grad(rgb.sum() + alpha.sum(), inputs, create_graph=True)
+    for d in grads:
+        with pytest.raises(RuntimeError, match="first derivatives"):
+            (d.square().sum() + sum(t.square().sum() for t in inputs)).backward(retain_graph=True)
+    for t in inputs:
+        t.grad = None
+    (rgb.sum() + depth.sum()).backward()
+    assert all(t.grad is not None for t in inputs)

@@ -16,6 +16,7 @@ from typing import List, Optional, Sequence
 
 import numpy as np
 import torch
+from torch.autograd.graph import increment_version
 
 _HERE = os.path.dirname(os.path.abspath(__file__))
 LIB_PATH = os.environ.get("LP_LIB_PATH", os.path.join(_HERE, "liblightplane.so"))
@@ -621,6 +622,11 @@ def lp_splat_bwd(target: _Grid, rays: Rays, splat: Splat, theta_w: List[torch.Te
     del keep
 
 
+def _written(*tensors: Optional[torch.Tensor]) -> None:
+    """Moves the versions of tensors that a call wrote through their addresses: a graph that has saved one of them notices."""
+    increment_version([t for t in tensors if t is not None])
+
+
 @dataclasses.dataclass
 class GroupNorm:
     """Group norm with an activation over channel-last tensors [N][...][C] (a voxel grid [B][NX][NY][NZ][C], a plane
@@ -709,6 +715,7 @@ def lp_group_norm_fwd(norm: GroupNorm, x: torch.Tensor, y: torch.Tensor, stats: 
     wp, wn = _workspace(workspace)
     _check(_lib.lp_group_norm_fwd(C.byref(q), x.data_ptr(), y.data_ptr(), _dev_f32(stats, "stats", (x.shape[0], norm.groups, 2)),
                                   wp, wn, _stream_ptr(stream)))
+    _written(y, stats)
 
 
 def lp_group_norm_bwd(norm: GroupNorm, x: torch.Tensor, stats: torch.Tensor, d_y: torch.Tensor, d_x: Optional[torch.Tensor],
@@ -727,6 +734,7 @@ def lp_group_norm_bwd(norm: GroupNorm, x: torch.Tensor, stats: torch.Tensor, d_y
     _check(_lib.lp_group_norm_bwd(C.byref(q), x.data_ptr(), _dev_f32(stats, "stats", (x.shape[0], norm.groups, 2)), d_y.data_ptr(),
                                   None if d_x is None else d_x.data_ptr(), _dev_f32(d_gamma, "d_gamma", c),
                                   _dev_f32(d_beta, "d_beta", c), wp, wn, _stream_ptr(stream)))
+    _written(d_x, d_gamma, d_beta)
 
 
 def _matrix_shape(t: torch.Tensor, name: str, k: int):
@@ -776,6 +784,7 @@ def lp_orthogonalize(mats: Sequence[torch.Tensor], outs: Sequence[torch.Tensor],
     arr, o = _matrices(mats, outs), _orth(steps, coeffs, eps)
     wp, wn = _workspace(workspace)
     _check(_lib.lp_orthogonalize(len(mats), arr, C.byref(o), wp, wn, _stream_ptr(stream)))
+    _written(*outs)
 
 
 def _muon_weights(weights, grads, momenta):
@@ -804,6 +813,7 @@ def lp_muon_step(weights: Sequence[torch.Tensor], grads: Sequence[torch.Tensor],
     q = _Muon(float(lr), float(momentum), float(weight_decay), int(nesterov), int(scale), _orth(steps, coeffs, eps))
     wp, wn = _workspace(workspace)
     _check(_lib.lp_muon_step(len(weights), arr, C.byref(q), wp, wn, _stream_ptr(stream)))
+    _written(*weights, *momenta)
 
 
 # ---------------------------------------------------------------------------------------

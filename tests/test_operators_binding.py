@@ -109,3 +109,50 @@ def test_second_derivatives_of_the_renderer_are_an_error(stub):
         t.grad = None
     (rgb.sum() + depth.sum()).backward()
     assert all(t.grad is not None for t in inputs)
+
+
+def test_what_a_call_writes_counts_as_written(stub):
+    """Tensors written through their addresses move in their version, so that a graph that has saved them notices."""
+    lp, lib = stub
+    _norm_calls_do_nothing(lp, lib)
+    lib.lp_muon_step = lib.lp_orthogonalize = lambda *args: lp.LP_OK
+
+    def moved(call, written, read):
+        before = [t._version for t in (*written, *read)]
+        call()
+        after = [t._version for t in (*written, *read)]
+        assert after == [b + (k < len(written)) for k, b in enumerate(before)]
+
+    w, g, m = ([torch.zeros(4, 4) for _ in range(2)] for _ in range(3))
+    ws = torch.zeros(16, dtype=torch.uint8)
+    moved(lambda: lp.lp_muon_step([t.detach() for t in w], g, m, ws, lr=0.1), w + m, g)
+    moved(lambda: lp.lp_orthogonalize(g, m, ws), m, g)
+    moved(lambda: lp.lp_orthogonalize(g, g, ws), g, m)
+    x, y, d_x, stats, gamma, beta = torch.zeros(2, 10, 8), torch.zeros(2, 10, 8), torch.zeros(2, 10, 8), torch.zeros(2, 2, 2), torch.zeros(8), torch.zeros(8)
+    norm = lp.GroupNorm(2)
+    moved(lambda: lp.lp_group_norm_fwd(norm, x, y, stats, None), [y, stats], [x])
+    moved(lambda: lp.lp_group_norm_fwd(norm, x, x, None, None), [x], [])
+    moved(lambda: lp.lp_group_norm_bwd(norm, x, stats, y, d_x, gamma, beta, None), [d_x, gamma, beta], [x, stats, y])
+    moved(lambda: lp.lp_group_norm_bwd(norm, x, stats, y, None, None, beta, None), [beta], [x, stats, y])
+    with torch.inference_mode():   # (tensors without a version)
+        w, g, m = ([torch.zeros(4, 4)] for _ in range(3))
+    lp.lp_muon_step(w, g, m, ws, lr=0.1)
+
+
+def test_a_graph_notices_a_step_of_the_optimiser(stub):
+    """The backward of a graph that was kept over the step would use the new weights as if they were the old ones."""
+    lp, lib = stub
+    from paper_2404_19760_amd.optim import Muon
+
+    def bytes_of_step(n, lists, size):
+        size._obj.value = 256
+        return lp.LP_OK
+
+    lib.lp_muon_workspace_bytes, lib.lp_muon_step = bytes_of_step, lambda *args: lp.LP_OK
+    w = torch.randn(4, 4, requires_grad=True)
+    x = torch.randn(3, 4, requires_grad=True)
+    loss = (x @ w).square().sum()
+    loss.backward(retain_graph=True)
+    Muon([w]).step()
+    with pytest.raises(RuntimeError, match="modified by an inplace operation"):
+        loss.backward()

@@ -683,16 +683,23 @@ def _channel_last(t: torch.Tensor, name: str, shape, dtype):
     return _position_stride(t, name)
 
 
-def _no_overlap(written: torch.Tensor, read: torch.Tensor, written_name: str, read_name: str) -> None:
-    """A tensor that is written is the one that is read or lies apart from it."""
-    if written.numel() == 0 or read.numel() == 0 or (written.data_ptr() == read.data_ptr() and written.dtype == read.dtype
-                                                    and written.stride() == read.stride()):
+def _no_overlap(written: torch.Tensor, written_step: int, read: torch.Tensor, read_step: int, written_name: str, read_name: str) -> None:
+    """A tensor that is written is the one that is read or shares no value with it (channels of a wider tensor may lie between
+    another one's).  The steps are those from position to position."""
+    if written.numel() == 0:
         return
-    end = lambda t: t.data_ptr() + t.element_size() * (1 + sum((n - 1) * s for n, s in zip(t.shape, t.stride())))
-    if written.untyped_storage().data_ptr() == read.untyped_storage().data_ptr() and \
-            written.data_ptr() < end(read) and read.data_ptr() < end(written) and \
-            (written.is_contiguous() or read.is_contiguous()):
-        raise ValueError(f"{written_name} must be {read_name} itself or not overlap it")
+    a, b, c, count = written.data_ptr(), read.data_ptr(), written.shape[-1], written.numel() // written.shape[-1]
+    if a == b and written_step == read_step and written.dtype == read.dtype:
+        return
+    a_size, b_size = written.element_size(), read.element_size()
+    a_step, b_step, a_width, b_width = written_step * a_size, read_step * b_size, c * a_size, c * b_size
+    if a + (count - 1) * a_step + a_width <= b or b + (count - 1) * b_step + b_width <= a:
+        return
+    if a_step == b_step:   # position j of `read` starts `behind` bytes behind position j + rows of `written`
+        rows, behind = divmod(b - a, a_step)
+        if not (behind < a_width and abs(rows) < count) and not (behind + b_width > a_step and abs(rows + 1) < count):
+            return
+    raise ValueError(f"{written_name} must be {read_name} itself or not overlap it")
 
 
 def _norm_bytes(q: _GroupNorm):
@@ -711,7 +718,7 @@ def lp_group_norm_fwd(norm: GroupNorm, x: torch.Tensor, y: torch.Tensor, stats: 
     """Enqueue the forward: y (shape of x; its type, or a 16-bit one where x is float32) and stats [N][groups][2] (None:
     not wanted) are written."""
     q = norm.c_struct(x, y.dtype, _channel_last(y, "y", x.shape, y.dtype))
-    _no_overlap(y, x, "y", "x")
+    _no_overlap(y, q.y_stride, x, q.x_stride, "y", "x")
     wp, wn = _workspace(workspace)
     _check(_lib.lp_group_norm_fwd(C.byref(q), x.data_ptr(), y.data_ptr(), _dev_f32(stats, "stats", (x.shape[0], norm.groups, 2)),
                                   wp, wn, _stream_ptr(stream)))
@@ -727,8 +734,8 @@ def lp_group_norm_bwd(norm: GroupNorm, x: torch.Tensor, stats: torch.Tensor, d_y
     if d_x is not None:
         if _channel_last(d_x, "d_x", x.shape, x.dtype) != q.x_stride:
             raise ValueError("d_x must have the strides of x")
-        _no_overlap(d_x, x, "d_x", "x")
-        _no_overlap(d_x, d_y, "d_x", "d_y")
+        _no_overlap(d_x, q.x_stride, x, q.x_stride, "d_x", "x")
+        _no_overlap(d_x, q.x_stride, d_y, q.y_stride, "d_x", "d_y")
     c = (x.shape[-1],)
     wp, wn = _workspace(workspace)
     _check(_lib.lp_group_norm_bwd(C.byref(q), x.data_ptr(), _dev_f32(stats, "stats", (x.shape[0], norm.groups, 2)), d_y.data_ptr(),

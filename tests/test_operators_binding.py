@@ -156,3 +156,35 @@ def test_a_graph_notices_a_step_of_the_optimiser(stub):
     Muon([w]).step()
     with pytest.raises(RuntimeError, match="modified by an inplace operation"):
         loss.backward()
+
+
+def test_overlap_of_what_is_written_and_what_is_read(stub):
+    """Slices of one tensor that share channels are refused (some threads would read what others have written), slices side by side,
+    tensors behind one another and a tensor itself are taken."""
+    lp, lib = stub
+    _norm_calls_do_nothing(lp, lib)
+    norm = lp.GroupNorm(2)
+    wide = torch.zeros(2, 5, 3, 24)
+    flat = torch.zeros(2 * 5 * 3 * 24)
+    halves = wide.view(torch.bfloat16)   # [..., 48], bytes as in `wide`
+    at = lambda a, c: wide[..., a:a + c]  # noqa: E731
+    lone = torch.zeros(1, 1, 8, 16)
+    taken = [(at(0, 8), at(8, 8)), (at(8, 8), at(0, 8)), (at(0, 12), at(12, 12)), (at(4, 8), at(4, 8)), (wide[:1], wide[1:]), (at(0, 8)[:1], at(4, 8)[1:]),
+             (at(4, 8)[1:], at(0, 8)[:1]), (flat[:80].view(1, 10, 8), flat[80:160].view(1, 10, 8)), (at(0, 8), halves[..., 16:24]),
+             (lone[:, 0], lone[:, 0].as_strided((1, 8, 16), (7, 16, 1)))]
+    refused = [(at(0, 8), at(4, 8)), (at(4, 8), at(0, 8)), (at(0, 8), at(7, 8)), (at(7, 8), at(0, 8)), (at(0, 8)[:1], at(1, 8)[:1]),
+               (at(0, 8)[:1, 1:], at(4, 8)[:1, :-1]), (at(0, 8), halves[..., 14:22]),
+               (at(0, 8), halves[..., 0:8]), (flat[:80].view(1, 10, 8), flat[79:159].view(1, 10, 8)), (flat[8:88].view(1, 10, 8), flat[:80].view(1, 10, 8)),
+               (wide, wide.view(torch.bfloat16)[..., :24]), (flat[:80].view(1, 10, 8), flat[:160].view(1, 10, 16)[..., 8:])]
+    for x, y in taken:
+        lp.lp_group_norm_fwd(norm, x, y, None, None)
+    for x, y in refused:
+        with pytest.raises(ValueError, match="overlap"):
+            lp.lp_group_norm_fwd(norm, x, y, None, None)
+    x, stats = torch.zeros(2, 5, 3, 24)[..., :8], torch.zeros(2, 2, 2)
+    lp.lp_group_norm_bwd(norm, x, stats, at(0, 8), at(0, 8), None, None, None)
+    lp.lp_group_norm_bwd(norm, x, stats, at(0, 8), at(8, 8), None, None, None)
+    with pytest.raises(ValueError, match="overlap"):
+        lp.lp_group_norm_bwd(norm, x, stats, at(0, 8), at(4, 8), None, None, None)
+    with pytest.raises(ValueError, match="overlap"):
+        lp.lp_group_norm_bwd(norm, at(0, 8), stats, x, at(4, 8), None, None, None)

@@ -385,7 +385,8 @@ typedef struct {
 
 /* Orthogonalises n lists of matrices.  `lists` is a HOST array; outputs are WRITTEN.  workspace: device,
    256-byte aligned, contents ignored on entry, undefined on exit.  n == 0 is a no-op, and so is a list with
-   count, rows or cols 0. */
+   count, rows or cols 0.  Lists are worked on at the same time: an out that overlaps another list's in or out,
+   or a part of its own in, is refused. */
 lp_status lp_orthogonalize(int32_t n, const lp_matrices* lists, const lp_orth* orth, void* workspace,
                            size_t workspace_bytes, void* stream);
 /* 0 where all matrices are at most 64 x 224 or 32 x 448, or their transposes (then NULL will do).
@@ -418,7 +419,8 @@ typedef struct {
 
 /* One step over n lists of weights:
      M <- momentum M + G,   U = G + momentum M (nesterov) or M,
-     W <- (1 - lr weight_decay) W - lr s orthogonalised(U). */
+     W <- (1 - lr weight_decay) W - lr s orthogonalised(U).
+   Lists may share a gradient; a weight or momentum that overlaps anything else of the call is refused. */
 lp_status lp_muon_step(int32_t n, const lp_muon_weights* lists, const lp_muon* muon, void* workspace,
                        size_t workspace_bytes, void* stream);
 lp_status lp_muon_workspace_bytes(int32_t n, const lp_muon_weights* lists, size_t* bytes);

@@ -1327,6 +1327,32 @@ lp_status run_set(const std::vector<HostList>& v, size_t first, size_t end, cons
     return launched("orthogonalisation launch");
 }
 
+// Whether something that is written lies over something else (but a result over its own list's input).
+bool overlap(const std::vector<HostList>& v)
+{
+    struct Range {
+        uintptr_t from, end;
+        bool written;
+    };
+    std::vector<Range> ranges;
+    ranges.reserve(3 * v.size());
+    for (const HostList& q : v) {
+        const uintptr_t bytes = (uintptr_t)q.count * q.rows * q.cols * (q.dtype == LP_F32 ? 4 : 2);
+        auto add = [&](const void* p, bool written) { ranges.push_back({(uintptr_t)p, (uintptr_t)p + bytes, written}); };
+        add(q.out, true);
+        if (q.momentum) add(q.momentum, true);
+        if (q.momentum || q.in != q.out) add(q.in, false);
+    }
+    std::sort(ranges.begin(), ranges.end(), [](const Range& a, const Range& b) { return a.from < b.from; });
+    uintptr_t all_end = 0, written_end = 0;   // of the ranges before
+    for (const Range& r : ranges) {
+        if (r.from < (r.written ? all_end : written_end)) return true;
+        all_end = std::max(all_end, r.end);
+        if (r.written) written_end = std::max(written_end, r.end);
+    }
+    return false;
+}
+
 lp_status run(const std::vector<HostList>& v, const Plan& plan, float eps, const Muon* muon, void* workspace, size_t workspace_bytes,
               hipStream_t s)
 {
@@ -1336,6 +1362,7 @@ lp_status run(const std::vector<HostList>& v, const Plan& plan, float eps, const
         return fail(LP_ERR_WORKSPACE, "workspace is NULL or smaller than the call's workspace_bytes function says");
     if (need && (uintptr_t)workspace % 256) return fail(LP_ERR_INVALID_ARG, "workspace must be 256-byte aligned");
     // (refused before anything is launched)
+    if (overlap(v)) return fail(LP_ERR_INVALID_ARG, "what a list writes must not overlap another list's tensors or its own (but out may be in)");
     for (size_t k = 0; k < v.size(); k += kMaxLists) {
         double tiles = 0.0;
         for (size_t i = k; i < v.size() && i < k + kMaxLists; ++i)

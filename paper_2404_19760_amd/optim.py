@@ -15,10 +15,12 @@ class Muon(torch.optim.Optimizer):
                  scale: int = LP_MUON_SCALE_ASPECT, steps: int = 5, coeffs=None, eps: float = 1e-7):
         super().__init__(params, dict(lr=lr, momentum=momentum, nesterov=nesterov, weight_decay=weight_decay, scale=scale,
                                       steps=steps, coeffs=coeffs, eps=eps))
-        for group in self.param_groups:
-            for p in group["params"]:
-                if p.dim() < 2 or p.dtype != torch.float32:
-                    raise ValueError("Muon takes float32 matrices [...][rows][cols]")
+
+    def add_param_group(self, param_group):
+        super().add_param_group(param_group)
+        if any(p.dim() < 2 or p.dtype != torch.float32 for p in self.param_groups[-1]["params"]):
+            self.param_groups.pop()
+            raise ValueError("Muon takes float32 matrices [...][rows][cols]")
 
     @torch.no_grad()
     def step(self, closure=None):

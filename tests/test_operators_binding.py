@@ -188,3 +188,17 @@ def test_overlap_of_what_is_written_and_what_is_read(stub):
         lp.lp_group_norm_bwd(norm, x, stats, at(0, 8), at(4, 8), None, None, None)
     with pytest.raises(ValueError, match="overlap"):
         lp.lp_group_norm_bwd(norm, at(0, 8), stats, x, at(4, 8), None, None, None)
+
+
+def test_groups_added_to_the_optimiser_are_checked(stub):
+    """As those given to the constructor: a vector or a 16-bit matrix would end a later step, behind groups that were stepped already."""
+    from paper_2404_19760_amd.optim import Muon
+    opt = Muon([torch.zeros(4, 4)])
+    for bad in ([torch.zeros(8)], [torch.zeros(4, 4), torch.zeros(4, 4, dtype=torch.float16)], torch.zeros(8)):
+        with pytest.raises(ValueError, match="matrices"):
+            opt.add_param_group({"params": bad})
+        assert len(opt.param_groups) == 1
+    opt.add_param_group({"params": [torch.zeros(2, 3, 4)], "lr": 0.5})
+    assert [g["lr"] for g in opt.param_groups] == [0.02, 0.5]
+    with pytest.raises(ValueError, match="matrices"):
+        Muon([{"params": [torch.zeros(4, 4)]}, {"params": [torch.zeros(8)]}])

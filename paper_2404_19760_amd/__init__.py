@@ -769,7 +769,7 @@ def _orth(steps: int, coeffs, eps: float) -> _Orth:
     """(a struct of `steps` steps; coeffs: one (a, b, c) for all steps, one for each, or None)"""
     if coeffs is None:
         return _Orth(int(steps), None, float(eps))
-    rows = [tuple(float(v) for v in r) for r in ([coeffs] * int(steps) if isinstance(coeffs[0], (int, float)) else coeffs)]
+    rows = [tuple(float(v) for v in r) for r in ([coeffs] * int(steps) if len(coeffs) and isinstance(coeffs[0], (int, float)) else coeffs)]
     if len(rows) != steps or any(len(r) != 3 for r in rows):
         raise ValueError("coeffs must be (a, b, c), or one of these for every step")
     flat = (C.c_float * max(1, 3 * len(rows)))(*[v for r in rows for v in r])

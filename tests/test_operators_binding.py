@@ -202,3 +202,10 @@ def test_groups_added_to_the_optimiser_are_checked(stub):
     assert [g["lr"] for g in opt.param_groups] == [0.02, 0.5]
     with pytest.raises(ValueError, match="matrices"):
         Muon([{"params": [torch.zeros(4, 4)]}, {"params": [torch.zeros(8)]}])
+
+
+def test_coefficients_without_any_are_refused(stub):
+    lp, _ = stub
+    for empty in ((), []):
+        with pytest.raises(ValueError, match="every step"):
+            lp._orth(5, empty, 0.0)

@@ -627,6 +627,13 @@ def _written(*tensors: Optional[torch.Tensor]) -> None:
     increment_version([t for t in tensors if t is not None])
 
 
+def _int32(value, name: str) -> int:
+    value = int(value)
+    if not -1 << 31 <= value < 1 << 31:   # (ctypes would cut it off)
+        raise ValueError(f"{name} does not fit 32 bits")
+    return value
+
+
 @dataclasses.dataclass
 class GroupNorm:
     """Group norm with an activation over channel-last tensors [N][...][C] (a voxel grid [B][NX][NY][NZ][C], a plane
@@ -648,7 +655,8 @@ class GroupNorm:
         if len(shape) < 2:
             raise ValueError("x must have a first axis of samples and a last axis of channels")
         n, c = shape[0], shape[-1]
-        return _GroupNorm(n, x.numel() // (n * c) if n and c else 0, c, int(self.groups), int(self.act), float(self.eps),
+        return _GroupNorm(n, x.numel() // (n * c) if n and c else 0, _int32(c, "the number of channels"), _int32(self.groups, "groups"),
+                          _int32(self.act, "act"), float(self.eps),
                           _GRID_DTYPES[x.dtype], _GRID_DTYPES[y_dtype], _position_stride(x, "x"), y_stride,
                           _dev_f32(self.gamma, "gamma", (c,)), _dev_f32(self.beta, "beta", (c,)),
                           _dev_f32(self.occupancy, "occupancy", shape[:-1]))
@@ -748,7 +756,7 @@ def _matrix_shape(t: torch.Tensor, name: str, k: int):
     if not (t.is_cuda and t.is_contiguous() and t.dim() >= 2):
         raise ValueError(f"{name}[{k}] must be a contiguous GPU tensor [...][rows][cols]")
     rows, cols = t.shape[-2], t.shape[-1]
-    return t.numel() // max(1, rows * cols), rows, cols
+    return t.numel() // max(1, rows * cols), _int32(rows, "the number of rows"), _int32(cols, "the number of columns")
 
 
 def _matrices(mats, outs):
@@ -767,13 +775,15 @@ def _matrices(mats, outs):
 
 def _orth(steps: int, coeffs, eps: float) -> _Orth:
     """(a struct of `steps` steps; coeffs: one (a, b, c) for all steps, one for each, or None)"""
+    steps = _int32(steps, "steps")
     if coeffs is None:
-        return _Orth(int(steps), None, float(eps))
-    rows = [tuple(float(v) for v in r) for r in ([coeffs] * int(steps) if len(coeffs) and isinstance(coeffs[0], (int, float)) else coeffs)]
+        return _Orth(steps, None, float(eps))
+    one = len(coeffs) and isinstance(coeffs[0], (int, float))
+    rows = [tuple(float(v) for v in r) for r in ([coeffs] * steps if one else coeffs)]
     if len(rows) != steps or any(len(r) != 3 for r in rows):
         raise ValueError("coeffs must be (a, b, c), or one of these for every step")
     flat = (C.c_float * max(1, 3 * len(rows)))(*[v for r in rows for v in r])
-    o = _Orth(int(steps), flat, float(eps))
+    o = _Orth(steps, flat, float(eps))
     o.keep = flat
     return o
 
@@ -817,7 +827,8 @@ def lp_muon_step(weights: Sequence[torch.Tensor], grads: Sequence[torch.Tensor],
                  scale: int = LP_MUON_SCALE_ASPECT, steps: int = 5, coeffs=None, eps: float = 1e-7, stream=None) -> None:
     """Enqueue one optimiser step: weights and momenta (float32 tensors [...][rows][cols]) are updated in place."""
     arr = _muon_weights(weights, grads, momenta)
-    q = _Muon(float(lr), float(momentum), float(weight_decay), int(nesterov), int(scale), _orth(steps, coeffs, eps))
+    q = _Muon(float(lr), float(momentum), float(weight_decay), _int32(nesterov, "nesterov"), _int32(scale, "scale"),
+              _orth(steps, coeffs, eps))
     wp, wn = _workspace(workspace)
     _check(_lib.lp_muon_step(len(weights), arr, C.byref(q), wp, wn, _stream_ptr(stream)))
     _written(*weights, *momenta)

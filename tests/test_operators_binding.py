@@ -209,3 +209,30 @@ def test_coefficients_without_any_are_refused(stub):
     for empty in ((), []):
         with pytest.raises(ValueError, match="every step"):
             lp._orth(5, empty, 0.0)
+
+
+def test_numbers_beyond_32_bits_are_refused(stub):
+    """The C structs hold 32 bits of them; what is beyond would be cut off without a word (2^32 + 8 columns taken for 8)."""
+    lp, lib = stub
+    _norm_calls_do_nothing(lp, lib)
+    lib.lp_orthogonalize = lib.lp_muon_step = lambda *args: lp.LP_OK
+    meta = lambda *shape: torch.empty(shape, device="meta")  # noqa: E731
+    ws, small = torch.zeros(16, dtype=torch.uint8), meta(4, 4)
+    for big in (meta(2, 2 ** 32 + 8), meta(2 ** 32 + 8, 2), meta(2, 2 ** 31)):
+        with pytest.raises(ValueError, match="32 bits"):
+            lp.lp_orthogonalize([big], [big], ws)
+        with pytest.raises(ValueError, match="32 bits"):
+            lp.lp_muon_step([big], [big], [big], ws, lr=0.1)
+    for kw in (dict(steps=2 ** 32 + 5), dict(steps=2 ** 32 + 5, coeffs=(1.0, 0.0, 0.0)), dict(steps=-2 ** 40)):
+        with pytest.raises(ValueError, match="32 bits"):
+            lp.lp_orthogonalize([small], [small], ws, **kw)
+    for kw in (dict(scale=2 ** 32), dict(nesterov=2 ** 32 + 1)):
+        with pytest.raises(ValueError, match="32 bits"):
+            lp.lp_muon_step([small], [small], [small], ws, lr=0.1, **kw)
+    x = meta(1, 3, 2 ** 32 + 8)
+    with pytest.raises(ValueError, match="32 bits"):
+        lp.lp_group_norm_fwd(lp.GroupNorm(2), x, torch.empty_like(x), None, None)
+    x = meta(1, 3, 8)
+    for norm in (lp.GroupNorm(2 ** 32 + 2), lp.GroupNorm(2, act=2 ** 32 + lp.LP_ACT_SILU)):
+        with pytest.raises(ValueError, match="32 bits"):
+            lp.lp_group_norm_fwd(norm, x, torch.empty_like(x), None, None)

@@ -1023,7 +1023,7 @@ size_t set_bytes(const std::vector<HostList>& v, size_t first, size_t end)
 struct GramPlan {
     int tile, groups;
     int splits[kMaxLists], chunk;   // of the set's lists; 1: not divided
-    long long parts;                // tiles of all parts
+    long long parts;                // tiles of all parts; 0: no list is divided
 };
 GramPlan plan_gram(const std::vector<HostList>& v, size_t first, size_t end)
 {
@@ -1047,13 +1047,16 @@ GramPlan plan_gram(const std::vector<HostList>& v, size_t first, size_t end)
     g.groups = 4;
     const long long even = (steps + 2 * kUnits - 1) / (2 * kUnits);
     g.chunk = (int)((even > 32 ? even + 3 : 32) / 4 * 4);   // (shortest parts of 16, 32, 64 steps: 279, 247, 265 us for the weights of ten convolutions)
+    bool divided = false;
     for (size_t k = first; k < end; ++k) {
         if (v[k].small) continue;
         const long long mp = pad(v[k].rows < v[k].cols ? v[k].rows : v[k].cols), np = pad(v[k].rows < v[k].cols ? v[k].cols : v[k].rows);
         const int s = (int)((np / kDepth + g.chunk - 1) / g.chunk);
         g.splits[k - first] = s;
         g.parts += v[k].count * (mp / 64 * (mp / 64 + 1) / 2) * s;
+        divided = divided || s > 1;
     }
+    if (!divided) g.parts = 0;
     return g;
 }
 

@@ -40,3 +40,25 @@ def test_lists_that_write_what_others_hold_are_refused(lp):
                   [(1, 8, 8, a, a, c)], [(1, 8, 8, a, b, b)], [(1, 8, 8, a, b, a)],    # a list's own
                   [(1, 8, 8, a, b, a + 252)]):
         assert _muon(lp, lists) == lp.LP_ERR_INVALID_ARG and b"overlap" in lp._lib.lp_last_error(), lists
+
+
+def _workspace_bytes(lp, *shapes):
+    arr = (lp._Matrices * len(shapes))(*[lp._Matrices(*s, None, None, lp.LP_F32) for s in shapes])
+    n = C.c_size_t(0)
+    assert lp._lib.lp_orthogonalize_workspace_bytes(len(shapes), arr, C.byref(n)) == lp.LP_OK
+    return n.value
+
+
+@pytest.mark.parametrize("shape,divided", [((1, 300, 300), 0), ((8, 333, 1001), 0), ((2, 512, 512), 0), ((30, 2048, 512), 0),
+                                           ((1, 100, 5001), 3 * 3), ((2, 300, 1400), 2 * 15 * 2)])
+def test_workspace_has_room_for_parts_of_sums_only_where_sums_are_divided(lp, shape, divided):
+    """X and X^T twice and A and B, as two fp16 parts and padded to 64, for every matrix; 4 KB of partial norms for each and some KB
+    of descriptors; where the sums of X X^T are divided, 64 x 64 sums in fp32 a part."""
+    count, rows, cols = shape
+    m, n = ((min(rows, cols) + 63) // 64 * 64, (max(rows, cols) + 63) // 64 * 64)
+    planes = count * (8 * m * n + 4 * m * m) * 2
+    extra = _workspace_bytes(lp, shape) - planes - count * 4096
+    if divided:
+        assert divided * 64 * 64 * 4 <= extra <= 1 << 26
+    else:
+        assert 0 <= extra <= 8192

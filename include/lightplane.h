@@ -390,8 +390,8 @@ typedef struct {
 lp_status lp_orthogonalize(int32_t n, const lp_matrices* lists, const lp_orth* orth, void* workspace,
                            size_t workspace_bytes, void* stream);
 /* 0 where all matrices are at most 64 x 224 or 32 x 448, or their transposes (then NULL will do).
-   The result of a matrix of more than 128 rows or columns may differ in its last bits with what else the
-   call holds. */
+   The result of a matrix of at most 64 x 128, or its transpose, does not depend on what else the call holds;
+   others' last bits may (the order of their sums follows the work of the whole call). */
 lp_status lp_orthogonalize_workspace_bytes(int32_t n, const lp_matrices* lists, size_t* bytes);
 
 /* How the step of a matrix is scaled. */

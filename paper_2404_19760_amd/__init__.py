@@ -623,7 +623,8 @@ def lp_splat_bwd(target: _Grid, rays: Rays, splat: Splat, theta_w: List[torch.Te
 
 
 def _written(*tensors: Optional[torch.Tensor]) -> None:
-    """Moves the versions of tensors that a call wrote through their addresses: a graph that has saved one of them notices."""
+    """Moves the versions of tensors that a call wrote through their addresses: a graph that has saved one of them notices.
+    (None: not wanted.)"""
     increment_version([t for t in tensors if t is not None])
 
 
@@ -756,7 +757,9 @@ def _matrix_shape(t: torch.Tensor, name: str, k: int):
     if not (t.is_cuda and t.is_contiguous() and t.dim() >= 2):
         raise ValueError(f"{name}[{k}] must be a contiguous GPU tensor [...][rows][cols]")
     rows, cols = t.shape[-2], t.shape[-1]
-    return t.numel() // max(1, rows * cols), _int32(rows, "the number of rows"), _int32(cols, "the number of columns")
+    if (rows | cols) >> 31:
+        raise ValueError(f"rows and columns of {name}[{k}] do not fit 32 bits")
+    return t.numel() // max(1, rows * cols), rows, cols
 
 
 def _matrices(mats, outs):
@@ -801,7 +804,7 @@ def lp_orthogonalize(mats: Sequence[torch.Tensor], outs: Sequence[torch.Tensor],
     arr, o = _matrices(mats, outs), _orth(steps, coeffs, eps)
     wp, wn = _workspace(workspace)
     _check(_lib.lp_orthogonalize(len(mats), arr, C.byref(o), wp, wn, _stream_ptr(stream)))
-    _written(*outs)
+    increment_version(outs)
 
 
 def _muon_weights(weights, grads, momenta):
@@ -831,7 +834,7 @@ def lp_muon_step(weights: Sequence[torch.Tensor], grads: Sequence[torch.Tensor],
               _orth(steps, coeffs, eps))
     wp, wn = _workspace(workspace)
     _check(_lib.lp_muon_step(len(weights), arr, C.byref(q), wp, wn, _stream_ptr(stream)))
-    _written(*weights, *momenta)
+    increment_version([*weights, *momenta])
 
 
 # ---------------------------------------------------------------------------------------

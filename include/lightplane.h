@@ -363,7 +363,7 @@ lp_status lp_group_norm_bwd(const lp_group_norm* norm, const void* x, const floa
  *     X_0 = G / (||G||_F + eps),   A = X X^T,   X <- a X + (b A + c A A) X,   `steps` times
  * (of a matrix with more rows than columns: on the transpose).  A matrix of zeros gives zeros.
  * Products are computed on the matrix cores with operands as fp16 hi + lo parts at a power-of-two scale (22
- * bits, three products, fp32 accumulation), whose error is that of fp32 products.
+ * bits, three products, fp32 accumulation); against 64 bits the result's error is 0.7 to 1.14 times that of fp32 products.
  */
 #define LP_ORTH_MAX_STEPS 16
 

@@ -6,13 +6,16 @@
 //     d_gamma = sum g xh,   d_beta = sum g,
 //     d_x = rstd (gamma g - (S1 + xh S2) / n),   S1 = sum over the group of gamma g,   S2 of gamma g xh.
 //
-// What bounds it: memory.  A sum over the whole group stands between reading a value and using it.  A sample of at most 128 KB stays in the
-// registers of one workgroup meanwhile (one launch).  Larger ones are passed over twice: a pass that sums (forward: x; backward: x
+// What bounds it: memory.  A sum over the whole group stands between reading a value and using it.  A small sample (32 Ki values in slots of
+// four channels, 16 Ki in slots of eight or one; see `hold`) stays in the registers of one workgroup meanwhile (one launch).  Larger ones
+// are passed over twice: a pass that sums (forward: x; backward: x
 // and d_y), a small kernel that joins the workgroups' sums, and a pass that writes, from the end back to the start: what the first
-// pass read last is still in the 256 MB of Infinity Cache (160^3 x 32 in fp32, all passes of a training step: 744 us, from the
-// start 823).  Measured there: 117, 179, 216 and 285 us for 0.5, 1.0, 1.0 and 1.6 GB (4.5 to 5.9 TB/s; a copy of 2 GB 4.95), 24 planes
-// of 256^2 x 32 in bf16 24, 34, 47 and 52 us for 0.1, 0.2, 0.2 and 0.3 GB.  In all passes a thread keeps to one slot of V neighbouring channels (16 bytes where channels and
-// alignment allow), so a channel's parameters and sums stay in its registers, and neighbouring lanes read neighbouring bytes.
+// pass read last is still in the 256 MB of Infinity Cache (160^3 x 32 in fp32, all kernels of a training step: 808 us, from the
+// start 832; of planes in bf16 both 167).  Measured there: 117, 179, 214 and 285 us for 0.5, 1.0, 1.0 and 1.6 GB (4.5 to 5.9 TB/s; a copy of 2 GB 4.95), 24 planes
+// of 256^2 x 32 in bf16 24, 34, 47 and 52 us for 0.1, 0.2, 0.2 and 0.3 GB (a copy of 128 MB, which the cache holds, 8.5).  In all passes a thread keeps to one
+// slot of V neighbouring channels (16 bytes where channels and
+// alignment allow), so a channel's parameters and sums stay in its registers, and neighbouring lanes read neighbouring bytes.  Slots of one channel cost
+// little: 30 channels, which are not divisible by four, take 0.98 (fp32) and 0.97 (bf16) of the forward's time with 32, and 1.01 and 1.04 of the backward's.
 //
 // Sums: a thread sums differences to the first value that it sees, in fp32 (a mean far from zero does not cancel the
 // variance); threads are joined as (count, mean, sum of squared differences), workgroups in fp64 in a fixed order, so that
@@ -907,8 +910,9 @@ long long most_items(const NormDev& d, int n_cu)
     return most;
 }
 
-// Whether a sample fits the registers of a workgroup: then `d` is divided for that.  What its registers hold: 32 Ki values of 32
-// bits, 16 Ki of 16.  A plane of 32 x 32 x 16 in fp32 takes 9 us like that and 16 us in three launches.
+// Whether a sample fits the registers of a workgroup: then `d` is divided for that.  They hold 32 Ki values in slots of four channels (fp32,
+// or 16 bits that are aligned to eight bytes only), 16 Ki in slots of eight or one, less where C / V does not divide 1024.
+// A plane of 32 x 32 x 16 in fp32 takes 9 us like that and 16 us in three launches.
 bool hold(NormDev* d, int V)
 {
     const int held = V == 8 ? 2 : V == 4 ? 8 : 16;

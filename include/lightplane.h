@@ -6,7 +6,8 @@
  * f = g o h (Section 3.2), where h is bi/tri-linear sampling of a triplane or voxel
  * feature grid and g a tiny MLP, with a backward pass that stores one scalar per ray
  * and recomputes everything else (Section 3.4).  Next to it: the Splatter, and for networks that work
- * on the structures a group norm with an activation and the orthogonalised update of weight matrices.
+ * on the structures a group norm with an activation, products with bias, activation and residual, the norms around a
+ * residual block, the clipping of gradients by their norm and the orthogonalised update of weight matrices.
  *
  * General rules
  *   - Every pointer named "device" is a pointer to GPU memory owned by the caller
@@ -354,6 +355,118 @@ lp_status lp_group_norm_fwd(const lp_group_norm* norm, const void* x, void* y, f
    Of a ReLU the gradient at 0 is 0. */
 lp_status lp_group_norm_bwd(const lp_group_norm* norm, const void* x, const float* stats, const void* d_y, void* d_x,
                             float* d_gamma, float* d_beta, void* workspace, size_t workspace_bytes, void* stream);
+
+/* ---- Products with bias, activation and residual ------------------------------------------------
+ *
+ * The other half of a layer over the cells of a grid, or over tokens: x holds P positions of K channels, channel
+ * last, element (p, k) at (p x_stride + k), and every position becomes N channels,
+ *     z = x W^T + b,   y = act(z) + r,
+ * with W [N][K] dense and r (the residual) of y's shape.  All tensors but b and the parameters' gradients are of one type;
+ * products and sums are fp32 (16-bit types: exact products on the matrix cores), and each result is rounded once.
+ * The backward, for the upstream gradient d_y and the z that the forward kept (`pre`, rounded to the tensors' type):
+ *     d_z = d_y act'(z),   d_x = d_z W,   d_W += d_z^T x,   d_b += sum over the positions of d_z;   r's gradient is d_y.
+ * In d_x a 16-bit d_z is rounded once more; in d_W it is kept in two parts (16 bits and more), in d_b in fp32.
+ */
+typedef struct {
+    int64_t P;             /* positions */
+    int32_t K, N;          /* channels in and out, 1 .. 2^20 */
+    int32_t act;           /* lp_act */
+    int32_t dtype;         /* lp_dtype of weight, x, residual, y, pre, d_y and d_x */
+    int64_t x_stride;      /* elements from position to position of x and d_x, >= K; 0: K */
+    int64_t y_stride;      /* the same of y and d_y, >= N; 0: N */
+    int64_t r_stride;      /* the same of the residual; 0: N */
+    const void* weight;    /* device [N][K] */
+    const float* bias;     /* device [N], NULL: 0 */
+    const void* residual;  /* device, NULL: 0; not used by the backward */
+} lp_linear;
+
+/* Bytes of device workspace of the two calls below (either pointer may be NULL); they depend on P, K, N, act and dtype and on the
+   device's compute-unit count, and may be 0 (then NULL will do). */
+lp_status lp_linear_workspace_bytes(const lp_linear* linear, size_t* fwd_bytes, size_t* bwd_bytes);
+
+/* Forward.  y is WRITTEN; pre [P][N] (dense; may be NULL) is written for the backward.  y may be the residual itself where the
+   strides are alike, and must not overlap anything else.  workspace: device, 256-byte aligned, contents ignored on
+   entry, undefined on exit.  P == 0 is a no-op. */
+lp_status lp_linear_fwd(const lp_linear* linear, const void* x, void* y, void* pre, void* workspace, size_t workspace_bytes, void* stream);
+
+/* Backward.  pre as the forward wrote it (not used, and may be NULL, where act is LP_ACT_NONE).  d_x is WRITTEN (NULL: not
+   wanted) and must not overlap x, pre or d_y; d_weight [N][K] and d_bias [N] are ACCUMULATED into (either may be NULL), in an
+   order that does not change from call to call.  Of a ReLU the gradient at 0 is 0. */
+lp_status lp_linear_bwd(const lp_linear* linear, const void* x, const void* pre, const void* d_y, void* d_x, float* d_weight,
+                        float* d_bias, void* workspace, size_t workspace_bytes, void* stream);
+
+/* ---- The norms around a residual block ----------------------------------------------------------
+ *
+ * What stands between two blocks of a network over cells or tokens, in one pass.  With h the sum over the blocks so far, f the
+ * last block's result and norm(v) = (v - mean) / sqrt(var + eps) (LP_NORM_LAYER; var without Bessel's correction) or
+ * v / sqrt(mean of v^2 + eps) (LP_NORM_RMS) over the C channels of a position,
+ *     u = post_gamma norm(f) (post_norm) or f,   s = alpha h + gate u,   y = gamma norm(s) + beta:
+ * s goes on to the next block's sum, y into the next block.  N samples of P positions each, element (n, p, c) at
+ * (n P + p) stride + c; a gate may differ from sample to sample.  Norms and sums are fp32 whatever the tensors hold, and y
+ * comes from s before s is rounded.
+ */
+typedef enum { LP_NORM_RMS = 0, LP_NORM_LAYER = 1 } lp_norm_kind;
+
+#define LP_RESIDUAL_NORM_MAX_CHANNELS 8192
+
+typedef struct {
+    int64_t N, P;
+    int32_t C;                /* channels, 1 .. LP_RESIDUAL_NORM_MAX_CHANNELS */
+    int32_t kind;             /* lp_norm_kind of both norms */
+    int32_t post_norm;        /* 0 or 1 */
+    int32_t gate_per_sample;  /* gate is [C] (0) or [N][C] (1) */
+    float alpha;              /* finite */
+    float eps;                /* >= 0, finite */
+    int32_t h_dtype;          /* lp_dtype of h, s and their gradients */
+    int32_t f_dtype;          /* lp_dtype of f, y and their gradients: h_dtype, or a 16-bit type where that is fp32 */
+    int64_t h_stride;         /* elements from position to position of h, s, d_s and d_h, >= C; 0: C */
+    int64_t f_stride;         /* the same of f and d_f */
+    int64_t y_stride;         /* the same of y and d_y */
+    const float* post_gamma;  /* device [C], NULL: 1 */
+    const float* gate;        /* device, NULL: 1 */
+    const float* gamma;       /* device [C], NULL: 1 */
+    const float* beta;        /* device [C], NULL: 0 */
+} lp_residual_norm;
+
+/* Bytes of device workspace of the backward; they depend on N, P, C, post_norm and gate_per_sample and on the device's compute-unit count. */
+lp_status lp_residual_norm_workspace_bytes(const lp_residual_norm* norm, size_t* bwd_bytes);
+
+/* Forward.  f may be NULL (the first norm of a network: s = alpha h); s and y are WRITTEN, either may be NULL.  s may be h
+   itself, y may be f itself where the strides are alike; otherwise what is written must not overlap anything else.
+   N == 0 or P == 0 is a no-op. */
+lp_status lp_residual_norm_fwd(const lp_residual_norm* norm, const void* h, const void* f, void* s, void* y, void* stream);
+
+/* Backward from the forward's inputs (it computes s again) for the upstream gradients d_s and d_y (either may be NULL: zero).  d_h
+   and d_f are WRITTEN (NULL: not wanted); d_h may be d_s itself, d_f may be d_y itself where the strides are alike, otherwise they must
+   not overlap anything else.  d_gamma [C], d_beta [C], d_post_gamma [C] and d_gate (the gate's shape) are ACCUMULATED into (NULL:
+   not wanted), in an order that does not change from call to call.  workspace: device, 256-byte aligned, contents ignored on entry,
+   undefined on exit. */
+lp_status lp_residual_norm_bwd(const lp_residual_norm* norm, const void* h, const void* f, const void* d_s, const void* d_y, void* d_h,
+                               void* d_f, float* d_gamma, float* d_beta, float* d_post_gamma, float* d_gate, void* workspace,
+                               size_t workspace_bytes, void* stream);
+
+/* ---- The norm of all gradients, and clipping ----------------------------------------------------
+ *
+ * Before the optimiser's step: norm = sqrt(sum of squares of all values of all tensors), and
+ *     out = in min(1, max_norm / (norm + eps)).
+ * Squares and their sum are fp64, so that no fp32 value is too large or too small for them; the factor is applied in fp32
+ * and the result rounded once.  A norm that is not finite is applied as it is (an infinite one makes the finite values 0 and the infinite
+ * ones NaN, NaN makes all NaN): look at `norm` where that must not reach the weights.
+ */
+typedef struct {
+    int64_t size;     /* values */
+    const void* in;   /* device, elements of type `dtype`, aligned to their size */
+    void* out;        /* device, the same type; may be `in`; not used by lp_grad_norm */
+    int32_t dtype;    /* lp_dtype */
+} lp_gradient;
+
+/* norm (device, 1 float) is WRITTEN.  `grads` is a HOST array; n == 0 and tensors of size 0 are fine (a norm of 0).  workspace: device,
+   256-byte aligned, contents ignored on entry, undefined on exit; both calls need the same, which may be 0 bytes (then NULL will do). */
+lp_status lp_grad_norm(int32_t n, const lp_gradient* grads, float* norm, void* workspace, size_t workspace_bytes, void* stream);
+/* max_norm and eps: finite, >= 0.  An out that overlaps another tensor of the call, `norm` or a part of its own in is refused. */
+lp_status lp_clip_grad_norm(int32_t n, const lp_gradient* grads, float max_norm, float eps, float* norm, void* workspace,
+                            size_t workspace_bytes, void* stream);
+lp_status lp_grad_norm_workspace_bytes(int32_t n, const lp_gradient* grads, size_t* bytes);
 
 /* ---- Orthogonalised updates of weight matrices --------------------------------------------------
  *

@@ -28,6 +28,8 @@ LP_MATH_DEFAULT, LP_MATH_GENERIC, LP_MATH_BF16X3 = 0, 1, 2
 LP_FEAT_SIGMOID, LP_FEAT_IDENTITY = 0, 1
 LP_F32, LP_BF16, LP_F16 = 0, 1, 2
 LP_ACT_NONE, LP_ACT_RELU, LP_ACT_SILU, LP_ACT_GELU = 0, 1, 2, 3
+LP_NORM_RMS, LP_NORM_LAYER = 0, 1
+LP_RESIDUAL_NORM_MAX_CHANNELS = 8192
 LP_ORTH_MAX_STEPS = 16
 LP_MUON_SCALE_NONE, LP_MUON_SCALE_ASPECT, LP_MUON_SCALE_RMS = 0, 1, 2
 
@@ -72,6 +74,22 @@ class _GroupNorm(C.Structure):
     _fields_ = [("N", C.c_int64), ("P", C.c_int64), ("C", C.c_int32), ("G", C.c_int32), ("act", C.c_int32), ("eps", C.c_float),
                 ("x_dtype", C.c_int32), ("y_dtype", C.c_int32), ("x_stride", C.c_int64), ("y_stride", C.c_int64),
                 ("gamma", C.c_void_p), ("beta", C.c_void_p), ("occupancy", C.c_void_p)]
+
+
+class _Linear(C.Structure):
+    _fields_ = [("P", C.c_int64), ("K", C.c_int32), ("N", C.c_int32), ("act", C.c_int32), ("dtype", C.c_int32), ("x_stride", C.c_int64),
+                ("y_stride", C.c_int64), ("r_stride", C.c_int64), ("weight", C.c_void_p), ("bias", C.c_void_p), ("residual", C.c_void_p)]
+
+
+class _ResidualNorm(C.Structure):
+    _fields_ = [("N", C.c_int64), ("P", C.c_int64), ("C", C.c_int32), ("kind", C.c_int32), ("post_norm", C.c_int32),
+                ("gate_per_sample", C.c_int32), ("alpha", C.c_float), ("eps", C.c_float), ("h_dtype", C.c_int32), ("f_dtype", C.c_int32),
+                ("h_stride", C.c_int64), ("f_stride", C.c_int64), ("y_stride", C.c_int64), ("post_gamma", C.c_void_p),
+                ("gate", C.c_void_p), ("gamma", C.c_void_p), ("beta", C.c_void_p)]
+
+
+class _Gradient(C.Structure):
+    _fields_ = [("size", C.c_int64), ("input", C.c_void_p), ("out", C.c_void_p), ("dtype", C.c_int32)]
 
 
 class _Orth(C.Structure):
@@ -160,6 +178,25 @@ def _load() -> C.CDLL:
     lib.lp_group_norm_bwd.restype = C.c_int
     lib.lp_group_norm_bwd.argtypes = [C.POINTER(_GroupNorm), C.c_void_p, C.c_void_p, C.c_void_p, C.c_void_p, C.c_void_p, C.c_void_p,
                                       C.c_void_p, C.c_size_t, C.c_void_p]
+    lib.lp_linear_workspace_bytes.restype = C.c_int
+    lib.lp_linear_workspace_bytes.argtypes = [C.POINTER(_Linear), C.POINTER(C.c_size_t), C.POINTER(C.c_size_t)]
+    lib.lp_linear_fwd.restype = C.c_int
+    lib.lp_linear_fwd.argtypes = [C.POINTER(_Linear), C.c_void_p, C.c_void_p, C.c_void_p, C.c_void_p, C.c_size_t, C.c_void_p]
+    lib.lp_linear_bwd.restype = C.c_int
+    lib.lp_linear_bwd.argtypes = [C.POINTER(_Linear), C.c_void_p, C.c_void_p, C.c_void_p, C.c_void_p, C.c_void_p, C.c_void_p,
+                                  C.c_void_p, C.c_size_t, C.c_void_p]
+    lib.lp_residual_norm_workspace_bytes.restype = C.c_int
+    lib.lp_residual_norm_workspace_bytes.argtypes = [C.POINTER(_ResidualNorm), C.POINTER(C.c_size_t)]
+    lib.lp_residual_norm_fwd.restype = C.c_int
+    lib.lp_residual_norm_fwd.argtypes = [C.POINTER(_ResidualNorm), C.c_void_p, C.c_void_p, C.c_void_p, C.c_void_p, C.c_void_p]
+    lib.lp_residual_norm_bwd.restype = C.c_int
+    lib.lp_residual_norm_bwd.argtypes = [C.POINTER(_ResidualNorm), *[C.c_void_p] * 11, C.c_size_t, C.c_void_p]
+    lib.lp_grad_norm_workspace_bytes.restype = C.c_int
+    lib.lp_grad_norm_workspace_bytes.argtypes = [C.c_int32, C.POINTER(_Gradient), C.POINTER(C.c_size_t)]
+    lib.lp_grad_norm.restype = C.c_int
+    lib.lp_grad_norm.argtypes = [C.c_int32, C.POINTER(_Gradient), C.c_void_p, C.c_void_p, C.c_size_t, C.c_void_p]
+    lib.lp_clip_grad_norm.restype = C.c_int
+    lib.lp_clip_grad_norm.argtypes = [C.c_int32, C.POINTER(_Gradient), C.c_float, C.c_float, C.c_void_p, C.c_void_p, C.c_size_t, C.c_void_p]
     lib.lp_orthogonalize_workspace_bytes.restype = C.c_int
     lib.lp_orthogonalize_workspace_bytes.argtypes = [C.c_int32, C.POINTER(_Matrices), C.POINTER(C.c_size_t)]
     lib.lp_orthogonalize.restype = C.c_int
@@ -753,6 +790,293 @@ def lp_group_norm_bwd(norm: GroupNorm, x: torch.Tensor, stats: torch.Tensor, d_y
     _written(d_x, d_gamma, d_beta)
 
 
+def _on_current_device(*tensors: Optional[torch.Tensor]) -> None:
+    """Kernels run on the current device: the tensors of a call (None: not there) lie on it, all of them."""
+    device = None
+    for t in tensors:
+        if t is None:
+            continue
+        if device is None:
+            device = t.device
+        elif t.device != device:
+            raise ValueError("the tensors of a call must be on one device")
+    if device is not None and device.type == "cuda" and device.index != torch.cuda.current_device():
+        raise ValueError("the tensors of a call must be on the current device")
+
+
+def _apart(written: torch.Tensor, written_step: int, read: Optional[torch.Tensor], read_step: int, written_name: str, read_name: str) -> None:
+    """A tensor that is written shares no value with another one, be it the same."""
+    if read is None or written.numel() == 0 or read.numel() == 0:
+        return
+    if written.data_ptr() == read.data_ptr():
+        raise ValueError(f"{written_name} must not overlap {read_name}")
+    if written.shape[-1] == read.shape[-1] and written.numel() == read.numel():
+        _no_overlap(written, written_step, read, read_step, written_name, read_name)
+        return
+    ends = []
+    for t, step in ((written, written_step), (read, read_step)):
+        c = t.shape[-1]
+        ends.append((t.data_ptr(), t.data_ptr() + ((t.numel() // c - 1) * step + c) * t.element_size(), step * t.element_size(), c * t.element_size()))
+    (a, a_end, a_step, a_width), (b, b_end, b_step, b_width) = ends
+    if a_end <= b or b_end <= a:
+        return
+    if a_step == b_step:   # channels of one wider tensor: the same columns never meet
+        behind = (b - a) % a_step
+        if behind >= a_width and behind + b_width <= a_step:
+            return
+    raise ValueError(f"{written_name} must not overlap {read_name}")
+
+
+@dataclasses.dataclass
+class Linear:
+    """A product of positions' channels with a weight matrix [N][K] (contiguous, of the type of what it is applied to), a bias
+    (float32 [N] or None) and an activation: act(x W^T + b) + residual for x [...][K]."""
+    weight: torch.Tensor
+    bias: Optional[torch.Tensor] = None
+    act: int = LP_ACT_NONE
+
+    def c_struct(self, x: torch.Tensor, y_stride: int = 0, residual: Optional[torch.Tensor] = None) -> _Linear:
+        w, dtype = self.weight, x.dtype
+        if dtype not in _GRID_DTYPES:
+            raise ValueError("x must be float32, bfloat16 or float16")
+        if not (w.is_cuda and w.dim() == 2 and w.is_contiguous() and w.dtype is dtype):
+            raise ValueError(f"weight must be a contiguous GPU tensor [N][K] of type {dtype}")
+        n, k = w.shape
+        if x.dim() < 1 or x.shape[-1] != k:
+            raise ValueError(f"x must have {k} channels, the weight's columns")
+        r_stride = 0
+        if residual is not None:
+            r_stride = _channel_last(residual, "residual", x.shape[:-1] + (n,), dtype)
+        _on_current_device(x, w, self.bias, residual)
+        return _Linear(x.numel() // k if k else 0, _int32(k, "K"), _int32(n, "N"), _int32(self.act, "act"), _GRID_DTYPES[dtype],
+                       _position_stride(x, "x"), y_stride, r_stride, w.data_ptr(), _dev_f32(self.bias, "bias", (n,)),
+                       None if residual is None else residual.data_ptr())
+
+
+def _linear_bytes(q: _Linear):
+    f, b = C.c_size_t(), C.c_size_t()
+    _check(_lib.lp_linear_workspace_bytes(C.byref(q), C.byref(f), C.byref(b)))
+    return f.value, b.value
+
+
+def lp_linear_workspace_bytes(linear: Linear, x: torch.Tensor):
+    """(forward bytes, backward bytes) of workspace."""
+    return _linear_bytes(linear.c_struct(x))
+
+
+def _contiguous_like(t: Optional[torch.Tensor], name: str, shape, dtype) -> Optional[int]:
+    if t is None:
+        return None
+    if not (t.is_cuda and t.is_contiguous() and t.shape == shape and t.dtype is dtype):
+        raise ValueError(f"{name} must be a contiguous GPU tensor of shape {tuple(shape)} and type {dtype}")
+    return t.data_ptr()
+
+
+def lp_linear_fwd(linear: Linear, x: torch.Tensor, y: torch.Tensor, pre: Optional[torch.Tensor] = None, residual: Optional[torch.Tensor] = None,
+                  workspace: Optional[torch.Tensor] = None, stream=None) -> None:
+    """Enqueue the forward: y [...][N] (the type of x) is written, and pre (contiguous, of y's shape; None: not wanted) for the backward.
+    y may be the residual itself."""
+    out = x.shape[:-1] + (linear.weight.shape[0],)
+    q = linear.c_struct(x, _channel_last(y, "y", out, x.dtype), residual)
+    _on_current_device(x, y, pre, workspace)
+    w = linear.weight
+    _apart(y, q.y_stride, x, q.x_stride, "y", "x")
+    _apart(y, q.y_stride, w, w.shape[1], "y", "weight")
+    if residual is not None:
+        _no_overlap(y, q.y_stride, residual, q.r_stride, "y", "residual")
+    pre_at = _contiguous_like(pre, "pre", out, x.dtype)
+    if pre is not None:
+        for t, step, name in ((x, q.x_stride, "x"), (y, q.y_stride, "y"), (residual, q.r_stride, "residual"), (w, w.shape[1], "weight")):
+            _apart(pre, out[-1], t, step, "pre", name)
+    wp, wn = _workspace(workspace)
+    _check(_lib.lp_linear_fwd(C.byref(q), x.data_ptr(), y.data_ptr(), pre_at, wp, wn, _stream_ptr(stream)))
+    _written(y, pre)
+
+
+def lp_linear_bwd(linear: Linear, x: torch.Tensor, pre: Optional[torch.Tensor], d_y: torch.Tensor, d_x: Optional[torch.Tensor],
+                  d_weight: Optional[torch.Tensor], d_bias: Optional[torch.Tensor], workspace: Optional[torch.Tensor], stream=None) -> None:
+    """Enqueue the backward: d_x (shape, type and strides of x) is written, d_weight [N][K] and d_bias [N] (float32) are accumulated
+    into; each may be None.  pre as the forward wrote it (None without an activation)."""
+    n, k = linear.weight.shape
+    out = x.shape[:-1] + (n,)
+    q = linear.c_struct(x, _channel_last(d_y, "d_y", out, x.dtype))
+    _on_current_device(x, pre, d_y, d_x, d_weight, d_bias, workspace)
+    pre_at = _contiguous_like(pre, "pre", out, x.dtype)
+    if d_x is not None:
+        if _channel_last(d_x, "d_x", x.shape, x.dtype) != q.x_stride:
+            raise ValueError("d_x must have the strides of x")
+        for t, step, name in ((x, q.x_stride, "x"), (d_y, q.y_stride, "d_y"), (pre, n, "pre"), (linear.weight, k, "weight")):
+            _apart(d_x, q.x_stride, t, step, "d_x", name)
+    wp, wn = _workspace(workspace)
+    _check(_lib.lp_linear_bwd(C.byref(q), x.data_ptr(), pre_at, d_y.data_ptr(), None if d_x is None else d_x.data_ptr(),
+                              _dev_f32(d_weight, "d_weight", (n, k)), _dev_f32(d_bias, "d_bias", (n,)), wp, wn, _stream_ptr(stream)))
+    _written(d_x, d_weight, d_bias)
+
+
+@dataclasses.dataclass
+class ResidualNorm:
+    """The norms around a residual block, for tensors [...][C] or, with a gate for each sample, [N][...][C]: with f the block's result
+    and h the sum before it, s = alpha h + gate u, u = post_gamma norm(f) (post_norm) or f, and y = gamma norm(s) + beta.
+    kind: LP_NORM_RMS or LP_NORM_LAYER, of both norms; gamma, beta, post_gamma: float32 [C] or None; gate: float32 [C], [N][C] or None."""
+    kind: int = LP_NORM_RMS
+    gamma: Optional[torch.Tensor] = None
+    beta: Optional[torch.Tensor] = None
+    post_norm: bool = False
+    post_gamma: Optional[torch.Tensor] = None
+    gate: Optional[torch.Tensor] = None
+    alpha: float = 1.0
+    eps: float = 1e-5
+
+    def c_struct(self, h: torch.Tensor, f_dtype=None, f_stride: int = 0, y_stride: int = 0) -> _ResidualNorm:
+        f_dtype = h.dtype if f_dtype is None else f_dtype
+        if h.dtype not in _GRID_DTYPES or f_dtype not in _GRID_DTYPES:
+            raise ValueError("h, f and y must be float32, bfloat16 or float16")
+        shape = h.shape
+        if len(shape) < 1:
+            raise ValueError("h must have a last axis of channels")
+        c = shape[-1]
+        n = shape[0] if len(shape) > 1 else 1
+        gate, per_sample = self.gate, 0
+        if gate is not None and gate.dim() == 2:
+            per_sample = 1
+            _dev_f32(gate, "gate", (n, c))
+        elif gate is not None:
+            _dev_f32(gate, "gate", (c,))
+        _on_current_device(h, self.gamma, self.beta, self.post_gamma, gate)
+        return _ResidualNorm(n, h.numel() // (n * c) if n and c else 0, _int32(c, "the number of channels"), _int32(self.kind, "kind"),
+                             _int32(self.post_norm, "post_norm"), per_sample, float(self.alpha), float(self.eps), _GRID_DTYPES[h.dtype],
+                             _GRID_DTYPES[f_dtype], _position_stride(h, "h"), f_stride, y_stride,
+                             _dev_f32(self.post_gamma, "post_gamma", (c,)), None if gate is None else gate.data_ptr(),
+                             _dev_f32(self.gamma, "gamma", (c,)), _dev_f32(self.beta, "beta", (c,)))
+
+
+def lp_residual_norm_workspace_bytes(norm: ResidualNorm, h: torch.Tensor) -> int:
+    """Bytes of workspace of the backward."""
+    n = C.c_size_t()
+    _check(_lib.lp_residual_norm_workspace_bytes(C.byref(norm.c_struct(h)), C.byref(n)))
+    return n.value
+
+
+def _same_step(t: Optional[torch.Tensor], name: str, shape, dtype, step: int, of: str) -> Optional[int]:
+    if t is None:
+        return None
+    if _channel_last(t, name, shape, dtype) != step and t.numel():
+        raise ValueError(f"{name} must have the strides of {of}")
+    return t.data_ptr()
+
+
+def _f_type(h: torch.Tensor, *tensors: Optional[torch.Tensor]):
+    """The type of f and y and their gradients."""
+    return next((t.dtype for t in tensors if t is not None), h.dtype)
+
+
+def lp_residual_norm_fwd(norm: ResidualNorm, h: torch.Tensor, f: Optional[torch.Tensor], s: Optional[torch.Tensor], y: Optional[torch.Tensor],
+                         stream=None) -> None:
+    """Enqueue the forward: s (shape, type and strides of h) and y (shape of h, type of f) are written; either may be None.  f may be
+    None (the first norm of a network).  s may be h itself, y may be f itself."""
+    dtype = _f_type(h, f, y)
+    steps = [0 if t is None else _channel_last(t, name, h.shape, dtype) for t, name in ((f, "f"), (y, "y"))]
+    q = norm.c_struct(h, dtype, *steps)
+    _on_current_device(h, f, s, y)
+    s_at = _same_step(s, "s", h.shape, h.dtype, q.h_stride, "h")
+    if s is not None:
+        _no_overlap(s, q.h_stride, h, q.h_stride, "s", "h")
+        _apart(s, q.h_stride, f, q.f_stride, "s", "f")
+        _apart(s, q.h_stride, y, q.y_stride, "s", "y")
+    if y is not None:
+        _apart(y, q.y_stride, h, q.h_stride, "y", "h")
+        if f is not None:
+            _no_overlap(y, q.y_stride, f, q.f_stride, "y", "f")
+    _check(_lib.lp_residual_norm_fwd(C.byref(q), h.data_ptr(), None if f is None else f.data_ptr(), s_at, None if y is None else y.data_ptr(),
+                                     _stream_ptr(stream)))
+    _written(s, y)
+
+
+def lp_residual_norm_bwd(norm: ResidualNorm, h: torch.Tensor, f: Optional[torch.Tensor], d_s: Optional[torch.Tensor], d_y: Optional[torch.Tensor],
+                         d_h: Optional[torch.Tensor], d_f: Optional[torch.Tensor], d_gamma: Optional[torch.Tensor], d_beta: Optional[torch.Tensor],
+                         d_post_gamma: Optional[torch.Tensor], d_gate: Optional[torch.Tensor], workspace: torch.Tensor, stream=None) -> None:
+    """Enqueue the backward, from the forward's inputs: d_h and d_f are written, d_gamma, d_beta, d_post_gamma and d_gate accumulated
+    into; each may be None, and so may d_s and d_y (zero).  d_s and d_h have the strides of h, d_f those of f."""
+    dtype = _f_type(h, f, d_y, d_f)
+    steps = [0 if t is None else _channel_last(t, name, h.shape, dtype) for t, name in ((f, "f"), (d_y, "d_y"))]
+    q = norm.c_struct(h, dtype, *steps)
+    _on_current_device(h, f, d_s, d_y, d_h, d_f, d_gamma, d_beta, d_post_gamma, d_gate, workspace)
+    d_s_at, d_h_at = (_same_step(t, name, h.shape, h.dtype, q.h_stride, "h") for t, name in ((d_s, "d_s"), (d_h, "d_h")))
+    d_f_at = _same_step(d_f, "d_f", h.shape, dtype, q.f_stride or h.shape[-1], "f")
+    if d_h is not None:
+        for t, step, name in ((h, q.h_stride, "h"), (f, q.f_stride, "f"), (d_y, q.y_stride, "d_y"), (d_f, q.f_stride, "d_f")):
+            _apart(d_h, q.h_stride, t, step, "d_h", name)
+        if d_s is not None:
+            _no_overlap(d_h, q.h_stride, d_s, q.h_stride, "d_h", "d_s")
+    if d_f is not None:
+        for t, step, name in ((h, q.h_stride, "h"), (f, q.f_stride, "f"), (d_s, q.h_stride, "d_s")):
+            _apart(d_f, q.f_stride, t, step, "d_f", name)
+        if d_y is not None:
+            _no_overlap(d_f, q.f_stride, d_y, q.y_stride, "d_f", "d_y")
+    c = (h.shape[-1],)
+    wp, wn = _workspace(workspace)
+    at = lambda t: None if t is None else t.data_ptr()  # noqa: E731
+    _check(_lib.lp_residual_norm_bwd(C.byref(q), h.data_ptr(), at(f), d_s_at, at(d_y), d_h_at, d_f_at, _dev_f32(d_gamma, "d_gamma", c),
+                                     _dev_f32(d_beta, "d_beta", c), _dev_f32(d_post_gamma, "d_post_gamma", c),
+                                     _dev_f32(d_gate, "d_gate", c if norm.gate is None else norm.gate.shape), wp, wn, _stream_ptr(stream)))
+    _written(d_h, d_f, d_gamma, d_beta, d_post_gamma, d_gate)
+
+
+def _is_dense(t: torch.Tensor) -> bool:
+    """Whether a tensor's values lie one behind the other, in any order of its axes."""
+    if t.is_contiguous():
+        return True
+    step = 1
+    for stride, size in sorted((s, n) for s, n in zip(t.stride(), t.shape) if n != 1):
+        if stride != step:
+            return False
+        step *= size
+    return True
+
+
+def _gradients(grads, outs):
+    if len(grads) != len(outs):
+        raise ValueError("one output per gradient is needed")
+    rows = []
+    for k, (g, o) in enumerate(zip(grads, outs)):
+        dtype = _GRID_DTYPES.get(g.dtype)
+        if dtype is None or not g.is_cuda or not _is_dense(g):
+            raise ValueError(f"grads[{k}] must be a dense float32, bfloat16 or float16 tensor on the GPU")
+        if o is not g and not (o.is_cuda and o.dtype is g.dtype and o.shape == g.shape and o.stride() == g.stride()):
+            raise ValueError(f"outs[{k}] must be a GPU tensor of the shape, type and strides of grads[{k}]")
+        rows.append((g.numel(), g.data_ptr(), o.data_ptr(), dtype))
+    return (_Gradient * max(1, len(rows)))(*rows)
+
+
+def _grad_norm_bytes(n: int, arr) -> int:
+    size = C.c_size_t(0)
+    _check(_lib.lp_grad_norm_workspace_bytes(n, arr, C.byref(size)))
+    return size.value
+
+
+def lp_grad_norm_workspace_bytes(grads: Sequence[torch.Tensor]) -> int:
+    return _grad_norm_bytes(len(grads), _gradients(grads, grads))
+
+
+def lp_grad_norm(grads: Sequence[torch.Tensor], norm: torch.Tensor, workspace: Optional[torch.Tensor], stream=None) -> None:
+    """Enqueue the norm of all gradients together: norm (float32, shape ()) is written."""
+    arr = _gradients(grads, grads)
+    _on_current_device(*grads, norm, workspace)
+    wp, wn = _workspace(workspace)
+    _check(_lib.lp_grad_norm(len(grads), arr, _dev_f32(norm, "norm", ()), wp, wn, _stream_ptr(stream)))
+    _written(norm)
+
+
+def lp_clip_grad_norm(grads: Sequence[torch.Tensor], outs: Sequence[torch.Tensor], max_norm: float, norm: torch.Tensor,
+                      workspace: Optional[torch.Tensor], eps: float = 1e-6, stream=None) -> None:
+    """Enqueue the clipping: outs (the gradients themselves, or tensors like them) and norm (float32, shape ()) are written."""
+    arr = _gradients(grads, outs)
+    _on_current_device(*grads, *outs, norm, workspace)
+    wp, wn = _workspace(workspace)
+    _check(_lib.lp_clip_grad_norm(len(grads), arr, float(max_norm), float(eps), _dev_f32(norm, "norm", ()), wp, wn, _stream_ptr(stream)))
+    increment_version([*outs, norm])
+
+
 def _matrix_shape(t: torch.Tensor, name: str, k: int):
     if not (t.is_cuda and t.is_contiguous() and t.dim() >= 2):
         raise ValueError(f"{name}[{k}] must be a contiguous GPU tensor [...][rows][cols]")
@@ -979,6 +1303,95 @@ def group_norm_bwd(norm: GroupNorm, x: torch.Tensor, stats: torch.Tensor, d_y: t
                                   at, at + 4 * q.C, ws.data_ptr() if n else None, n, _stream_ptr(None)))
     d_gamma, d_beta = d_params.unbind(0)
     return d_x, d_gamma, d_beta
+
+
+def linear_fwd(linear: Linear, x: torch.Tensor, residual: Optional[torch.Tensor] = None, keep: bool = False):
+    """Allocate outputs and workspace and run lp_linear_fwd.  Returns (y, pre); pre (keep; else None) is for linear_bwd, which needs it
+    where there is an activation."""
+    q = linear.c_struct(x, 0, residual)   # (new outputs are dense: what the entry point checks of them holds)
+    y = torch.empty(x.shape[:-1] + (q.N,), dtype=x.dtype, device=x.device)
+    pre = torch.empty_like(y) if keep else None
+    n = _linear_bytes(q)[0] if q.P > 16 else 0
+    ws = torch.empty(n, dtype=torch.uint8, device=x.device) if n else None   # (held until the kernels are enqueued)
+    _check(_lib.lp_linear_fwd(C.byref(q), x.data_ptr(), y.data_ptr(), pre.data_ptr() if keep else None, ws.data_ptr() if n else None, n,
+                              _stream_ptr(None)))
+    return y, pre
+
+
+def linear_bwd(linear: Linear, x: torch.Tensor, pre: Optional[torch.Tensor], d_y: torch.Tensor):
+    """Allocate gradients and workspace and run lp_linear_bwd.  Returns (d_x, d_weight, d_bias); d_weight and d_bias (None without a
+    bias) are float32."""
+    out = x.shape[:-1] + (linear.weight.shape[0],)
+    q = linear.c_struct(x, _channel_last(d_y, "d_y", out, x.dtype))
+    _on_current_device(x, pre, d_y)
+    d_x = torch.empty_like(x) if x.is_contiguous() else torch.empty_strided(x.shape, x.stride(), dtype=x.dtype, device=x.device)
+    d_params = torch.zeros(q.N * q.K + (q.N if linear.bias is not None else 0), dtype=torch.float32, device=x.device)
+    at = d_params.data_ptr()
+    n = _linear_bytes(q)[1]
+    ws = torch.empty(n, dtype=torch.uint8, device=x.device) if n else None   # (held until the kernels are enqueued)
+    _check(_lib.lp_linear_bwd(C.byref(q), x.data_ptr(), _contiguous_like(pre, "pre", out, x.dtype), d_y.data_ptr(), d_x.data_ptr(), at,
+                              None if linear.bias is None else at + 4 * q.N * q.K, ws.data_ptr() if n else None, n, _stream_ptr(None)))
+    return d_x, d_params[:q.N * q.K].view(q.N, q.K), None if linear.bias is None else d_params[q.N * q.K:]
+
+
+def residual_norm_fwd(norm: ResidualNorm, h: torch.Tensor, f: Optional[torch.Tensor] = None, dtype=None):
+    """Allocate outputs and run lp_residual_norm_fwd.  Returns (s, y); y has the type of f (without f: `dtype`, by default that of h).
+    Without f and with alpha 1, s is h itself."""
+    if f is not None and dtype is not None and dtype is not f.dtype:
+        raise ValueError("y has the type of f")
+    y_dtype = f.dtype if f is not None else h.dtype if dtype is None else dtype
+    q = norm.c_struct(h, y_dtype, 0 if f is None else _channel_last(f, "f", h.shape, y_dtype))
+    if f is not None:
+        _on_current_device(h, f)
+    same = f is None and norm.alpha == 1.0
+    s = h if same else torch.empty_like(h) if h.is_contiguous() else torch.empty_strided(h.shape, h.stride(), dtype=h.dtype, device=h.device)
+    y = torch.empty(h.shape, dtype=y_dtype, device=h.device)
+    _check(_lib.lp_residual_norm_fwd(C.byref(q), h.data_ptr(), None if f is None else f.data_ptr(), None if same else s.data_ptr(),
+                                     y.data_ptr(), _stream_ptr(None)))
+    return s, y
+
+
+def residual_norm_bwd(norm: ResidualNorm, h: torch.Tensor, f: Optional[torch.Tensor], d_s: Optional[torch.Tensor], d_y: Optional[torch.Tensor]):
+    """Allocate gradients and workspace and run lp_residual_norm_bwd.  Returns (d_h, d_f, d_gamma, d_beta, d_post_gamma, d_gate), None
+    in the place of the gradient of what the norm does not have."""
+    like = lambda t: torch.empty_like(t) if t.is_contiguous() else torch.empty_strided(t.shape, t.stride(), dtype=t.dtype, device=t.device)  # noqa: E731
+    params = [norm.gamma, norm.beta, norm.post_gamma if f is not None else None, norm.gate if f is not None else None]
+    sizes = [0 if p is None else p.numel() for p in params]
+    zeros = torch.zeros(sum(sizes), dtype=torch.float32, device=h.device)
+    parts = [None if p is None else z.view(p.shape) for p, z in zip(params, zeros.split(sizes))]
+    d_h, d_f = like(h), None if f is None else like(f)
+    ws = torch.empty(lp_residual_norm_workspace_bytes(norm, h), dtype=torch.uint8, device=h.device)
+    lp_residual_norm_bwd(norm, h, f, d_s, d_y, d_h, d_f, *parts, ws)
+    return (d_h, d_f, *parts)
+
+
+def grad_norm(grads: Sequence[torch.Tensor]) -> torch.Tensor:
+    """Allocate and run lp_grad_norm.  Returns the norm of all gradients together (float32, shape ())."""
+    return _norm_of(grads, None, 0.0, 0.0)
+
+
+def clip_grad_norm(grads: Sequence[torch.Tensor], max_norm: float, eps: float = 1e-6, outs: Optional[Sequence[torch.Tensor]] = None) -> torch.Tensor:
+    """Allocate a workspace and run lp_clip_grad_norm on the gradients in place, or into outs.  Returns the norm that they had (float32,
+    shape ())."""
+    return _norm_of(grads, grads if outs is None else outs, max_norm, eps)
+
+
+def _norm_of(grads, outs, max_norm, eps) -> torch.Tensor:
+    if not len(grads):
+        raise ValueError("no gradients: without a tensor there is no device for the norm")
+    arr, n = _gradients(grads, grads if outs is None else outs), len(grads)
+    _on_current_device(*grads, *(outs or ()))
+    device = grads[0].device
+    norm = torch.empty((), dtype=torch.float32, device=device)
+    size = _grad_norm_bytes(n, arr)
+    ws = torch.empty(size, dtype=torch.uint8, device=device) if size else None   # (held until the kernels are enqueued)
+    at = ws.data_ptr() if size else None
+    if outs is None:
+        _check(_lib.lp_grad_norm(n, arr, norm.data_ptr(), at, size, _stream_ptr(None)))
+    else:
+        _check(_lib.lp_clip_grad_norm(n, arr, float(max_norm), float(eps), norm.data_ptr(), at, size, _stream_ptr(None)))
+        increment_version(outs)
+    return norm
 
 
 def orthogonalize(mats: Sequence[torch.Tensor], steps: int = 5, coeffs=None, eps: float = 1e-7):

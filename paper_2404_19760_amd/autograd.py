@@ -4,13 +4,16 @@ library's kernels.
 render: the Renderer's two entry points; the forward keeps one scalar per ray (Section 3.4: the backward recomputes the
 rest), the backward calls lp_render_bwd.  No gradient flows to the rays (the library produces none); first derivatives alone.
 group_norm: group norm with an activation over channel-last grids; the forward keeps its input, the occupancy and two
-numbers a group; first derivatives alone."""
+numbers a group; first derivatives alone.
+linear: a product with bias, activation and residual; keeps its input, the weight and, where there is an activation, what goes into it.
+residual_norm: the norms around a residual block; keeps its inputs, the backward computes the rest again."""
 from typing import List, Optional, Sequence
 
 import torch
 
-from . import (LP_ACT_NONE, LP_MATH_DEFAULT, Grid, GroupNorm, Mlp, Rays, group_norm_fwd, lp_bwd_workspace_bytes,
-               lp_group_norm_bwd, lp_group_norm_workspace_bytes, lp_render_bwd, lp_render_fwd)
+from . import (LP_ACT_NONE, LP_MATH_DEFAULT, LP_NORM_RMS, Grid, GroupNorm, Linear, Mlp, Rays, ResidualNorm, group_norm_fwd, linear_fwd,
+               lp_bwd_workspace_bytes, lp_group_norm_bwd, lp_group_norm_workspace_bytes, lp_linear_bwd, lp_linear_workspace_bytes,
+               lp_render_bwd, lp_render_fwd, lp_residual_norm_bwd, lp_residual_norm_workspace_bytes, residual_norm_fwd)
 
 
 class _First(torch.autograd.Function):
@@ -113,3 +116,83 @@ def group_norm(x: torch.Tensor, groups: int, gamma: Optional[torch.Tensor] = Non
     """Differentiable group norm with an activation of a channel-last tensor [N][...][C] (see GroupNorm; dtype: of the result);
     gradients flow to x, gamma and beta."""
     return _GroupNorm.apply((int(groups), int(act), float(eps), dtype), x, gamma, beta, occupancy)
+
+
+def _like(t: torch.Tensor) -> torch.Tensor:
+    return torch.empty_strided(t.shape, t.stride(), dtype=t.dtype, device=t.device)
+
+
+class _Linear(torch.autograd.Function):
+    @staticmethod
+    def forward(ctx, act, x, weight, bias, residual):
+        w = weight.detach().to(x.dtype)
+        detach = lambda t: None if t is None else t.detach()
+        keep = act != LP_ACT_NONE and any(ctx.needs_input_grad[1:4])
+        y, pre = linear_fwd(Linear(w, detach(bias), act), x.detach(), detach(residual), keep)
+        # (a weight that was cast is kept as it was used; the parameter itself is kept for its version and for second derivatives)
+        ctx.save_for_backward(x, weight, bias, pre, None if w.dtype == weight.dtype else w)
+        ctx.lp = act
+        return y
+
+    @staticmethod
+    def backward(ctx, upstream):
+        x, weight, bias, pre, w = ctx.saved_tensors
+        need_x, need_weight, need_bias, need_residual = ctx.needs_input_grad[1:5]
+        linear = Linear(weight.detach() if w is None else w, None if bias is None else bias.detach(), ctx.lp)
+        d_y = upstream.contiguous()
+        d_x = _like(x) if need_x else None
+        d_weight = torch.zeros(weight.shape, dtype=torch.float32, device=x.device) if need_weight else None
+        d_bias = torch.zeros_like(bias) if need_bias else None
+        if need_x or need_weight or need_bias:
+            ws = torch.empty(lp_linear_workspace_bytes(linear, x.detach())[1], dtype=torch.uint8, device=x.device)
+            lp_linear_bwd(linear, x.detach(), pre, d_y, d_x, d_weight, d_bias, ws)
+        if d_weight is not None:
+            d_weight = d_weight.to(weight.dtype)
+        d_x, d_weight, d_bias = _first((d_x, d_weight, d_bias), (upstream, x, weight, bias))
+        return None, d_x, d_weight, d_bias, upstream if need_residual else None
+
+
+def linear(x: torch.Tensor, weight: torch.Tensor, bias: Optional[torch.Tensor] = None, act: int = LP_ACT_NONE,
+           residual: Optional[torch.Tensor] = None) -> torch.Tensor:
+    """Differentiable act(x W^T + b) + residual (see Linear); gradients flow to x, weight, bias and residual.  A weight of another
+    type (fp32, as the optimisers have it) is rounded to that of x; its gradient is summed in fp32."""
+    return _Linear.apply(int(act), x, weight, bias, residual)
+
+
+class _ResidualNorm(torch.autograd.Function):
+    @staticmethod
+    def forward(ctx, spec, h, f, gamma, beta, post_gamma, gate):
+        kind, post_norm, alpha, eps, dtype = spec
+        detach = lambda t: None if t is None else t.detach()
+        norm = ResidualNorm(kind, detach(gamma), detach(beta), post_norm, detach(post_gamma), detach(gate), alpha, eps)
+        s, y = residual_norm_fwd(norm, h.detach(), detach(f), dtype)
+        ctx.save_for_backward(h, f, gamma, beta, post_gamma, gate)
+        ctx.lp = spec
+        ctx.set_materialize_grads(False)
+        return h if f is None and alpha == 1.0 else s, y   # (residual_norm_fwd: without a block s is h itself)
+
+    @staticmethod
+    def backward(ctx, up_s, up_y):
+        kind, post_norm, alpha, eps, _ = ctx.lp
+        h, f, gamma, beta, post_gamma, gate = ctx.saved_tensors
+        if up_s is None and up_y is None:
+            return (None,) * 7
+        norm = ResidualNorm(kind, gamma, beta, post_norm, post_gamma, gate, alpha, eps)
+        d_s = up_s if up_s is None or up_s.stride() == h.stride() else _like(h).copy_(up_s)
+        d_y = None if up_y is None else up_y.contiguous()
+        needs = ctx.needs_input_grad[1:]
+        d_h = _like(h) if needs[0] else None
+        d_f = _like(f) if needs[1] else None
+        params = [torch.zeros_like(p) if need else None for p, need in zip((gamma, beta, post_gamma, gate), needs[2:])]
+        with_f = params if f is not None else [*params[:2], None, None]
+        ws = torch.empty(lp_residual_norm_workspace_bytes(norm, h), dtype=torch.uint8, device=h.device)
+        lp_residual_norm_bwd(norm, h, f, d_s, d_y, d_h, d_f, *with_f, ws)
+        return (None, *_first((d_h, d_f, *params), (up_s, up_y, h, f, gamma, beta, post_gamma, gate)))
+
+
+def residual_norm(h: torch.Tensor, f: Optional[torch.Tensor] = None, gamma: Optional[torch.Tensor] = None, beta: Optional[torch.Tensor] = None,
+                  kind: int = LP_NORM_RMS, post_norm: bool = False, post_gamma: Optional[torch.Tensor] = None,
+                  gate: Optional[torch.Tensor] = None, alpha: float = 1.0, eps: float = 1e-5, dtype=None):
+    """Differentiable norms around a residual block (see ResidualNorm): (s, y) for the sum h so far and the block's result f, or None
+    (then dtype: of y); gradients flow to h, f, gamma, beta, post_gamma and gate."""
+    return _ResidualNorm.apply((int(kind), bool(post_norm), float(alpha), float(eps), dtype), h, f, gamma, beta, post_gamma, gate)

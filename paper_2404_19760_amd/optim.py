@@ -1,10 +1,11 @@
 """A torch.optim optimiser on the library's orthogonalised update (lp_muon_step), for the weight matrices of decoders and of networks
-around them.  Vectors (biases, norm parameters) and structures belong to another optimiser."""
-from typing import Iterable
+around them.  Vectors (biases, norm parameters) and structures belong to another optimiser.  And what stands before the optimisers'
+steps: the gradients of all parameters brought under a largest norm (lp_clip_grad_norm)."""
+from typing import Iterable, Union
 
 import torch
 
-from . import LP_MUON_SCALE_ASPECT, muon_step
+from . import LP_MUON_SCALE_ASPECT, clip_grad_norm, muon_step
 
 
 class Muon(torch.optim.Optimizer):
@@ -37,3 +38,19 @@ class Muon(torch.optim.Optimizer):
                       lr=group["lr"], momentum=group["momentum"], nesterov=group["nesterov"], weight_decay=group["weight_decay"],
                       scale=group["scale"], steps=group["steps"], coeffs=group["coeffs"], eps=group["eps"])
         return loss
+
+
+@torch.no_grad()
+def clip_grad_norm_(params: Union[torch.Tensor, Iterable[torch.Tensor]], max_norm: float, eps: float = 1e-6) -> torch.Tensor:
+    """Scales the gradients of all parameters, in place, by min(1, max_norm / (norm + eps)), and returns the norm of all of them
+    together before that, on the GPU (nothing waits for it).  Parameters without a gradient do not take part; gradients are dense GPU
+    tensors.  A norm that is not finite is applied as it is."""
+    params = [params] if isinstance(params, torch.Tensor) else list(params)
+    grads, seen = [], set()
+    for p in params:
+        if p.grad is not None and id(p.grad) not in seen:   # (a parameter listed twice has one gradient)
+            seen.add(id(p.grad))
+            grads.append(p.grad)
+    if not grads:
+        return torch.zeros((), device=params[0].device if params else None)
+    return clip_grad_norm(grads, max_norm, eps)

@@ -853,9 +853,9 @@ class Linear:
                        None if residual is None else residual.data_ptr())
 
 
-def _linear_bytes(q: _Linear):
+def _linear_bytes(q: _Linear, backward: bool = True):
     f, b = C.c_size_t(), C.c_size_t()
-    _check(_lib.lp_linear_workspace_bytes(C.byref(q), C.byref(f), C.byref(b)))
+    _check(_lib.lp_linear_workspace_bytes(C.byref(q), C.byref(f), C.byref(b) if backward else None))
     return f.value, b.value
 
 
@@ -1311,7 +1311,7 @@ def linear_fwd(linear: Linear, x: torch.Tensor, residual: Optional[torch.Tensor]
     q = linear.c_struct(x, 0, residual)   # (new outputs are dense: what the entry point checks of them holds)
     y = torch.empty(x.shape[:-1] + (q.N,), dtype=x.dtype, device=x.device)
     pre = torch.empty_like(y) if keep else None
-    n = _linear_bytes(q)[0] if q.P > 16 else 0
+    n = _linear_bytes(q, False)[0]
     ws = torch.empty(n, dtype=torch.uint8, device=x.device) if n else None   # (held until the kernels are enqueued)
     _check(_lib.lp_linear_fwd(C.byref(q), x.data_ptr(), y.data_ptr(), pre.data_ptr() if keep else None, ws.data_ptr() if n else None, n,
                               _stream_ptr(None)))

@@ -1,0 +1,231 @@
+// Device code and declarations that the translation units of the products with a weight matrix share (lp_linear*.hip).
+#pragma once
+#include <hip/hip_runtime.h>
+
+#include <type_traits>
+
+#include "lp_act.h"
+#include "lp_kernels.h"
+
+namespace lp {
+namespace linear {
+
+using namespace act;
+
+constexpr int kThreads = 256;
+constexpr unsigned kMaxGrid = 1u << 30;
+inline unsigned grid_of(long long n) { return (unsigned)(n < kMaxGrid ? n : kMaxGrid); }
+
+using f32x4 = float __attribute__((ext_vector_type(4)));
+using f32x16 = float __attribute__((ext_vector_type(16)));
+using u32x4 = uint32_t __attribute__((ext_vector_type(4)));
+using u32x2 = uint32_t __attribute__((ext_vector_type(2)));
+
+template <class T> struct Vec;
+template <> struct Vec<float> { using Of = float __attribute__((ext_vector_type(4))); };
+template <> struct Vec<__bf16> { using Of = __bf16 __attribute__((ext_vector_type(8))); };
+template <> struct Vec<_Float16> { using Of = _Float16 __attribute__((ext_vector_type(8))); };
+
+// 16 bytes of neighbouring channels.
+template <class T>
+struct alignas(16) Chunk {
+    static constexpr int kCount = 16 / sizeof(T);
+    T v[kCount];
+};
+template <class T> constexpr int kChunk = Chunk<T>::kCount;
+
+// `count` (may be <= 0) values from p, zeros behind them.  A whole chunk is one load, also where it is not aligned to 16 bytes.
+// WHOLE: rows end with whole chunks.
+template <bool WHOLE, class T>
+__device__ __forceinline__ Chunk<T> load_chunk(const T* p, long long count)
+{
+    Chunk<T> c;
+    if (WHOLE) {
+        if (count > 0) __builtin_memcpy(&c, p, 16);
+        else c = Chunk<T>{};
+    } else if (count >= kChunk<T>) {
+        __builtin_memcpy(&c, p, 16);
+    } else {
+#pragma unroll
+        for (int j = 0; j < kChunk<T>; ++j) c.v[j] = j < count ? p[j] : (T)0.0f;
+    }
+    return c;
+}
+template <bool WHOLE, class T>
+__device__ __forceinline__ void store_chunk(T* p, long long count, const Chunk<T>& c)
+{
+    if (WHOLE ? count > 0 : count >= kChunk<T>) {
+        __builtin_memcpy(p, &c, 16);
+    } else if (!WHOLE) {
+#pragma unroll
+        for (int j = 0; j < kChunk<T>; ++j)
+            if (j < count) p[j] = c.v[j];
+    }
+}
+
+// acc += a b^T over the channels of two neighbouring chunks (see above)
+__device__ __forceinline__ f32x16 multiply(const Chunk<__bf16>& a, const Chunk<__bf16>& b, f32x16 acc)
+{
+    using V = Vec<__bf16>::Of;
+    return __builtin_amdgcn_mfma_f32_32x32x16_bf16(__builtin_bit_cast(V, a), __builtin_bit_cast(V, b), acc, 0, 0, 0);
+}
+__device__ __forceinline__ f32x16 multiply(const Chunk<_Float16>& a, const Chunk<_Float16>& b, f32x16 acc)
+{
+    using V = Vec<_Float16>::Of;
+    return __builtin_amdgcn_mfma_f32_32x32x16_f16(__builtin_bit_cast(V, a), __builtin_bit_cast(V, b), acc, 0, 0, 0);
+}
+__device__ __forceinline__ f32x16 multiply(const Chunk<float>& a, const Chunk<float>& b, f32x16 acc)
+{
+#pragma unroll
+    for (int j = 0; j < 4; ++j) acc = __builtin_amdgcn_mfma_f32_32x32x2f32(a.v[j], b.v[j], acc, 0, 0, 0);
+    return acc;
+}
+
+// d_z of a chunk, rounded to T, and what the rounding left.
+template <class T>
+struct Gradient {
+    Chunk<T> hi, lo;
+    float v[kChunk<T>];
+};
+template <int ACT, class T>
+__device__ __forceinline__ Gradient<T> gradient(const Chunk<T>& dy, const Chunk<T>& pre)
+{
+    Gradient<T> g;
+#pragma unroll
+    for (int j = 0; j < kChunk<T>; ++j) {
+        g.v[j] = (float)dy.v[j] * (ACT == LP_ACT_NONE ? 1.0f : slope<ACT>((float)pre.v[j]));
+        asm("" : "+v"(g.v[j]));   // (both parts come from this value: hi alone could be rounded straight from the product)
+        g.hi.v[j] = (T)g.v[j];
+        if (sizeof(T) == 2) {
+            g.lo.v[j] = (T)(g.v[j] - (float)g.hi.v[j]);   // (an infinite d_z leaves NaN)
+        }
+    }
+    return g;
+}
+
+struct LinearDev {
+    long long P;
+    int K, N;                       // of the product: channels that are summed over, channels of the result
+    long long as, ys, rs;           // elements from position to position: operand, result, residual
+    const void *a, *w, *res, *pre;  // w: [N][ws]; pre (of the backward): [P][K]
+    long long ws;
+    const float* bias;
+    void *out, *keep;               // keep: [P][N]
+    long long tiles_p;
+    int tiles_n;
+};
+
+__device__ __forceinline__ int chunk_at(int row, int chunk) { return row * 128 + ((chunk ^ (row & 7)) << 4); }
+
+// Tile of a workgroup: neighbouring workgroups go to the chip's eight XCDs in turn, so each of these takes one run of the
+// tiles; channels' tiles of the same positions follow one another (their positions are read from the XCD's L2).
+__device__ __forceinline__ long long tile_of(long long b, long long tiles)
+{
+    const long long each = (tiles + 7) / 8;
+    return (b & 7) * each + (b >> 3);
+}
+
+__device__ __forceinline__ u32x2 read_transposed(const char* at)
+{
+    typedef __attribute__((__vector_size__(4 * sizeof(short)))) short s16x4;
+    typedef __attribute__((address_space(3))) s16x4 Lds;
+    return __builtin_bit_cast(u32x2, __builtin_amdgcn_ds_read_tr16_b64_v4i16((Lds*)at));
+}
+
+// The results of a wave's blocks of 32 x 32 (channels, positions) for positions p0 .. and channels n0 ..: value e of a lane is channel
+// 8 (e / 4) + 4 h + e % 4 of position l32 of a block.  They are turned over in the wave's own LDS, 32 positions at a time, so that
+// neighbouring lanes write neighbouring channels.
+template <class T, int ACT, bool BACK, bool WHOLE, int BLOCKS_P, int BLOCKS_N>
+__device__ __forceinline__ void finish(const LinearDev& d, const f32x16 (&acc)[BLOCKS_N][BLOCKS_P], float* turn, long long p0, int n0, int lane)
+{
+    constexpr int E = kChunk<T>, kAcross = 32 * BLOCKS_N / E, kDown = 64 / kAcross, kPitch = 32 * BLOCKS_N + 4;
+    const int l32 = lane & 31, h = lane >> 5, n = n0 + lane % kAcross * E;
+    float bias[E];
+#pragma unroll
+    for (int j = 0; j < E; ++j) bias[j] = d.bias && n + j < d.N ? d.bias[n + j] : 0.0f;
+#pragma unroll
+    for (int jp = 0; jp < BLOCKS_P; ++jp) {
+#pragma unroll
+        for (int i = 0; i < BLOCKS_N; ++i)
+#pragma unroll
+            for (int e = 0; e < 16; e += 4)
+                *(f32x4*)(turn + l32 * kPitch + i * 32 + 2 * e + 4 * h) = f32x4{acc[i][jp][e], acc[i][jp][e + 1], acc[i][jp][e + 2], acc[i][jp][e + 3]};
+        __builtin_amdgcn_fence(__ATOMIC_RELEASE, "wavefront");
+        __builtin_amdgcn_wave_barrier();
+        __builtin_amdgcn_fence(__ATOMIC_ACQUIRE, "wavefront");
+#pragma unroll
+        for (int r = 0; r < 32 / kDown; ++r) {
+            const int at = r * kDown + lane / kAcross;
+            const long long p = p0 + jp * 32 + at;
+            const int count = p < d.P ? d.N - n : 0;
+            float z[E];
+#pragma unroll
+            for (int j = 0; j < E; j += 4) *(f32x4*)(z + j) = *(const f32x4*)(turn + at * kPitch + lane % kAcross * E + j);
+            Chunk<T> out;
+#pragma unroll
+            for (int j = 0; j < E; ++j) {
+                z[j] += bias[j];
+                out.v[j] = (T)z[j];
+            }
+            if (!BACK) {
+                if (d.keep) store_chunk<WHOLE>((T*)d.keep + p * d.N + n, count, out);
+                Chunk<T> res = {};
+                if (d.res) res = load_chunk<WHOLE>((const T*)d.res + p * d.rs + n, count);
+#pragma unroll
+                for (int j = 0; j < E; ++j) out.v[j] = (T)(activate<ACT>(z[j]) + (float)res.v[j]);
+            }
+            store_chunk<WHOLE>((T*)d.out + p * d.ys + n, count, out);
+        }
+        __builtin_amdgcn_wave_barrier();
+    }
+}
+
+// ---- launchers -------------------------------------------------------------------------------------------------
+
+// Calls f with the activation as a constant.
+template <class F>
+void with_act_of(int act, F&& f)
+{
+    switch (act) {
+        case LP_ACT_RELU: f(std::integral_constant<int, LP_ACT_RELU>()); break;
+        case LP_ACT_SILU: f(std::integral_constant<int, LP_ACT_SILU>()); break;
+        case LP_ACT_GELU: f(std::integral_constant<int, LP_ACT_GELU>()); break;
+        default: f(std::integral_constant<int, LP_ACT_NONE>());
+    }
+}
+
+// Whether rows end with whole chunks.
+inline bool whole(const LinearDev& d, int dtype) { return d.K % (dtype == LP_F32 ? 4 : 8) == 0 && d.N % (dtype == LP_F32 ? 4 : 8) == 0; }
+
+// The general kernel (lp_linear_tile.hip).  back: d_x from d_y and pre.
+void launch_tiles(int dtype, int act, bool back, LinearDev d, hipStream_t s);
+
+// 16-bit types, more than 128 channels (lp_linear_wide.hip): the weights in the operands' order, and the products with them.
+__host__ __device__ constexpr int wide_blocks(int k) { return (k + 63) / 64 * 4; }   // of 16 summed channels
+void launch_pack(int dtype, bool turned, const void* w, int rows, int cols, int pitch, void* out, hipStream_t s);
+void launch_wide(int dtype, int act, bool back, LinearDev d, hipStream_t s);   // back: act is LP_ACT_NONE
+
+// 16-bit types, gradients of the parameters, and d_x where there are few channels (lp_linear_back.hip, lp_linear_back_f16.hip).
+struct BackDev {
+    long long P;
+    int K, N;
+    long long xs, ys;
+    const void *x, *dy, *pre, *w;
+    void *d_x, *dz;              // dz: [P][N]
+    float *parts, *bias_parts;   // [splits][N][K], [splits][N]
+    long long chunk;             // positions of a part
+    int tiles_n, tiles_k, splits;
+    int d_weight, d_bias;        // wanted
+    int whole;                   // rows end with whole chunks
+};
+
+// How the positions are divided for the parameters' gradients.
+struct Parts {
+    int bn, bk, tiles_n, tiles_k, splits;
+    long long chunk;
+};
+hipError_t launch_back_bf16(int act, const BackDev& d, const Parts& p, bool skinny, hipStream_t s);
+hipError_t launch_back_f16(int act, const BackDev& d, const Parts& p, bool skinny, hipStream_t s);
+
+}  // namespace linear
+}  // namespace lp

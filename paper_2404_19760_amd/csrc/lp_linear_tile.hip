@@ -1,0 +1,126 @@
+// Products of positions with a weight matrix in tiles, for all types and sizes, and d_x from d_y and what the forward kept.
+#include "lp_linear.h"
+
+namespace lp {
+namespace linear {
+
+namespace {
+
+// ---- tiles -----------------------------------------------------------------------------------------------------
+//
+// A workgroup of four waves makes BP positions x BN channels.  A step is 128 bytes of channels of both operands, staged through
+// registers into one of two LDS buffers while the other one is multiplied.  A row's eight chunks lie at chunk ^ (row mod 8): eight
+// rows' same chunk, and a row's eight chunks, both touch every bank once.
+template <int BP, int BN>
+struct TileShape {
+    static constexpr int kWavesN = BN >= 128 ? 2 : 1, kWavesP = 4 / kWavesN;
+    static constexpr int kP = BP / kWavesP, kN = BN / kWavesN;          // of a wave
+    static constexpr int kBlocksP = kP / 32, kBlocksN = kN / 32;
+    static constexpr int kPitch = kN + 4;                               // floats of a position's row while results are turned over
+    static constexpr int kStage = (BP + BN) * 128;                      // bytes of a step
+    static constexpr int kLds = 2 * kStage > 4 * 32 * kPitch * 4 ? 2 * kStage : 4 * 32 * kPitch * 4;
+};
+
+template <class T, int ACT, bool BACK, bool WHOLE, int BP, int BN>
+__global__ __launch_bounds__(kThreads, 2) void linear_tile_kernel(LinearDev d)
+{
+    using S = TileShape<BP, BN>;
+    constexpr int E = kChunk<T>;
+    constexpr int kLoadsA = BP * 8 / kThreads, kLoadsW = BN * 8 / kThreads;
+    __shared__ alignas(16) char lds[S::kLds];
+    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, l32 = lane & 31, h = lane >> 5;
+    const int wave_p = wave / S::kWavesN * S::kP, wave_n = wave % S::kWavesN * S::kN;
+    const int c8 = threadIdx.x & 7, row = threadIdx.x >> 3;
+    const long long tiles = d.tiles_p * d.tiles_n, rounds = (tiles + 7) / 8 * 8;
+    for (long long b = blockIdx.x; b < rounds; b += gridDim.x) {
+        const long long tile = tile_of(b, tiles);
+        if (tile >= tiles) continue;
+        const long long p0 = tile / d.tiles_n * BP;
+        const int n0 = (int)(tile % d.tiles_n) * BN;
+        Chunk<T> a[kLoadsA], pre[BACK && ACT != LP_ACT_NONE ? kLoadsA : 1], w[kLoadsW];
+        auto ask = [&](int k0) {
+            const int k = k0 + c8 * E;
+#pragma unroll
+            for (int u = 0; u < kLoadsA; ++u) {
+                const long long p = p0 + row + u * 32;
+                const int count = p < d.P ? d.K - k : 0;
+                a[u] = load_chunk<WHOLE>((const T*)d.a + p * d.as + k, count);
+                if (BACK && ACT != LP_ACT_NONE) pre[u] = load_chunk<WHOLE>((const T*)d.pre + p * d.K + k, count);
+            }
+#pragma unroll
+            for (int u = 0; u < kLoadsW; ++u) {
+                const int n = n0 + row + u * 32;
+                w[u] = load_chunk<WHOLE>((const T*)d.w + n * d.ws + k, n < d.N ? d.K - k : 0);
+            }
+        };
+        auto put = [&](int buffer) {
+            char* to = lds + buffer * S::kStage;
+#pragma unroll
+            for (int u = 0; u < kLoadsA; ++u) {
+                Chunk<T> v = a[u];
+                if (BACK && ACT != LP_ACT_NONE) v = gradient<ACT>(a[u], pre[u]).hi;
+                *(Chunk<T>*)(to + chunk_at(row + u * 32, c8)) = v;
+            }
+#pragma unroll
+            for (int u = 0; u < kLoadsW; ++u) *(Chunk<T>*)(to + BP * 128 + chunk_at(row + u * 32, c8)) = w[u];
+        };
+        f32x16 acc[S::kBlocksN][S::kBlocksP] = {};
+        const int steps = (d.K + 8 * E - 1) / (8 * E);
+        ask(0);
+        put(0);
+        __syncthreads();
+        for (int s = 0; s < steps; ++s) {
+            if (s + 1 < steps) ask((s + 1) * 8 * E);
+            const char* from = lds + (s & 1) * S::kStage;
+#pragma unroll
+            for (int q = 0; q < 4; ++q) {
+                Chunk<T> wv[S::kBlocksN], av[S::kBlocksP];
+#pragma unroll
+                for (int i = 0; i < S::kBlocksN; ++i) wv[i] = *(const Chunk<T>*)(from + BP * 128 + chunk_at(wave_n + i * 32 + l32, 2 * q + h));
+#pragma unroll
+                for (int i = 0; i < S::kBlocksP; ++i) av[i] = *(const Chunk<T>*)(from + chunk_at(wave_p + i * 32 + l32, 2 * q + h));
+#pragma unroll
+                for (int i = 0; i < S::kBlocksN; ++i)
+#pragma unroll
+                    for (int j = 0; j < S::kBlocksP; ++j) acc[i][j] = multiply(wv[i], av[j], acc[i][j]);
+            }
+            if (s + 1 < steps) put((s + 1) & 1);
+            __syncthreads();
+        }
+        finish<T, ACT, BACK, WHOLE, S::kBlocksP, S::kBlocksN>(d, acc, (float*)lds + wave * 32 * S::kPitch, p0 + wave_p, n0 + wave_n, lane);
+        __syncthreads();   // (the next tile's first step lies where results were)
+    }
+}
+
+template <class T, int ACT, bool BACK>
+void tiles(LinearDev d, bool whole, hipStream_t s)
+{
+    auto go = [&](auto bn) {
+        constexpr int BN = decltype(bn)::value;
+        d.tiles_p = (d.P + 127) / 128;
+        d.tiles_n = (d.N + BN - 1) / BN;
+        const dim3 grid(grid_of((d.tiles_p * d.tiles_n + 7) / 8 * 8));
+        if (whole) hipLaunchKernelGGL((linear_tile_kernel<T, ACT, BACK, true, 128, BN>), grid, dim3(kThreads), 0, s, d);
+        else hipLaunchKernelGGL((linear_tile_kernel<T, ACT, BACK, false, 128, BN>), grid, dim3(kThreads), 0, s, d);
+    };
+    if (d.N <= 32) go(std::integral_constant<int, 32>());
+    else if (d.N <= 64) go(std::integral_constant<int, 64>());
+    else go(std::integral_constant<int, 128>());
+}
+
+}  // namespace
+
+// Tiles of 128 x 128 results, narrower ones where there are few channels.
+void launch_tiles(int dtype, int act, bool back, LinearDev d, hipStream_t s)
+{
+    const bool w = whole(d, dtype);
+    with_act_of(act, [&](auto a) {
+        constexpr int A = decltype(a)::value;
+        if (dtype == LP_BF16) back ? tiles<__bf16, A, true>(d, w, s) : tiles<__bf16, A, false>(d, w, s);
+        else if (dtype == LP_F16) back ? tiles<_Float16, A, true>(d, w, s) : tiles<_Float16, A, false>(d, w, s);
+        else back ? tiles<float, A, true>(d, w, s) : tiles<float, A, false>(d, w, s);
+    });
+}
+
+}  // namespace linear
+}  // namespace lp

@@ -81,6 +81,43 @@ __device__ __forceinline__ f32x16 multiply(const Chunk<float>& a, const Chunk<fl
     return acc;
 }
 
+// The GELU and its slope for tensors of 16 bits, whose results are rounded by 2^-12 and more (a slope's product with d_y by 2^-16 in two
+// parts).  As in lp_act.h the tail of the normal distribution beyond |z| is t Q(t) exp(-z^2 / 2), t = 1 / (1 + p |z|), but
+// with one Q of degree 4 for all z: for the value a fit of least relative error of the tail (3.6e-5 with fp32 rounding, so a negative z's value
+// stays within a seventh of half a step of fp16), for the slope one of least absolute error (3.1e-7).  20 instructions' time instead of
+// 31: the vector instructions of the activation bound wide blocks as much as the matrix cores.
+__device__ __forceinline__ float tail_of(float z, float& e, float p, const float (&q)[5])
+{
+    e = __builtin_amdgcn_exp2f(z * z * -0.72134752f);
+    const float t = __builtin_amdgcn_rcpf(fmaf(p, fabsf(z), 1.0f));
+    float v = q[4];
+#pragma unroll
+    for (int k = 3; k >= 0; --k) v = fmaf(v, t, q[k]);
+    return v * t * e;
+}
+template <int ACT, class T>
+__device__ __forceinline__ float activate_as(float z)
+{
+    if constexpr (ACT == LP_ACT_GELU && sizeof(T) == 2) {
+        float e;
+        const float tail = tail_of(z, e, 0.38f, {0.151225137f, 0.157829468f, 0.0919797578f, 0.188876449f, -0.08992834f});
+        return fmaf(-fminf(fabsf(z), 64.0f), tail, fmaxf(z, 0.0f));   // (of an infinite z the tail is 0, and of NaN it is NaN)
+    } else {
+        return activate<ACT>(z);
+    }
+}
+template <int ACT, class T>
+__device__ __forceinline__ float slope_as(float z)
+{
+    if constexpr (ACT == LP_ACT_GELU && sizeof(T) == 2) {
+        float e;
+        const float tail = tail_of(z, e, 0.34f, {0.130569511f, 0.179848642f, -0.0278562922f, 0.320559185f, -0.103121231f});
+        return fmaf(z * kInvSqrt2Pi, e, 0.5f + __builtin_copysignf(0.5f - tail, z));
+    } else {
+        return slope<ACT>(z);
+    }
+}
+
 // d_z of a chunk, rounded to T, and what the rounding left.
 template <class T>
 struct Gradient {
@@ -93,7 +130,7 @@ __device__ __forceinline__ Gradient<T> gradient(const Chunk<T>& dy, const Chunk<
     Gradient<T> g;
 #pragma unroll
     for (int j = 0; j < kChunk<T>; ++j) {
-        g.v[j] = (float)dy.v[j] * (ACT == LP_ACT_NONE ? 1.0f : slope<ACT>((float)pre.v[j]));
+        g.v[j] = (float)dy.v[j] * (ACT == LP_ACT_NONE ? 1.0f : slope_as<ACT, T>((float)pre.v[j]));
         asm("" : "+v"(g.v[j]));   // (both parts come from this value: hi alone could be rounded straight from the product)
         g.hi.v[j] = (T)g.v[j];
         if (sizeof(T) == 2) {
@@ -139,10 +176,14 @@ template <class T, int ACT, bool BACK, bool WHOLE, int BLOCKS_P, int BLOCKS_N>
 __device__ __forceinline__ void finish(const LinearDev& d, const f32x16 (&acc)[BLOCKS_N][BLOCKS_P], float* turn, long long p0, int n0, int lane)
 {
     constexpr int E = kChunk<T>, kAcross = 32 * BLOCKS_N / E, kDown = 64 / kAcross, kPitch = 32 * BLOCKS_N + 4;
+    constexpr int kTimes = 32 / kDown;
     const int l32 = lane & 31, h = lane >> 5, n = n0 + lane % kAcross * E;
+    const long long first = p0 + lane / kAcross;   // the lane's first position; the others follow at distances that all lanes share
     float bias[E];
 #pragma unroll
     for (int j = 0; j < E; ++j) bias[j] = d.bias && n + j < d.N ? d.bias[n + j] : 0.0f;
+    T *out = (T*)d.out + first * d.ys + n, *keep = (T*)d.keep + first * d.N + n;
+    const T* res = (const T*)d.res + first * d.rs + n;
 #pragma unroll
     for (int jp = 0; jp < BLOCKS_P; ++jp) {
 #pragma unroll
@@ -153,28 +194,34 @@ __device__ __forceinline__ void finish(const LinearDev& d, const f32x16 (&acc)[B
         __builtin_amdgcn_fence(__ATOMIC_RELEASE, "wavefront");
         __builtin_amdgcn_wave_barrier();
         __builtin_amdgcn_fence(__ATOMIC_ACQUIRE, "wavefront");
+        int count[kTimes];
+        Chunk<T> added[kTimes];
 #pragma unroll
-        for (int r = 0; r < 32 / kDown; ++r) {
-            const int at = r * kDown + lane / kAcross;
-            const long long p = p0 + jp * 32 + at;
-            const int count = p < d.P ? d.N - n : 0;
+        for (int r = 0; r < kTimes; ++r) {
+            count[r] = first + (jp * 32 + r * kDown) < d.P ? d.N - n : 0;
+            added[r] = Chunk<T>{};
+        }
+        if (!BACK && d.res)
+#pragma unroll
+            for (int r = 0; r < kTimes; ++r) added[r] = load_chunk<WHOLE>(res + (jp * 32 + r * kDown) * d.rs, count[r]);
+#pragma unroll
+        for (int r = 0; r < kTimes; ++r) {
             float z[E];
+            const float* from = turn + (r * kDown + lane / kAcross) * kPitch + lane % kAcross * E;
 #pragma unroll
-            for (int j = 0; j < E; j += 4) *(f32x4*)(z + j) = *(const f32x4*)(turn + at * kPitch + lane % kAcross * E + j);
-            Chunk<T> out;
+            for (int j = 0; j < E; j += 4) *(f32x4*)(z + j) = *(const f32x4*)(from + j);
+            Chunk<T> v;
 #pragma unroll
             for (int j = 0; j < E; ++j) {
                 z[j] += bias[j];
-                out.v[j] = (T)z[j];
+                v.v[j] = (T)z[j];
             }
             if (!BACK) {
-                if (d.keep) store_chunk<WHOLE>((T*)d.keep + p * d.N + n, count, out);
-                Chunk<T> res = {};
-                if (d.res) res = load_chunk<WHOLE>((const T*)d.res + p * d.rs + n, count);
+                if (d.keep) store_chunk<WHOLE>(keep + (long long)(jp * 32 + r * kDown) * d.N, count[r], v);
 #pragma unroll
-                for (int j = 0; j < E; ++j) out.v[j] = (T)(activate<ACT>(z[j]) + (float)res.v[j]);
+                for (int j = 0; j < E; ++j) v.v[j] = (T)(activate_as<ACT, T>(z[j]) + (float)added[r].v[j]);
             }
-            store_chunk<WHOLE>((T*)d.out + p * d.ys + n, count, out);
+            store_chunk<WHOLE>(out + (jp * 32 + r * kDown) * d.ys, count[r], v);
         }
         __builtin_amdgcn_wave_barrier();
     }

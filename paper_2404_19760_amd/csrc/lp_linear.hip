@@ -60,7 +60,7 @@ __global__ __launch_bounds__(kThreads) void linear_rows_kernel(LinearDev d)
             if (lane != i * ROWS + r || n >= d.N || r >= d.P) continue;
             const float z = sum[i][r] + (d.bias ? d.bias[n] : 0.0f);
             if (d.keep) ((T*)d.keep)[(long long)r * d.N + n] = (T)z;
-            float y = activate<ACT>(z);
+            float y = activate_as<ACT, T>(z);
             if (d.res) y += (float)((const T*)d.res)[r * d.rs + n];
             ((T*)d.out)[r * d.ys + n] = (T)y;
         }

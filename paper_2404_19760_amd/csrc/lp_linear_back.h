@@ -25,7 +25,8 @@ struct BackShape {
     static constexpr int kWaves = SKINNY ? 4 : WN * WK, kThreadsOf = 64 * kWaves;
     static constexpr int kPitchN = image_pitch(BN), kPitchK = image_pitch(BK);
     static constexpr int kBlocksN = BN / WN / 32, kBlocksK = BK / WK / 32;
-    static constexpr int kLoadsN = ROWS * (BN / 8) / kThreadsOf, kLoadsK = ROWS * (BK / 8) / kThreadsOf > 0 ? ROWS * (BK / 8) / kThreadsOf : 1;
+    static constexpr int kLoadsN = ROWS * (BN / 8) / kThreadsOf, kLoadsK = ROWS * (BK / 8) / kThreadsOf;
+    static_assert(ROWS * (BN / 8) % kThreadsOf == 0 && ROWS * (BK / 8) % kThreadsOf == 0);
     static constexpr int kImageN = ROWS * kPitchN, kImageK = ROWS * kPitchK;
     static constexpr int kWeights = SKINNY ? BN * BK * 2 : 0;
     static constexpr int stage(bool split) { return kImageN * (split ? 2 : 1) + kImageK; }
@@ -69,21 +70,25 @@ __global__ __launch_bounds__(S::kThreadsOf, S::kSkinny && (S::kBN < 128 || S::kB
     const bool write_dz = d.dz && k0 == 0;
     Chunk<T> dy[S::kLoadsN], pre[S::kLoadsN], x[S::kLoadsK];
     float bias[8] = {};
+    // a lane's rows of the next positions; those of its other loads lie at distances that all lanes share
+    const T *dy_at = (const T*)d.dy + (first + rn) * d.ys + n, *pre_at = (const T*)d.pre + (first + rn) * d.N + n, *x_at = (const T*)d.x + (first + rk) * d.xs + k;
+    T* dz_at = (T*)d.dz + (first + rn) * d.N + n;
     auto ask = [&](long long p0) {
+        const int left = (int)min((long long)S::kRows, end - p0);   // (<= 0 behind the last position)
 #pragma unroll
         for (int u = 0; u < S::kLoadsN; ++u) {
-            const long long p = p0 + rn + u * kDownN;
-            const int count = p < end ? d.N - n : 0;
-            dy[u] = load_chunk<WHOLE>((const T*)d.dy + p * d.ys + n, count);
-            if (kSplit) pre[u] = load_chunk<WHOLE>((const T*)d.pre + p * d.N + n, count);
+            const int count = rn + u * kDownN < left ? d.N - n : 0;
+            dy[u] = load_chunk<WHOLE>(dy_at + u * kDownN * d.ys, count);
+            if (kSplit) pre[u] = load_chunk<WHOLE>(pre_at + (long long)u * kDownN * d.N, count);
         }
 #pragma unroll
-        for (int u = 0; u < S::kLoadsK; ++u) {
-            const long long p = p0 + rk + u * kDownK;
-            x[u] = load_chunk<WHOLE>((const T*)d.x + p * d.xs + k, p < end && rk + u * kDownK < S::kRows ? d.K - k : 0);
-        }
+        for (int u = 0; u < S::kLoadsK; ++u) x[u] = load_chunk<WHOLE>(x_at + u * kDownK * d.xs, rk + u * kDownK < left ? d.K - k : 0);
+        dy_at += S::kRows * d.ys;
+        pre_at += (long long)S::kRows * d.N;
+        x_at += S::kRows * d.xs;
     };
     auto put = [&](char* to, long long p0) {
+        const int left = (int)min((long long)S::kRows, end - p0);
 #pragma unroll
         for (int u = 0; u < S::kLoadsN; ++u) {
             const int at = (rn + u * kDownN) * S::kPitchN + cn * 16;
@@ -92,14 +97,11 @@ __global__ __launch_bounds__(S::kThreadsOf, S::kSkinny && (S::kBN < 128 || S::kB
             if (kSplit) *(Chunk<T>*)(to + kLo + at) = g.lo;
 #pragma unroll
             for (int j = 0; j < 8; ++j) bias[j] += g.v[j];
-            if (write_dz) {
-                const long long p = p0 + rn + u * kDownN;
-                store_chunk<WHOLE>((T*)d.dz + p * d.N + n, p < end ? d.N - n : 0, g.hi);
-            }
+            if (write_dz) store_chunk<WHOLE>(dz_at + (long long)u * kDownN * d.N, rn + u * kDownN < left ? d.N - n : 0, g.hi);
         }
+        dz_at += (long long)S::kRows * d.N;
 #pragma unroll
-        for (int u = 0; u < S::kLoadsK; ++u)
-            if (rk + u * kDownK < S::kRows) *(Chunk<T>*)(to + kX + (rk + u * kDownK) * S::kPitchK + ck * 16) = x[u];
+        for (int u = 0; u < S::kLoadsK; ++u) *(Chunk<T>*)(to + kX + (rk + u * kDownK) * S::kPitchK + ck * 16) = x[u];
     };
     f32x16 acc[S::kBlocksN][S::kBlocksK] = {};
     auto multiply_all = [&](const char* from) {
@@ -136,13 +138,14 @@ __global__ __launch_bounds__(S::kThreadsOf, S::kSkinny && (S::kBN < 128 || S::kB
             *(Chunk<T>*)(weights + f * 1024 + lane * 16) = v;
         }
         constexpr int kGroups = S::kRows / 16, kPer = 4 / kGroups;   // groups of 16 positions; waves of a group
+        const int r = wave % kGroups * 16 + (lane & 15);
+        T* dx_at = (T*)d.d_x + (first + r) * d.xs + 8 * (lane >> 4);
         for (long long p0 = first; p0 < end; p0 += S::kRows) {
             put(lds, p0);
             __syncthreads();
             if (p0 + S::kRows < end) ask(p0 + S::kRows);
             if (multiplies) multiply_all(lds);
             if (d.d_x) {
-                const int group = wave % kGroups, r = group * 16 + (lane & 15);
                 Chunk<T> g[S::kBN / 32];
 #pragma unroll
                 for (int i = 0; i < S::kBN / 32; ++i) g[i] = *(const Chunk<T>*)(lds + r * S::kPitchN + i * 64 + (lane >> 4) * 16);
@@ -159,11 +162,11 @@ __global__ __launch_bounds__(S::kThreadsOf, S::kSkinny && (S::kBN < 128 || S::kB
                     Chunk<T> out;
 #pragma unroll
                     for (int j = 0; j < 8; ++j) out.v[j] = (T)res[j >> 2][j & 3];
-                    const long long p = p0 + r;
                     const int kk = k32 * 32 + 8 * (lane >> 4);
-                    store_chunk<WHOLE>((T*)d.d_x + p * d.xs + kk, p < end ? d.K - kk : 0, out);
+                    store_chunk<WHOLE>(dx_at + k32 * 32, p0 + r < end ? d.K - kk : 0, out);
                 }
             }
+            dx_at += S::kRows * d.xs;
             __syncthreads();
         }
     } else {

@@ -180,41 +180,55 @@ __global__ __launch_bounds__(kThreads, 2) void linear_weight_kernel(WeightDev d)
     }
 }
 
-// out += the sum of its parts, in an order that depends on their number alone: a workgroup 64 values, 16 lanes x 4 of them, 64 lanes share the parts.
-constexpr int kJoinThreads = 1024;
-__global__ __launch_bounds__(kJoinThreads) void linear_join_kernel(const float* parts, float* out, const float* bias_parts, float* d_bias, long long count, int N, int splits)
+// out += the sum of its parts, in an order that depends on the sizes alone: a lane four values, `lanes` (a power of two) share the parts.
+struct JoinDev {
+    const float *parts, *bias_parts;
+    float *out, *d_bias;
+    long long count;
+    int N, splits, lanes, bias_lanes;
+};
+__global__ __launch_bounds__(kThreads) void linear_join_kernel(JoinDev d)
 {
-    __shared__ f32x4 lds[kJoinThreads];
-    const long long blocks = out ? (count + 63) / 64 : 0, all = blocks + (d_bias ? (N + 63) / 64 : 0);
+    __shared__ f32x4 lds[kThreads];
+    const int each = kThreads / d.lanes * 4, bias_each = kThreads / d.bias_lanes * 4;   // values of a workgroup
+    const long long blocks = d.out ? (d.count + each - 1) / each : 0, all = blocks + (d.d_bias ? (d.N + bias_each - 1) / bias_each : 0);
     for (long long b = blockIdx.x; b < all; b += gridDim.x) {
         const bool weight = b < blocks;
-        const long long i = (weight ? b : b - blocks) * 64 + (threadIdx.x & 15) * 4, size = weight ? count : N;
-        const float* from = (weight ? parts : bias_parts) + i;
-        const int in = (int)min(4ll, size - i);
+        const int lanes = weight ? d.lanes : d.bias_lanes, across = kThreads / lanes, c = threadIdx.x % across, lane = threadIdx.x / across;
+        const long long size = weight ? d.count : d.N, i = (weight ? b : b - blocks) * (across * 4) + c * 4;
+        const float* from = (weight ? d.parts : d.bias_parts) + i;
+        float* to = (weight ? d.out : d.d_bias) + i;
+        const int in = (int)max(0ll, min(4ll, size - i));
         f32x4 sum = {};
-        for (int s = threadIdx.x >> 4; s < splits; s += 64) {
-            const float* at = from + s * size;
-            f32x4 v = {};
-            if (in == 4) {
-                __builtin_memcpy(&v, at, 16);
-            } else {
+        if (in == 4) {
+#pragma unroll 4
+            for (int s = lane; s < d.splits; s += lanes) {
+                f32x4 v;
+                __builtin_memcpy(&v, from + s * size, 16);
+                sum += v;
+            }
+        } else {
+            for (int s = lane; s < d.splits; s += lanes)
 #pragma unroll
                 for (int j = 0; j < 4; ++j)
-                    if (j < in) v[j] = at[j];
-            }
-            sum += v;
+                    if (j < in) sum[j] += from[s * size + j];
         }
         __syncthreads();   // (the sums before have been read)
         lds[threadIdx.x] = sum;
         __syncthreads();
-        if (threadIdx.x >= 64) continue;
-        // value (threadIdx.x): lane threadIdx.x / 4 of the 16, its value threadIdx.x mod 4
-        float total = 0.0f;
-        const int lanes = min(splits, 64);
-        for (int s = 0; s < lanes; ++s) total += ((const float*)&lds[s * 16])[threadIdx.x];
-        const long long to = (weight ? b : b - blocks) * 64 + threadIdx.x;
-        if (to < size) (weight ? out : d_bias)[to] += total;
+        if (lane) continue;
+        for (int s = 1; s < lanes; ++s) sum += lds[s * across + c];
+#pragma unroll
+        for (int j = 0; j < 4; ++j)
+            if (j < in) to[j] += sum[j];
     }
+}
+// Lanes that share the parts: as many as it takes to give every compute unit work.
+int join_lanes(long long count, int splits)
+{
+    int lanes = 1;
+    while (lanes < 64 && lanes * 2 <= splits && count * lanes < 512ll * kThreads * 4) lanes *= 2;
+    return lanes;
 }
 
 // W^T with rows of `pitch` elements.
@@ -421,8 +435,11 @@ lp_status backward(const lp_linear* q, const void* x, const void* pre, const voi
         });
     }
     if (params && join) {
-        const long long count = (long long)c.N * c.K, blocks = (d_weight ? (count + 63) / 64 : 0) + (d_bias ? (c.N + 63) / 64 : 0);
-        hipLaunchKernelGGL(linear_join_kernel, dim3(grid_of(blocks)), dim3(kJoinThreads), 0, s, parts, d_weight, bias_parts, d_bias, count, c.N, p.splits);
+        const long long count = (long long)c.N * c.K;
+        const JoinDev j = {parts, bias_parts, d_weight, d_bias, count, c.N, p.splits, join_lanes(count, p.splits), join_lanes(c.N, p.splits)};
+        const long long each = kThreads / j.lanes * 4, bias_each = kThreads / j.bias_lanes * 4;
+        const long long blocks = (d_weight ? (count + each - 1) / each : 0) + (d_bias ? (c.N + bias_each - 1) / bias_each : 0);
+        hipLaunchKernelGGL(linear_join_kernel, dim3(grid_of(blocks)), dim3(kThreads), 0, s, j);
     }
     if (d_x && !skinny) {
         LinearDev d;

@@ -12,6 +12,7 @@ from __future__ import annotations
 import ctypes as C
 import dataclasses
 import os
+import struct
 from typing import List, Optional, Sequence
 
 import numpy as np
@@ -790,18 +791,19 @@ def lp_group_norm_bwd(norm: GroupNorm, x: torch.Tensor, stats: torch.Tensor, d_y
     _written(d_x, d_gamma, d_beta)
 
 
-def _on_current_device(*tensors: Optional[torch.Tensor]) -> None:
+# (what torch.cuda.current_device() asks for behind its own initialisation, which a tensor on the GPU has been through)
+_current_device = getattr(torch._C, "_cuda_getDevice", torch.cuda.current_device)
+
+
+def _on_current_device(first: torch.Tensor, *others: Optional[torch.Tensor]) -> torch.device:
     """Kernels run on the current device: the tensors of a call (None: not there) lie on it, all of them."""
-    device = None
-    for t in tensors:
-        if t is None:
-            continue
-        if device is None:
-            device = t.device
-        elif t.device != device:
+    device = first.device
+    for t in others:
+        if t is not None and t.device != device:
             raise ValueError("the tensors of a call must be on one device")
-    if device is not None and device.type == "cuda" and device.index != torch.cuda.current_device():
+    if device.type == "cuda" and device.index != _current_device():
         raise ValueError("the tensors of a call must be on the current device")
+    return device
 
 
 def _apart(written: torch.Tensor, written_step: int, read: Optional[torch.Tensor], read_step: int, written_name: str, read_name: str) -> None:
@@ -844,13 +846,14 @@ class Linear:
         n, k = w.shape
         if x.dim() < 1 or x.shape[-1] != k:
             raise ValueError(f"x must have {k} channels, the weight's columns")
-        r_stride = 0
+        if (k | n) >> 31:
+            raise ValueError("weight's rows and columns do not fit 32 bits")
+        bias, r_stride, r_at = self.bias, 0, None
         if residual is not None:
-            r_stride = _channel_last(residual, "residual", x.shape[:-1] + (n,), dtype)
-        _on_current_device(x, w, self.bias, residual)
-        return _Linear(x.numel() // k if k else 0, _int32(k, "K"), _int32(n, "N"), _int32(self.act, "act"), _GRID_DTYPES[dtype],
-                       _position_stride(x, "x"), y_stride, r_stride, w.data_ptr(), _dev_f32(self.bias, "bias", (n,)),
-                       None if residual is None else residual.data_ptr())
+            r_stride, r_at = _channel_last(residual, "residual", x.shape[:-1] + (n,), dtype), residual.data_ptr()
+        _on_current_device(x, w, bias, residual)
+        return _Linear(x.numel() // k if k else 0, k, n, _int32(self.act, "act"), _GRID_DTYPES[dtype], _position_stride(x, "x"), y_stride,
+                       r_stride, w.data_ptr(), None if bias is None else _dev_f32(bias, "bias", (n,)), r_at)
 
 
 def _linear_bytes(q: _Linear, backward: bool = True):
@@ -936,18 +939,16 @@ class ResidualNorm:
             raise ValueError("h must have a last axis of channels")
         c = shape[-1]
         n = shape[0] if len(shape) > 1 else 1
-        gate, per_sample = self.gate, 0
-        if gate is not None and gate.dim() == 2:
-            per_sample = 1
-            _dev_f32(gate, "gate", (n, c))
-        elif gate is not None:
-            _dev_f32(gate, "gate", (c,))
-        _on_current_device(h, self.gamma, self.beta, self.post_gamma, gate)
+        gamma, beta, post_gamma, gate, per_sample, gate_at = self.gamma, self.beta, self.post_gamma, self.gate, 0, None
+        if gate is not None:
+            per_sample = int(gate.dim() == 2)
+            gate_at = _dev_f32(gate, "gate", (n, c) if per_sample else (c,))
+        _on_current_device(h, gamma, beta, post_gamma, gate)
         return _ResidualNorm(n, h.numel() // (n * c) if n and c else 0, _int32(c, "the number of channels"), _int32(self.kind, "kind"),
-                             _int32(self.post_norm, "post_norm"), per_sample, float(self.alpha), float(self.eps), _GRID_DTYPES[h.dtype],
+                             _int32(self.post_norm, "post_norm"), per_sample, self.alpha, self.eps, _GRID_DTYPES[h.dtype],
                              _GRID_DTYPES[f_dtype], _position_stride(h, "h"), f_stride, y_stride,
-                             _dev_f32(self.post_gamma, "post_gamma", (c,)), None if gate is None else gate.data_ptr(),
-                             _dev_f32(self.gamma, "gamma", (c,)), _dev_f32(self.beta, "beta", (c,)))
+                             None if post_gamma is None else _dev_f32(post_gamma, "post_gamma", (c,)), gate_at,
+                             None if gamma is None else _dev_f32(gamma, "gamma", (c,)), None if beta is None else _dev_f32(beta, "beta", (c,)))
 
 
 def lp_residual_norm_workspace_bytes(norm: ResidualNorm, h: torch.Tensor) -> int:
@@ -1035,17 +1036,24 @@ def _is_dense(t: torch.Tensor) -> bool:
 
 
 def _gradients(grads, outs):
+    """The call's structs (tensors are also checked to be on the current device)."""
     if len(grads) != len(outs):
         raise ValueError("one output per gradient is needed")
-    rows = []
-    for k, (g, o) in enumerate(zip(grads, outs)):
-        dtype = _GRID_DTYPES.get(g.dtype)
-        if dtype is None or not g.is_cuda or not _is_dense(g):
-            raise ValueError(f"grads[{k}] must be a dense float32, bfloat16 or float16 tensor on the GPU")
-        if o is not g and not (o.is_cuda and o.dtype is g.dtype and o.shape == g.shape and o.stride() == g.stride()):
-            raise ValueError(f"outs[{k}] must be a GPU tensor of the shape, type and strides of grads[{k}]")
-        rows.append((g.numel(), g.data_ptr(), o.data_ptr(), dtype))
-    return (_Gradient * max(1, len(rows)))(*rows)
+    values, device = [], None
+    for k, g in enumerate(grads):
+        o, dtype, dense = outs[k], g.dtype, g.is_contiguous()
+        if not (g.is_cuda if device is None else g.device == device) or dtype not in _GRID_DTYPES or not (dense or _is_dense(g)):
+            raise ValueError(f"grads[{k}] must be a dense float32, bfloat16 or float16 tensor on the GPU, all on one device")
+        at = to = g.data_ptr()
+        if o is not g:
+            if not (o.dtype is dtype and o.shape == g.shape and o.device == g.device and (o.is_contiguous() if dense else o.stride() == g.stride())):
+                raise ValueError(f"outs[{k}] must be a tensor of the shape, type and strides of grads[{k}], all on one device")
+            to = o.data_ptr()
+        if device is None:
+            device = _on_current_device(g)
+        values += (g.numel(), at, to, _GRID_DTYPES[dtype])
+    # (one buffer of structs, laid out as _Gradient is)
+    return (_Gradient * max(1, len(grads))).from_buffer(bytearray(struct.pack("qQQi4x" * len(grads), *values) or C.sizeof(_Gradient)))
 
 
 def _grad_norm_bytes(n: int, arr) -> int:
@@ -1061,7 +1069,7 @@ def lp_grad_norm_workspace_bytes(grads: Sequence[torch.Tensor]) -> int:
 def lp_grad_norm(grads: Sequence[torch.Tensor], norm: torch.Tensor, workspace: Optional[torch.Tensor], stream=None) -> None:
     """Enqueue the norm of all gradients together: norm (float32, shape ()) is written."""
     arr = _gradients(grads, grads)
-    _on_current_device(*grads, norm, workspace)
+    _on_current_device(norm, *grads[:1], workspace)
     wp, wn = _workspace(workspace)
     _check(_lib.lp_grad_norm(len(grads), arr, _dev_f32(norm, "norm", ()), wp, wn, _stream_ptr(stream)))
     _written(norm)
@@ -1071,7 +1079,7 @@ def lp_clip_grad_norm(grads: Sequence[torch.Tensor], outs: Sequence[torch.Tensor
                       workspace: Optional[torch.Tensor], eps: float = 1e-6, stream=None) -> None:
     """Enqueue the clipping: outs (the gradients themselves, or tensors like them) and norm (float32, shape ()) are written."""
     arr = _gradients(grads, outs)
-    _on_current_device(*grads, *outs, norm, workspace)
+    _on_current_device(norm, *grads[:1], workspace)
     wp, wn = _workspace(workspace)
     _check(_lib.lp_clip_grad_norm(len(grads), arr, float(max_norm), float(eps), _dev_f32(norm, "norm", ()), wp, wn, _stream_ptr(stream)))
     increment_version([*outs, norm])
@@ -1309,7 +1317,8 @@ def linear_fwd(linear: Linear, x: torch.Tensor, residual: Optional[torch.Tensor]
     """Allocate outputs and workspace and run lp_linear_fwd.  Returns (y, pre); pre (keep; else None) is for linear_bwd, which needs it
     where there is an activation."""
     q = linear.c_struct(x, 0, residual)   # (new outputs are dense: what the entry point checks of them holds)
-    y = torch.empty(x.shape[:-1] + (q.N,), dtype=x.dtype, device=x.device)
+    shape = x.shape
+    y = x.new_empty((shape[0], q.N) if len(shape) == 2 else shape[:-1] + (q.N,))
     pre = torch.empty_like(y) if keep else None
     n = _linear_bytes(q, False)[0]
     ws = torch.empty(n, dtype=torch.uint8, device=x.device) if n else None   # (held until the kernels are enqueued)
@@ -1343,9 +1352,9 @@ def residual_norm_fwd(norm: ResidualNorm, h: torch.Tensor, f: Optional[torch.Ten
     q = norm.c_struct(h, y_dtype, 0 if f is None else _channel_last(f, "f", h.shape, y_dtype))
     if f is not None:
         _on_current_device(h, f)
-    same = f is None and norm.alpha == 1.0
-    s = h if same else torch.empty_like(h) if h.is_contiguous() else torch.empty_strided(h.shape, h.stride(), dtype=h.dtype, device=h.device)
-    y = torch.empty(h.shape, dtype=y_dtype, device=h.device)
+    same, dense = f is None and norm.alpha == 1.0, h.is_contiguous()
+    s = h if same else torch.empty_like(h) if dense else torch.empty_strided(h.shape, h.stride(), dtype=h.dtype, device=h.device)
+    y = torch.empty_like(h) if dense and y_dtype is h.dtype else torch.empty(h.shape, dtype=y_dtype, device=h.device)
     _check(_lib.lp_residual_norm_fwd(C.byref(q), h.data_ptr(), None if f is None else f.data_ptr(), None if same else s.data_ptr(),
                                      y.data_ptr(), _stream_ptr(None)))
     return s, y
@@ -1380,11 +1389,10 @@ def _norm_of(grads, outs, max_norm, eps) -> torch.Tensor:
     if not len(grads):
         raise ValueError("no gradients: without a tensor there is no device for the norm")
     arr, n = _gradients(grads, grads if outs is None else outs), len(grads)
-    _on_current_device(*grads, *(outs or ()))
-    device = grads[0].device
-    norm = torch.empty((), dtype=torch.float32, device=device)
+    first = grads[0]
+    norm = first.new_empty(()) if first.dtype is torch.float32 else torch.empty((), dtype=torch.float32, device=first.device)
     size = _grad_norm_bytes(n, arr)
-    ws = torch.empty(size, dtype=torch.uint8, device=device) if size else None   # (held until the kernels are enqueued)
+    ws = torch.empty(size, dtype=torch.uint8, device=first.device) if size else None   # (held until the kernels are enqueued)
     at = ws.data_ptr() if size else None
     if outs is None:
         _check(_lib.lp_grad_norm(n, arr, norm.data_ptr(), at, size, _stream_ptr(None)))

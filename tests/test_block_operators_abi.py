@@ -16,6 +16,14 @@ def _set(q, kw):
     return q
 
 
+def test_gradients_are_packed_as_they_are_laid_out(lp):
+    """The binding makes the structs of a list of gradients from one buffer."""
+    import struct
+    assert struct.calcsize("qQQi4x") == C.sizeof(lp._Gradient)
+    q = lp._Gradient.from_buffer(bytearray(struct.pack("qQQi4x", 1, 2, 3, 4)))
+    assert (q.size, q.input, q.out, q.dtype) == (1, 2, 3, 4)
+
+
 def test_linear_refusals(lp):
     lib = lp._lib
     one = C.c_void_p(4096)

@@ -47,10 +47,37 @@ struct NormDev {
 template <class T, int V>
 struct alignas(sizeof(T) * V) Pack { T v[V]; };
 
-template <int V, int R>
-struct Lane {   // a lane's slots of one position
-    float v[R * V];
-};
+// v of another lane: what DPP reaches within a row of 16 lanes.
+template <int CONTROL>
+__device__ __forceinline__ float from_lane(float v)
+{
+    return __builtin_bit_cast(float, __builtin_amdgcn_update_dpp(0, __builtin_bit_cast(int, v), CONTROL, 0xf, 0xf, true));
+}
+// Sums over groups of `lanes` neighbouring lanes, for all of them.  Each step adds what the lanes of the other half have: of pairs and fours by
+// permutations of four lanes, of eight and 16 by mirrors (all lanes of a half hold the same by then), of 32 and 64 by swaps of rows.
+// (By shuffles through LDS a step takes some 100 cycles instead of 10, and the four to six sums of a position follow one another.)
+template <int K>
+__device__ __forceinline__ void lane_sums(float (&v)[K], int lanes)
+{
+    auto each = [&](auto&& f) {
+#pragma unroll
+        for (int k = 0; k < K; ++k) v[k] = f(v[k]);
+    };
+    if (lanes >= 2) each([](float a) { return a + from_lane<0xb1>(a); });    // quad_perm 1, 0, 3, 2
+    if (lanes >= 4) each([](float a) { return a + from_lane<0x4e>(a); });    // quad_perm 2, 3, 0, 1
+    if (lanes >= 8) each([](float a) { return a + from_lane<0x141>(a); });   // row_half_mirror
+    if (lanes >= 16) each([](float a) { return a + from_lane<0x140>(a); });  // row_mirror
+    if (lanes >= 32)
+        each([](float a) {
+            const auto r = __builtin_amdgcn_permlane16_swap(__builtin_bit_cast(unsigned, a), __builtin_bit_cast(unsigned, a), false, false);
+            return __builtin_bit_cast(float, (unsigned)r[0]) + __builtin_bit_cast(float, (unsigned)r[1]);
+        });
+    if (lanes >= 64)
+        each([](float a) {
+            const auto r = __builtin_amdgcn_permlane32_swap(__builtin_bit_cast(unsigned, a), __builtin_bit_cast(unsigned, a), false, false);
+            return __builtin_bit_cast(float, (unsigned)r[0]) + __builtin_bit_cast(float, (unsigned)r[1]);
+        });
+}
 
 // A group of lanes and where a lane stands in it.
 template <bool WIDE>
@@ -71,9 +98,7 @@ struct Group {
     template <int K>
     __device__ __forceinline__ void sum(float (&v)[K]) const
     {
-        for (int m = 1; m < (WIDE ? 64 : lanes); m <<= 1)
-#pragma unroll
-            for (int k = 0; k < K; ++k) v[k] += __shfl_xor(v[k], m);
+        lane_sums(v, WIDE ? 64 : lanes);
         if (!WIDE) return;
         const int waves = blockDim.x >> 6;
         __syncthreads();   // (the sums before have been read)
@@ -192,14 +217,25 @@ __global__ __launch_bounds__(WIDE ? kWideThreads : kThreads) void residual_norm_
     for (long long item = blockIdx.x; item < items; item += gridDim.x) {
         const long long n = item / d.chunks, first = (item - n * d.chunks) * d.chunk, end = min(d.P, first + d.chunk);
         parameter<V, R>(d, g, d.gate ? d.gate + n * d.C : nullptr, 1.0f, gate);
+        // (the next position is asked for before this one's sums)
+        Pack<TH, V> hp[R], h_next[R];
+        Pack<TF, V> fp[R], f_next[R];
+        auto ask = [&](long long p) {
+            if (p >= end) return;
+            load<TH, V, R>(d, g, h + (n * d.P + p) * d.hs, h_next);
+            if (f) load<TF, V, R>(d, g, f + (n * d.P + p) * d.fs, f_next);
+        };
+        ask(first + g.index);
         for (long long p = first + g.index; p < end; p += d.groups) {
             const long long at = n * d.P + p;
-            Pack<TH, V> hp[R];
-            Pack<TF, V> fp[R];
-            load<TH, V, R>(d, g, h + at * d.hs, hp);
+#pragma unroll
+            for (int r = 0; r < R; ++r) {
+                hp[r] = h_next[r];
+                fp[r] = f_next[r];
+            }
+            ask(p + d.groups);
             float v[R * V], t[R * V];
             if (f) {
-                load<TF, V, R>(d, g, f + at * d.fs, fp);
                 widen<TF, V, R>(d, g, fp, v);
                 if (d.post) {
                     normalise<V, R>(d, g, v);
@@ -226,7 +262,7 @@ __global__ __launch_bounds__(WIDE ? kWideThreads : kThreads) void residual_norm_
 
 // Column sums of an item: [3][C] of d_y xh, d_y and g fh.
 template <class TH, class TF, int V, int R, bool WIDE>
-__global__ __launch_bounds__(WIDE ? kWideThreads : kThreads) void residual_norm_grad_kernel(NormDev d, const TH* h, const TF* f, const TH* d_s,
+__global__ __launch_bounds__(WIDE ? kWideThreads : kThreads, R * V <= kHeld ? 3 : 2) void residual_norm_grad_kernel(NormDev d, const TH* h, const TF* f, const TH* d_s,
                                                                                    const TF* d_y, TH* d_h, TF* d_f, float* parts)
 {
     __shared__ float lds[WIDE ? 2 * 16 : kThreads / 64 * kWaveChannels];
@@ -243,16 +279,29 @@ __global__ __launch_bounds__(WIDE ? kWideThreads : kThreads) void residual_norm_
         for (int k = 0; k < 3; ++k)
 #pragma unroll
             for (int e = 0; e < R * V; ++e) sums[k][e] = 0.0f;
+        Pack<TH, V> hp[R], dsp[R], h_next[R], ds_next[R];
+        Pack<TF, V> fp[R], dyp[R], f_next[R], dy_next[R];
+        auto ask = [&](long long p) {
+            if (p >= end) return;
+            const long long at = n * d.P + p;
+            if (d_y) {
+                load<TH, V, R>(d, g, h + at * d.hs, h_next);
+                load<TF, V, R>(d, g, d_y + at * d.ys, dy_next);
+            }
+            if (f) load<TF, V, R>(d, g, f + at * d.fs, f_next);
+            if (d_s) load<TH, V, R>(d, g, d_s + at * d.hs, ds_next);
+        };
+        ask(first + g.index);
         for (long long p = first + g.index; p < end; p += d.groups) {
             const long long at = n * d.P + p;
-            Pack<TH, V> hp[R], dsp[R];
-            Pack<TF, V> fp[R], dyp[R];
-            if (d_y) {
-                load<TH, V, R>(d, g, h + at * d.hs, hp);
-                load<TF, V, R>(d, g, d_y + at * d.ys, dyp);
+#pragma unroll
+            for (int r = 0; r < R; ++r) {
+                hp[r] = h_next[r];
+                fp[r] = f_next[r];
+                dsp[r] = ds_next[r];
+                dyp[r] = dy_next[r];
             }
-            if (f) load<TF, V, R>(d, g, f + at * d.fs, fp);
-            if (d_s) load<TH, V, R>(d, g, d_s + at * d.hs, dsp);
+            ask(p + d.groups);
             float fh[R * V], grad[R * V], rstd_f = 1.0f;
             if (f) {
                 widen<TF, V, R>(d, g, fp, fh);
@@ -343,30 +392,38 @@ __global__ __launch_bounds__(WIDE ? kWideThreads : kThreads) void residual_norm_
     }
 }
 
-// Columns' sums over `n` rows `stride` apart, for 64 columns from c0 on: thread (row lane, column); the result is in row lane 0.
+// Columns' sums over `n` rows `stride` apart, of kJoinColumns columns: thread (row lane, column); the result is in row lane 0.
+constexpr int kJoinColumns = 16;
 __device__ __forceinline__ double column_sum(const float* at, long long n, long long stride, bool in, double* lds)
 {
-    constexpr int kRows = kJoinThreads / 64;
-    const int row = threadIdx.x >> 6;
+    constexpr int kRows = kJoinThreads / kJoinColumns;
+    const int row = threadIdx.x / kJoinColumns;
     double sum = 0.0;
-    if (in)
+    if (in) {
+#pragma unroll 8
         for (long long i = row; i < n; i += kRows) sum += (double)at[i * stride];
+    }
+    // the rows of a wave, then the waves
+    sum += __shfl_xor(sum, 16);
+    sum += __shfl_xor(sum, 32);
     __syncthreads();
-    lds[threadIdx.x] = sum;
+    if ((threadIdx.x & 63) < kJoinColumns) lds[(threadIdx.x >> 6) * kJoinColumns + (threadIdx.x & 63)] = sum;
     __syncthreads();
     if (row) return 0.0;
-    for (int r = 1; r < kRows; ++r) sum += lds[r * 64 + threadIdx.x];
+    sum = 0.0;
+#pragma unroll
+    for (int w = 0; w < kJoinThreads / 64; ++w) sum += lds[w * kJoinColumns + threadIdx.x];
     return sum;
 }
 
-// Workgroup (64 columns; y = 0: d_gamma, 1: d_beta, from 2 on: the samples' T).  T goes to the gate, and to the post norm's gradient
+// Workgroup (kJoinColumns columns; y = 0: d_gamma, 1: d_beta, from 2 on: the samples' T).  T goes to the gate, and to the post norm's gradient
 // where there is one sample, else as gate T into `terms` [N][C] for the kernel below.
 __global__ __launch_bounds__(kJoinThreads) void residual_norm_join_kernel(NormDev d, const float* parts, float* d_gamma, float* d_beta,
                                                                          float* d_post_gamma, float* d_gate, float* terms)
 {
-    __shared__ double lds[kJoinThreads];
-    const int c = blockIdx.x * 64 + (threadIdx.x & 63);
-    const bool in = c < d.C, first = threadIdx.x < 64;
+    __shared__ double lds[kJoinThreads / 64 * kJoinColumns];
+    const int c = blockIdx.x * kJoinColumns + threadIdx.x % kJoinColumns;
+    const bool in = c < d.C, first = threadIdx.x < kJoinColumns;
     const long long row = 3ll * d.C;
     if (blockIdx.y < 2) {
         float* out = blockIdx.y ? d_beta : d_gamma;
@@ -387,10 +444,10 @@ __global__ __launch_bounds__(kJoinThreads) void residual_norm_join_kernel(NormDe
 }
 __global__ __launch_bounds__(kJoinThreads) void residual_norm_terms_kernel(NormDev d, const float* terms, float* d_post_gamma)
 {
-    __shared__ double lds[kJoinThreads];
-    const int c = blockIdx.x * 64 + (threadIdx.x & 63);
+    __shared__ double lds[kJoinThreads / 64 * kJoinColumns];
+    const int c = blockIdx.x * kJoinColumns + threadIdx.x % kJoinColumns;
     const double sum = column_sum(terms + c, d.N, d.C, c < d.C, lds);
-    if (c < d.C && threadIdx.x < 64) d_post_gamma[c] += (float)sum;
+    if (c < d.C && threadIdx.x < kJoinColumns) d_post_gamma[c] += (float)sum;
 }
 
 // ---- host ------------------------------------------------------------------------------------------------------
@@ -618,7 +675,7 @@ lp_status backward(const lp_residual_norm* q, const void* h, const void* f, cons
                            (const TF*)d_y, (TH*)d_h, (TF*)d_f, parts);
     });
     if (sums) {
-        const dim3 grid((d.C + 63) / 64, 2 + (unsigned)(d.N < 4096 ? d.N : 4096));
+        const dim3 grid((d.C + kJoinColumns - 1) / kJoinColumns, 2 + (unsigned)(d.N < 4096 ? d.N : 4096));
         hipLaunchKernelGGL(residual_norm_join_kernel, grid, dim3(kJoinThreads), 0, stream, d, parts, d_gamma, d_beta, d_post_gamma, d_gate, terms);
         if (terms) hipLaunchKernelGGL(residual_norm_terms_kernel, dim3(grid.x), dim3(kJoinThreads), 0, stream, d, terms, d_post_gamma);
     }

@@ -114,53 +114,67 @@ struct Group {
     }
 };
 
-// A lane's slots: slot r holds channels ((r lanes + lane) V) ..
-template <class T, int V, int R, class G>
+// A lane's slots: slot r holds channels ((r lanes + lane) V) ..  WHOLE: C is a multiple of V; else the last slot's values are moved one by
+// one.  Slots need not be aligned to their size.
+template <bool WHOLE, class T, int V, int R, class G>
 __device__ __forceinline__ void load(const NormDev& d, const G& g, const T* row, Pack<T, V> (&out)[R])
 {
 #pragma unroll
     for (int r = 0; r < R; ++r) {
         const int c = (r * g.lanes + g.lane) * V;
-        if (c < d.C) out[r] = *(const Pack<T, V>*)(row + c);
+        if (c + (WHOLE ? 0 : V - 1) < d.C) {
+            __builtin_memcpy(&out[r], row + c, sizeof(out[r]));
+        } else if (!WHOLE) {
+#pragma unroll
+            for (int j = 0; j < V; ++j)
+                if (c + j < d.C) out[r].v[j] = row[c + j];
+        }
     }
 }
-template <class T, int V, int R, class G>
+template <bool WHOLE, class T, int V, int R, class G>
 __device__ __forceinline__ void store(const NormDev& d, const G& g, T* row, const float (&v)[R * V])
 {
 #pragma unroll
     for (int r = 0; r < R; ++r) {
         const int c = (r * g.lanes + g.lane) * V;
-        if (c >= d.C) continue;
         Pack<T, V> q;
 #pragma unroll
         for (int j = 0; j < V; ++j) q.v[j] = (T)v[r * V + j];   // rounded once
-        *(Pack<T, V>*)(row + c) = q;
+        if (c + (WHOLE ? 0 : V - 1) < d.C) {
+            __builtin_memcpy(row + c, &q, sizeof(q));
+        } else if (!WHOLE) {
+#pragma unroll
+            for (int j = 0; j < V; ++j)
+                if (c + j < d.C) row[c + j] = q.v[j];
+        }
     }
 }
+// Whether a lane's value is one of a channel.
+template <bool WHOLE, int V, class G>
+__device__ __forceinline__ bool on(const NormDev& d, const G& g, int r, int j) { return (r * g.lanes + g.lane) * V + (WHOLE ? 0 : j) < d.C; }
+
 // A parameter's values (NULL: `none`); lanes without channels hold zeros.
-template <int V, int R, class G>
+template <bool WHOLE, int V, int R, class G>
 __device__ __forceinline__ void parameter(const NormDev& d, const G& g, const float* p, float none, float (&out)[R * V])
 {
 #pragma unroll
     for (int r = 0; r < R; ++r) {
         const int c = (r * g.lanes + g.lane) * V;
 #pragma unroll
-        for (int j = 0; j < V; ++j) out[r * V + j] = c < d.C ? (p ? p[c + j] : none) : 0.0f;
+        for (int j = 0; j < V; ++j) out[r * V + j] = on<WHOLE, V>(d, g, r, j) ? (p ? p[c + j] : none) : 0.0f;
     }
 }
-template <class T, int V, int R, class G>
+template <bool WHOLE, class T, int V, int R, class G>
 __device__ __forceinline__ void widen(const NormDev& d, const G& g, const Pack<T, V> (&in)[R], float (&out)[R * V])
 {
 #pragma unroll
-    for (int r = 0; r < R; ++r) {
-        const bool on = (r * g.lanes + g.lane) * V < d.C;
+    for (int r = 0; r < R; ++r)
 #pragma unroll
-        for (int j = 0; j < V; ++j) out[r * V + j] = on ? (float)in[r].v[j] : 0.0f;   // (zeros behind the last channel: they add nothing to sums)
-    }
+        for (int j = 0; j < V; ++j) out[r * V + j] = on<WHOLE, V>(d, g, r, j) ? (float)in[r].v[j] : 0.0f;   // (zeros behind the last channel: they add nothing to sums)
 }
 
 // v becomes norm(v); the result is what it was multiplied with.  Variances are of differences to the mean.
-template <int V, int R, class G>
+template <bool WHOLE, int V, int R, class G>
 __device__ __forceinline__ float normalise(const NormDev& d, const G& g, float (&v)[R * V])
 {
     const float over = 1.0f / (float)d.C;
@@ -171,11 +185,9 @@ __device__ __forceinline__ float normalise(const NormDev& d, const G& g, float (
         g.sum(sum);
         const float mean = sum[0] * over;
 #pragma unroll
-        for (int r = 0; r < R; ++r) {
-            const bool on = (r * g.lanes + g.lane) * V < d.C;
+        for (int r = 0; r < R; ++r)
 #pragma unroll
-            for (int j = 0; j < V; ++j) v[r * V + j] = on ? v[r * V + j] - mean : 0.0f;
-        }
+            for (int j = 0; j < V; ++j) v[r * V + j] = on<WHOLE, V>(d, g, r, j) ? v[r * V + j] - mean : 0.0f;
     }
     float squares[1] = {0.0f};
 #pragma unroll
@@ -204,112 +216,146 @@ __device__ __forceinline__ void normalise_grad(const NormDev& d, const G& g, con
     for (int k = 0; k < R * V; ++k) e[k] = rstd * (e[k] - fmaf(xh[k], along, mean));
 }
 
-template <class TH, class TF, int V, int R, bool WIDE>
+template <class TH, class TF, int V, int R, bool WIDE, bool WHOLE>
 __global__ __launch_bounds__(WIDE ? kWideThreads : kThreads) void residual_norm_kernel(NormDev d, const TH* h, const TF* f, TH* s, TF* y)
 {
+    constexpr int kAhead = WIDE || R > 1 ? 1 : 2;
     __shared__ float lds[2 * 16];
     const Group<WIDE> g(d, lds);
     float post_gamma[R * V], gate[R * V], gamma[R * V], beta[R * V];
-    parameter<V, R>(d, g, d.post_gamma, 1.0f, post_gamma);
-    parameter<V, R>(d, g, d.gamma, 1.0f, gamma);
-    parameter<V, R>(d, g, d.beta, 0.0f, beta);
+    parameter<WHOLE, V, R>(d, g, d.post_gamma, 1.0f, post_gamma);
+    parameter<WHOLE, V, R>(d, g, d.gamma, 1.0f, gamma);
+    parameter<WHOLE, V, R>(d, g, d.beta, 0.0f, beta);
     const long long items = d.N * d.chunks;
     for (long long item = blockIdx.x; item < items; item += gridDim.x) {
         const long long n = item / d.chunks, first = (item - n * d.chunks) * d.chunk, end = min(d.P, first + d.chunk);
-        parameter<V, R>(d, g, d.gate ? d.gate + n * d.C : nullptr, 1.0f, gate);
-        // (the next position is asked for before this one's sums)
-        Pack<TH, V> hp[R], h_next[R];
-        Pack<TF, V> fp[R], f_next[R];
-        auto ask = [&](long long p) {
-            if (p >= end) return;
-            load<TH, V, R>(d, g, h + (n * d.P + p) * d.hs, h_next);
-            if (f) load<TF, V, R>(d, g, f + (n * d.P + p) * d.fs, f_next);
+        parameter<WHOLE, V, R>(d, g, d.gate ? d.gate + n * d.C : nullptr, 1.0f, gate);
+        // (the next positions are asked for before this one's sums)
+        Pack<TH, V> hp[R], h_next[kAhead][R];
+        Pack<TF, V> fp[R], f_next[kAhead][R];
+        const long long start = n * d.P + first + g.index;
+        const TH* h_at = h + start * d.hs;
+        const TF* f_at = f + start * d.fs;
+        TH* s_at = s + start * d.hs;
+        TF* y_at = y + start * d.ys;
+        auto ask = [&](long long p, Pack<TH, V> (&hn)[R], Pack<TF, V> (&fn)[R]) {
+            if (p < end) {
+                load<WHOLE, TH, V, R>(d, g, h_at, hn);
+                if (f) load<WHOLE, TF, V, R>(d, g, f_at, fn);
+            }
+            h_at += d.groups * d.hs;
+            f_at += d.groups * d.fs;
         };
-        ask(first + g.index);
-        for (long long p = first + g.index; p < end; p += d.groups) {
-            const long long at = n * d.P + p;
+        const long long mine = first + g.index;
+#pragma unroll
+        for (int u = 0; u < kAhead; ++u) ask(mine + u * d.groups, h_next[u], f_next[u]);
+        for (long long p = mine; p < end; p += d.groups) {
 #pragma unroll
             for (int r = 0; r < R; ++r) {
-                hp[r] = h_next[r];
-                fp[r] = f_next[r];
+                hp[r] = h_next[0][r];
+                fp[r] = f_next[0][r];
+#pragma unroll
+                for (int u = 1; u < kAhead; ++u) {
+                    h_next[u - 1][r] = h_next[u][r];
+                    f_next[u - 1][r] = f_next[u][r];
+                }
             }
-            ask(p + d.groups);
+            ask(p + kAhead * d.groups, h_next[kAhead - 1], f_next[kAhead - 1]);
             float v[R * V], t[R * V];
             if (f) {
-                widen<TF, V, R>(d, g, fp, v);
+                widen<WHOLE, TF, V, R>(d, g, fp, v);
                 if (d.post) {
-                    normalise<V, R>(d, g, v);
+                    normalise<WHOLE, V, R>(d, g, v);
 #pragma unroll
                     for (int e = 0; e < R * V; ++e) v[e] *= post_gamma[e];
                 }
-                widen<TH, V, R>(d, g, hp, t);
+                widen<WHOLE, TH, V, R>(d, g, hp, t);
 #pragma unroll
                 for (int e = 0; e < R * V; ++e) t[e] = fmaf(gate[e], v[e], d.alpha * t[e]);
             } else {
-                widen<TH, V, R>(d, g, hp, t);
+                widen<WHOLE, TH, V, R>(d, g, hp, t);
 #pragma unroll
                 for (int e = 0; e < R * V; ++e) t[e] *= d.alpha;
             }
-            if (s) store<TH, V, R>(d, g, s + at * d.hs, t);
+            if (s) store<WHOLE, TH, V, R>(d, g, s_at, t);
+            s_at += d.groups * d.hs;
             if (!y) continue;
-            normalise<V, R>(d, g, t);
+            normalise<WHOLE, V, R>(d, g, t);
 #pragma unroll
             for (int e = 0; e < R * V; ++e) t[e] = fmaf(gamma[e], t[e], beta[e]);
-            store<TF, V, R>(d, g, y + at * d.ys, t);
+            store<WHOLE, TF, V, R>(d, g, y_at, t);
+            y_at += d.groups * d.ys;
         }
     }
 }
 
 // Column sums of an item: [3][C] of d_y xh, d_y and g fh.
-template <class TH, class TF, int V, int R, bool WIDE>
+template <class TH, class TF, int V, int R, bool WIDE, bool WHOLE>
 __global__ __launch_bounds__(WIDE ? kWideThreads : kThreads, R * V <= kHeld ? 3 : 2) void residual_norm_grad_kernel(NormDev d, const TH* h, const TF* f, const TH* d_s,
                                                                                    const TF* d_y, TH* d_h, TF* d_f, float* parts)
 {
+    constexpr int kAhead = WIDE || R > 1 ? 1 : 2;
     __shared__ float lds[WIDE ? 2 * 16 : kThreads / 64 * kWaveChannels];
     const Group<WIDE> g(d, lds);
     float post_gamma[R * V], gate[R * V], gamma[R * V];
-    parameter<V, R>(d, g, d.post_gamma, 1.0f, post_gamma);
-    parameter<V, R>(d, g, d.gamma, 1.0f, gamma);
+    parameter<WHOLE, V, R>(d, g, d.post_gamma, 1.0f, post_gamma);
+    parameter<WHOLE, V, R>(d, g, d.gamma, 1.0f, gamma);
     const long long items = d.N * d.chunks;
     for (long long item = blockIdx.x; item < items; item += gridDim.x) {
         const long long n = item / d.chunks, first = (item - n * d.chunks) * d.chunk, end = min(d.P, first + d.chunk);
-        parameter<V, R>(d, g, d.gate ? d.gate + n * d.C : nullptr, 1.0f, gate);
+        parameter<WHOLE, V, R>(d, g, d.gate ? d.gate + n * d.C : nullptr, 1.0f, gate);
         float sums[3][R * V];
 #pragma unroll
         for (int k = 0; k < 3; ++k)
 #pragma unroll
             for (int e = 0; e < R * V; ++e) sums[k][e] = 0.0f;
-        Pack<TH, V> hp[R], dsp[R], h_next[R], ds_next[R];
-        Pack<TF, V> fp[R], dyp[R], f_next[R], dy_next[R];
-        auto ask = [&](long long p) {
-            if (p >= end) return;
-            const long long at = n * d.P + p;
-            if (d_y) {
-                load<TH, V, R>(d, g, h + at * d.hs, h_next);
-                load<TF, V, R>(d, g, d_y + at * d.ys, dy_next);
+        Pack<TH, V> hp[R], dsp[R], h_next[kAhead][R], ds_next[kAhead][R];
+        Pack<TF, V> fp[R], dyp[R], f_next[kAhead][R], dy_next[kAhead][R];
+        const long long start = n * d.P + first + g.index, mine = first + g.index;
+        const TH *h_at = h + start * d.hs, *ds_at = d_s + start * d.hs;
+        const TF *f_at = f + start * d.fs, *dy_at = d_y + start * d.ys;
+        TH* dh_at = d_h + start * d.hs;
+        TF* df_at = d_f + start * d.fs;
+        auto ask = [&](long long p, int u) {
+            if (p < end) {
+                if (d_y) {
+                    load<WHOLE, TH, V, R>(d, g, h_at, h_next[u]);
+                    load<WHOLE, TF, V, R>(d, g, dy_at, dy_next[u]);
+                }
+                if (f) load<WHOLE, TF, V, R>(d, g, f_at, f_next[u]);
+                if (d_s) load<WHOLE, TH, V, R>(d, g, ds_at, ds_next[u]);
             }
-            if (f) load<TF, V, R>(d, g, f + at * d.fs, f_next);
-            if (d_s) load<TH, V, R>(d, g, d_s + at * d.hs, ds_next);
+            h_at += d.groups * d.hs;
+            ds_at += d.groups * d.hs;
+            f_at += d.groups * d.fs;
+            dy_at += d.groups * d.ys;
         };
-        ask(first + g.index);
-        for (long long p = first + g.index; p < end; p += d.groups) {
-            const long long at = n * d.P + p;
+#pragma unroll
+        for (int u = 0; u < kAhead; ++u) ask(mine + u * d.groups, u);
+        for (long long p = mine; p < end; p += d.groups) {
 #pragma unroll
             for (int r = 0; r < R; ++r) {
-                hp[r] = h_next[r];
-                fp[r] = f_next[r];
-                dsp[r] = ds_next[r];
-                dyp[r] = dy_next[r];
+                hp[r] = h_next[0][r];
+                fp[r] = f_next[0][r];
+                dsp[r] = ds_next[0][r];
+                dyp[r] = dy_next[0][r];
+#pragma unroll
+                for (int u = 1; u < kAhead; ++u) {
+                    h_next[u - 1][r] = h_next[u][r];
+                    f_next[u - 1][r] = f_next[u][r];
+                    ds_next[u - 1][r] = ds_next[u][r];
+                    dy_next[u - 1][r] = dy_next[u][r];
+                }
             }
-            ask(p + d.groups);
+            ask(p + kAhead * d.groups, kAhead - 1);
             float fh[R * V], grad[R * V], rstd_f = 1.0f;
             if (f) {
-                widen<TF, V, R>(d, g, fp, fh);
-                if (d.post) rstd_f = normalise<V, R>(d, g, fh);
+                widen<WHOLE, TF, V, R>(d, g, fp, fh);
+                if (d.post) rstd_f = normalise<WHOLE, V, R>(d, g, fh);
             }
             if (d_y) {
                 float t[R * V];
-                widen<TH, V, R>(d, g, hp, t);
+                widen<WHOLE, TH, V, R>(d, g, hp, t);
                 if (f) {
 #pragma unroll
                     for (int e = 0; e < R * V; ++e) t[e] = fmaf(gate[e], d.post ? post_gamma[e] * fh[e] : fh[e], d.alpha * t[e]);
@@ -317,8 +363,8 @@ __global__ __launch_bounds__(WIDE ? kWideThreads : kThreads, R * V <= kHeld ? 3 
 #pragma unroll
                     for (int e = 0; e < R * V; ++e) t[e] *= d.alpha;
                 }
-                const float rstd = normalise<V, R>(d, g, t);
-                widen<TF, V, R>(d, g, dyp, grad);
+                const float rstd = normalise<WHOLE, V, R>(d, g, t);
+                widen<WHOLE, TF, V, R>(d, g, dyp, grad);
 #pragma unroll
                 for (int e = 0; e < R * V; ++e) {
                     sums[0][e] = fmaf(grad[e], t[e], sums[0][e]);
@@ -332,7 +378,7 @@ __global__ __launch_bounds__(WIDE ? kWideThreads : kThreads, R * V <= kHeld ? 3 
             }
             if (d_s) {
                 float up[R * V];
-                widen<TH, V, R>(d, g, dsp, up);
+                widen<WHOLE, TH, V, R>(d, g, dsp, up);
 #pragma unroll
                 for (int e = 0; e < R * V; ++e) grad[e] += up[e];
             }
@@ -340,7 +386,8 @@ __global__ __launch_bounds__(WIDE ? kWideThreads : kThreads, R * V <= kHeld ? 3 
                 float r[R * V];
 #pragma unroll
                 for (int e = 0; e < R * V; ++e) r[e] = d.alpha * grad[e];
-                store<TH, V, R>(d, g, d_h + at * d.hs, r);
+                store<WHOLE, TH, V, R>(d, g, dh_at, r);
+                dh_at += d.groups * d.hs;
             }
             if (!f) continue;
 #pragma unroll
@@ -349,7 +396,8 @@ __global__ __launch_bounds__(WIDE ? kWideThreads : kThreads, R * V <= kHeld ? 3 
 #pragma unroll
             for (int e = 0; e < R * V; ++e) grad[e] *= d.post ? gate[e] * post_gamma[e] : gate[e];
             if (d.post) normalise_grad<V, R>(d, g, fh, rstd_f, grad);
-            store<TF, V, R>(d, g, d_f + at * d.fs, grad);
+            store<WHOLE, TF, V, R>(d, g, df_at, grad);
+            df_at += d.groups * d.fs;
         }
         if (!parts) continue;
         float* part = parts + item * 3 * d.C;
@@ -361,7 +409,7 @@ __global__ __launch_bounds__(WIDE ? kWideThreads : kThreads, R * V <= kHeld ? 3 
                     const int c = (r * g.lanes + g.lane) * V;
 #pragma unroll
                     for (int j = 0; j < V; ++j)
-                        if (c < d.C) part[k * d.C + c + j] = sums[k][r * V + j];
+                        if (on<WHOLE, V>(d, g, r, j)) part[k * d.C + c + j] = sums[k][r * V + j];
                 }
         } else {
             const int wave = threadIdx.x >> 6;
@@ -378,7 +426,7 @@ __global__ __launch_bounds__(WIDE ? kWideThreads : kThreads, R * V <= kHeld ? 3 
                         const int c = (r * g.lanes + g.lane) * V;
 #pragma unroll
                         for (int j = 0; j < V; ++j)
-                            if (c < d.C) lds[wave * kWaveChannels + c + j] = sums[k][r * V + j];
+                            if (on<WHOLE, V>(d, g, r, j)) lds[wave * kWaveChannels + c + j] = sums[k][r * V + j];
                     }
                 __syncthreads();
                 for (int c = threadIdx.x; c < d.C; c += kThreads) {
@@ -495,7 +543,7 @@ lp_status validate(const lp_residual_norm* q, NormDev* d)
 // is counted with the fewest positions at a time.
 void divide(NormDev* d, int n_cu, int per_cu)
 {
-    const long long target = ((long long)per_cu * n_cu + d->N - 1) / (d->N > 0 ? d->N : 1), most = (d->P + 4ll * d->groups - 1) / (4ll * d->groups);
+    const long long target = (long long)per_cu * n_cu / (d->N > 0 ? d->N : 1), most = (d->P + 4ll * d->groups - 1) / (4ll * d->groups);
     long long chunks = target < most ? target : most;
     if (chunks < 1) chunks = 1;
     d->chunk = (d->P + chunks - 1) / chunks;
@@ -506,14 +554,14 @@ void divide(NormDev* d, int n_cu, int per_cu)
 
 struct Shape {
     int V, R;
-    bool wide;
+    bool wide, whole;
     unsigned threads;
 };
 
 // Lanes and slots of a position: few idle lanes first, then few slots.
 Shape shape(NormDev* d, int V)
 {
-    Shape s = {V, 1, false, kThreads};
+    Shape s = {V, 1, false, d->C % V == 0, kThreads};
     const int slots = (d->C + V - 1) / V;
     if (d->C > kWaveChannels) {
         s.wide = true;
@@ -539,33 +587,25 @@ Shape shape(NormDev* d, int V)
     return s;
 }
 
-constexpr int kForwardPerUnit = 8, kBackwardPerUnit = 4;
+// Workgroups a compute unit, as many as its registers hold at once: a few more would run alone at the end (24 x 256^2 x 32, gradients: 4 take
+// 202 us, 3 and 6 take 213 and 223, 43 for each of the 24 samples, 1032 on 1024 places, 285).  With eight channels a lane the gradients' kernel has
+// room for three, but two are faster (65536 x 512 in bf16: 101 us, three 106).
+constexpr int kForwardPerUnit = 5;
+int backward_per_unit(const Shape& s) { return s.R * s.V >= kHeld ? 2 : 4; }
 
 struct Sizes {
     size_t parts, terms;
 };
-Sizes sizes(const NormDev& d, int n_cu)
+Sizes sizes(const NormDev& d, int V, int n_cu)
 {
-    long long items = 0;
-    for (int V : {1, 4, 8}) {
-        if (d.C % V) continue;
-        NormDev t = d;
-        shape(&t, V);
-        divide(&t, n_cu, kBackwardPerUnit);
-        if (t.N * t.chunks > items) items = t.N * t.chunks;
-    }
+    NormDev t = d;
+    const Shape shp = shape(&t, V);
+    divide(&t, n_cu, backward_per_unit(shp));
+    const long long items = t.N * t.chunks;
     return {align256((size_t)items * 3 * d.C * sizeof(float)), d.post && d.N > 1 ? align256((size_t)d.N * d.C * sizeof(float)) : 0};
 }
 
-// The widest slot that channels, strides and addresses allow: 16 bytes of h.
-int slot_width(const NormDev& d, int h_bytes, int f_bytes, std::initializer_list<const void*> hs, std::initializer_list<const void*> fs)
-{
-    const int V = 16 / h_bytes;
-    bool ok = d.C % V == 0 && d.hs % V == 0 && d.fs % V == 0 && d.ys % V == 0;
-    for (const void* p : hs) ok = ok && (uintptr_t)p % (V * h_bytes) == 0;
-    for (const void* p : fs) ok = ok && (uintptr_t)p % (V * f_bytes) == 0;
-    return ok ? V : 1;
-}
+int slot_width(const lp_residual_norm* q) { return 16 / dtype_bytes(q->h_dtype); }   // 16 bytes of h
 
 // Calls f with the types, the slots' width and number and whether a position takes a workgroup as constants.
 template <class T> struct Type { using type = T; };
@@ -573,26 +613,21 @@ template <class F, class H, class B>
 void with_shape(const Shape& s, F&& f, Type<H> h, Type<B> b)
 {
     constexpr int W = 16 / sizeof(H);
-    auto one = [&](auto v, auto r) {
-        if (s.V != v.value || s.R != r.value) return;
-        constexpr int held = decltype(v)::value * decltype(r)::value;
+    auto one = [&](auto r) {
+        if (s.R != r.value) return;
+        constexpr int held = W * decltype(r)::value;
+        auto v = std::integral_constant<int, W>();
+        auto go = [&](auto wide) { s.whole ? f(h, b, v, r, wide, std::true_type()) : f(h, b, v, r, wide, std::false_type()); };
         if constexpr (held >= kHeld) {
-            if (s.wide) f(h, b, v, r, std::true_type());
+            if (s.wide) go(std::true_type());
         }
         if constexpr (held <= kHeld) {
-            if (!s.wide) f(h, b, v, r, std::false_type());
+            if (!s.wide) go(std::false_type());
         }
     };
-    auto narrow = std::integral_constant<int, 1>();
-    auto w = std::integral_constant<int, W>();
-    one(narrow, std::integral_constant<int, 1>());
-    one(narrow, std::integral_constant<int, 2>());
-    one(narrow, std::integral_constant<int, 4>());
-    one(narrow, std::integral_constant<int, 8>());
-    one(narrow, std::integral_constant<int, 16>());
-    one(w, std::integral_constant<int, 1>());
-    one(w, std::integral_constant<int, 2>());
-    if constexpr (W == 4) one(w, std::integral_constant<int, 4>());
+    one(std::integral_constant<int, 1>());
+    one(std::integral_constant<int, 2>());
+    if constexpr (W == 4) one(std::integral_constant<int, 4>());
 }
 template <class F>
 void dispatch(int h_dtype, int f_dtype, const Shape& s, F&& f)
@@ -632,12 +667,12 @@ lp_status forward(const lp_residual_norm* q, const void* h, const void* f, void*
     std::string err;
     int n_cu = 0;
     if (compute_units(&n_cu, &err)) return fail(LP_ERR_HIP, err);
-    const Shape shp = shape(&d, slot_width(d, dtype_bytes(q->h_dtype), dtype_bytes(q->f_dtype), {h, s}, {f, y}));
+    const Shape shp = shape(&d, slot_width(q));
     divide(&d, n_cu, kForwardPerUnit);
-    dispatch(q->h_dtype, q->f_dtype, shp, [&](auto th, auto tf, auto v, auto r, auto wide) {
+    dispatch(q->h_dtype, q->f_dtype, shp, [&](auto th, auto tf, auto v, auto r, auto wide, auto whole) {
         using TH = typename decltype(th)::type;
         using TF = typename decltype(tf)::type;
-        hipLaunchKernelGGL((residual_norm_kernel<TH, TF, decltype(v)::value, decltype(r)::value, decltype(wide)::value>),
+        hipLaunchKernelGGL((residual_norm_kernel<TH, TF, decltype(v)::value, decltype(r)::value, decltype(wide)::value, decltype(whole)::value>),
                            dim3(grid_of(d.N * d.chunks)), dim3(shp.threads), 0, stream, d, (const TH*)h, (const TF*)f, (TH*)s, (TF*)y);
     });
     return launched("residual norm forward launch");
@@ -657,20 +692,20 @@ lp_status backward(const lp_residual_norm* q, const void* h, const void* f, cons
     std::string err;
     int n_cu = 0;
     if (compute_units(&n_cu, &err)) return fail(LP_ERR_HIP, err);
-    const Sizes size = sizes(d, n_cu);
+    const Sizes size = sizes(d, slot_width(q), n_cu);
     if (!workspace || workspace_bytes < size.parts + size.terms)
         return fail(LP_ERR_WORKSPACE, "workspace is NULL or smaller than lp_residual_norm_workspace_bytes");
     if ((uintptr_t)workspace % 256) return fail(LP_ERR_INVALID_ARG, "workspace must be 256-byte aligned");
-    const Shape shp = shape(&d, slot_width(d, dtype_bytes(q->h_dtype), dtype_bytes(q->f_dtype), {h, d_s, d_h}, {f, d_y, d_f}));
-    divide(&d, n_cu, kBackwardPerUnit);
+    const Shape shp = shape(&d, slot_width(q));
+    divide(&d, n_cu, backward_per_unit(shp));
     const bool sums = d_gamma || d_beta || d_post_gamma || d_gate;
     if (!sums && !d_h && !d_f) return LP_OK;
     float* parts = sums ? (float*)workspace : nullptr;
     float* terms = d.N > 1 && d_post_gamma ? (float*)((char*)workspace + size.parts) : nullptr;
-    dispatch(q->h_dtype, q->f_dtype, shp, [&](auto th, auto tf, auto v, auto r, auto wide) {
+    dispatch(q->h_dtype, q->f_dtype, shp, [&](auto th, auto tf, auto v, auto r, auto wide, auto whole) {
         using TH = typename decltype(th)::type;
         using TF = typename decltype(tf)::type;
-        hipLaunchKernelGGL((residual_norm_grad_kernel<TH, TF, decltype(v)::value, decltype(r)::value, decltype(wide)::value>),
+        hipLaunchKernelGGL((residual_norm_grad_kernel<TH, TF, decltype(v)::value, decltype(r)::value, decltype(wide)::value, decltype(whole)::value>),
                            dim3(grid_of(d.N * d.chunks)), dim3(shp.threads), 0, stream, d, (const TH*)h, (const TF*)f, (const TH*)d_s,
                            (const TF*)d_y, (TH*)d_h, (TF*)d_f, parts);
     });
@@ -697,7 +732,7 @@ try {
     std::string err;
     int n_cu = 0;
     if (lp::compute_units(&n_cu, &err)) return lp::fail(LP_ERR_HIP, err);
-    const lp::Sizes size = lp::sizes(d, n_cu);
+    const lp::Sizes size = lp::sizes(d, lp::slot_width(norm), n_cu);
     *bwd_bytes = size.parts + size.terms;
     return LP_OK;
 } catch (...) {

@@ -247,6 +247,10 @@ inline bool whole(const LinearDev& d, int dtype) { return d.K % (dtype == LP_F32
 // The general kernel (lp_linear_tile.hip).  back: d_x from d_y and pre.
 void launch_tiles(int dtype, int act, bool back, LinearDev d, hipStream_t s);
 
+// Few channels (lp_linear_stream.hip).  back: d_x from d_y and pre, fp32 alone; the weight is W as it is, with rows of ws elements.
+inline bool is_few(int dtype, int summed, int made) { return made <= 128 && summed * (dtype == LP_F32 ? 4 : 2) <= 256; }
+void launch_stream(int dtype, int act, bool back, const LinearDev& d, int n_cu, hipStream_t s);
+
 // 16-bit types, more than 128 channels (lp_linear_wide.hip): the weights in the operands' order, and the products with them.
 __host__ __device__ constexpr int wide_blocks(int k) { return (k + 63) / 64 * 4; }   // of 16 summed channels
 void launch_pack(int dtype, bool turned, const void* w, int rows, int cols, int pitch, void* out, hipStream_t s);

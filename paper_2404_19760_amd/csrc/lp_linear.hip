@@ -383,6 +383,11 @@ lp_status forward(const lp_linear* q, const void* x, void* y, void* pre, void* w
         launch_pack(c.dtype, false, d.w, c.N, c.K, c.K, workspace, s);
         d.w = workspace;
         launch_wide(c.dtype, c.act, false, d, s);
+    } else if (is_few(c.dtype, c.K, c.N)) {
+        std::string err;
+        int n_cu = 0;
+        if (compute_units(&n_cu, &err)) return fail(LP_ERR_HIP, err);
+        launch_stream(c.dtype, c.act, false, d, n_cu, s);
     } else {
         launch_tiles(c.dtype, c.act, false, d, s);
     }
@@ -451,7 +456,11 @@ lp_status backward(const lp_linear* q, const void* x, const void* pre, const voi
             d.as = c.N;
             act = LP_ACT_NONE;
         }
-        if (is_wide(c, c.K) && act == LP_ACT_NONE) {
+        if (!halves && is_few(c.dtype, c.N, c.K)) {
+            d.w = c.weight;
+            d.ws = c.K;
+            launch_stream(c.dtype, act, true, d, n_cu, s);
+        } else if (is_wide(c, c.K) && act == LP_ACT_NONE) {
             launch_pack(c.dtype, true, c.weight, c.K, c.N, c.K, at, s);
             launch_wide(c.dtype, act, true, d, s);
         } else {

@@ -1,0 +1,110 @@
+// Products of positions of few channels with a weight matrix: up to 256 bytes of summed channels, up to 128 channels made.
+//
+// Memory bounds them (32 -> 64 channels in fp32: 384 bytes and 4096 operations a position), so nothing is shared between waves but the
+// weights, which lie in LDS as the matrix instructions' operands for as long as the workgroup lives: a wave takes 32 positions at a time,
+// asks for the next 32 before it multiplies, and never waits for another wave.  The positions' channels go straight to registers: of a row's
+// 16-byte chunks lanes 0 .. 31 ask for the even ones, lanes 32 .. 63 for the odd ones.
+#include "lp_linear.h"
+
+namespace lp {
+namespace linear {
+
+namespace {
+
+constexpr int kTurn = 32 * 36 * 4;   // bytes in which a wave turns over 32 x 32 results
+
+// PAIRS: pairs of chunks of a row; BLOCKS: of 32 channels.  BACK: d_x from d_y and pre, the weights are W's columns.
+template <class T, int ACT, bool BACK, bool WHOLE, int PAIRS, int BLOCKS>
+__global__ __launch_bounds__(kThreads, PAIRS * BLOCKS > 16 ? 2 : 3) void linear_stream_kernel(LinearDev d)
+{
+    constexpr int E = kChunk<T>;
+    constexpr bool kSlope = BACK && ACT != LP_ACT_NONE;
+    __shared__ alignas(16) char lds[PAIRS * BLOCKS * 1024 + 4 * kTurn];
+    const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), l32 = lane & 31, h = lane >> 5;
+    const long long step = (long long)gridDim.x * 128;
+    long long p0 = (long long)blockIdx.x * 128 + wave * 32;
+    const T *a_at = (const T*)d.a + (p0 + l32) * d.as + h * E, *pre_at = (const T*)d.pre + (p0 + l32) * d.K + h * E;
+    Chunk<T> a[PAIRS], pre[kSlope ? PAIRS : 1];
+    auto ask = [&](long long p) {
+#pragma unroll
+        for (int f = 0; f < PAIRS; ++f) {
+            const int count = p + l32 < d.P ? d.K - (2 * f + h) * E : 0;
+            a[f] = load_chunk<WHOLE>(a_at + 2 * f * E, count);
+            if (kSlope) pre[f] = load_chunk<WHOLE>(pre_at + 2 * f * E, count);
+        }
+        a_at += step * d.as;
+        pre_at += step * d.K;
+    };
+    if (p0 < d.P) ask(p0);
+    for (int b = wave; b < PAIRS * BLOCKS; b += 4) {
+        const int n = b / PAIRS * 32 + l32, k = (2 * (b % PAIRS) + h) * E;
+        Chunk<T> w;
+        if (BACK) {
+#pragma unroll
+            for (int j = 0; j < E; ++j) w.v[j] = n < d.N && k + j < d.K ? ((const T*)d.w)[(k + j) * d.ws + n] : (T)0.0f;
+        } else {
+            w = load_chunk<false>((const T*)d.w + n * d.ws + k, n < d.N ? d.K - k : 0);
+        }
+        *(Chunk<T>*)(lds + b * 1024 + lane * 16) = w;
+    }
+    __syncthreads();
+    float* turn = (float*)(lds + PAIRS * BLOCKS * 1024 + wave * kTurn);
+    for (; p0 < d.P; p0 += step) {
+        Chunk<T> av[PAIRS];
+#pragma unroll
+        for (int f = 0; f < PAIRS; ++f) av[f] = kSlope ? gradient<ACT>(a[f], pre[f]).hi : a[f];
+        if (p0 + step < d.P) ask(p0 + step);
+        f32x16 acc[BLOCKS] = {};
+#pragma unroll
+        for (int f = 0; f < PAIRS; ++f)
+#pragma unroll
+            for (int i = 0; i < BLOCKS; ++i) acc[i] = multiply(*(const Chunk<T>*)(lds + (i * PAIRS + f) * 1024 + lane * 16), av[f], acc[i]);
+#pragma unroll
+        for (int i = 0; i < BLOCKS; ++i) {
+            if (i * 32 >= d.N) break;
+            const f32x16 one[1][1] = {{acc[i]}};
+            finish<T, ACT, BACK, WHOLE, 1, 1>(d, one, turn, p0, i * 32, lane);
+        }
+    }
+}
+
+template <class T, int ACT, bool BACK, int PAIRS, int BLOCKS>
+void go(const LinearDev& d, bool whole, int n_cu, hipStream_t s)
+{
+    const long long groups = (d.P + 127) / 128, most = (PAIRS * BLOCKS > 16 ? 2ll : 3ll) * n_cu;
+    const dim3 grid((unsigned)(groups < most ? groups : most));
+    if (whole) hipLaunchKernelGGL((linear_stream_kernel<T, ACT, BACK, true, PAIRS, BLOCKS>), grid, dim3(kThreads), 0, s, d);
+    else hipLaunchKernelGGL((linear_stream_kernel<T, ACT, BACK, false, PAIRS, BLOCKS>), grid, dim3(kThreads), 0, s, d);
+}
+
+template <class T, int ACT, bool BACK>
+void stream(const LinearDev& d, bool whole, int n_cu, hipStream_t s)
+{
+    auto blocks = [&](auto pairs) {
+        constexpr int P = decltype(pairs)::value;
+        if (d.N <= 32) go<T, ACT, BACK, P, 1>(d, whole, n_cu, s);
+        else if (d.N <= 64) go<T, ACT, BACK, P, 2>(d, whole, n_cu, s);
+        else go<T, ACT, BACK, P, 4>(d, whole, n_cu, s);
+    };
+    const int bytes = d.K * (int)sizeof(T);
+    if (bytes <= 64) blocks(std::integral_constant<int, 2>());
+    else if (bytes <= 128) blocks(std::integral_constant<int, 4>());
+    else if (bytes <= 160) blocks(std::integral_constant<int, 5>());
+    else blocks(std::integral_constant<int, 8>());
+}
+
+}  // namespace
+
+void launch_stream(int dtype, int act, bool back, const LinearDev& d, int n_cu, hipStream_t s)
+{
+    const bool w = whole(d, dtype);
+    with_act_of(act, [&](auto a) {
+        constexpr int A = decltype(a)::value;
+        if (dtype == LP_BF16) stream<__bf16, A, false>(d, w, n_cu, s);
+        else if (dtype == LP_F16) stream<_Float16, A, false>(d, w, n_cu, s);
+        else back ? stream<float, A, true>(d, w, n_cu, s) : stream<float, A, false>(d, w, n_cu, s);
+    });
+}
+
+}  // namespace linear
+}  // namespace lp

@@ -35,31 +35,62 @@ struct alignas(16) Chunk {
 template <class T> constexpr int kChunk = Chunk<T>::kCount;
 
 // `count` (may be <= 0) values from p, zeros behind them.  A whole chunk is one load, also where it is not aligned to 16 bytes.
-// WHOLE: rows end with whole chunks.
+// WHOLE: rows end with whole chunks.  Else all lanes that reach behind a row's end do so by as much (it is the end of the same row size):
+// what is left is moved in pieces of 8, 4 and 2 bytes, whose sizes are the same for all of them.
 template <bool WHOLE, class T>
 __device__ __forceinline__ Chunk<T> load_chunk(const T* p, long long count)
 {
-    Chunk<T> c;
-    if (WHOLE) {
-        if (count > 0) __builtin_memcpy(&c, p, 16);
-        else c = Chunk<T>{};
-    } else if (count >= kChunk<T>) {
-        __builtin_memcpy(&c, p, 16);
-    } else {
-#pragma unroll
-        for (int j = 0; j < kChunk<T>; ++j) c.v[j] = j < count ? p[j] : (T)0.0f;
+    u32x4 w = {0, 0, 0, 0};
+    if (count >= (WHOLE ? 1 : kChunk<T>)) {
+        __builtin_memcpy(&w, p, 16);
+    } else if (!WHOLE && count > 0) {
+        const char* at = (const char*)p;
+        const int bytes = __builtin_amdgcn_readfirstlane((int)count) * (int)sizeof(T);
+        if (bytes & 8) {
+            u32x2 v;
+            __builtin_memcpy(&v, at, 8);
+            w[0] = v[0];
+            w[1] = v[1];
+        }
+        if (bytes & 4) {
+            uint32_t v;
+            __builtin_memcpy(&v, at + (bytes & 8), 4);
+            if (bytes & 8) w[2] = v; else w[0] = v;
+        }
+        if (sizeof(T) == 2 && bytes & 2) {
+            uint16_t v;
+            __builtin_memcpy(&v, at + (bytes & 12), 2);
+            switch (bytes & 12) {
+                case 0: w[0] = v; break;
+                case 4: w[1] = v; break;
+                case 8: w[2] = v; break;
+                default: w[3] = v;
+            }
+        }
     }
-    return c;
+    return __builtin_bit_cast(Chunk<T>, w);
 }
 template <bool WHOLE, class T>
 __device__ __forceinline__ void store_chunk(T* p, long long count, const Chunk<T>& c)
 {
-    if (WHOLE ? count > 0 : count >= kChunk<T>) {
-        __builtin_memcpy(p, &c, 16);
-    } else if (!WHOLE) {
-#pragma unroll
-        for (int j = 0; j < kChunk<T>; ++j)
-            if (j < count) p[j] = c.v[j];
+    const u32x4 w = __builtin_bit_cast(u32x4, c);
+    if (count >= (WHOLE ? 1 : kChunk<T>)) {
+        __builtin_memcpy(p, &w, 16);
+    } else if (!WHOLE && count > 0) {
+        char* at = (char*)p;
+        const int bytes = __builtin_amdgcn_readfirstlane((int)count) * (int)sizeof(T);
+        if (bytes & 8) {
+            const u32x2 v = {w[0], w[1]};
+            __builtin_memcpy(at, &v, 8);
+        }
+        if (bytes & 4) {
+            const uint32_t v = bytes & 8 ? w[2] : w[0];
+            __builtin_memcpy(at + (bytes & 8), &v, 4);
+        }
+        if (sizeof(T) == 2 && bytes & 2) {
+            const uint16_t v = (uint16_t)((bytes & 12) == 0 ? w[0] : (bytes & 12) == 4 ? w[1] : (bytes & 12) == 8 ? w[2] : w[3]);
+            __builtin_memcpy(at + (bytes & 12), &v, 2);
+        }
     }
 }
 
@@ -172,18 +203,31 @@ __device__ __forceinline__ u32x2 read_transposed(const char* at)
 // The results of a wave's blocks of 32 x 32 (channels, positions) for positions p0 .. and channels n0 ..: value e of a lane is channel
 // 8 (e / 4) + 4 h + e % 4 of position l32 of a block.  They are turned over in the wave's own LDS, 32 positions at a time, so that
 // neighbouring lanes write neighbouring channels.
+// The residual of 32 positions (of the lane's chunks) may have been asked for before.
+template <class T, int BLOCKS_N> constexpr int kFinishTimes = 32 / (64 / (32 * BLOCKS_N / kChunk<T>));   // chunks of a lane
+template <class T, bool WHOLE, int BLOCKS_N>
+__device__ __forceinline__ void ask_residual(const LinearDev& d, long long p0, int n0, int lane, Chunk<T> (&added)[kFinishTimes<T, BLOCKS_N>])
+{
+    constexpr int kAcross = 32 * BLOCKS_N / kChunk<T>, kDown = 64 / kAcross;
+    const int n = n0 + lane % kAcross * kChunk<T>;
+    const long long first = p0 + lane / kAcross;
+    const T* res = (const T*)d.res + first * d.rs + n;
+#pragma unroll
+    for (int r = 0; r < kFinishTimes<T, BLOCKS_N>; ++r)
+        added[r] = load_chunk<WHOLE>(res + r * kDown * d.rs, first + r * kDown < d.P ? d.N - n : 0);
+}
 template <class T, int ACT, bool BACK, bool WHOLE, int BLOCKS_P, int BLOCKS_N>
-__device__ __forceinline__ void finish(const LinearDev& d, const f32x16 (&acc)[BLOCKS_N][BLOCKS_P], float* turn, long long p0, int n0, int lane)
+__device__ __forceinline__ void finish(const LinearDev& d, const f32x16 (&acc)[BLOCKS_N][BLOCKS_P], float* turn, long long p0, int n0, int lane,
+                                       const Chunk<T> (*asked)[kFinishTimes<T, BLOCKS_N>] = nullptr)
 {
     constexpr int E = kChunk<T>, kAcross = 32 * BLOCKS_N / E, kDown = 64 / kAcross, kPitch = 32 * BLOCKS_N + 4;
-    constexpr int kTimes = 32 / kDown;
+    constexpr int kTimes = kFinishTimes<T, BLOCKS_N>;
     const int l32 = lane & 31, h = lane >> 5, n = n0 + lane % kAcross * E;
     const long long first = p0 + lane / kAcross;   // the lane's first position; the others follow at distances that all lanes share
     float bias[E];
 #pragma unroll
     for (int j = 0; j < E; ++j) bias[j] = d.bias && n + j < d.N ? d.bias[n + j] : 0.0f;
     T *out = (T*)d.out + first * d.ys + n, *keep = (T*)d.keep + first * d.N + n;
-    const T* res = (const T*)d.res + first * d.rs + n;
 #pragma unroll
     for (int jp = 0; jp < BLOCKS_P; ++jp) {
 #pragma unroll
@@ -201,9 +245,14 @@ __device__ __forceinline__ void finish(const LinearDev& d, const f32x16 (&acc)[B
             count[r] = first + (jp * 32 + r * kDown) < d.P ? d.N - n : 0;
             added[r] = Chunk<T>{};
         }
-        if (!BACK && d.res)
+        if (!BACK && d.res) {
+            if (asked) {
 #pragma unroll
-            for (int r = 0; r < kTimes; ++r) added[r] = load_chunk<WHOLE>(res + (jp * 32 + r * kDown) * d.rs, count[r]);
+                for (int r = 0; r < kTimes; ++r) added[r] = (*asked)[r];
+            } else {
+                ask_residual<T, WHOLE, BLOCKS_N>(d, p0 + jp * 32, n0, lane, added);
+            }
+        }
 #pragma unroll
         for (int r = 0; r < kTimes; ++r) {
             float z[E];

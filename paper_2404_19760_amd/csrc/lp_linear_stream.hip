@@ -22,6 +22,7 @@ __global__ __launch_bounds__(kThreads, PAIRS * BLOCKS > 16 ? 2 : 3) void linear_
     __shared__ alignas(16) char lds[PAIRS * BLOCKS * 1024 + 4 * kTurn];
     const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), l32 = lane & 31, h = lane >> 5;
     const long long step = (long long)gridDim.x * 128;
+    const int n0 = blockIdx.y * (BLOCKS * 32);   // the first of its channels
     long long p0 = (long long)blockIdx.x * 128 + wave * 32;
     const T *a_at = (const T*)d.a + (p0 + l32) * d.as + h * E, *pre_at = (const T*)d.pre + (p0 + l32) * d.K + h * E;
     Chunk<T> a[PAIRS], pre[kSlope ? PAIRS : 1];
@@ -29,15 +30,20 @@ __global__ __launch_bounds__(kThreads, PAIRS * BLOCKS > 16 ? 2 : 3) void linear_
 #pragma unroll
         for (int f = 0; f < PAIRS; ++f) {
             const int count = p + l32 < d.P ? d.K - (2 * f + h) * E : 0;
-            a[f] = load_chunk<WHOLE>(a_at + 2 * f * E, count);
-            if (kSlope) pre[f] = load_chunk<WHOLE>(pre_at + 2 * f * E, count);
+            if (WHOLE || (2 * f + 2) * E <= d.K) {   // (the same for all lanes)
+                a[f] = load_chunk<true>(a_at + 2 * f * E, count);
+                if (kSlope) pre[f] = load_chunk<true>(pre_at + 2 * f * E, count);
+            } else {
+                a[f] = load_chunk<false>(a_at + 2 * f * E, count);
+                if (kSlope) pre[f] = load_chunk<false>(pre_at + 2 * f * E, count);
+            }
         }
         a_at += step * d.as;
         pre_at += step * d.K;
     };
     if (p0 < d.P) ask(p0);
     for (int b = wave; b < PAIRS * BLOCKS; b += 4) {
-        const int n = b / PAIRS * 32 + l32, k = (2 * (b % PAIRS) + h) * E;
+        const int n = n0 + b / PAIRS * 32 + l32, k = (2 * (b % PAIRS) + h) * E;
         Chunk<T> w;
         if (BACK) {
 #pragma unroll
@@ -53,6 +59,16 @@ __global__ __launch_bounds__(kThreads, PAIRS * BLOCKS > 16 ? 2 : 3) void linear_
         Chunk<T> av[PAIRS];
 #pragma unroll
         for (int f = 0; f < PAIRS; ++f) av[f] = kSlope ? gradient<ACT>(a[f], pre[f]).hi : a[f];
+        // (the residual of two blocks of channels is on its way while others are finished)
+        Chunk<T> added[2][kFinishTimes<T, 1>];
+        auto residual = [&](int n, Chunk<T> (&to)[kFinishTimes<T, 1>]) {
+            if (WHOLE || n + 32 <= d.N) ask_residual<T, true, 1>(d, p0, n, lane, to);
+            else ask_residual<T, false, 1>(d, p0, n, lane, to);
+        };
+        if (!BACK && d.res) {
+            residual(n0, added[0]);
+            if (BLOCKS > 1) residual(n0 + 32, added[1]);
+        }
         if (p0 + step < d.P) ask(p0 + step);
         f32x16 acc[BLOCKS] = {};
 #pragma unroll
@@ -61,9 +77,11 @@ __global__ __launch_bounds__(kThreads, PAIRS * BLOCKS > 16 ? 2 : 3) void linear_
             for (int i = 0; i < BLOCKS; ++i) acc[i] = multiply(*(const Chunk<T>*)(lds + (i * PAIRS + f) * 1024 + lane * 16), av[f], acc[i]);
 #pragma unroll
         for (int i = 0; i < BLOCKS; ++i) {
-            if (i * 32 >= d.N) break;
+            if (n0 + i * 32 >= d.N) break;
             const f32x16 one[1][1] = {{acc[i]}};
-            finish<T, ACT, BACK, WHOLE, 1, 1>(d, one, turn, p0, i * 32, lane);
+            if (WHOLE || n0 + i * 32 + 32 <= d.N) finish<T, ACT, BACK, true, 1, 1>(d, one, turn, p0, n0 + i * 32, lane, &added[i & 1]);
+            else finish<T, ACT, BACK, false, 1, 1>(d, one, turn, p0, n0 + i * 32, lane, &added[i & 1]);
+            if (!BACK && d.res && i + 2 < BLOCKS) residual(n0 + (i + 2) * 32, added[i & 1]);
         }
     }
 }
@@ -72,7 +90,7 @@ template <class T, int ACT, bool BACK, int PAIRS, int BLOCKS>
 void go(const LinearDev& d, bool whole, int n_cu, hipStream_t s)
 {
     const long long groups = (d.P + 127) / 128, most = (PAIRS * BLOCKS > 16 ? 2ll : 3ll) * n_cu;
-    const dim3 grid((unsigned)(groups < most ? groups : most));
+    const dim3 grid((unsigned)(groups < most ? groups : most), (d.N + BLOCKS * 32 - 1) / (BLOCKS * 32));
     if (whole) hipLaunchKernelGGL((linear_stream_kernel<T, ACT, BACK, true, PAIRS, BLOCKS>), grid, dim3(kThreads), 0, s, d);
     else hipLaunchKernelGGL((linear_stream_kernel<T, ACT, BACK, false, PAIRS, BLOCKS>), grid, dim3(kThreads), 0, s, d);
 }
@@ -84,6 +102,7 @@ void stream(const LinearDev& d, bool whole, int n_cu, hipStream_t s)
         constexpr int P = decltype(pairs)::value;
         if (d.N <= 32) go<T, ACT, BACK, P, 1>(d, whole, n_cu, s);
         else if (d.N <= 64) go<T, ACT, BACK, P, 2>(d, whole, n_cu, s);
+        else if ((d.P + 127) / 128 < 8 * n_cu) go<T, ACT, BACK, P, 2>(d, whole, n_cu, s);
         else go<T, ACT, BACK, P, 4>(d, whole, n_cu, s);
     };
     const int bytes = d.K * (int)sizeof(T);

@@ -183,7 +183,7 @@ struct LinearDev {
     int tiles_n;
 };
 
-__device__ __forceinline__ int chunk_at(int row, int chunk) { return row * 128 + ((chunk ^ (row & 7)) << 4); }
+__device__ __forceinline__ int chunk_at(int row, int chunk) { return row * 128 + ((chunk ^ (row >> 1 & 7)) << 4); }
 
 // Tile of a workgroup: neighbouring workgroups go to the chip's eight XCDs in turn, so each of these takes one run of the
 // tiles; channels' tiles of the same positions follow one another (their positions are read from the XCD's L2).

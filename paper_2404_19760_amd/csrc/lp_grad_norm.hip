@@ -5,7 +5,9 @@
 // What bounds it: memory, and launches for a small decoder's gradients.  A sum over everything stands between reading a value and
 // using it.  Up to 32 Ki values stay in the registers of one workgroup meanwhile (one launch).  More are passed over twice: workgroups
 // leave their sums in the workspace, and those of the second pass add all of them up before they scale their part; they go through the
-// values from the end backwards, so that what the first pass read last is still in the Infinity Cache.
+// values from the end backwards, so that what the first pass read last is still in the Infinity Cache.  Where the values are more than
+// it holds, results go past it, so as not to drive out what is yet to be read (150 million values in fp32, 0.6 GB: 312 us; with
+// ordinary stores 344, from the start on 352).
 //
 // Squares and sums are fp64: the square of an fp32 value is exact there and neither overflows nor vanishes, and memory is far slower than
 // the two instructions a value.  The order of the sums depends on the sizes alone.
@@ -44,6 +46,7 @@ struct Set {
     int n, items;       // tensors; parts, or slots
     int before;         // parts of the sets before this one
     long long chunk;    // values of a part
+    int past_cache;     // results are stored past the caches
 };
 
 // What is done with the sum of all squares.
@@ -59,6 +62,7 @@ __device__ __forceinline__ float factor_of(double squares, const Clip& c)
     return f >= 1.0 || norm == 0.0 ? 1.0f : (float)f;   // (NaN stays NaN)
 }
 
+using u32x4 = uint32_t __attribute__((ext_vector_type(4)));
 template <class T, int V>
 struct alignas(sizeof(T) * V) Pack { T v[V]; };
 
@@ -126,7 +130,7 @@ __device__ __forceinline__ double squares_of(const T* p, long long count)
 }
 
 template <class T>
-__device__ __forceinline__ void scale_part(const T* in, T* out, long long count, float factor)
+__device__ __forceinline__ void scale_part(const T* in, T* out, long long count, float factor, bool past_cache)
 {
     constexpr int V = 16 / sizeof(T), U = 4;
     using P = Pack<T, V>;
@@ -148,7 +152,11 @@ __device__ __forceinline__ void scale_part(const T* in, T* out, long long count,
 #pragma unroll
         for (int u = 0; u < U; ++u) v[u] = body[i + u * kThreads];
 #pragma unroll
-        for (int u = 0; u < U; ++u) to[i + u * kThreads] = scaled(v[u]);
+        for (int u = 0; u < U; ++u) {
+            const P r = scaled(v[u]);
+            if (past_cache) __builtin_nontemporal_store(__builtin_bit_cast(u32x4, r), (u32x4*)&to[i + u * kThreads]);
+            else to[i + u * kThreads] = r;
+        }
     }
     for (; i < packs; i += kThreads) to[i] = scaled(body[i]);
     if (threadIdx.x < head) out[threadIdx.x] = (T)((float)in[threadIdx.x] * factor);
@@ -200,9 +208,9 @@ __global__ __launch_bounds__(kThreads) void grad_scale_kernel(Set<MAX> a, const 
     const TensorDev& t = a.t[k];
     if (factor == 1.0f && t.in == t.out) return;   // (nothing changes)
     const long long at = (item - t.first) * a.chunk, count = min(a.chunk, t.size - at);
-    if (t.dtype == LP_F32) scale_part((const float*)t.in + at, (float*)t.out + at, count, factor);
-    else if (t.dtype == LP_BF16) scale_part((const __bf16*)t.in + at, (__bf16*)t.out + at, count, factor);
-    else scale_part((const _Float16*)t.in + at, (_Float16*)t.out + at, count, factor);
+    if (t.dtype == LP_F32) scale_part((const float*)t.in + at, (float*)t.out + at, count, factor, a.past_cache != 0);
+    else if (t.dtype == LP_BF16) scale_part((const __bf16*)t.in + at, (__bf16*)t.out + at, count, factor, a.past_cache != 0);
+    else scale_part((const _Float16*)t.in + at, (_Float16*)t.out + at, count, factor, a.past_cache != 0);
 }
 
 // Everything in one workgroup: slots of four neighbouring values, held between the sum and the scaling.
@@ -279,19 +287,21 @@ int dtype_bytes(int t) { return t == LP_F32 ? 4 : 2; }
 // How a call is divided.
 struct Division {
     bool small;
+    int past_cache;
     long long chunk, items;   // values of a part; parts of all tensors
     size_t bytes;
 };
 
-// Parts for eight workgroups a compute unit, in whole blocks of kLeast values (so that a part starts as its tensor is aligned).
+// Parts for 32 workgroups a compute unit, in whole blocks of kLeast values (so that a part starts as its tensor is aligned).
 lp_status divide(const std::vector<lp_gradient>& v, Division* out)
 {
     Division& d = *out;
     d = {};
-    double total = 0.0;
+    double total = 0.0, bytes = 0.0;
     long long slots = 0;
     for (const lp_gradient& g : v) {
         total += (double)g.size;
+        bytes += (double)g.size * dtype_bytes(g.dtype);
         if (slots <= kSmallThreads * kSmallSlots) slots += (g.size + 3) / 4;
     }
     d.small = v.size() <= kSmallTensors && slots <= kSmallThreads * kSmallSlots;
@@ -299,7 +309,8 @@ lp_status divide(const std::vector<lp_gradient>& v, Division* out)
     std::string err;
     int n_cu = 0;
     if (compute_units(&n_cu, &err)) return fail(LP_ERR_HIP, err);
-    d.chunk = ((long long)(total / (8.0 * n_cu)) + kLeast) / kLeast * kLeast;
+    d.past_cache = bytes > 256e6;   // the Infinity Cache
+    d.chunk = ((long long)(total / (32.0 * n_cu)) + kLeast) / kLeast * kLeast;
     for (const lp_gradient& g : v) d.items += (g.size + d.chunk - 1) / d.chunk;
     if (d.items > 1ll << 30) return fail(LP_ERR_UNSUPPORTED, "too many tensors for one call");
     d.bytes = ((size_t)(d.items + 1) * sizeof(double) + 255) / 256 * 256;
@@ -358,12 +369,13 @@ lp_status launched(const char* what)
 }
 
 template <int MAX>
-Set<MAX> set_of(const std::vector<lp_gradient>& v, size_t first, size_t end, long long per_item, long long chunk, int before)
+Set<MAX> set_of(const std::vector<lp_gradient>& v, size_t first, size_t end, long long per_item, long long chunk, int before, int past_cache = 0)
 {
     Set<MAX> a;
     std::memset(&a, 0, sizeof(a));
     a.chunk = chunk;
     a.before = before;
+    a.past_cache = past_cache;
     for (size_t k = first; k < end; ++k) {
         a.t[a.n++] = {v[k].in, v[k].out, (long long)v[k].size, a.items, v[k].dtype};
         a.items += (int)((v[k].size + per_item - 1) / per_item);
@@ -407,8 +419,8 @@ lp_status run(const std::vector<lp_gradient>& v, Clip c, void* workspace, size_t
             auto go = [&](const auto& a) {
                 hipLaunchKernelGGL(grad_scale_kernel, dim3(a.items), dim3(kThreads), 0, s, a, sums, n, c, write_norm);
             };
-            if (end - k <= kSmallTensors) go(set_of<kSmallTensors>(v, k, end, d.chunk, d.chunk, before[set]));
-            else go(set_of<kSetTensors>(v, k, end, d.chunk, d.chunk, before[set]));
+            if (end - k <= kSmallTensors) go(set_of<kSmallTensors>(v, k, end, d.chunk, d.chunk, before[set], d.past_cache));
+            else go(set_of<kSetTensors>(v, k, end, d.chunk, d.chunk, before[set], d.past_cache));
         }
     }
     return launched("gradient norm launch");

@@ -46,7 +46,6 @@ struct Set {
     int n, items;       // tensors; parts, or slots
     int before;         // parts of the sets before this one
     long long chunk;    // values of a part
-    int past_cache;     // results are stored past the caches
 };
 
 // What is done with the sum of all squares.
@@ -129,8 +128,8 @@ __device__ __forceinline__ double squares_of(const T* p, long long count)
     return sum[0] + sum[1];
 }
 
-template <class T>
-__device__ __forceinline__ void scale_part(const T* in, T* out, long long count, float factor, bool past_cache)
+template <bool PAST_CACHE, class T>
+__device__ __forceinline__ void scale_part(const T* in, T* out, long long count, float factor)
 {
     constexpr int V = 16 / sizeof(T), U = 4;
     using P = Pack<T, V>;
@@ -154,7 +153,7 @@ __device__ __forceinline__ void scale_part(const T* in, T* out, long long count,
 #pragma unroll
         for (int u = 0; u < U; ++u) {
             const P r = scaled(v[u]);
-            if (past_cache) __builtin_nontemporal_store(__builtin_bit_cast(u32x4, r), (u32x4*)&to[i + u * kThreads]);
+            if (PAST_CACHE) __builtin_nontemporal_store(__builtin_bit_cast(u32x4, r), (u32x4*)&to[i + u * kThreads]);
             else to[i + u * kThreads] = r;
         }
     }
@@ -197,7 +196,8 @@ __global__ __launch_bounds__(kThreads) void grad_join_kernel(const double* parts
     *norm = (float)sqrt(sum);
 }
 
-template <int MAX>
+// PAST_CACHE: results are stored past the caches.
+template <bool PAST_CACHE, int MAX>
 __global__ __launch_bounds__(kThreads) void grad_scale_kernel(Set<MAX> a, const double* parts, int n, Clip c, int write_norm)
 {
     __shared__ double lds[kThreads / 64];
@@ -208,9 +208,9 @@ __global__ __launch_bounds__(kThreads) void grad_scale_kernel(Set<MAX> a, const 
     const TensorDev& t = a.t[k];
     if (factor == 1.0f && t.in == t.out) return;   // (nothing changes)
     const long long at = (item - t.first) * a.chunk, count = min(a.chunk, t.size - at);
-    if (t.dtype == LP_F32) scale_part((const float*)t.in + at, (float*)t.out + at, count, factor, a.past_cache != 0);
-    else if (t.dtype == LP_BF16) scale_part((const __bf16*)t.in + at, (__bf16*)t.out + at, count, factor, a.past_cache != 0);
-    else scale_part((const _Float16*)t.in + at, (_Float16*)t.out + at, count, factor, a.past_cache != 0);
+    if (t.dtype == LP_F32) scale_part<PAST_CACHE>((const float*)t.in + at, (float*)t.out + at, count, factor);
+    else if (t.dtype == LP_BF16) scale_part<PAST_CACHE>((const __bf16*)t.in + at, (__bf16*)t.out + at, count, factor);
+    else scale_part<PAST_CACHE>((const _Float16*)t.in + at, (_Float16*)t.out + at, count, factor);
 }
 
 // Everything in one workgroup: slots of four neighbouring values, held between the sum and the scaling.
@@ -287,7 +287,7 @@ int dtype_bytes(int t) { return t == LP_F32 ? 4 : 2; }
 // How a call is divided.
 struct Division {
     bool small;
-    int past_cache;
+    bool past_cache;
     long long chunk, items;   // values of a part; parts of all tensors
     size_t bytes;
 };
@@ -369,13 +369,12 @@ lp_status launched(const char* what)
 }
 
 template <int MAX>
-Set<MAX> set_of(const std::vector<lp_gradient>& v, size_t first, size_t end, long long per_item, long long chunk, int before, int past_cache = 0)
+Set<MAX> set_of(const std::vector<lp_gradient>& v, size_t first, size_t end, long long per_item, long long chunk, int before)
 {
     Set<MAX> a;
     std::memset(&a, 0, sizeof(a));
     a.chunk = chunk;
     a.before = before;
-    a.past_cache = past_cache;
     for (size_t k = first; k < end; ++k) {
         a.t[a.n++] = {v[k].in, v[k].out, (long long)v[k].size, a.items, v[k].dtype};
         a.items += (int)((v[k].size + per_item - 1) / per_item);
@@ -417,10 +416,11 @@ lp_status run(const std::vector<lp_gradient>& v, Clip c, void* workspace, size_t
             const size_t k = set * kSetTensors, end = std::min(v.size(), k + kSetTensors);
             const int write_norm = !join && set == 0;
             auto go = [&](const auto& a) {
-                hipLaunchKernelGGL(grad_scale_kernel, dim3(a.items), dim3(kThreads), 0, s, a, sums, n, c, write_norm);
+                if (d.past_cache) hipLaunchKernelGGL((grad_scale_kernel<true>), dim3(a.items), dim3(kThreads), 0, s, a, sums, n, c, write_norm);
+                else hipLaunchKernelGGL((grad_scale_kernel<false>), dim3(a.items), dim3(kThreads), 0, s, a, sums, n, c, write_norm);
             };
-            if (end - k <= kSmallTensors) go(set_of<kSmallTensors>(v, k, end, d.chunk, d.chunk, before[set], d.past_cache));
-            else go(set_of<kSetTensors>(v, k, end, d.chunk, d.chunk, before[set], d.past_cache));
+            if (end - k <= kSmallTensors) go(set_of<kSmallTensors>(v, k, end, d.chunk, d.chunk, before[set]));
+            else go(set_of<kSetTensors>(v, k, end, d.chunk, d.chunk, before[set]));
         }
     }
     return launched("gradient norm launch");

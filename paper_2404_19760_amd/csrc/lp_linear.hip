@@ -340,6 +340,9 @@ lp_status launched(const char* what)
     return e == hipSuccess ? LP_OK : fail(LP_ERR_HIP, std::string(what) + ": " + hipGetErrorString(e));
 }
 
+// Bytes that a call moves of `channels` channels a position.
+double bytes_of(const Call& c, double channels) { return (double)c.P * channels * dtype_bytes(c.dtype); }
+
 lp_status aligned(int dtype, std::initializer_list<const void*> ps)
 {
     for (const void* p : ps)
@@ -375,6 +378,7 @@ lp_status forward(const lp_linear* q, const void* x, void* y, void* pre, void* w
     std::memset(&d, 0, sizeof(d));
     d.P = c.P; d.K = c.K; d.N = c.N; d.as = c.xs; d.ys = c.ys; d.rs = c.rs;
     d.a = x; d.w = c.weight; d.ws = c.K; d.res = c.residual; d.bias = c.bias; d.out = y; d.keep = pre;
+    d.past_cache = bytes_of(c, c.K + (double)c.N * (1 + (pre != nullptr) + (c.residual != nullptr))) > kCacheBytes;
     if (c.P <= kFewRows) {
         if (c.dtype == LP_BF16) few_rows<__bf16>(d, c.act, s);
         else if (c.dtype == LP_F16) few_rows<_Float16>(d, c.act, s);

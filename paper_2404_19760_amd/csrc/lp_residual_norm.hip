@@ -32,6 +32,9 @@ constexpr int kHeld = 8;           // channels of a position that a lane holds; 
 constexpr int kWaveChannels = 64 * kHeld, kWideThreads = 512;
 constexpr int kJoinThreads = 1024;
 constexpr unsigned kMaxGrid = 1u << 20;
+// Where a call moves more than the Infinity Cache holds, results are stored past the caches: they would only drive out what is yet to
+// be read (gradients of 65536 x 512 in bf16, 0.4 GB: 101 -> 90 us).
+constexpr double kCacheBytes = 256e6;
 
 struct NormDev {
     long long N, P;                // samples, positions of a sample (a gate that is the same for all: one sample)
@@ -42,6 +45,7 @@ struct NormDev {
     const float *post_gamma, *gate, *gamma, *beta;
     long long chunk;               // positions of an item
     int chunks;                    // items of a sample
+    int past_cache;                // results are stored past the caches
 };
 
 template <class T, int V>
@@ -141,7 +145,14 @@ __device__ __forceinline__ void store(const NormDev& d, const G& g, T* row, cons
 #pragma unroll
         for (int j = 0; j < V; ++j) q.v[j] = (T)v[r * V + j];   // rounded once
         if (c + (WHOLE ? 0 : V - 1) < d.C) {
-            __builtin_memcpy(row + c, &q, sizeof(q));
+            if (d.past_cache) {
+                typedef uint32_t Any __attribute__((ext_vector_type(sizeof(T) * V / 4), aligned(2)));
+                asm volatile("" ::: "memory");   // (with nothing around it both stores would become one ordinary one)
+                __builtin_nontemporal_store(__builtin_bit_cast(Any, q), (Any*)(row + c));
+                asm volatile("" ::: "memory");
+            } else {
+                __builtin_memcpy(row + c, &q, sizeof(q));
+            }
         } else if (!WHOLE) {
 #pragma unroll
             for (int j = 0; j < V; ++j)
@@ -639,6 +650,12 @@ void dispatch(int h_dtype, int f_dtype, const Shape& s, F&& f)
     else with_shape(s, f, Type<float>(), Type<float>());
 }
 
+// Bytes that a call moves of tensors like h and like f.
+double bytes_of(const lp_residual_norm* q, int hs, int fs)
+{
+    return (double)q->N * (double)q->P * q->C * (hs * dtype_bytes(q->h_dtype) + fs * dtype_bytes(q->f_dtype));
+}
+
 unsigned grid_of(long long items) { return (unsigned)(items < kMaxGrid ? items : kMaxGrid); }
 
 lp_status launched(const char* what)
@@ -669,6 +686,7 @@ lp_status forward(const lp_residual_norm* q, const void* h, const void* f, void*
     if (compute_units(&n_cu, &err)) return fail(LP_ERR_HIP, err);
     const Shape shp = shape(&d, slot_width(q));
     divide(&d, n_cu, kForwardPerUnit);
+    d.past_cache = bytes_of(q, 1 + (s != nullptr), (f != nullptr) + (y != nullptr)) > kCacheBytes;
     dispatch(q->h_dtype, q->f_dtype, shp, [&](auto th, auto tf, auto v, auto r, auto wide, auto whole) {
         using TH = typename decltype(th)::type;
         using TF = typename decltype(tf)::type;
@@ -698,6 +716,7 @@ lp_status backward(const lp_residual_norm* q, const void* h, const void* f, cons
     if ((uintptr_t)workspace % 256) return fail(LP_ERR_INVALID_ARG, "workspace must be 256-byte aligned");
     const Shape shp = shape(&d, slot_width(q));
     divide(&d, n_cu, backward_per_unit(shp));
+    d.past_cache = bytes_of(q, 1 + (d_s != nullptr) + (d_h != nullptr), (f != nullptr) + (d_y != nullptr) + (d_f != nullptr)) > kCacheBytes;
     const bool sums = d_gamma || d_beta || d_post_gamma || d_gate;
     if (!sums && !d_h && !d_f) return LP_OK;
     float* parts = sums ? (float*)workspace : nullptr;

@@ -1,8 +1,10 @@
 """Lifts views of a scene into a voxel grid and trains a small network on it, from the Splatter to the optimiser:
 
-    pixel features -> Splatter -> grid (+ a learned one) -> group norm + SiLU over the cells the Splatter reached -> Renderer -> loss
+    pixel features -> Splatter -> grid (+ a learned one) -> group norm + SiLU over the cells the Splatter reached
+        -> residual block over the cells (layer norm, product + SiLU, product + residual) -> Renderer -> loss
 
-The decoder's matrices are stepped by Muon (orthogonalised updates), everything else by Adam.  The views are rendered from a random
+Gradients are clipped by their norm; the matrices of the decoder and of the block are stepped by Muon (orthogonalised updates), everything
+else by Adam.  The views are rendered from a random
 scene by the library itself.  Needs a GPU:
 
     python examples/fit_views.py [--steps 200] [--res 48] [--size 64]
@@ -19,7 +21,7 @@ if ROOT not in sys.path:
 
 import paper_2404_19760_amd as lp  # noqa: E402
 from paper_2404_19760_amd import autograd as lp_autograd  # noqa: E402
-from paper_2404_19760_amd.optim import Muon  # noqa: E402
+from paper_2404_19760_amd.optim import Muon, clip_grad_norm_  # noqa: E402
 
 CHANNELS, HIDDEN, GROUPS = 16, 64, 4
 BG = (1.0, 1.0, 1.0)
@@ -65,18 +67,25 @@ def fit(steps=200, res=48, size=64, samples=64, n_views=8, seed=0, log=print):
     net = mlp(gen)
     latent = torch.zeros_like(lifted, requires_grad=True)
     gamma, beta = (torch.full((CHANNELS,), v, device="cuda", requires_grad=True) for v in (1.0, 0.0))
-    for t in net.weights + net.biases:
+    # the block: its last matrix is zero, so that it starts as nothing beside the sum
+    block = [torch.randn(2 * CHANNELS, CHANNELS, generator=gen, device="cuda") * (2.0 / CHANNELS) ** 0.5, torch.zeros(CHANNELS, 2 * CHANNELS, device="cuda")]
+    block_biases = [torch.zeros(2 * CHANNELS, device="cuda"), torch.zeros(CHANNELS, device="cuda")]
+    for t in net.weights + net.biases + block + block_biases:
         t.requires_grad_(True)
-    muon = Muon(net.weights, lr=0.02)
-    adam = torch.optim.Adam([latent, gamma, beta, *net.biases], lr=2e-2)
+    muon = Muon(net.weights + block, lr=0.02)
+    adam = torch.optim.Adam([latent, gamma, beta, *net.biases, *block_biases], lr=2e-2)
+    params = [p for o in (muon, adam) for g in o.param_groups for p in g["params"]]
     losses = []
     for step in range(steps):
         x = lp_autograd.group_norm(lifted + latent, GROUPS, gamma, beta, lp.LP_ACT_SILU, occupancy=weight)
+        h, normed = lp_autograd.residual_norm(x, kind=lp.LP_NORM_LAYER)
+        x = lp_autograd.linear(lp_autograd.linear(normed, block[0], block_biases[0], lp.LP_ACT_SILU), block[1], block_biases[1], residual=h)
         rgb, _, _ = lp_autograd.render(lp.Grid(lp.LP_GRID_VOXEL, [x], shape), net, rays, BG)
         loss = (rgb - target).square().mean()
         muon.zero_grad()
         adam.zero_grad()
         loss.backward()
+        clip_grad_norm_(params, 1.0)
         muon.step()
         adam.step()
         losses.append(loss.detach())

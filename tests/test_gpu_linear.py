@@ -265,8 +265,9 @@ def test_offsets_beyond_32_bits(lp):
     assert not d_x.any()
 
 
-def test_captured_and_replayed(lp):
-    t = _case(3000, 72, 160, torch.bfloat16, 9)
+@pytest.mark.parametrize("p,k,n", [(3000, 72, 160), (700, 512, 136), (2000, 32, 64)])
+def test_captured_and_replayed(lp, p, k, n):
+    t = _case(p, k, n, torch.bfloat16, 9)
     lin = lp.Linear(t["w"], t["b"], lp.LP_ACT_GELU)
 
     def step():

@@ -163,6 +163,30 @@ def test_parts_of_the_block(lp, c):
         assert all(o is None or torch.equal(o, g) for o, g in zip(outs, whole)), wanted
 
 
+@pytest.mark.parametrize("opt", OPTIONS, ids=lambda o: f"{o['kind']}-{o['post']}-{o['gate']}")
+def test_gradients_against_differences(lp, opt):
+    """The backward's gradients are the slopes of the formulas along random directions (differences in 64 bits, good to the square of their step)."""
+    t = _case(3, 20, 40, torch.float32, torch.float32, opt, 12)
+    norm = _lp_norm(lp, t, opt)
+    got = dict(zip(("h", "f", "gamma", "beta", "post_gamma", "gate"), lp.residual_norm_bwd(norm, t["h"], t["f"], t["d_s"], t["d_y"])))
+    host = {k: v.double().cpu() for k, v in t.items() if v is not None}
+
+    def loss(values):
+        u = {**host, **values}
+        s, y = _reference({**u, **{k: None for k in t if k not in u}}, opt)[:2]
+        return float((s * u["d_s"]).sum() + (y * u["d_y"]).sum())
+
+    gen = torch.Generator().manual_seed(13)
+    names = [k for k, g in got.items() if g is not None]
+    for _ in range(4):
+        way = {k: torch.randn(host[k].shape, generator=gen).double() for k in names}
+        slope = (loss({k: host[k] + 1e-5 * way[k] for k in names}) - loss({k: host[k] - 1e-5 * way[k] for k in names})) / 2e-5
+        terms = [got[k].double().cpu() * way[k] for k in names]
+        # (fp32 gradients are good to TOL of the largest; the differences' own error is some 1e-8)
+        bound = sum(TOL * float(got[k].abs().max()) * way[k].numel() ** 0.5 * 3 for k in names) + 1e-6
+        assert abs(sum(float(v.sum()) for v in terms) - slope) <= bound
+
+
 def test_in_place_and_accumulation(lp):
     opt = OPTIONS[1]
     t = _case(2, 90, 72, torch.bfloat16, torch.bfloat16, opt, 1)

@@ -1363,14 +1363,26 @@ def residual_norm_fwd(norm: ResidualNorm, h: torch.Tensor, f: Optional[torch.Ten
 def residual_norm_bwd(norm: ResidualNorm, h: torch.Tensor, f: Optional[torch.Tensor], d_s: Optional[torch.Tensor], d_y: Optional[torch.Tensor]):
     """Allocate gradients and workspace and run lp_residual_norm_bwd.  Returns (d_h, d_f, d_gamma, d_beta, d_post_gamma, d_gate), None
     in the place of the gradient of what the norm does not have."""
-    like = lambda t: torch.empty_like(t) if t.is_contiguous() else torch.empty_strided(t.shape, t.stride(), dtype=t.dtype, device=t.device)  # noqa: E731
-    params = [norm.gamma, norm.beta, norm.post_gamma if f is not None else None, norm.gate if f is not None else None]
+    shape, dtype = h.shape, _f_type(h, f, d_y)
+    q = norm.c_struct(h, dtype, 0 if f is None else _channel_last(f, "f", shape, dtype), 0 if d_y is None else _channel_last(d_y, "d_y", shape, dtype))
+    _on_current_device(h, f, d_s, d_y)
+    d_s_at = _same_step(d_s, "d_s", shape, h.dtype, q.h_stride, "h")
+    # (new gradients do not overlap anything: what the entry point checks of them holds)
+    d_h = torch.empty_like(h) if h.is_contiguous() else torch.empty_strided(shape, h.stride(), dtype=h.dtype, device=h.device)
+    d_f = None if f is None else torch.empty_like(f) if f.is_contiguous() else torch.empty_strided(shape, f.stride(), dtype=dtype, device=f.device)
+    params = (norm.gamma, norm.beta, None, None) if f is None else (norm.gamma, norm.beta, norm.post_gamma, norm.gate)
     sizes = [0 if p is None else p.numel() for p in params]
     zeros = torch.zeros(sum(sizes), dtype=torch.float32, device=h.device)
-    parts = [None if p is None else z.view(p.shape) for p, z in zip(params, zeros.split(sizes))]
-    d_h, d_f = like(h), None if f is None else like(f)
-    ws = torch.empty(lp_residual_norm_workspace_bytes(norm, h), dtype=torch.uint8, device=h.device)
-    lp_residual_norm_bwd(norm, h, f, d_s, d_y, d_h, d_f, *parts, ws)
+    at, parts, ats, first = zeros.data_ptr(), [], [], 0
+    for p, size in zip(params, sizes):
+        parts.append(None if p is None else zeros[first:first + size].view(p.shape) if p.dim() > 1 else zeros[first:first + size])
+        ats.append(None if p is None else at + 4 * first)
+        first += size
+    n = C.c_size_t()
+    _check(_lib.lp_residual_norm_workspace_bytes(C.byref(q), C.byref(n)))
+    ws = torch.empty(n.value, dtype=torch.uint8, device=h.device)   # (held until the kernels are enqueued)
+    _check(_lib.lp_residual_norm_bwd(C.byref(q), h.data_ptr(), None if f is None else f.data_ptr(), d_s_at, None if d_y is None else d_y.data_ptr(),
+                                     d_h.data_ptr(), None if f is None else d_f.data_ptr(), *ats, ws.data_ptr(), n.value, _stream_ptr(None)))
     return (d_h, d_f, *parts)
 
 

@@ -68,8 +68,8 @@ __global__ __launch_bounds__(kThreads) void linear_rows_kernel(LinearDev d)
 
 // ---- gradients of the parameters in fp32 -----------------------------------------------------------------------
 //
-// A workgroup sums a part of the positions into 128 channels of d_z x 128 channels of x, with fp32 matrix instructions; both operands lie in LDS as
-// they lie in memory, row by row, 32 positions in one of two buffers while the other one is multiplied.
+// A workgroup sums a part of the positions into 128 or 64 channels of d_z x 128 channels of x, with fp32 matrix instructions; both operands lie in LDS as
+// they lie in memory, row by row, 32 positions in one of two buffers while the other one is multiplied and 64 more are on their way.
 struct WeightDev {
     long long P;
     int K, N;
@@ -82,77 +82,87 @@ struct WeightDev {
 };
 constexpr int kWeightTile = 128, kWeightRows = 32;
 
-template <int ACT>
+// BN: channels of d_z (the four waves make 64 x 64 or 32 x 64 of the sums each)
+template <int ACT, int BN>
 __global__ __launch_bounds__(kThreads, 2) void linear_weight_kernel(WeightDev d)
 {
-    constexpr int E = 4, kRows = kWeightRows, kPitch = kWeightTile * 4 + 64;
-    constexpr int kAcross = kWeightTile / E, kDown = kThreads / kAcross, kLoads = kRows / kDown;
-    constexpr int kImage = kRows * kPitch, kStage = kImage * 2;
+    constexpr int E = 4, kRows = kWeightRows, kPitchN = BN * 4 + 64, kPitchK = kWeightTile * 4 + 64, kBlocks = BN / 64;
+    constexpr int kAcrossN = BN / E, kDownN = kThreads / kAcrossN, kLoadsN = kRows / kDownN;
+    constexpr int kAcrossK = kWeightTile / E, kDownK = kThreads / kAcrossK, kLoadsK = kRows / kDownK;
+    constexpr int kImage = kRows * kPitchN, kStage = kImage + kRows * kPitchK;
     __shared__ alignas(16) char lds[2 * kStage];
     const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, l32 = lane & 31, h = lane >> 5;
-    const int c = threadIdx.x % kAcross, row = threadIdx.x / kAcross;
-    const int wave_n = (wave >> 1) * 64, wave_k = (wave & 1) * 64;
+    const int cn = threadIdx.x % kAcrossN, rn = threadIdx.x / kAcrossN, ck = threadIdx.x % kAcrossK, rk = threadIdx.x / kAcrossK;
+    const int wave_n = (wave >> 1) * (BN / 2), wave_k = (wave & 1) * 64;
     const int tiles = d.tiles_n * d.tiles_k, split = blockIdx.x / tiles, tile = blockIdx.x % tiles;
-    const int n0 = tile / d.tiles_k * kWeightTile, k0 = tile % d.tiles_k * kWeightTile;
+    const int n0 = tile / d.tiles_k * BN, k0 = tile % d.tiles_k * kWeightTile;
     const long long first = split * d.chunk, end = min(d.P, first + d.chunk);
-    Chunk<float> dy[kLoads], pre[kLoads], x[kLoads];
+    struct Staged {
+        Chunk<float> dy[kLoadsN], pre[kLoadsN], x[kLoadsK];
+    } staged[2];
     float bias[E] = {};
-    const int n = n0 + c * E, k = k0 + c * E;
+    const int n = n0 + cn * E, k = k0 + ck * E;
     const bool sum_bias = d.d_bias && k0 == 0;
-    auto ask = [&](long long p0) {
+    auto ask = [&](long long p0, Staged& to) {   // (behind the last position: zeros)
 #pragma unroll
-        for (int u = 0; u < kLoads; ++u) {
-            const long long p = p0 + row + u * kDown;
-            const bool in = p < end;
-            dy[u] = load_chunk<false>(d.dy + p * d.ys + n, in ? d.N - n : 0);
-            if (ACT != LP_ACT_NONE) pre[u] = load_chunk<false>(d.pre + p * d.N + n, in ? d.N - n : 0);
-            x[u] = load_chunk<false>(d.x + p * d.xs + k, in ? d.K - k : 0);
+        for (int u = 0; u < kLoadsN; ++u) {
+            const long long p = p0 + rn + u * kDownN;
+            const int count = p < end ? d.N - n : 0;
+            to.dy[u] = load_chunk<false>(d.dy + p * d.ys + n, count);
+            if (ACT != LP_ACT_NONE) to.pre[u] = load_chunk<false>(d.pre + p * d.N + n, count);
+        }
+#pragma unroll
+        for (int u = 0; u < kLoadsK; ++u) {
+            const long long p = p0 + rk + u * kDownK;
+            to.x[u] = load_chunk<false>(d.x + p * d.xs + k, p < end ? d.K - k : 0);
         }
     };
-    auto put = [&](int buffer) {
+    auto put = [&](int buffer, const Staged& from) {
         char* to = lds + buffer * kStage;
 #pragma unroll
-        for (int u = 0; u < kLoads; ++u) {
-            const int at = (row + u * kDown) * kPitch + c * 16;
-            const Gradient<float> g = gradient<ACT>(dy[u], pre[u]);
-            *(Chunk<float>*)(to + at) = g.hi;
-            *(Chunk<float>*)(to + kImage + at) = x[u];
+        for (int u = 0; u < kLoadsN; ++u) {
+            const Gradient<float> g = gradient<ACT>(from.dy[u], from.pre[u]);
+            *(Chunk<float>*)(to + (rn + u * kDownN) * kPitchN + cn * 16) = g.hi;
 #pragma unroll
             for (int j = 0; j < E; ++j) bias[j] += g.v[j];
         }
+#pragma unroll
+        for (int u = 0; u < kLoadsK; ++u) *(Chunk<float>*)(to + kImage + (rk + u * kDownK) * kPitchK + ck * 16) = from.x[u];
     };
-    f32x16 acc[2][2] = {};
-    if (first < end) {
-        ask(first);
-        put(0);
-    }
-    __syncthreads();
-    int buffer = 0;
-    for (long long p = first; p < end; p += kRows) {
-        const bool more = p + kRows < end;
-        if (more) ask(p + kRows);
-        const char* from = lds + buffer * kStage;
+    f32x16 acc[kBlocks][2] = {};
+    auto multiply_all = [&](const char* from) {
 #pragma unroll
         for (int r = 0; r < kRows; r += 2) {
-            float xv[2], g[2];
+            float xv[2], g[kBlocks];
 #pragma unroll
-            for (int i = 0; i < 2; ++i) {
-                g[i] = *(const float*)(from + (r + h) * kPitch + (wave_n + i * 32 + l32) * 4);
-                xv[i] = *(const float*)(from + kImage + (r + h) * kPitch + (wave_k + i * 32 + l32) * 4);
-            }
+            for (int i = 0; i < kBlocks; ++i) g[i] = *(const float*)(from + (r + h) * kPitchN + (wave_n + i * 32 + l32) * 4);
 #pragma unroll
-            for (int i = 0; i < 2; ++i)
+            for (int j = 0; j < 2; ++j) xv[j] = *(const float*)(from + kImage + (r + h) * kPitchK + (wave_k + j * 32 + l32) * 4);
+#pragma unroll
+            for (int i = 0; i < kBlocks; ++i)
 #pragma unroll
                 for (int j = 0; j < 2; ++j) acc[i][j] = __builtin_amdgcn_mfma_f32_32x32x2f32(g[i], xv[j], acc[i][j], 0, 0, 0);
         }
-        if (more) put(buffer ^ 1);
-        __syncthreads();
-        buffer ^= 1;
+    };
+    ask(first, staged[0]);
+    ask(first + kRows, staged[1]);
+    put(0, staged[0]);
+    __syncthreads();
+    for (long long p = first; p < end; p += 2 * kRows) {
+#pragma unroll
+        for (int u = 0; u < 2; ++u) {
+            const long long at = p + u * kRows;
+            if (at >= end) break;
+            if (at + 2 * kRows < end) ask(at + 2 * kRows, staged[u]);
+            multiply_all(lds + u * kStage);
+            if (at + kRows < end) put(u ^ 1, staged[u ^ 1]);
+            __syncthreads();
+        }
     }
     if (d.d_weight) {
         float* out = d.parts ? d.parts + (long long)split * d.N * d.K : d.d_weight;
 #pragma unroll
-        for (int i = 0; i < 2; ++i)
+        for (int i = 0; i < kBlocks; ++i)
 #pragma unroll
             for (int j = 0; j < 2; ++j) {
                 const int kk = k0 + wave_k + j * 32 + l32;
@@ -166,13 +176,13 @@ __global__ __launch_bounds__(kThreads, 2) void linear_weight_kernel(WeightDev d)
             }
     }
     if (sum_bias) {
-        float* sums = (float*)lds;   // [kDown][128]
+        float* sums = (float*)lds;   // [kDownN][BN]
 #pragma unroll
-        for (int j = 0; j < E; ++j) sums[row * kWeightTile + c * E + j] = bias[j];
+        for (int j = 0; j < E; ++j) sums[rn * BN + cn * E + j] = bias[j];
         __syncthreads();
-        if (threadIdx.x < kWeightTile && n0 + (int)threadIdx.x < d.N) {
+        if (threadIdx.x < BN && n0 + (int)threadIdx.x < d.N) {
             float sum = 0.0f;
-            for (int r = 0; r < kDown; ++r) sum += sums[r * kWeightTile + threadIdx.x];
+            for (int r = 0; r < kDownN; ++r) sum += sums[r * BN + threadIdx.x];
             const int nn = n0 + threadIdx.x;
             if (d.parts) d.bias_parts[(long long)split * d.N + nn] = sum;
             else d.d_bias[nn] += sum;
@@ -288,13 +298,16 @@ Parts parts_of(const Call& c, int n_cu)
     Parts p;
     p.bn = p.bk = kWeightTile;
     long long per_cu = 2, step = 32, least = 256;
-    if (c.dtype != LP_F32) {
+    if (c.dtype == LP_F32) {
+        if (c.N <= 64) p.bn = 64;
+        least = 128;
+    } else {
         if (c.K <= 128 && c.N <= 128) {
             p.bn = c.N <= 64 ? 64 : 128;
             p.bk = c.K <= 32 ? 32 : c.K <= 64 ? 64 : 128;
             per_cu = 3;
             step = 64;
-            least = 512;
+            least = 64;
         } else {
             p.bk = c.K <= 128 ? 128 : c.K <= 256 ? 256 : 512;
             per_cu = p.bk == 512 ? 1 : 2;
@@ -440,7 +453,9 @@ lp_status backward(const lp_linear* q, const void* x, const void* pre, const voi
         d.bias_parts = join ? bias_parts : nullptr;
         d.chunk = p.chunk; d.tiles_n = p.tiles_n; d.tiles_k = tiles_k; d.splits = p.splits;
         with_act_of(c.act, [&](auto a) {
-            hipLaunchKernelGGL((linear_weight_kernel<decltype(a)::value>), dim3((unsigned)(d.tiles_n * d.tiles_k * p.splits)), dim3(kThreads), 0, s, d);
+            const dim3 grid((unsigned)(d.tiles_n * d.tiles_k * p.splits));
+            if (p.bn == 64) hipLaunchKernelGGL((linear_weight_kernel<decltype(a)::value, 64>), grid, dim3(kThreads), 0, s, d);
+            else hipLaunchKernelGGL((linear_weight_kernel<decltype(a)::value, kWeightTile>), grid, dim3(kThreads), 0, s, d);
         });
     }
     if (params && join) {

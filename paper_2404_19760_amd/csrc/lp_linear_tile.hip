@@ -37,41 +37,45 @@ __global__ __launch_bounds__(kThreads, 2) void linear_tile_kernel(LinearDev d)
         if (tile >= tiles) continue;
         const long long p0 = tile / d.tiles_n * BP;
         const int n0 = (int)(tile % d.tiles_n) * BN;
-        Chunk<T> a[kLoadsA], pre[BACK && ACT != LP_ACT_NONE ? kLoadsA : 1], w[kLoadsW];
-        auto ask = [&](int k0) {
-            const int k = k0 + c8 * E;
+        // (two steps are asked for ahead: where there are few tiles nothing else hides the memory's latency)
+        struct Staged {
+            Chunk<T> a[kLoadsA], pre[BACK && ACT != LP_ACT_NONE ? kLoadsA : 1], w[kLoadsW];
+        } staged[2];
+        // (only the last step can meet the end of a row: moving what is left of one waits for every piece)
+        auto ask_as = [&](auto all, int step, Staged& to) {
+            constexpr bool kAll = decltype(all)::value;
+            const int k = step * (8 * E) + c8 * E;
 #pragma unroll
             for (int u = 0; u < kLoadsA; ++u) {
                 const long long p = p0 + row + u * 32;
                 const int count = p < d.P ? d.K - k : 0;
-                a[u] = load_chunk<WHOLE>((const T*)d.a + p * d.as + k, count);
-                if (BACK && ACT != LP_ACT_NONE) pre[u] = load_chunk<WHOLE>((const T*)d.pre + p * d.K + k, count);
+                to.a[u] = load_chunk<kAll>((const T*)d.a + p * d.as + k, count);
+                if (BACK && ACT != LP_ACT_NONE) to.pre[u] = load_chunk<kAll>((const T*)d.pre + p * d.K + k, count);
             }
 #pragma unroll
             for (int u = 0; u < kLoadsW; ++u) {
                 const int n = n0 + row + u * 32;
-                w[u] = load_chunk<WHOLE>((const T*)d.w + n * d.ws + k, n < d.N ? d.K - k : 0);
+                to.w[u] = load_chunk<kAll>((const T*)d.w + n * d.ws + k, n < d.N ? d.K - k : 0);
             }
         };
-        auto put = [&](int buffer) {
+        auto ask = [&](int step, Staged& to) {
+            if (WHOLE || (step + 1) * (8 * E) <= d.K) ask_as(std::true_type(), step, to);
+            else ask_as(std::false_type(), step, to);
+        };
+        auto put = [&](int buffer, const Staged& from) {
             char* to = lds + buffer * S::kStage;
 #pragma unroll
             for (int u = 0; u < kLoadsA; ++u) {
-                Chunk<T> v = a[u];
-                if (BACK && ACT != LP_ACT_NONE) v = gradient<ACT>(a[u], pre[u]).hi;
+                Chunk<T> v = from.a[u];
+                if (BACK && ACT != LP_ACT_NONE) v = gradient<ACT>(from.a[u], from.pre[u]).hi;
                 *(Chunk<T>*)(to + chunk_at(row + u * 32, c8)) = v;
             }
 #pragma unroll
-            for (int u = 0; u < kLoadsW; ++u) *(Chunk<T>*)(to + BP * 128 + chunk_at(row + u * 32, c8)) = w[u];
+            for (int u = 0; u < kLoadsW; ++u) *(Chunk<T>*)(to + BP * 128 + chunk_at(row + u * 32, c8)) = from.w[u];
         };
         f32x16 acc[S::kBlocksN][S::kBlocksP] = {};
         const int steps = (d.K + 8 * E - 1) / (8 * E);
-        ask(0);
-        put(0);
-        __syncthreads();
-        for (int s = 0; s < steps; ++s) {
-            if (s + 1 < steps) ask((s + 1) * 8 * E);
-            const char* from = lds + (s & 1) * S::kStage;
+        auto multiply_all = [&](const char* from) {
 #pragma unroll
             for (int q = 0; q < 4; ++q) {
                 Chunk<T> wv[S::kBlocksN], av[S::kBlocksP];
@@ -84,10 +88,25 @@ __global__ __launch_bounds__(kThreads, 2) void linear_tile_kernel(LinearDev d)
 #pragma unroll
                     for (int j = 0; j < S::kBlocksP; ++j) acc[i][j] = multiply(wv[i], av[j], acc[i][j]);
             }
-            if (s + 1 < steps) put((s + 1) & 1);
-            __syncthreads();
+        };
+        ask(0, staged[0]);
+        if (steps > 1) ask(1, staged[1]);
+        put(0, staged[0]);
+        __syncthreads();
+        for (int first = 0; first < steps; first += 2) {
+#pragma unroll
+            for (int u = 0; u < 2; ++u) {
+                const int s = first + u;
+                if (s >= steps) break;
+                if (s + 2 < steps) ask(s + 2, staged[u]);
+                multiply_all(lds + u * S::kStage);
+                if (s + 1 < steps) put(u ^ 1, staged[u ^ 1]);
+                __syncthreads();
+            }
         }
-        finish<T, ACT, BACK, WHOLE, S::kBlocksP, S::kBlocksN>(d, acc, (float*)lds + wave * 32 * S::kPitch, p0 + wave_p, n0 + wave_n, lane);
+        float* turn = (float*)lds + wave * 32 * S::kPitch;
+        if (WHOLE || n0 + wave_n + S::kN <= d.N) finish<T, ACT, BACK, true, S::kBlocksP, S::kBlocksN>(d, acc, turn, p0 + wave_p, n0 + wave_n, lane);
+        else finish<T, ACT, BACK, false, S::kBlocksP, S::kBlocksN>(d, acc, turn, p0 + wave_p, n0 + wave_n, lane);
         __syncthreads();   // (the next tile's first step lies where results were)
     }
 }

@@ -62,8 +62,13 @@ __global__ __launch_bounds__(kThreads, 2) void linear_wide_kernel(LinearDev d)
         auto ask = [&](int step) {
             const int k = step * 64;
             const int count = d.K - k - c8 * 8;
+            if (WHOLE || k + 64 <= d.K) {   // (only the last step can meet the end of a row)
 #pragma unroll
-            for (int u = 0; u < 4; ++u) staged[u] = load_chunk<WHOLE>(at[u] + k, rows_in >> u & 1 ? count : 0);
+                for (int u = 0; u < 4; ++u) staged[u] = load_chunk<true>(at[u] + k, rows_in >> u & 1 ? count : 0);
+            } else {
+#pragma unroll
+                for (int u = 0; u < 4; ++u) staged[u] = load_chunk<false>(at[u] + k, rows_in >> u & 1 ? count : 0);
+            }
         };
         auto put = [&](int buffer) {
 #pragma unroll
@@ -107,7 +112,8 @@ __global__ __launch_bounds__(kThreads, 2) void linear_wide_kernel(LinearDev d)
             }
             __syncthreads();
         }
-        finish<T, ACT, BACK, WHOLE, 4, 2>(d, acc, (float*)lds + wave * 32 * 68, p0, n0, lane);
+        if (WHOLE || n0 + 64 <= d.N) finish<T, ACT, BACK, true, 4, 2>(d, acc, (float*)lds + wave * 32 * 68, p0, n0, lane);
+        else finish<T, ACT, BACK, false, 4, 2>(d, acc, (float*)lds + wave * 32 * 68, p0, n0, lane);
         __syncthreads();   // (the next tile's first step lies where results were)
     }
 }

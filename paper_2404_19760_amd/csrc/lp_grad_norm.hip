@@ -179,18 +179,20 @@ __global__ __launch_bounds__(kThreads) void grad_squares_kernel(Set<MAX> a, doub
 }
 
 // The sum of the parts, for all threads of the workgroup; it needs no other workgroup's result than the parts.
+template <int THREADS>
 __device__ __forceinline__ double all_parts(const double* parts, int n, double* lds)
 {
     double sum = 0.0;
-    for (int i = threadIdx.x; i < n; i += kThreads) sum += parts[i];
-    return all_of<kThreads>(sum, lds);
+#pragma unroll 8
+    for (int i = threadIdx.x; i < n; i += THREADS) sum += parts[i];
+    return all_of<THREADS>(sum, lds);
 }
 
 // One workgroup: the parts' sum into the place of `total` (NULL: none), and the norm.
-__global__ __launch_bounds__(kThreads) void grad_join_kernel(const double* parts, int n, double* total, float* norm)
+__global__ __launch_bounds__(kSmallThreads) void grad_join_kernel(const double* parts, int n, double* total, float* norm)
 {
-    __shared__ double lds[kThreads / 64];
-    const double sum = all_parts(parts, n, lds);
+    __shared__ double lds[kSmallThreads / 64];
+    const double sum = all_parts<kSmallThreads>(parts, n, lds);
     if (threadIdx.x) return;
     if (total) *total = sum;
     *norm = (float)sqrt(sum);
@@ -201,7 +203,7 @@ template <bool PAST_CACHE, int MAX>
 __global__ __launch_bounds__(kThreads) void grad_scale_kernel(Set<MAX> a, const double* parts, int n, Clip c, int write_norm)
 {
     __shared__ double lds[kThreads / 64];
-    const double sum = all_parts(parts, n, lds);
+    const double sum = all_parts<kThreads>(parts, n, lds);
     if (write_norm && blockIdx.x == 0 && threadIdx.x == 0) *c.norm = (float)sqrt(sum);
     const float factor = factor_of(sum, c);
     const int item = a.items - 1 - blockIdx.x, k = tensor_of(a, item);
@@ -408,7 +410,7 @@ lp_status run(const std::vector<lp_gradient>& v, Clip c, void* workspace, size_t
         else go(set_of<kSetTensors>(v, k, end, d.chunk, d.chunk, items));
     }
     const bool join = !c.scale || items > kJoinAtOnce;
-    if (join) hipLaunchKernelGGL(grad_join_kernel, dim3(1), dim3(kThreads), 0, s, parts, items, c.scale ? parts + items : nullptr, c.norm);
+    if (join) hipLaunchKernelGGL(grad_join_kernel, dim3(1), dim3(kSmallThreads), 0, s, parts, items, c.scale ? parts + items : nullptr, c.norm);
     if (c.scale) {
         const double* sums = join ? parts + items : parts;
         const int n = join ? 1 : items;

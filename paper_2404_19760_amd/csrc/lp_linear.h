@@ -193,6 +193,8 @@ struct LinearDev {
     long long tiles_p;
     int tiles_n;
     int past_cache;                 // results are stored past the caches
+    float* parts;                   // of the general kernel: sums of a part of the steps
+    int splits, split_steps;        // parts, steps of one
 };
 
 __device__ __forceinline__ int chunk_at(int row, int chunk) { return row * 128 + ((chunk ^ (row >> 1 & 7)) << 4); }
@@ -305,7 +307,9 @@ void with_act_of(int act, F&& f)
 // Whether rows end with whole chunks.
 inline bool whole(const LinearDev& d, int dtype) { return d.K % (dtype == LP_F32 ? 4 : 8) == 0 && d.N % (dtype == LP_F32 ? 4 : 8) == 0; }
 
-// The general kernel (lp_linear_tile.hip).  back: d_x from d_y and pre.
+// The general kernel (lp_linear_tile.hip).  back: d_x from d_y and pre.  d.splits > 1: with d.parts.
+constexpr int kTileP = 128;
+inline int tile_channels(int made) { return made <= 32 ? 32 : made <= 64 ? 64 : 128; }
 void launch_tiles(int dtype, int act, bool back, LinearDev d, hipStream_t s);
 
 // Few channels (lp_linear_stream.hip).  back: d_x from d_y and pre, fp32 alone; the weight is W as it is, with rows of ws elements.

@@ -12,6 +12,7 @@
 #include <cstring>
 #include <initializer_list>
 
+#include "lp_lanes.h"
 #include "lp_linear.h"
 
 namespace lp {
@@ -20,7 +21,7 @@ using namespace linear;
 
 namespace {
 
-constexpr int kFewRows = 8;   // positions that go to the kernel without matrix cores, at most
+constexpr int kFewRows = 8;   // positions that a wave of the kernel without matrix cores makes, at most
 
 // ---- few positions ---------------------------------------------------------------------------------------------
 //
@@ -30,7 +31,7 @@ template <class T, int ACT, int ROWS>
 __global__ __launch_bounds__(kThreads) void linear_rows_kernel(LinearDev d)
 {
     constexpr int E = kChunk<T>;
-    const int lane = threadIdx.x & 63, n0 = (blockIdx.x * (kThreads / 64) + (threadIdx.x >> 6)) * kOutputs;
+    const int lane = threadIdx.x & 63, n0 = (blockIdx.x * (kThreads / 64) + (threadIdx.x >> 6)) * kOutputs, r0 = blockIdx.y * ROWS;
     if (n0 >= d.N) return;
     float sum[kOutputs][ROWS] = {};
     for (int k = lane * E; k < d.K; k += 64 * E) {
@@ -38,7 +39,7 @@ __global__ __launch_bounds__(kThreads) void linear_rows_kernel(LinearDev d)
 #pragma unroll
         for (int i = 0; i < kOutputs; ++i) w[i] = load_chunk<false>((const T*)d.w + (n0 + i) * d.ws + k, n0 + i < d.N ? d.K - k : 0);
 #pragma unroll
-        for (int r = 0; r < ROWS; ++r) x[r] = load_chunk<false>((const T*)d.a + r * d.as + k, r < d.P ? d.K - k : 0);
+        for (int r = 0; r < ROWS; ++r) x[r] = load_chunk<false>((const T*)d.a + (r0 + r) * d.as + k, r0 + r < d.P ? d.K - k : 0);
 #pragma unroll
         for (int i = 0; i < kOutputs; ++i)
 #pragma unroll
@@ -47,22 +48,18 @@ __global__ __launch_bounds__(kThreads) void linear_rows_kernel(LinearDev d)
                 for (int j = 0; j < E; ++j) sum[i][r] = fmaf((float)w[i].v[j], (float)x[r].v[j], sum[i][r]);
     }
 #pragma unroll
-    for (int m = 32; m; m >>= 1)
-#pragma unroll
-        for (int i = 0; i < kOutputs; ++i)
-#pragma unroll
-            for (int r = 0; r < ROWS; ++r) sum[i][r] += __shfl_xor(sum[i][r], m);
+    for (int i = 0; i < kOutputs; ++i) lane_sums(sum[i], 64);
 #pragma unroll
     for (int i = 0; i < kOutputs; ++i)
 #pragma unroll
         for (int r = 0; r < ROWS; ++r) {
             const int n = n0 + i;
-            if (lane != i * ROWS + r || n >= d.N || r >= d.P) continue;
+            if (lane != i * ROWS + r || n >= d.N || r0 + r >= d.P) continue;
             const float z = sum[i][r] + (d.bias ? d.bias[n] : 0.0f);
-            if (d.keep) ((T*)d.keep)[(long long)r * d.N + n] = (T)z;
+            if (d.keep) ((T*)d.keep)[(long long)(r0 + r) * d.N + n] = (T)z;
             float y = activate_as<ACT, T>(z);
-            if (d.res) y += (float)((const T*)d.res)[r * d.rs + n];
-            ((T*)d.out)[r * d.ys + n] = (T)y;
+            if (d.res) y += (float)((const T*)d.res)[(r0 + r) * d.rs + n];
+            ((T*)d.out)[(r0 + r) * d.ys + n] = (T)y;
         }
 }
 
@@ -315,8 +312,12 @@ Parts parts_of(const Call& c, int n_cu)
     }
     p.tiles_n = (c.N + p.bn - 1) / p.bn;
     p.tiles_k = (c.K + p.bk - 1) / p.bk;
-    const long long tiles = (long long)p.tiles_n * p.tiles_k, target = (per_cu * n_cu + tiles - 1) / tiles, most = (c.P + least - 1) / least;
+    const long long tiles = (long long)p.tiles_n * p.tiles_k, target = (per_cu * n_cu + tiles - 1) / tiles;
+    // (nor more sums of parts than twice what the positions hold: they are written and read again)
+    const long long most = (c.P + least - 1) / least;
+    const double light = 2.0 * c.P * (c.K + 2.0 * c.N) * dtype_bytes(c.dtype) / (4.0 * c.N * c.K);
     long long splits = target < most ? target : most;
+    if ((double)splits > light) splits = (long long)light;
     if (splits < 1) splits = 1;
     p.chunk = ((c.P + splits - 1) / splits + step - 1) / step * step;
     if (p.chunk < step) p.chunk = step;
@@ -330,9 +331,30 @@ bool is_wide(const Call& c, int channels) { return c.dtype != LP_F32 && channels
 size_t packed_bytes(int rows, int cols) { return align256((size_t)((rows + 31) / 32) * wide_blocks(cols) * 1024); }
 bool is_skinny(const Call& c) { return c.dtype != LP_F32 && c.K <= 128 && c.N <= 128; }
 
+// How the general kernel divides long sums of few tiles: at least four steps (of 128 bytes) a part, some parts at most, for up to one workgroup and a
+// half a compute unit.
+struct Split {
+    int splits, steps;
+    size_t bytes;
+};
+Split split_of(const Call& c, int summed, int made, int n_cu)
+{
+    const int steps = (int)(((long long)summed * dtype_bytes(c.dtype) + 127) / 128), bn = tile_channels(made);
+    const long long tiles = ((c.P + kTileP - 1) / kTileP) * ((made + bn - 1) / bn), room = 3ll * n_cu / 2 / (tiles > 0 ? tiles : 1);
+    long long splits = steps / 4 < room ? steps / 4 : room;
+    const int most = c.dtype == LP_F32 ? 8 : 4;   // (a step of fp32 takes 2 us, of 16 bits a third; adding up a part 1 to 2)
+    if (splits > most) splits = most;
+    Split s = {1, steps, 0};
+    if (splits < 2) return s;
+    s.steps = (int)((steps + splits - 1) / splits);
+    s.splits = (steps + s.steps - 1) / s.steps;
+    s.bytes = align256((size_t)tiles * s.splits * kTileP * bn * sizeof(float));
+    return s;
+}
+
 struct Sizes {
-    size_t weight, parts, bias_parts, dz;
-    size_t all() const { return weight + parts + bias_parts + dz; }
+    size_t weight, parts, bias_parts, dz, split;
+    size_t all() const { return weight + parts + bias_parts + dz + split; }
 };
 Sizes sizes(const Call& c, int n_cu)
 {
@@ -343,6 +365,7 @@ Sizes sizes(const Call& c, int n_cu)
     s.weight = is_skinny(c) ? 0 : is_wide(c, c.K) ? packed_bytes(c.K, c.N) : align256((size_t)c.K * ((c.N + E - 1) / E * E) * dtype_bytes(c.dtype));
     s.parts = halves || p.splits > 1 ? align256((size_t)p.splits * c.N * c.K * sizeof(float)) : 0;
     s.bias_parts = halves || p.splits > 1 ? align256((size_t)p.splits * c.N * sizeof(float)) : 0;
+    s.split = split_of(c, c.N, c.K, n_cu).bytes;
     s.dz = halves && !is_skinny(c) && c.act != LP_ACT_NONE ? align256((size_t)c.P * c.N * 2) : 0;
     return s;
 }
@@ -366,13 +389,40 @@ lp_status aligned(int dtype, std::initializer_list<const void*> ps)
 template <class T>
 void few_rows(const LinearDev& d, int act, hipStream_t s)
 {
-    const dim3 grid((d.N + kThreads / 64 * kOutputs - 1) / (kThreads / 64 * kOutputs));
+    dim3 grid((d.N + kThreads / 64 * kOutputs - 1) / (kThreads / 64 * kOutputs));
+    if (d.P > kFewRows) grid.y = (unsigned)((d.P + kFewRows - 1) / kFewRows);
     with_act_of(act, [&](auto a) {
         constexpr int A = decltype(a)::value;
         if (d.P == 1) hipLaunchKernelGGL((linear_rows_kernel<T, A, 1>), grid, dim3(kThreads), 0, s, d);
         else if (d.P <= 4) hipLaunchKernelGGL((linear_rows_kernel<T, A, 4>), grid, dim3(kThreads), 0, s, d);
         else hipLaunchKernelGGL((linear_rows_kernel<T, A, kFewRows>), grid, dim3(kThreads), 0, s, d);
     });
+}
+
+// Which kernel makes a forward.
+enum Way { kRowsWay, kStreamWay, kWideWay, kTileWay };
+// Up to eight positions go to the kernel without matrix cores.  Some more do where a tile's steps would follow one another on a few compute
+// units: fp32 products are slow there (32 x 1024 -> 256: 12 us, tiles 50; 300 x 2048 -> 512 38 and 63; 100 x 2048 -> 2048, 2^18 results, 45
+// and 43), in 16 bits with long sums alone (64 x 1024 -> 256: 11 us, tiles 15; 64 x 256 -> 256 10 and 9; 32 x 2048 -> 2048, 2^16 results, 18 and 15).
+Way way_of(const Call& c)
+{
+    const long long made = c.P * c.N;
+    if (c.P <= kFewRows) return kRowsWay;
+    if (is_few(c.dtype, c.K, c.N)) return kStreamWay;
+    if (c.dtype == LP_F32 ? c.P <= 512 && made < 1 << 18 : c.P <= 128 && made < 1 << 16 && c.K >= 512) return kRowsWay;
+    return is_wide(c, c.N) ? kWideWay : kTileWay;
+}
+// Its workspace; *n_cu is set where the kernel goes by it.
+lp_status forward_bytes(const Call& c, int* n_cu, size_t* bytes)
+{
+    *bytes = 0;
+    const Way way = way_of(c);
+    if (way == kWideWay) *bytes = packed_bytes(c.N, c.K);
+    if (way != kStreamWay && way != kTileWay) return LP_OK;
+    std::string err;
+    if (compute_units(n_cu, &err)) return fail(LP_ERR_HIP, err);
+    if (way == kTileWay) *bytes = split_of(c, c.K, c.N, *n_cu).bytes;
+    return LP_OK;
 }
 
 lp_status forward(const lp_linear* q, const void* x, void* y, void* pre, void* workspace, size_t workspace_bytes, hipStream_t s)
@@ -383,29 +433,33 @@ lp_status forward(const lp_linear* q, const void* x, void* y, void* pre, void* w
     if (c.P == 0) return LP_OK;
     if (!x || !y || !c.weight) return fail(LP_ERR_INVALID_ARG, "x, y and linear->weight must not be NULL");
     if ((st = aligned(c.dtype, {x, y, pre, c.weight, c.residual})) != LP_OK) return st;
-    const bool wide = is_wide(c, c.N);
-    if (wide && (!workspace || workspace_bytes < packed_bytes(c.N, c.K)))
+    const Way way = way_of(c);
+    int n_cu = 0;
+    size_t need = 0;
+    if ((st = forward_bytes(c, &n_cu, &need)) != LP_OK) return st;
+    if (need && (!workspace || workspace_bytes < need))
         return fail(LP_ERR_WORKSPACE, "workspace is NULL or smaller than lp_linear_workspace_bytes");
-    if (wide && (uintptr_t)workspace % 256) return fail(LP_ERR_INVALID_ARG, "workspace must be 256-byte aligned");
+    if (need && (uintptr_t)workspace % 256) return fail(LP_ERR_INVALID_ARG, "workspace must be 256-byte aligned");
     LinearDev d;
     std::memset(&d, 0, sizeof(d));
     d.P = c.P; d.K = c.K; d.N = c.N; d.as = c.xs; d.ys = c.ys; d.rs = c.rs;
     d.a = x; d.w = c.weight; d.ws = c.K; d.res = c.residual; d.bias = c.bias; d.out = y; d.keep = pre;
     d.past_cache = bytes_of(c, c.K + (double)c.N * (1 + (pre != nullptr) + (c.residual != nullptr))) > kCacheBytes;
-    if (c.P <= kFewRows) {
+    if (way == kRowsWay) {
         if (c.dtype == LP_BF16) few_rows<__bf16>(d, c.act, s);
         else if (c.dtype == LP_F16) few_rows<_Float16>(d, c.act, s);
         else few_rows<float>(d, c.act, s);
-    } else if (wide) {
+    } else if (way == kWideWay) {
         launch_pack(c.dtype, false, d.w, c.N, c.K, c.K, workspace, s);
         d.w = workspace;
         launch_wide(c.dtype, c.act, false, d, s);
-    } else if (is_few(c.dtype, c.K, c.N)) {
-        std::string err;
-        int n_cu = 0;
-        if (compute_units(&n_cu, &err)) return fail(LP_ERR_HIP, err);
+    } else if (way == kStreamWay) {
         launch_stream(c.dtype, c.act, false, d, n_cu, s);
     } else {
+        const Split split = split_of(c, c.K, c.N, n_cu);
+        d.splits = split.splits;
+        d.split_steps = split.steps;
+        d.parts = (float*)workspace;
         launch_tiles(c.dtype, c.act, false, d, s);
     }
     return launched("linear forward launch");
@@ -488,6 +542,10 @@ lp_status backward(const lp_linear* q, const void* x, const void* pre, const voi
             const dim3 grid(grid_of(((c.K + 31ll) / 32) * ((c.N + 31ll) / 32)));
             if (halves) hipLaunchKernelGGL((linear_turn_kernel<uint16_t>), grid, dim3(kThreads), 0, s, (const uint16_t*)c.weight, c.N, c.K, (uint16_t*)at, d.ws);
             else hipLaunchKernelGGL((linear_turn_kernel<float>), grid, dim3(kThreads), 0, s, (const float*)c.weight, c.N, c.K, (float*)at, d.ws);
+            const Split split = split_of(c, c.N, c.K, n_cu);
+            d.splits = split.splits;
+            d.split_steps = split.steps;
+            d.parts = (float*)(at + size.all() - size.split);
             launch_tiles(c.dtype, act, true, d, s);
         }
     }
@@ -505,10 +563,14 @@ try {
     lp::Call c;
     const lp_status st = lp::validate(linear, &c);
     if (st != LP_OK) return st;
-    if (fwd_bytes) *fwd_bytes = c.P && lp::is_wide(c, c.N) ? lp::packed_bytes(c.N, c.K) : 0;
+    int n_cu = 0;
+    if (fwd_bytes) {
+        *fwd_bytes = 0;
+        const lp_status found = c.P ? lp::forward_bytes(c, &n_cu, fwd_bytes) : LP_OK;
+        if (found != LP_OK) return found;
+    }
     if (!bwd_bytes) return LP_OK;
     std::string err;
-    int n_cu = 0;
     if (lp::compute_units(&n_cu, &err)) return lp::fail(LP_ERR_HIP, err);
     const lp::Sizes size = lp::sizes(c, n_cu);
     *bwd_bytes = size.all();

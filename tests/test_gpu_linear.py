@@ -19,7 +19,8 @@ ACTS = ["none", "relu", "silu", "gelu"]
 DTYPES = [torch.float32, torch.bfloat16, torch.float16]
 SIZES = [(1, 512, 2048), (1, 3, 5), (2, 4099, 7), (3, 72, 97), (8, 65, 33), (9, 64, 64), (16, 32, 32), (127, 31, 33), (128, 128, 128), (129, 129, 129),
          (1000, 72, 97), (4099, 16, 8), (300, 200, 1), (300, 1, 70), (257, 640, 384), (64, 2048, 512), (5000, 40, 130), (20011, 32, 128), (777, 64, 256),
-         (600, 200, 136), (1030, 264, 520), (513, 530, 145), (515, 129, 131), (2000, 512, 64), (700, 1040, 40), (129, 128, 33), (1000, 64, 32), (333, 65, 128)]
+         (600, 200, 136), (1030, 264, 520), (513, 530, 145), (515, 129, 131), (2000, 512, 64), (700, 1040, 40), (129, 128, 33), (1000, 64, 32), (333, 65, 128),
+         (13, 1024, 256), (70, 515, 40), (300, 2048, 100), (150, 777, 300), (200, 100, 1100)]
 
 
 def _act(z, act):

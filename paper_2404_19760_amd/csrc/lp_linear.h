@@ -160,10 +160,10 @@ __device__ __forceinline__ float slope_as(float z)
     }
 }
 
-// d_z of a chunk, rounded to T, and what the rounding left.
+// d_z of a chunk, rounded to T, what that left, rounded to T (of fp16: to bf16, and there is no third part), and what that left.
 template <class T>
 struct Gradient {
-    Chunk<T> hi, lo;
+    Chunk<T> part[3];
     float v[kChunk<T>];
 };
 template <int ACT, class T>
@@ -173,10 +173,19 @@ __device__ __forceinline__ Gradient<T> gradient(const Chunk<T>& dy, const Chunk<
 #pragma unroll
     for (int j = 0; j < kChunk<T>; ++j) {
         g.v[j] = (float)dy.v[j] * (ACT == LP_ACT_NONE ? 1.0f : slope_as<ACT, T>((float)pre.v[j]));
-        asm("" : "+v"(g.v[j]));   // (both parts come from this value: hi alone could be rounded straight from the product)
-        g.hi.v[j] = (T)g.v[j];
-        if (sizeof(T) == 2) {
-            g.lo.v[j] = (T)(g.v[j] - (float)g.hi.v[j]);   // (an infinite d_z leaves NaN)
+        float rest = g.v[j];
+#pragma unroll
+        for (int k = 0; k < 3; ++k) {
+            asm("" : "+v"(rest));   // (a part and what it leaves come from one value: the first could be rounded straight from the product)
+            if (k == 0) g.v[j] = rest;
+            if constexpr (std::is_same<T, _Float16>::value) {
+                if (k == 1) {
+                    g.part[k].v[j] = __builtin_bit_cast(_Float16, (__bf16)rest);
+                    break;
+                }
+            }
+            g.part[k].v[j] = (T)rest;
+            rest -= (float)g.part[k].v[j];   // (an infinite d_z leaves NaN)
         }
     }
     return g;

@@ -119,7 +119,7 @@ __global__ __launch_bounds__(kThreads, 2) void linear_weight_kernel(WeightDev d)
 #pragma unroll
         for (int u = 0; u < kLoadsN; ++u) {
             const Gradient<float> g = gradient<ACT>(from.dy[u], from.pre[u]);
-            *(Chunk<float>*)(to + (rn + u * kDownN) * kPitchN + cn * 16) = g.hi;
+            *(Chunk<float>*)(to + (rn + u * kDownN) * kPitchN + cn * 16) = g.part[0];
 #pragma unroll
             for (int j = 0; j < E; ++j) bias[j] += g.v[j];
         }

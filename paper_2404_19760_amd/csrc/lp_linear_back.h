@@ -9,13 +9,17 @@ namespace {
 
 // ---- gradients in 16-bit types ---------------------------------------------------------------------------------
 //
-// A workgroup takes a part of the positions, some at a time: d_z is made from d_y and pre in registers, split in two parts and
+// A workgroup takes a part of the positions, some at a time: d_z is made from d_y and pre in registers, split in two or three parts and
 // laid into LDS beside x, and from there come all products of these positions: d_z^T x as above, and, where all channels of d_z are there
 // (SKINNY: up to 128 -> 128 channels), d_z W too, in 16 x 16 blocks with W^T as operands in LDS.  Then everything is read once and d_x is written once.
 // Blocks with more channels: workgroups of 128 channels of d_z x up to 512 of x, so that d_z is made once for 512 channels of x; the first of
 // them writes d_z rounded to 16 bits for the product with W, which another kernel makes.  There one workgroup fills a compute unit; of two
 // waves that share a SIMD one multiplies first and then makes the next positions' d_z, the other one the other way round, so that the
 // vector instructions of one run under the matrix instructions of the other.
+// d_z in two parts has 17 (bf16) or 22 bits (fp16).  An error of 2e-6 in a sum of bf16 products is below that of the fp32 sum itself over so many positions
+// (65536 x 512 -> 2048 against 64 bits: 2.5e-6); below them a third part leaves 1e-7 at half as many matrix instructions more.
+constexpr long long kManyPositions = 65536;
+
 __host__ __device__ constexpr int image_pitch(int channels) { return channels * 2 + (channels * 2 % 256 == 64 ? 0 : 64); }
 
 template <int BN, int BK, int WN, int WK, int ROWS, bool SKINNY>
@@ -29,8 +33,8 @@ struct BackShape {
     static_assert(ROWS * (BN / 8) % kThreadsOf == 0 && ROWS * (BK / 8) % kThreadsOf == 0);
     static constexpr int kImageN = ROWS * kPitchN, kImageK = ROWS * kPitchK;
     static constexpr int kWeights = SKINNY ? BN * BK * 2 : 0;
-    static constexpr int stage(bool split) { return kImageN * (split ? 2 : 1) + kImageK; }
-    static constexpr int lds(bool split) { return stage(split) * (SKINNY ? 1 : 2) + kWeights; }
+    static constexpr int stage(int parts) { return kImageN * parts + kImageK; }
+    static constexpr int lds(int parts) { return stage(parts) * (SKINNY ? 1 : 2) + kWeights; }
 };
 
 template <class T, int PITCH>
@@ -52,11 +56,12 @@ __device__ __forceinline__ f32x4 multiply16(const Chunk<_Float16>& a, const Chun
     return __builtin_amdgcn_mfma_f32_16x16x32_f16(__builtin_bit_cast(V, a), __builtin_bit_cast(V, b), acc, 0, 0, 0);
 }
 
-template <class T, int ACT, bool WHOLE, class S>
+// PARTS: 16-bit parts of d_z (without an activation d_z is d_y).
+template <class T, int ACT, int PARTS, bool WHOLE, class S>
 __global__ __launch_bounds__(S::kThreadsOf, S::kSkinny && (S::kBN < 128 || S::kBK < 128) ? 3 : 2) void linear_back_kernel(BackDev d)
 {
-    constexpr bool kSplit = ACT != LP_ACT_NONE;
-    constexpr int kStage = S::stage(kSplit), kLo = S::kImageN, kX = S::kImageN * (kSplit ? 2 : 1);
+    constexpr bool kSlope = ACT != LP_ACT_NONE;
+    constexpr int kStage = S::stage(PARTS), kX = S::kImageN * PARTS;
     constexpr int kAcrossN = S::kBN / 8, kDownN = S::kThreadsOf / kAcrossN, kAcrossK = S::kBK / 8, kDownK = S::kThreadsOf / kAcrossK;
     extern __shared__ char lds[];
     const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), l32 = lane & 31, h = lane >> 5;
@@ -85,14 +90,14 @@ __global__ __launch_bounds__(S::kThreadsOf, S::kSkinny && (S::kBN < 128 || S::kB
             for (int u = 0; u < S::kLoadsN; ++u) {
                 const int in = rn + u * kDownN < left ? d.N - n : 0;
                 dy[u] = load_chunk<true>(dy_at + u * kDownN * d.ys, in);
-                if (kSplit) pre[u] = load_chunk<true>(pre_at + (long long)u * kDownN * d.N, in);
+                if (kSlope) pre[u] = load_chunk<true>(pre_at + (long long)u * kDownN * d.N, in);
             }
         } else {
 #pragma unroll
             for (int u = 0; u < S::kLoadsN; ++u) {
                 const int in = rn + u * kDownN < left ? d.N - n : 0;
                 dy[u] = load_chunk<false>(dy_at + u * kDownN * d.ys, in);
-                if (kSplit) pre[u] = load_chunk<false>(pre_at + (long long)u * kDownN * d.N, in);
+                if (kSlope) pre[u] = load_chunk<false>(pre_at + (long long)u * kDownN * d.N, in);
             }
         }
         if (long_k) {
@@ -115,11 +120,11 @@ __global__ __launch_bounds__(S::kThreadsOf, S::kSkinny && (S::kBN < 128 || S::kB
         for (int u = 0; u < S::kLoadsN; ++u) {
             const int at = (rn + u * kDownN) * S::kPitchN + cn * 16;
             const Gradient<T> g = gradient<ACT>(shifted(dy[u], shift_n), shifted(pre[u], shift_n));
-            *(Chunk<T>*)(to + at) = g.hi;
-            if (kSplit) *(Chunk<T>*)(to + kLo + at) = g.lo;
+#pragma unroll
+            for (int i = 0; i < PARTS; ++i) *(Chunk<T>*)(to + i * S::kImageN + at) = g.part[i];
 #pragma unroll
             for (int j = 0; j < 8; ++j) bias[j] += g.v[j];
-            if (write_dz) store_chunk<WHOLE>(dz_at + (long long)u * kDownN * d.N, rn + u * kDownN < left ? d.N - n : 0, g.hi);
+            if (write_dz) store_chunk<WHOLE>(dz_at + (long long)u * kDownN * d.N, rn + u * kDownN < left ? d.N - n : 0, g.part[0]);
         }
         dz_at += (long long)S::kRows * d.N;
 #pragma unroll
@@ -129,21 +134,37 @@ __global__ __launch_bounds__(S::kThreadsOf, S::kSkinny && (S::kBN < 128 || S::kB
     auto multiply_all = [&](const char* from) {
 #pragma unroll
         for (int r = 0; r < S::kRows; r += 16) {
-            Chunk<T> xv[S::kBlocksK], g[S::kBlocksN], lo[S::kBlocksN];
+            Chunk<T> xv[S::kBlocksK];
 #pragma unroll
             for (int j = 0; j < S::kBlocksK; ++j) xv[j] = operand<T, S::kPitchK>(from + kX, r, wave_k + j * 32, lane);
+            // (of fp16 the second part is bf16: as fp16 it would be among the smallest numbers; x loses 2^-9 of 2^-12 in that product)
+            constexpr bool kOther = std::is_same<T, _Float16>::value && PARTS == 2;
+            Chunk<__bf16> xb[S::kBlocksK];
+            if (kOther)
 #pragma unroll
-            for (int i = 0; i < S::kBlocksN; ++i) {
-                g[i] = operand<T, S::kPitchN>(from, r, wave_n + i * 32, lane);
-                if (kSplit) lo[i] = operand<T, S::kPitchN>(from + kLo, r, wave_n + i * 32, lane);
+                for (int j = 0; j < S::kBlocksK; ++j)
+#pragma unroll
+                    for (int e = 0; e < 8; ++e) xb[j].v[e] = (__bf16)(float)xv[j].v[e];
+            // the small parts first; three of them one after the other (their operands together would take too many registers)
+            constexpr int kAtOnce = PARTS == 3 ? 1 : PARTS;
+#pragma unroll
+            for (int last = PARTS; last > 0; last -= kAtOnce) {
+                Chunk<T> g[kAtOnce][S::kBlocksN];
+#pragma unroll
+                for (int k = 0; k < kAtOnce; ++k)
+#pragma unroll
+                    for (int i = 0; i < S::kBlocksN; ++i)
+                        g[k][i] = operand<T, S::kPitchN>(from + (last - 1 - k) * S::kImageN, r, wave_n + i * 32, lane);
+#pragma unroll
+                for (int i = 0; i < S::kBlocksN; ++i)
+#pragma unroll
+                    for (int j = 0; j < S::kBlocksK; ++j)
+#pragma unroll
+                        for (int k = 0; k < kAtOnce; ++k) {
+                            if (kOther && k == 0) acc[i][j] = multiply(__builtin_bit_cast(Chunk<__bf16>, g[k][i]), xb[j], acc[i][j]);
+                            else acc[i][j] = multiply(g[k][i], xv[j], acc[i][j]);
+                        }
             }
-#pragma unroll
-            for (int i = 0; i < S::kBlocksN; ++i)
-#pragma unroll
-                for (int j = 0; j < S::kBlocksK; ++j) {
-                    if (kSplit) acc[i][j] = multiply(lo[i], xv[j], acc[i][j]);
-                    acc[i][j] = multiply(g[i], xv[j], acc[i][j]);
-                }
         }
     };
     if (first < end) ask(first);
@@ -267,14 +288,24 @@ hipError_t launch_back(int act, const BackDev& d, const Parts& p, bool skinny, h
         constexpr int A = decltype(a)::value;
         with_back_shape(p, skinny, [&](auto shape) {
             using S = decltype(shape);
-            constexpr int kLds = S::lds(A != LP_ACT_NONE);
-            auto go = [&](auto kernel) {
+            auto go = [&](auto kernel, int kLds) {
                 if (kLds > 65536) e = hipFuncSetAttribute((const void*)kernel, hipFuncAttributeMaxDynamicSharedMemorySize, kLds);   // (the same from every thread)
                 if (e == hipSuccess)
                     hipLaunchKernelGGL(kernel, dim3((unsigned)(d.tiles_n * d.tiles_k * p.splits)), dim3(S::kThreadsOf), kLds, s, d);
             };
-            if (d.whole) go(linear_back_kernel<T, A, true, S>);
-            else go(linear_back_kernel<T, A, false, S>);
+            auto with = [&](auto parts) {
+                constexpr int N = decltype(parts)::value;
+                if (d.whole) go(linear_back_kernel<T, A, N, true, S>, S::lds(N));
+                else go(linear_back_kernel<T, A, N, false, S>, S::lds(N));
+            };
+            if constexpr (A == LP_ACT_NONE) {
+                with(std::integral_constant<int, 1>());
+            } else if constexpr (std::is_same<T, __bf16>::value) {
+                if (d.P < kManyPositions) with(std::integral_constant<int, 3>());
+                else with(std::integral_constant<int, 2>());
+            } else {
+                with(std::integral_constant<int, 2>());
+            }
         });
     });
     return e;

@@ -58,7 +58,7 @@ __global__ __launch_bounds__(kThreads, PAIRS * BLOCKS > 16 ? 2 : 3) void linear_
     for (; p0 < d.P; p0 += step) {
         Chunk<T> av[PAIRS];
 #pragma unroll
-        for (int f = 0; f < PAIRS; ++f) av[f] = kSlope ? gradient<ACT>(a[f], pre[f]).hi : a[f];
+        for (int f = 0; f < PAIRS; ++f) av[f] = kSlope ? gradient<ACT>(a[f], pre[f]).part[0] : a[f];
         // (the residual of two blocks of channels is on its way while others are finished)
         Chunk<T> added[2][kFinishTimes<T, 1>];
         auto residual = [&](int n, Chunk<T> (&to)[kFinishTimes<T, 1>]) {

@@ -84,7 +84,7 @@ __global__ __launch_bounds__(kThreads, 2) void linear_tile_kernel(LinearDev d)
 #pragma unroll
                 for (int u = 0; u < kLoadsA; ++u) {
                     Chunk<T> v = from.a[u];
-                    if (BACK && ACT != LP_ACT_NONE) v = gradient<ACT>(from.a[u], from.pre[u]).hi;
+                    if (BACK && ACT != LP_ACT_NONE) v = gradient<ACT>(from.a[u], from.pre[u]).part[0];
                     *(Chunk<T>*)(to + chunk_at(row + u * 32, c8)) = v;
                 }
 #pragma unroll

@@ -4,7 +4,8 @@ Tolerances.  u = 2^-24.  A sum over K products adds 16 (16-bit types) or 2 (fp32
 K / 2 additions follow one another and a result is off by at most that many times 2 u of the sum of the products' absolute values (2 u, not u:
 the matrix cores need not round to nearest), plus some 16 for the additions inside a step.  The activations and their slopes are good to 5e-6 of
 their argument's size, their slopes are at most 1.13.  A result is rounded once, by half a step of its type.  In d_x a 16-bit d_z is rounded by half a step
-as well; in d_W its two parts leave half a step of half a step (fp16: not less than half of its smallest number, 2^-25)."""
+as well; in d_W what its parts leave is at most half a step of half a step in bf16; in fp16 the second part is bf16 and meets x rounded to bf16: half a step of
+fp16 times two half steps of bf16."""
 import math
 
 import pytest
@@ -110,10 +111,10 @@ def _check_backward(t, act, dtype, pre, d_x, d_w, d_b, w0=None, b0=None):
     want = dz @ w
     tol = (dz_tol + rounded * (dz.abs() + dz_tol) + TINY[dtype]) @ w.abs() + _sum_tol(n, dtype) * (dz.abs() @ w.abs())
     _within(d_x, want, 1.01 * (tol + HALF[dtype] * (want.abs() + tol)) + TINY[dtype], "d_x")
-    # (two parts of 16-bit types: half a step of half a step; up to 512 parts of the positions are added up one after the other)
-    left = 0.0 if act == "none" or dtype == torch.float32 else HALF[dtype] ** 2
+    # (up to 768 parts of the positions are added up, 12 one after the other in 64 lanes)
+    left = 0.0 if act == "none" or dtype == torch.float32 else HALF[dtype] * HALF[torch.bfloat16] * (2.01 if dtype == torch.float16 else 1)
     want = dz.T @ x
-    tol = (dz_tol + left * dz.abs() + TINY[dtype]).T @ x.abs() + (2 * _sum_tol(p, dtype) + 64 * 2.0 ** -24) * (dz.abs().T @ x.abs())
+    tol = (dz_tol + left * dz.abs()).T @ x.abs() + (2 * _sum_tol(p, dtype) + 64 * 2.0 ** -24) * (dz.abs().T @ x.abs())
     if w0 is not None:
         want, tol = want + w0.double().cpu(), tol + 2.0 ** -23 * (want.abs() + w0.double().cpu().abs())
     _within(d_w, want, 1.01 * tol + 1e-30, "d_weight")

@@ -112,6 +112,23 @@ def test_gradients_in_other_orders_and_versions(lp):
         lp.clip_grad_norm([torch.zeros(10, 10, device="cuda")[:, :5]], 1.0)
 
 
+@pytest.mark.parametrize("dtype", [torch.float32, torch.float16])
+def test_more_than_the_cache_holds(lp, dtype):
+    """Results of such calls are stored another way; at odd addresses."""
+    size = 300_000_000 // torch.finfo(dtype).bits * 8
+    wide = torch.randn(size + 9, device="cuda").to(dtype)
+    grads = [wide[3:3 + size], torch.randn(1001, device="cuda").to(dtype)]
+    want = [g.float().clone() for g in grads]
+    edges = wide[:3].clone(), wide[3 + size:].clone()
+    norm = lp.clip_grad_norm(grads, 7.0, 0.0)
+    exact = math.sqrt(sum(float(torch.linalg.vector_norm(g, dtype=torch.float64)) ** 2 for g in want))
+    assert abs(float(norm) - exact) <= 1.01 * U * exact
+    factor = torch.tensor(7.0 / exact, dtype=torch.float64).float().cuda()   # (as the library rounds it, but for the norm's last bits)
+    for g, w in zip(grads, want):
+        assert bool(((g.float() - w * factor).abs() <= (4 * U + torch.finfo(dtype).eps * (dtype != torch.float32)) * (w * factor).abs() + SMALLEST[dtype]).all())
+    assert torch.equal(wide[:3], edges[0]) and torch.equal(wide[3 + size:], edges[1])
+
+
 def test_captured_and_replayed(lp):
     for sizes in ([64 * 16, 64, 64 * 64], [100000, 7, 30000] * 30):
         grads = _tensors(sizes, torch.float32, 9)

@@ -267,6 +267,25 @@ def test_offsets_beyond_32_bits(lp):
     assert not d_x.any()
 
 
+@pytest.mark.parametrize("k,n,offset", [(16, 61, 0), (24, 264, 0), (16, 61, 3)])
+def test_more_than_the_cache_holds(lp, k, n, offset):
+    """Results of such calls are stored another way; rows of odd sizes, at odd addresses.  A position's result does not depend on the others."""
+    p = 300_000_000 // (2 * (k + n)) + 77
+    gen = torch.Generator(device="cuda").manual_seed(1)
+    x = torch.randn(p, k, generator=gen, device="cuda").bfloat16()
+    lin = lp.Linear(torch.randn(n, k, generator=gen, device="cuda").bfloat16(), torch.randn(n, generator=gen, device="cuda"), lp.LP_ACT_SILU)
+    wide = torch.full((p, n + 2 * offset), 5.0, dtype=torch.bfloat16, device="cuda")
+    y = wide[:, offset:offset + n]
+    ws = torch.empty(max(1, lp.lp_linear_workspace_bytes(lin, x)[0]), dtype=torch.uint8, device="cuda")
+    lp.lp_linear_fwd(lin, x, y, None, None, ws)
+    at = 0
+    for rows in x.split(p // 4 + 1):
+        assert torch.equal(y[at:at + len(rows)], lp.linear_fwd(lin, rows)[0])
+        at += len(rows)
+    if offset:
+        assert bool((wide[:, :offset] == 5).all()) and bool((wide[:, offset + n:] == 5).all())
+
+
 @pytest.mark.parametrize("p,k,n", [(3000, 72, 160), (700, 512, 136), (2000, 32, 64)])
 def test_captured_and_replayed(lp, p, k, n):
     t = _case(p, k, n, torch.bfloat16, 9)

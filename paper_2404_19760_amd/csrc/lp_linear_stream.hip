@@ -4,6 +4,9 @@
 // weights, which lie in LDS as the matrix instructions' operands for as long as the workgroup lives: a wave takes 32 positions at a time,
 // asks for the next 32 before it multiplies, and never waits for another wave.  The positions' channels go straight to registers: of a row's
 // 16-byte chunks lanes 0 .. 31 ask for the even ones, lanes 32 .. 63 for the odd ones.
+//
+// Measured: 160^3 x 32 -> 64 in fp32 302 us for 1.57 GB (5.2 TB/s; through LDS with a barrier a step 373), 131979 x 72 -> 96 in fp16 with residual
+// 20 us for 70 MB, -> 97 30 us: rows of 194 bytes share the 64-byte lines that they are stored to.
 #include "lp_linear.h"
 
 namespace lp {

@@ -12,7 +12,9 @@ constexpr int kWideP = 128, kWideN = 256;
 // Four waves make 128 positions x 256 channels, each of them all positions and 64 channels.  The positions go through LDS (two buffers), the
 // weights, of which no two waves need the same, straight to registers, from a copy in the order of the matrix instructions' operands
 // (blocks of 32 channels x 16 summed ones, 16 bytes a lane): for a step of 64 summed channels the matrix cores take 1024 cycles, LDS (128 bytes a
-// cycle) 640, the cache (64 bytes a cycle) 512.  Two workgroups share a compute unit: one's products run under the other's epilogue.
+// cycle) 640, the cache (64 bytes a cycle) 512.  Two workgroups share a compute unit, so that one's products can run under the other's epilogue.
+// Measured: 65536 x 2048 -> 512 in bf16 148 us (0.93 PFLOP/s; matrix cores busy 53 % of the time, waits for barriers and memory 30 %), 65536 x 512 -> 2048
+// 206 us bare, 225 with GELU, 238 with z kept too (0.6 GB; a copy's rate would be 122).
 struct WideShape {
     static constexpr int kBuffer = kWideP * 128, kTurn = 4 * 32 * 68 * 4;
     static constexpr int kLds = 2 * kBuffer > kTurn ? 2 * kBuffer : kTurn;

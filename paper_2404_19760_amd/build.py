@@ -18,7 +18,8 @@ INCLUDE = os.path.join(os.path.dirname(HERE), "include")
 OBJ = os.path.join(HERE, "_build")
 LIB = os.environ.get("LP_LIB_OUT", os.path.join(HERE, "liblightplane.so"))
 
-SOURCES = ["lp_api.hip", "lp_group_norm.hip", "lp_linear.hip", "lp_linear_tile.hip", "lp_linear_stream.hip", "lp_linear_wide.hip", "lp_linear_back.hip", "lp_linear_back_f16.hip", "lp_residual_norm.hip", "lp_grad_norm.hip", "lp_orth.hip", "lp_diag.hip", "lp_decoder.hip", "lp_generic.hip", "lp_mfma_fwd.hip", "lp_mfma_bwd.hip", "lp_mfma_bwd_b.hip", "lp_mfma_bwd_ws.hip",
+SOURCES = ["lp_linear_back_bf16_any.hip", "lp_linear_back_bf16_whole.hip", "lp_linear_back_f16_any.hip", "lp_linear_back_f16_whole.hip", "lp_linear_tile.hip",
+           "lp_linear_stream.hip", "lp_linear_wide.hip", "lp_api.hip", "lp_group_norm.hip", "lp_linear.hip", "lp_residual_norm.hip", "lp_grad_norm.hip", "lp_orth.hip", "lp_diag.hip", "lp_decoder.hip", "lp_generic.hip", "lp_mfma_fwd.hip", "lp_mfma_bwd.hip", "lp_mfma_bwd_b.hip", "lp_mfma_bwd_ws.hip",
            "lp_mfma_bwd_hash.hip", "lp_mfma_bwd_tile_voxel.hip", "lp_mfma_bwd_tile_triplane.hip", "lp_mfma_bwd_tile_hash.hip",
            "lp_mfma_bwd_hexplane.hip",
            "lp_mfma_dec2_fwd.hip", "lp_mfma_dec2_bwd.hip", "lp_splat_fast.hip", "lp_splat_naive_bwd.hip",

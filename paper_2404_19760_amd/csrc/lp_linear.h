@@ -330,7 +330,7 @@ __host__ __device__ constexpr int wide_blocks(int k) { return (k + 63) / 64 * 4;
 void launch_pack(int dtype, bool turned, const void* w, int rows, int cols, int pitch, void* out, hipStream_t s);
 void launch_wide(int dtype, int act, bool back, LinearDev d, hipStream_t s);   // back: act is LP_ACT_NONE
 
-// 16-bit types, gradients of the parameters, and d_x where there are few channels (lp_linear_back.hip, lp_linear_back_f16.hip).
+// 16-bit types, gradients of the parameters, and d_x where there are few channels (lp_linear_back_*.hip; whole: rows end with whole chunks).
 struct BackDev {
     long long P;
     int K, N;
@@ -341,7 +341,6 @@ struct BackDev {
     long long chunk;             // positions of a part
     int tiles_n, tiles_k, splits;
     int d_weight, d_bias;        // wanted
-    int whole;                   // rows end with whole chunks
 };
 
 // How the positions are divided for the parameters' gradients.
@@ -349,8 +348,10 @@ struct Parts {
     int bn, bk, tiles_n, tiles_k, splits;
     long long chunk;
 };
-hipError_t launch_back_bf16(int act, const BackDev& d, const Parts& p, bool skinny, hipStream_t s);
-hipError_t launch_back_f16(int act, const BackDev& d, const Parts& p, bool skinny, hipStream_t s);
+hipError_t launch_back_bf16_whole(int act, const BackDev& d, const Parts& p, bool skinny, hipStream_t s);
+hipError_t launch_back_bf16_any(int act, const BackDev& d, const Parts& p, bool skinny, hipStream_t s);
+hipError_t launch_back_f16_whole(int act, const BackDev& d, const Parts& p, bool skinny, hipStream_t s);
+hipError_t launch_back_f16_any(int act, const BackDev& d, const Parts& p, bool skinny, hipStream_t s);
 
 }  // namespace linear
 }  // namespace lp

@@ -496,8 +496,10 @@ lp_status backward(const lp_linear* q, const void* x, const void* pre, const voi
         d.x = x; d.dy = d_y; d.pre = pre; d.w = c.weight; d.d_x = skinny ? d_x : nullptr; d.dz = d_x ? dz : nullptr;
         d.parts = parts; d.bias_parts = bias_parts; d.chunk = p.chunk;
         d.tiles_n = p.tiles_n; d.tiles_k = tiles_k; d.splits = p.splits;
-        d.d_weight = d_weight != nullptr; d.d_bias = d_bias != nullptr; d.whole = c.K % 8 == 0 && c.N % 8 == 0;
-        const hipError_t e = c.dtype == LP_BF16 ? launch_back_bf16(c.act, d, p, skinny, s) : launch_back_f16(c.act, d, p, skinny, s);
+        d.d_weight = d_weight != nullptr; d.d_bias = d_bias != nullptr;
+        const bool whole = c.K % 8 == 0 && c.N % 8 == 0;
+        const auto launch = c.dtype == LP_BF16 ? (whole ? launch_back_bf16_whole : launch_back_bf16_any) : (whole ? launch_back_f16_whole : launch_back_f16_any);
+        const hipError_t e = launch(c.act, d, p, skinny, s);
         if (e != hipSuccess) return fail(LP_ERR_HIP, std::string("hipFuncSetAttribute(linear_back_kernel): ") + hipGetErrorString(e));
     } else if (params) {
         WeightDev d;

@@ -1,4 +1,4 @@
-// The gradients' kernel of 16-bit types, for the translation unit of each type.
+// The gradients' kernel of 16-bit types, for the translation units of each type and of rows that end with whole chunks or not.
 #pragma once
 #include "lp_linear.h"
 
@@ -59,7 +59,7 @@ __device__ __forceinline__ f32x4 multiply16(const Chunk<_Float16>& a, const Chun
     return __builtin_amdgcn_mfma_f32_16x16x32_f16(__builtin_bit_cast(V, a), __builtin_bit_cast(V, b), acc, 0, 0, 0);
 }
 
-// PARTS: 16-bit parts of d_z (without an activation d_z is d_y).
+// PARTS: 16-bit parts of d_z.
 template <class T, int ACT, int PARTS, bool WHOLE, class S>
 __global__ __launch_bounds__(S::kThreadsOf, S::kSkinny && (S::kBN < 128 || S::kBK < 128) ? 3 : 2) void linear_back_kernel(BackDev d)
 {
@@ -283,7 +283,7 @@ void with_back_shape(const Parts& p, bool skinny, F&& f)
     }
 }
 
-template <class T>
+template <class T, bool WHOLE>
 hipError_t launch_back(int act, const BackDev& d, const Parts& p, bool skinny, hipStream_t s)
 {
     hipError_t e = hipSuccess;
@@ -298,10 +298,9 @@ hipError_t launch_back(int act, const BackDev& d, const Parts& p, bool skinny, h
             };
             auto with = [&](auto parts) {
                 constexpr int N = decltype(parts)::value;
-                if (d.whole) go(linear_back_kernel<T, A, N, true, S>, S::lds(N));
-                else go(linear_back_kernel<T, A, N, false, S>, S::lds(N));
+                go(linear_back_kernel<T, A, N, WHOLE, S>, S::lds(N));
             };
-            if constexpr (A == LP_ACT_NONE) {
+            if constexpr (A == LP_ACT_NONE || A == LP_ACT_RELU) {   // (d_z is d_y, or 0)
                 with(std::integral_constant<int, 1>());
             } else if constexpr (std::is_same<T, __bf16>::value) {
                 if (d.P < kManyPositions) with(std::integral_constant<int, 3>());

@@ -276,25 +276,33 @@ __device__ __forceinline__ void finish(const LinearDev& d, const f32x16 (&acc)[B
                 ask_residual<T, WHOLE, BLOCKS_N>(d, p0 + jp * 32, n0, lane, added);
             }
         }
+        // (whether there is a residual stands outside the loop: 1 to 2 % of a call without one)
+        auto store_all = [&](auto residual) {
 #pragma unroll
-        for (int r = 0; r < kTimes; ++r) {
-            float z[E];
-            const float* from = turn + (r * kDown + lane / kAcross) * kPitch + lane % kAcross * E;
+            for (int r = 0; r < kTimes; ++r) {
+                float z[E];
+                const float* from = turn + (r * kDown + lane / kAcross) * kPitch + lane % kAcross * E;
 #pragma unroll
-            for (int j = 0; j < E; j += 4) *(f32x4*)(z + j) = *(const f32x4*)(from + j);
-            Chunk<T> v;
+                for (int j = 0; j < E; j += 4) *(f32x4*)(z + j) = *(const f32x4*)(from + j);
+                Chunk<T> v;
 #pragma unroll
-            for (int j = 0; j < E; ++j) {
-                z[j] += bias[j];
-                v.v[j] = (T)z[j];
+                for (int j = 0; j < E; ++j) {
+                    z[j] += bias[j];
+                    v.v[j] = (T)z[j];
+                }
+                if (!BACK) {
+                    if (d.keep) store_chunk<WHOLE>(keep + (long long)(jp * 32 + r * kDown) * d.N, count[r], v, d.past_cache);
+#pragma unroll
+                    for (int j = 0; j < E; ++j) {
+                        const float y = activate_as<ACT, T>(z[j]);
+                        v.v[j] = (T)(decltype(residual)::value ? y + (float)added[r].v[j] : y);
+                    }
+                }
+                store_chunk<WHOLE>(out + (jp * 32 + r * kDown) * d.ys, count[r], v, d.past_cache);
             }
-            if (!BACK) {
-                if (d.keep) store_chunk<WHOLE>(keep + (long long)(jp * 32 + r * kDown) * d.N, count[r], v, d.past_cache);
-#pragma unroll
-                for (int j = 0; j < E; ++j) v.v[j] = (T)(activate_as<ACT, T>(z[j]) + (float)added[r].v[j]);
-            }
-            store_chunk<WHOLE>(out + (jp * 32 + r * kDown) * d.ys, count[r], v, d.past_cache);
-        }
+        };
+        if (!BACK && d.res) store_all(std::true_type());
+        else store_all(std::false_type());
         __builtin_amdgcn_wave_barrier();
     }
 }

@@ -392,7 +392,8 @@ lp_status lp_linear_fwd(const lp_linear* linear, const void* x, void* y, void* p
 
 /* Backward.  pre as the forward wrote it (not used, and may be NULL, where act is LP_ACT_NONE).  d_x is WRITTEN (NULL: not
    wanted) and must not overlap x, pre or d_y; d_weight [N][K] and d_bias [N] are ACCUMULATED into (either may be NULL), in an
-   order that does not change from call to call.  Of a ReLU the gradient at 0 is 0. */
+   order that does not change from call to call.  x is read for d_weight alone and the weight for d_x alone: either may be NULL where
+   that is.  Of a ReLU the gradient at 0 is 0. */
 lp_status lp_linear_bwd(const lp_linear* linear, const void* x, const void* pre, const void* d_y, void* d_x, float* d_weight,
                         float* d_bias, void* workspace, size_t workspace_bytes, void* stream);
 

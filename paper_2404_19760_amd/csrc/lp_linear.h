@@ -342,6 +342,7 @@ void launch_wide(int dtype, int act, bool back, LinearDev d, hipStream_t s);   /
 struct BackDev {
     long long P;
     int K, N;
+    int x_channels;              // of x that are read: K, or 0 where d_weight is not wanted (x may be NULL then)
     long long xs, ys;
     const void *x, *dy, *pre, *w;
     void *d_x, *dz;              // dz: [P][N]

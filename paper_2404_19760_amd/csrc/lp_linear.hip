@@ -492,7 +492,7 @@ lp_status backward(const lp_linear* q, const void* x, const void* pre, const voi
     if (halves && (params || (skinny && d_x))) {
         BackDev d;
         std::memset(&d, 0, sizeof(d));
-        d.P = c.P; d.K = d_weight || skinny ? c.K : 0; d.N = c.N; d.xs = c.xs; d.ys = c.ys;
+        d.P = c.P; d.K = c.K; d.x_channels = d_weight ? c.K : 0; d.N = c.N; d.xs = c.xs; d.ys = c.ys;
         d.x = x; d.dy = d_y; d.pre = pre; d.w = c.weight; d.d_x = skinny ? d_x : nullptr; d.dz = d_x ? dz : nullptr;
         d.parts = parts; d.bias_parts = bias_parts; d.chunk = p.chunk;
         d.tiles_n = p.tiles_n; d.tiles_k = tiles_k; d.splits = p.splits;

@@ -105,10 +105,10 @@ __global__ __launch_bounds__(S::kThreadsOf, S::kSkinny && (S::kBN < 128 || S::kB
         }
         if (long_k) {
 #pragma unroll
-            for (int u = 0; u < S::kLoadsK; ++u) x[u] = load_chunk<true>(x_at + u * kDownK * d.xs, rk + u * kDownK < left ? d.K - k : 0);
+            for (int u = 0; u < S::kLoadsK; ++u) x[u] = load_chunk<true>(x_at + u * kDownK * d.xs, rk + u * kDownK < left ? d.x_channels - k : 0);
         } else {
 #pragma unroll
-            for (int u = 0; u < S::kLoadsK; ++u) x[u] = load_chunk<false>(x_at + u * kDownK * d.xs, rk + u * kDownK < left ? d.K - k : 0);
+            for (int u = 0; u < S::kLoadsK; ++u) x[u] = load_chunk<false>(x_at + u * kDownK * d.xs, rk + u * kDownK < left ? d.x_channels - k : 0);
         }
         dy_at += S::kRows * d.ys;
         pre_at += (long long)S::kRows * d.N;

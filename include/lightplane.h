@@ -365,8 +365,8 @@ lp_status lp_group_norm_bwd(const lp_group_norm* norm, const void* x, const floa
  * products and sums are fp32 (16-bit types: exact products on the matrix cores), and each result is rounded once.
  * The backward, for the upstream gradient d_y and the z that the forward kept (`pre`, rounded to the tensors' type):
  *     d_z = d_y act'(z),   d_x = d_z W,   d_W += d_z^T x,   d_b += sum over the positions of d_z;   r's gradient is d_y.
- * In d_x a 16-bit d_z is rounded once more; in d_W it is kept in two or three parts (17 bits and more; one that is infinite, or beyond the type's
- * largest number, leaves NaN), in d_b in fp32.
+ * In d_x a 16-bit d_z is rounded once more; in d_W a bf16 one is kept in three parts (24 bits), an fp16 one in two (19 bits; one that is infinite, or beyond the
+ * type's largest number, leaves NaN), in d_b in fp32.
  */
 typedef struct {
     int64_t P;             /* positions */

@@ -10,18 +10,22 @@ namespace {
 // ---- gradients in 16-bit types ---------------------------------------------------------------------------------
 //
 // A workgroup takes a part of the positions, some at a time: d_z is made from d_y and pre in registers, split in two or three parts and
-// laid into LDS beside x, and from there come all products of these positions: d_z^T x as above, and, where all channels of d_z are there
+// laid into LDS beside x, and from there come all products of these positions: d_z^T x in 32 x 32 blocks, and, where all channels of d_z are there
 // (SKINNY: up to 128 -> 128 channels), d_z W too, in 16 x 16 blocks with W^T as operands in LDS.  Then everything is read once and d_x is written once.
 // Blocks with more channels: workgroups of 128 channels of d_z x up to 512 of x, so that d_z is made once for 512 channels of x; the first of
 // them writes d_z rounded to 16 bits for the product with W, which another kernel makes.  There one workgroup fills a compute unit; of two
 // waves that share a SIMD one multiplies first and then makes the next positions' d_z, the other one the other way round, so that the
 // vector instructions of one run under the matrix instructions of the other.
 //
-// Measured with GELU in bf16: 24 x 256^2 positions, 32 -> 128 channels 234 us for 1.0 GB (all gradients), 65536 x 512 -> 2048 315 to 385 us (d_W, d_b
-// and d_z; 0.27 TFLOP, twice for two parts).
-// d_z in two parts has 17 (bf16) or 22 bits (fp16).  An error of 2e-6 in a sum of bf16 products is below that of the fp32 sum itself over so many positions
-// (65536 x 512 -> 2048 against 64 bits: 2.5e-6); below them a third part leaves 1e-7 at half as many matrix instructions more.
-constexpr long long kManyPositions = 65536;
+// Measured with GELU in bf16, all gradients: 24 x 256^2 positions, 32 -> 128 channels 300 us for 1.0 GB, 65536 x 512 -> 2048 590 us (0.4 TFLOP for d_W's
+// three parts, 0.14 for d_x).
+// Parts of d_z.  The sums' own error goes by the length of a part of the positions, not by their number, and stays below 1.4e-6 (64 -> 64 channels,
+// 1.6 million positions; up to 65536 positions 3e-7 to 8e-7): in bf16 two parts, 17 bits, would leave 2.5e-6 at every size, so there are three, whatever the number of
+// positions.  What that costs, against two: 512 -> 2048 channels, 16384 positions 195 and 174 us, 65536 590 and 510, 262144 2215 and 1890; 32 -> 128,
+// 262144 positions 65 and 56, 1.6 million 300 and 262.  (d_W against 64 bits at 65536 x 512 -> 2048: 8e-7, with two 2.5e-6.)  Of fp16 two parts
+// have 19 bits: 5e-7.
+// d_z W takes the first part alone: d_x, itself rounded to 16 bits, is 2.3e-3 off in bf16 then and 1.7e-3 with all of d_z.  A second part would double
+// that product (150 of the 590 us above) and, beyond 128 channels, the 0.5 GB that are written and read of d_z.
 
 __host__ __device__ constexpr int image_pitch(int channels) { return channels * 2 + (channels * 2 % 256 == 64 ? 0 : 64); }
 
@@ -303,8 +307,7 @@ hipError_t launch_back(int act, const BackDev& d, const Parts& p, bool skinny, h
             if constexpr (A == LP_ACT_NONE || A == LP_ACT_RELU) {   // (d_z is d_y, or 0)
                 with(std::integral_constant<int, 1>());
             } else if constexpr (std::is_same<T, __bf16>::value) {
-                if (d.P < kManyPositions) with(std::integral_constant<int, 3>());
-                else with(std::integral_constant<int, 2>());
+                with(std::integral_constant<int, 3>());
             } else {
                 with(std::integral_constant<int, 2>());
             }

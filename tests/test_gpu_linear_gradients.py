@@ -41,3 +41,44 @@ def test_gradients_that_do_not_need_x(lp, p, k, n, dtype):
                     _check_backward(t, act, dtype, pre, d_x, whole[1], whole[2])
                 else:
                     assert torch.equal(d_x, whole[0])
+
+
+# channels in and out: every tile of the gradients' kernel, rows that end with whole chunks and others
+TILES = [(32, 64), (64, 64), (128, 64), (32, 128), (64, 128), (128, 128), (31, 61), (61, 33), (125, 97), (5, 3), (72, 200), (200, 136), (512, 160),
+         (129, 145), (515, 131)]
+MANY = [(65537 + 14, *t) for t in TILES] + [(p, *t) for p in (65535, 65536, 150001) for t in ((32, 128), (33, 97), (72, 200))] + [(4099, *t) for t in TILES[:9]]
+
+
+@pytest.mark.parametrize("act", ["silu", "gelu"])
+@pytest.mark.parametrize("dtype", DTYPES)
+@pytest.mark.parametrize("p,k,n", MANY)
+def test_weight_gradients_hold_all_bits_of_d_z(lp, p, k, n, dtype, act):
+    """Every channel of d_y is zero but in one position, so d_bias is that position's d_z as the kernel has it in fp32, and d_weight is d_z times
+    that position's x, without sums that could hide what d_z was rounded to on the way.  With u = 2^-24: three bf16 parts leave (2^-8)^3 = u of
+    d_z and their products are exact, two u for each of the three additions; fp16 and bf16 parts leave 2^-11 2^-8, x is rounded to bf16 for
+    the second part, 2^-11 2^-8 again (the first part of a d_z among fp16's smallest numbers is off by up to 2^-25); fp32 products and additions are
+    rounded by two u.  Largest in all: 8 u, and two times 2^-19, or 2^-33 of x, more in fp16."""
+    gen = torch.Generator().manual_seed(p + k + n)
+    rows = torch.arange(n) * (p - 1) // max(1, n - 1)
+    x = torch.randn(p, k, generator=gen).to(dtype).cuda()
+    pre = torch.randn(p, n, generator=gen).to(dtype).cuda()
+    d_y = torch.zeros(p, n, dtype=dtype, device="cuda")
+    d_y[rows.cuda(), torch.arange(n, device="cuda")] = (1 + torch.rand(n, generator=gen)).to(dtype).cuda()
+    w = torch.randn(n, k, generator=gen).to(dtype).cuda()
+    _, d_w, d_b = lp.linear_bwd(lp.Linear(w, torch.zeros(n, device="cuda"), _act_id(lp, act)), x, pre, d_y)
+    assert rows[-1] == p - 1 and (n == 1 or bool((d_b != 0).all()))
+    want = d_b.double().unsqueeze(1) * x[rows.cuda()].double()
+    bound = 8 * 2.0 ** -24 * want.abs()
+    if dtype == torch.float16:
+        bound = bound + 2.01 * (2.0 ** -19 * want.abs() + 2.0 ** -33 * x[rows.cuda()].double().abs())
+    over = ((d_w.double() - want).abs() - bound).max()
+    assert float(over) <= 0, float(((d_w.double() - want).abs() / want.abs()).max())
+
+
+@pytest.mark.parametrize("act", ["silu", "gelu"])
+@pytest.mark.parametrize("p,k,n", [(65535, 32, 128), (65536, 32, 128), (65537, 33, 97), (65551, 72, 200), (65536, 136, 160)])
+def test_gradients_of_many_positions(lp, p, k, n, act):
+    t = _case(p, k, n, torch.bfloat16, p, "odd" if p % 2 else "")
+    pre = _pre(t, act, torch.bfloat16)
+    d_x, d_w, d_b = lp.linear_bwd(lp.Linear(t["w"], t["b"], _act_id(lp, act)), t["x"], pre, t["d_y"])
+    _check_backward(t, act, torch.bfloat16, pre, d_x, d_w, d_b)

@@ -14,7 +14,7 @@
 #include <hip/hip_runtime.h>
 
 #include <algorithm>
-#include <climits>
+#include <cfloat>
 #include <cmath>
 #include <cstring>
 #include <vector>
@@ -55,11 +55,13 @@ struct Clip {
     int scale;   // 0: the norm alone
 };
 
-__device__ __forceinline__ float factor_of(double squares, const Clip& c)
+__device__ __forceinline__ double factor_of(double squares, const Clip& c)
 {
     const double norm = sqrt(squares), f = (double)c.max_norm / (norm + (double)c.eps);
-    return f >= 1.0 || norm == 0.0 ? 1.0f : (float)f;   // (NaN stays NaN)
+    return f >= 1.0 || norm == 0.0 ? 1.0 : f;   // (NaN stays NaN)
 }
+// Whether a factor has fewer bits in fp32, or none: norms beyond 1e38 times the largest one.  It is applied in fp64 then.
+__device__ __forceinline__ bool is_tiny(double factor) { return factor > 0.0 && factor < (double)FLT_MIN; }
 
 using u32x4 = uint32_t __attribute__((ext_vector_type(4)));
 template <class T, int V>
@@ -162,6 +164,12 @@ __device__ __forceinline__ void scale_part(const T* in, T* out, long long count,
     if (threadIdx.x < count - tail) out[tail + threadIdx.x] = (T)((float)in[tail + threadIdx.x] * factor);
 }
 
+template <class T>
+__device__ __forceinline__ void scale_exactly(const T* in, T* out, long long count, double factor)
+{
+    for (long long i = threadIdx.x; i < count; i += kThreads) out[i] = (T)(float)((double)in[i] * factor);
+}
+
 // One workgroup a part: its sum of squares.
 template <int MAX>
 __global__ __launch_bounds__(kThreads) void grad_squares_kernel(Set<MAX> a, double* parts)
@@ -205,11 +213,18 @@ __global__ __launch_bounds__(kThreads) void grad_scale_kernel(Set<MAX> a, const 
     __shared__ double lds[kThreads / 64];
     const double sum = all_parts<kThreads>(parts, n, lds);
     if (write_norm && blockIdx.x == 0 && threadIdx.x == 0) *c.norm = (float)sqrt(sum);
-    const float factor = factor_of(sum, c);
+    const double exact = factor_of(sum, c);
+    const float factor = (float)exact;
     const int item = a.items - 1 - blockIdx.x, k = tensor_of(a, item);
     const TensorDev& t = a.t[k];
     if (factor == 1.0f && t.in == t.out) return;   // (nothing changes)
     const long long at = (item - t.first) * a.chunk, count = min(a.chunk, t.size - at);
+    if (is_tiny(exact)) {
+        if (t.dtype == LP_F32) scale_exactly((const float*)t.in + at, (float*)t.out + at, count, exact);
+        else if (t.dtype == LP_BF16) scale_exactly((const __bf16*)t.in + at, (__bf16*)t.out + at, count, exact);
+        else scale_exactly((const _Float16*)t.in + at, (_Float16*)t.out + at, count, exact);
+        return;
+    }
     if (t.dtype == LP_F32) scale_part<PAST_CACHE>((const float*)t.in + at, (float*)t.out + at, count, factor);
     else if (t.dtype == LP_BF16) scale_part<PAST_CACHE>((const __bf16*)t.in + at, (__bf16*)t.out + at, count, factor);
     else scale_part<PAST_CACHE>((const _Float16*)t.in + at, (_Float16*)t.out + at, count, factor);
@@ -269,7 +284,15 @@ __global__ __launch_bounds__(kSmallThreads) void grad_small_kernel(Set<kSmallTen
     sum = all_of<kSmallThreads>(sum, lds);
     if (threadIdx.x == 0) *c.norm = (float)sqrt(sum);
     if (!c.scale) return;
-    const float factor = factor_of(sum, c);
+    const double exact = factor_of(sum, c);
+    float factor = (float)exact;
+    if (is_tiny(exact)) {
+#pragma unroll
+        for (int s = 0; s < kSmallSlots; ++s)
+#pragma unroll
+            for (int j = 0; j < 4; ++j) v[s][j] = (float)((double)v[s][j] * exact);
+        factor = 1.0f;
+    }
 #pragma unroll
     for (int s = 0; s < kSmallSlots; ++s) {
         const int slot = s * kSmallThreads + threadIdx.x;

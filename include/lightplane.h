@@ -453,7 +453,7 @@ lp_status lp_residual_norm_bwd(const lp_residual_norm* norm, const void* h, cons
  *     out = in min(1, max_norm / (norm + eps)).
  * Squares and their sum are fp64, so that no fp32 value is too large or too small for them; the factor is applied in fp32 (in
  * fp64 where it is below fp32's normal numbers) and the result rounded once.  `norm` is rounded to fp32: infinite beyond its largest
- * number, with results that are clipped as others are.  A norm that is not finite is applied as it is (an infinite one makes the finite values 0 and the infinite
+ * number, with results that are clipped as others are.  A norm that is not finite in fp64 is applied as it is (an infinite one makes the finite values 0 and the infinite
  * ones NaN, NaN makes all NaN): look at `norm` where that must not reach the weights.
  */
 typedef struct {

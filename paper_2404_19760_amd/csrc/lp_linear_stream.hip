@@ -5,6 +5,9 @@
 // asks for the next 32 before it multiplies, and never waits for another wave.  The positions' channels go straight to registers: of a row's
 // 16-byte chunks lanes 0 .. 31 ask for the even ones, lanes 32 .. 63 for the odd ones.
 //
+// Rows are taken in steps of 64 bytes, two pairs of chunks (each step is a kernel of its own; what a row leaves of its last one is multiplied as zeros):
+// 131979 x 48 -> 128 in fp32 takes 39 us with six pairs and 46 with eight, x 36 36 and, with the five pairs that would do, 31; x 72 -> 128 in
+// fp16 18.4 and 18.1.
 // Measured: 160^3 x 32 -> 64 in fp32 302 us for 1.57 GB (5.2 TB/s; through LDS with a barrier a step 373), 131979 x 72 -> 96 in fp16 with residual
 // 20 us for 70 MB, -> 97 30 us: rows of 194 bytes share the 64-byte lines that they are stored to.
 #include "lp_linear.h"
@@ -105,13 +108,17 @@ void stream(const LinearDev& d, bool whole, int n_cu, hipStream_t s)
         constexpr int P = decltype(pairs)::value;
         if (d.N <= 32) go<T, ACT, BACK, P, 1>(d, whole, n_cu, s);
         else if (d.N <= 64) go<T, ACT, BACK, P, 2>(d, whole, n_cu, s);
+        // Up to 128 channels, few positions (below eight groups of 128 for each compute unit): two workgroups share the channels and both read the
+        // positions.  Twice as many workgroups, with half the products and results of a group each, fill the chip better: x 72 -> 128 in fp16, 20000
+        // positions 6.1 us instead of 8.1, 131979 18.4 instead of 20.7 (with residual 24 and 32).  With more of them reading once is faster:
+        // 400000 positions 39 us instead of 41, x 128 50 instead of 57, 1 million 109 instead of 125 (not with a residual: 67 instead of 52).
         else if ((d.P + 127) / 128 < 8 * n_cu) go<T, ACT, BACK, P, 2>(d, whole, n_cu, s);
         else go<T, ACT, BACK, P, 4>(d, whole, n_cu, s);
     };
     const int bytes = d.K * (int)sizeof(T);
     if (bytes <= 64) blocks(std::integral_constant<int, 2>());
     else if (bytes <= 128) blocks(std::integral_constant<int, 4>());
-    else if (bytes <= 160) blocks(std::integral_constant<int, 5>());
+    else if (bytes <= 192) blocks(std::integral_constant<int, 6>());
     else blocks(std::integral_constant<int, 8>());
 }
 

@@ -15,7 +15,8 @@ using namespace act;
 constexpr int kThreads = 256;
 constexpr unsigned kMaxGrid = 1u << 30;
 // Where a call moves more than the Infinity Cache holds, results are stored past the caches: they would only drive out what is yet to
-// be read (65536 x 512 -> 2048 in bf16 with pre, 0.6 GB: 272 -> 238 us; 160^3 x 32 -> 64 in fp32, whose x no other workgroup reads, stays at 338).
+// be read (65536 x 512 -> 2048 in bf16 with pre, 0.6 GB: 272 -> 238 us in the tile loop of that time; 160^3 x 32 -> 64 in fp32, whose x no other
+// workgroup reads, takes the same either way).
 constexpr double kCacheBytes = 256e6;
 inline unsigned grid_of(long long n) { return (unsigned)(n < kMaxGrid ? n : kMaxGrid); }
 
@@ -105,7 +106,7 @@ __device__ __forceinline__ void store_chunk(T* p, long long count, const Chunk<T
     }
 }
 
-// acc += a b^T over the channels of two neighbouring chunks (see above)
+// acc += a b^T over the channels of two neighbouring chunks of a row, of which lanes 0 .. 31 hold the first, lanes 32 .. 63 the second
 __device__ __forceinline__ f32x16 multiply(const Chunk<__bf16>& a, const Chunk<__bf16>& b, f32x16 acc)
 {
     using V = Vec<__bf16>::Of;
@@ -206,6 +207,8 @@ struct LinearDev {
     int splits, split_steps;        // parts, steps of one
 };
 
+// Where a chunk of a row of 128 bytes lies in LDS.  Two neighbouring rows fill the 64 banks once; turned over by row / 2, the same chunk of 16
+// neighbouring rows, which a matrix operand reads at once, touches every bank once too, and so do a row pair's chunks, which are written at once.
 __device__ __forceinline__ int chunk_at(int row, int chunk) { return row * 128 + ((chunk ^ (row >> 1 & 7)) << 4); }
 
 // Tile of a workgroup: neighbouring workgroups go to the chip's eight XCDs in turn, so each of these takes one run of the

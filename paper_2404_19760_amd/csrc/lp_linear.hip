@@ -2,7 +2,7 @@
 //
 //     z = x W^T + b,   y = act(z) + r;   d_z = d_y act'(z),   d_x = d_z W,   d_W += d_z^T x,   d_b += sum d_z
 //
-// What bounds it: memory where a grid's positions have few channels (32 -> 64 channels in fp32: 380 bytes for 4096 operations a position), the
+// What bounds it: memory where a grid's positions have few channels (32 -> 64 channels in fp32: 384 bytes for 4096 operations a position), the
 // matrix cores for blocks of some hundred channels, latency for single tokens.
 //
 // Everything moves in chunks of 16 bytes along the channels.  A 32 x 32 block of results is made from chunks the same way in all types: of two

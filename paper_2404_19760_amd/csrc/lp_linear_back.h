@@ -9,7 +9,7 @@ namespace {
 
 // ---- gradients in 16-bit types ---------------------------------------------------------------------------------
 //
-// A workgroup takes a part of the positions, some at a time: d_z is made from d_y and pre in registers, split in two or three parts and
+// A workgroup takes a part of the positions, some at a time: d_z is made from d_y and pre in registers, split in parts and
 // laid into LDS beside x, and from there come all products of these positions: d_z^T x in 32 x 32 blocks, and, where all channels of d_z are there
 // (SKINNY: up to 128 -> 128 channels), d_z W too, in 16 x 16 blocks with W^T as operands in LDS.  Then everything is read once and d_x is written once.
 // Blocks with more channels: workgroups of 128 channels of d_z x up to 512 of x, so that d_z is made once for 512 channels of x; the first of
@@ -17,8 +17,8 @@ namespace {
 // waves that share a SIMD one multiplies first and then makes the next positions' d_z, the other one the other way round, so that the
 // vector instructions of one run under the matrix instructions of the other.
 //
-// Measured with GELU in bf16, all gradients: 24 x 256^2 positions, 32 -> 128 channels 300 us for 1.0 GB, 65536 x 512 -> 2048 590 us (0.4 TFLOP for d_W's
-// three parts, 0.14 for d_x).
+// Measured with GELU in bf16, all gradients: 24 x 256^2 positions, 32 -> 128 channels 278 to 300 us for 1.0 GB, 65536 x 512 -> 2048 590 us, of which this
+// kernel takes 412 (0.41 TFLOP for d_W's three parts: 1.0 PFLOP/s).
 // Parts of d_z.  The sums' own error goes by the length of a part of the positions, not by their number, and stays below 1.4e-6 (64 -> 64 channels,
 // 1.6 million positions; up to 65536 positions 3e-7 to 8e-7): in bf16 two parts, 17 bits, would leave 2.5e-6 at every size, so there are three, whatever the number of
 // positions.  What that costs, against two: 512 -> 2048 channels, 16384 positions 195 and 174 us, 65536 590 and 510, 262144 2215 and 1890; 32 -> 128,

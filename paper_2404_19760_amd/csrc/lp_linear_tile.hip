@@ -10,8 +10,8 @@ namespace {
 //
 // A workgroup of four waves makes BP positions x BN channels.  A step is 128 bytes of channels of both operands, staged through
 // registers into one of two LDS buffers while the other one is multiplied.  Latency bounds it where there are few tiles (a step of 16-bit types takes some
-// 0.6 us then, of fp32 2), fp32 matrix instructions for large fp32 products (20000 x 1024 -> 1024 with GELU: 400 us, 0.1 PFLOP/s, 2.5 rounds of tiles).  A row's eight chunks lie at chunk ^ (row mod 8): eight
-// rows' same chunk, and a row's eight chunks, both touch every bank once.
+// 0.6 us then, of fp32 2), fp32 matrix instructions for large fp32 products (20000 x 1024 -> 1024 with GELU: 400 us, 0.1 PFLOP/s, 2.5 rounds of tiles).  Chunks lie in LDS as
+// chunk_at says.
 template <int BP, int BN>
 struct TileShape {
     static constexpr int kWavesN = BN >= 128 ? 2 : 1, kWavesP = 4 / kWavesN;

@@ -391,9 +391,9 @@ lp_status lp_linear_workspace_bytes(const lp_linear* linear, size_t* fwd_bytes, 
 lp_status lp_linear_fwd(const lp_linear* linear, const void* x, void* y, void* pre, void* workspace, size_t workspace_bytes, void* stream);
 
 /* Backward.  pre as the forward wrote it (not used, and may be NULL, where act is LP_ACT_NONE).  d_x is WRITTEN (NULL: not
-   wanted) and must not overlap x, pre or d_y; d_weight [N][K] and d_bias [N] are ACCUMULATED into (either may be NULL), in an
-   order that does not change from call to call.  x is read for d_weight alone and the weight for d_x alone: either may be NULL where
-   that is.  Of a ReLU the gradient at 0 is 0. */
+   wanted); d_weight [N][K] and d_bias [N] are ACCUMULATED into (either may be NULL), in an order that does not change from call to
+   call.  None of the three may overlap anything else that the call is given.  x is read for d_weight alone and the weight for d_x
+   alone: either may be NULL where that is.  Of a ReLU the gradient at 0 is 0. */
 lp_status lp_linear_bwd(const lp_linear* linear, const void* x, const void* pre, const void* d_y, void* d_x, float* d_weight,
                         float* d_bias, void* workspace, size_t workspace_bytes, void* stream);
 
@@ -441,7 +441,7 @@ lp_status lp_residual_norm_fwd(const lp_residual_norm* norm, const void* h, cons
 /* Backward from the forward's inputs (it computes s again) for the upstream gradients d_s and d_y (either may be NULL: zero).  d_h
    and d_f are WRITTEN (NULL: not wanted); d_h may be d_s itself, d_f may be d_y itself where the strides are alike, otherwise they must
    not overlap anything else.  d_gamma [C], d_beta [C], d_post_gamma [C] and d_gate (the gate's shape) are ACCUMULATED into (NULL:
-   not wanted), in an order that does not change from call to call.  workspace: device, 256-byte aligned, contents ignored on entry,
+   not wanted), in an order that does not change from call to call, and must not overlap anything else.  workspace: device, 256-byte aligned, contents ignored on entry,
    undefined on exit. */
 lp_status lp_residual_norm_bwd(const lp_residual_norm* norm, const void* h, const void* f, const void* d_s, const void* d_y, void* d_h,
                                void* d_f, float* d_gamma, float* d_beta, float* d_post_gamma, float* d_gate, void* workspace,

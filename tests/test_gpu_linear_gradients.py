@@ -82,3 +82,23 @@ def test_gradients_of_many_positions(lp, p, k, n, act):
     pre = _pre(t, act, torch.bfloat16)
     d_x, d_w, d_b = lp.linear_bwd(lp.Linear(t["w"], t["b"], _act_id(lp, act)), t["x"], pre, t["d_y"])
     _check_backward(t, act, torch.bfloat16, pre, d_x, d_w, d_b)
+
+
+@pytest.mark.parametrize("act", ["none", "relu", "silu", "gelu"])
+@pytest.mark.parametrize("dtype", DTYPES)
+@pytest.mark.parametrize("p,k,n", [(700, 136, 200), (513, 264, 130), (30, 200, 72), (1000, 145, 257)])
+def test_gradients_through_frozen_weights(lp, p, k, n, dtype, act):
+    """x alone wants a gradient: more than 128 channels of it, which come straight from d_y and pre, through autograd and the entry point."""
+    from paper_2404_19760_amd import autograd as lpa
+    t = _case(p, k, n, dtype, p + k + n, "odd")
+    x = t["x"].detach().requires_grad_(True)
+    lpa.linear(x, t["w"], t["b"], _act_id(lp, act)).backward(t["d_y"])
+    lin = lp.Linear(t["w"], t["b"], _act_id(lp, act))
+    _, pre = lp.linear_fwd(lin, t["x"], keep=True)
+    pre = None if act == "none" else pre
+    ws = torch.empty(lp.lp_linear_workspace_bytes(lin, t["x"])[1], dtype=torch.uint8, device="cuda")
+    d_x = torch.empty_strided(t["x"].shape, t["x"].stride(), dtype=dtype, device="cuda")
+    lp.lp_linear_bwd(lin, t["x"], pre, t["d_y"], d_x, None, None, ws)
+    _, d_w, d_b = lp.linear_bwd(lin, t["x"], pre, t["d_y"])
+    _check_backward(t, act, dtype, pre, d_x, d_w, d_b)
+    assert torch.equal(x.grad, d_x)
